@@ -1,0 +1,276 @@
+// Grouped matrix products: entry points of include/llmoe.h.  Arguments are
+// checked before any HIP call.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "../../include/llmoe.h"
+#include "ll_host.hpp"
+#include "ll_linear.hpp"
+
+using namespace llc;
+using namespace llc::lin;
+
+namespace {
+
+constexpr size_t kMaxExtent = 0x7fffffff;
+
+int esize(ll_dtype dt) { return dt == LL_F32 ? 4 : 2; }
+bool aligned(const void *p, size_t to) { return (uintptr_t)p % to == 0; }
+bool overlap(const void *a, size_t an, const void *b, size_t bn) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a != nullptr && b != nullptr && an != 0 && bn != 0 && x < y + bn && y < x + an;
+}
+size_t span(size_t rows, size_t ld, size_t len, int es) { return rows == 0 ? 0 : ((rows - 1) * ld + len) * es; }
+
+int check_desc(const ll_linear_desc *d) {
+  if (d == nullptr || d->size != sizeof(ll_linear_desc)) return LL_ERR_INVALID;
+  if (d->dt != LL_F32 && d->dt != LL_BF16) return LL_ERR_UNSUPPORTED;
+  if ((int)d->act < LL_ACT_NONE || (int)d->act > LL_ACT_GEGLU) return LL_ERR_INVALID;
+  if (d->groups < 1 || (d->offsets == nullptr && d->groups != 1) || !aligned(d->offsets, 4)) return LL_ERR_INVALID;
+  if (d->in < 1 || d->out < 1) return LL_ERR_INVALID;
+  if (d->groups > LL_MOE_MAX_EXPERTS || d->rows > kMaxExtent) return LL_ERR_UNSUPPORTED;
+  // a tile's rows lie within 2^31 bytes of its first one
+  constexpr size_t kMaxFeatures = 1u << 20;
+  if (d->in > kMaxFeatures || d->out > kMaxFeatures) return LL_ERR_UNSUPPORTED;
+  for (size_t ld : {d->ldx, d->ldw, d->ldy, d->ldz, d->ldr})
+    if (ld > 2 * kMaxFeatures) return LL_ERR_UNSUPPORTED;
+  if (d->ldw < d->in || (d->groups > 1 && d->wstride < (d->out - 1) * d->ldw + d->in)) return LL_ERR_INVALID;
+  return LL_OK;
+}
+
+size_t weight_span(const ll_linear_desc *d, int es) {
+  return ((size_t)(d->groups - 1) * d->wstride + (d->out - 1) * d->ldw + d->in) * es;
+}
+
+int check_rows(const void *p, size_t ld, size_t len, int es, bool any) {
+  if ((any && p == nullptr) || !aligned(p, es) || ld < len) return LL_ERR_INVALID;
+  return LL_OK;
+}
+
+using tile_fn = void (*)(Args);
+
+template <typename T, Pass PASS, int BM, int BN, int WM, int WN>
+tile_fn pick(bool gate, bool vec) {
+  if constexpr (PASS == kForward) {
+    if (gate)
+      return vec ? k_tile<T, PASS, BM, BN, WM, WN, true, true> : k_tile<T, PASS, BM, BN, WM, WN, true, false>;
+  }
+  return vec ? k_tile<T, PASS, BM, BN, WM, WN, false, true> : k_tile<T, PASS, BM, BN, WM, WN, false, false>;
+}
+
+template <Pass PASS>
+int launch_tiles(Args &a, ll_dtype dt, bool gate, bool vec, void *stream) {
+  constexpr int kB = 128;
+  const uint32_t width = gate ? a.n / 2 : a.n;
+  const uint32_t per_n = gate ? kB / 2 : kB;
+  a.tiles_n = (width + per_n - 1) / per_n;
+  uint64_t tiles;
+  if (PASS == kGradW) {
+    a.tiles_m = (a.m + kB - 1) / kB;
+    tiles = (uint64_t)a.tiles_m * a.groups;
+  } else {
+    // every group with rows may add one partial tile
+    tiles = a.offsets == nullptr ? (a.rows + kB - 1) / kB : a.rows / kB + std::min<uint64_t>(a.groups, a.rows);
+  }
+  const uint64_t grid = tiles * a.tiles_n;
+  if (grid * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
+  const tile_fn fn = dt == LL_F32 ? pick<float, PASS, kB, kB, 2, 2>(gate, vec) : pick<__bf16, PASS, kB, kB, 2, 2>(gate, vec);
+  hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
+  return launch_status();
+}
+
+// Four consecutive elements at multiples of 4 are aligned in every row.
+bool four(const void *p, size_t ld, int es) { return p == nullptr || (aligned(p, 4 * es) && ld % 4 == 0); }
+bool chunked(const void *p, size_t ld, size_t len, int es) {
+  return aligned(p, 16) && ld * es % 16 == 0 && len * es % 16 == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ll_linear_desc_init(ll_linear_desc *d, ll_dtype dt, ll_act act, int groups, size_t rows, size_t in, size_t out) {
+  if (d == nullptr) return LL_ERR_INVALID;
+  *d = ll_linear_desc{};
+  d->size = sizeof(ll_linear_desc);
+  d->dt = dt;
+  d->act = act;
+  d->groups = groups;
+  d->rows = rows;
+  d->in = in;
+  d->out = out;
+  d->ldx = in;
+  d->ldw = in;
+  d->wstride = in * out;
+  d->ldy = gated((int)act) ? out / 2 : out;
+  d->ldz = out;
+  d->ldr = d->ldy;
+  return LL_OK;
+}
+
+int ll_linear_bytes(const ll_linear_desc *d, ll_linear_pass pass, size_t *bytes) {
+  if (bytes == nullptr || (int)pass < LL_LINEAR_FORWARD || (int)pass > LL_LINEAR_GRAD_W) return LL_ERR_INVALID;
+  const int st = check_desc(d);
+  if (st != LL_OK) return st;
+  *bytes = 0;
+  return LL_OK;
+}
+
+int ll_linear(const ll_linear_desc *d, const void *x, const void *w, const void *bias, const void *residual, void *y,
+              void *z, void *workspace, size_t workspace_bytes, void *stream) {
+  int st = check_desc(d);
+  if (st != LL_OK) return st;
+  const int es = esize(d->dt);
+  const bool gate = gated((int)d->act), any = d->rows != 0;
+  if (gate && d->out % 2 != 0) return LL_ERR_INVALID;
+  const size_t width = gate ? d->out / 2 : d->out;
+  st = check_rows(x, d->ldx, d->in, es, any);
+  if (st == LL_OK) st = check_rows(w, d->ldw, d->in, es, any);
+  if (st == LL_OK) st = check_rows(y, d->ldy, width, es, any);
+  if (st == LL_OK && z != nullptr) st = check_rows(z, d->ldz, d->out, es, any);
+  if (st == LL_OK && residual != nullptr) st = check_rows(residual, d->ldr, width, es, any);
+  if (st != LL_OK) return st;
+  if (!aligned(bias, es) || !aligned(workspace, 16)) return LL_ERR_INVALID;
+  const size_t yb = span(d->rows, d->ldy, width, es), zb = span(d->rows, d->ldz, d->out, es);
+  const size_t xb = span(d->rows, d->ldx, d->in, es), rb = span(d->rows, d->ldr, width, es);
+  if (overlap(x, xb, y, yb) || overlap(x, xb, z, zb) || overlap(y, yb, z, zb) || overlap(residual, rb, z, zb) ||
+      overlap(w, weight_span(d, es), y, yb) || overlap(w, weight_span(d, es), z, zb) ||
+      (overlap(residual, rb, y, yb) && !(residual == y && d->ldr == d->ldy)))
+    return LL_ERR_INVALID;
+  if (!any) return LL_OK;
+  Args a{};
+  a.p = x;
+  a.ldp = d->ldx;
+  a.q = w;
+  a.ldq = d->ldw;
+  a.qstride = d->wstride;
+  a.offsets = d->offsets;
+  a.groups = d->groups;
+  a.rows = a.m = (uint32_t)d->rows;
+  a.n = (uint32_t)d->out;
+  a.k = (uint32_t)d->in;
+  a.bias = bias;
+  a.res = residual;
+  a.ldr = d->ldr;
+  a.zout = z;
+  a.ldz = d->ldz;
+  a.c = y;
+  a.ldc = d->ldy;
+  a.act = (int)d->act;
+  a.vec_c = four(y, d->ldy, es) && four(z, d->ldz, es) && four(residual, d->ldr, es);
+  const bool vec = chunked(x, d->ldx, d->in, es) && chunked(w, d->ldw, d->in, es) && d->wstride * es % 16 == 0 &&
+                   d->out * d->ldw * es < 0xF0000000ull;
+  return launch_tiles<kForward>(a, d->dt, gate, vec, stream);
+}
+
+int ll_linear_grad_x(const ll_linear_desc *d, const void *dz, const void *w, const void *z, void *dx, void *workspace,
+                     size_t workspace_bytes, void *stream) {
+  int st = check_desc(d);
+  if (st != LL_OK) return st;
+  const int es = esize(d->dt);
+  const bool any = d->rows != 0;
+  const size_t width = gated((int)d->act) ? 2 * d->in : d->in;
+  st = check_rows(dz, d->ldy, d->out, es, any);
+  if (st == LL_OK) st = check_rows(w, d->ldw, d->in, es, any);
+  if (st == LL_OK) st = check_rows(dx, d->ldx, width, es, any);
+  if (st == LL_OK && d->act != LL_ACT_NONE) st = check_rows(z, d->ldz, width, es, any);
+  if (st != LL_OK) return st;
+  if (!aligned(workspace, 16)) return LL_ERR_INVALID;
+  const size_t xb = span(d->rows, d->ldx, width, es);
+  if (overlap(dz, span(d->rows, d->ldy, d->out, es), dx, xb) || overlap(w, weight_span(d, es), dx, xb) ||
+      (d->act != LL_ACT_NONE && overlap(z, span(d->rows, d->ldz, width, es), dx, xb)))
+    return LL_ERR_INVALID;
+  if (!any) return LL_OK;
+  Args a{};
+  a.p = dz;
+  a.ldp = d->ldy;
+  a.q = w;
+  a.ldq = d->ldw;
+  a.qstride = d->wstride;
+  a.offsets = d->offsets;
+  a.groups = d->groups;
+  a.rows = a.m = (uint32_t)d->rows;
+  a.n = (uint32_t)d->in;
+  a.k = (uint32_t)d->out;
+  a.z = z;
+  a.ldz = d->ldz;
+  a.c = dx;
+  a.ldc = d->ldx;
+  a.act = (int)d->act;
+  a.vec_c = four(dx, d->ldx, es) && four(z, d->ldz, es);
+  const bool vec = chunked(dz, d->ldy, d->out, es) && chunked(w, d->ldw, d->in, es) && d->wstride * es % 16 == 0;
+  return launch_tiles<kGradX>(a, d->dt, false, vec, stream);
+}
+
+int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, void *dw, void *dbias, uint32_t flags,
+                     void *workspace, size_t workspace_bytes, void *stream) {
+  int st = check_desc(d);
+  if (st != LL_OK) return st;
+  if ((flags & ~(LL_GRAD_F32 | LL_GRAD_ADD)) != 0) return LL_ERR_INVALID;
+  const int es = esize(d->dt);
+  const int gs = (flags & LL_GRAD_F32) ? 4 : es;
+  const bool any = d->rows != 0;
+  st = check_rows(dz, d->ldy, d->out, es, any);
+  if (st == LL_OK) st = check_rows(x, d->ldx, d->in, es, any);
+  if (st == LL_OK) st = check_rows(dw, d->ldw, d->in, gs, true);
+  if (st != LL_OK) return st;
+  if (!aligned(dbias, gs) || !aligned(workspace, 16)) return LL_ERR_INVALID;
+  const size_t wb = weight_span(d, gs), bb = (size_t)d->groups * d->out * gs;
+  const size_t yb = span(d->rows, d->ldy, d->out, es), xb = span(d->rows, d->ldx, d->in, es);
+  if (overlap(dz, yb, dw, wb) || overlap(x, xb, dw, wb) || overlap(dz, yb, dbias, bb) || overlap(x, xb, dbias, bb) ||
+      overlap(dw, wb, dbias, bb))
+    return LL_ERR_INVALID;
+  Args a{};
+  a.p = dz;
+  a.ldp = d->ldy;
+  a.q = x;
+  a.ldq = d->ldx;
+  a.cstride = d->wstride;
+  a.offsets = d->offsets;
+  a.groups = d->groups;
+  a.rows = (uint32_t)d->rows;
+  a.m = (uint32_t)d->out;
+  a.n = (uint32_t)d->in;
+  a.c = dw;
+  a.ldc = d->ldw;
+  a.dbias = dbias;
+  a.flags = flags;
+  // the gradient's own element size decides its alignment
+  a.vec_c = four(dw, d->ldw, gs) && d->wstride % 4 == 0;
+  const bool vec = chunked(dz, d->ldy, d->out, es) && chunked(x, d->ldx, d->in, es);
+  a.k = a.rows;
+  return launch_tiles<kGradW>(a, d->dt, false, vec, stream);
+}
+
+int ll_act_grad(const void *dy, size_t lddy, const void *z, size_t ldz, size_t rows, size_t features, ll_dtype dt,
+                ll_act act, void *dz, size_t lddz, void *stream) {
+  if (dt != LL_F32 && dt != LL_BF16) return LL_ERR_UNSUPPORTED;
+  if ((int)act < LL_ACT_NONE || (int)act > LL_ACT_GEGLU) return LL_ERR_INVALID;
+  if (rows > kMaxExtent || features > kMaxExtent / 2) return LL_ERR_UNSUPPORTED;
+  const int es = esize(dt);
+  const bool gate = gated((int)act);
+  const size_t width = gate ? 2 * features : features;
+  int st = check_rows(dy, lddy, features, es, true);
+  if (st == LL_OK) st = check_rows(z, ldz, width, es, true);
+  if (st == LL_OK) st = check_rows(dz, lddz, width, es, true);
+  if (st != LL_OK) return st;
+  const size_t ob = span(rows, lddz, width, es);
+  if (overlap(dy, span(rows, lddy, features, es), dz, ob) && !(!gate && dy == dz && lddy == lddz)) return LL_ERR_INVALID;
+  if (overlap(z, span(rows, ldz, width, es), dz, ob) && !(z == dz && ldz == lddz)) return LL_ERR_INVALID;
+  if (rows == 0 || features == 0) return LL_OK;
+  ActArgs a{dy, z, dz, lddy, ldz, lddz, (uint32_t)rows, (uint32_t)features, (int)act};
+  const bool vec = chunked(dy, lddy, features, es) && chunked(z, ldz, features, es) && chunked(dz, lddz, features, es);
+  int cus = 0;
+  st = device_cus(&cus);
+  if (st != LL_OK) return st;
+  const uint64_t items = (uint64_t)rows * features / (vec ? 16 / es : 1);
+  const unsigned grid = (unsigned)std::min<uint64_t>((items + 255) / 256, (uint64_t)cus * 16);
+  const auto fn = dt == LL_F32 ? (vec ? k_act_grad<float, true> : k_act_grad<float, false>)
+                               : (vec ? k_act_grad<__bf16, true> : k_act_grad<__bf16, false>);
+  hipLaunchKernelGGL(fn, dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
+  return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,538 @@
+// Routing, dispatch and combine kernels (include/llmoe.h).
+//
+// All of them are bound by memory, or at small sizes by the launch: each
+// reads its rows once and writes its rows once.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/llmoe.h"
+#include "ll_num.hpp"
+
+namespace llc {
+namespace moe {
+
+constexpr int kThreads = 256;
+constexpr float kNegInf = -__builtin_inff();
+
+// ---------------------------------------------------------------- routing
+//
+// W lanes hold one token's logits, NPL consecutive ones each, so that among
+// equal keys the lowest lane holds the lowest index.  k rounds: every lane's
+// best key, the maximum over the lanes, the lowest lane that has it.
+struct RouteArgs {
+  const void *logits;
+  uint64_t ld;
+  uint32_t tokens;
+  int experts, k;
+  const float *bias;
+  int score, normalise;
+  float scale;
+  int32_t *ids;
+  float *weights;
+  const float *dweights;
+  void *dlogits;
+  uint64_t ldd;
+};
+
+// The logits of one lane; past the last expert, and for NaN, -Infinity.
+template <typename T, int NPL, bool VEC>
+__device__ __forceinline__ void load_logits(const T *row, int e0, int experts, float (&l)[NPL]) {
+  Pack<T, NPL, VEC> p;
+  if (VEC && e0 + NPL <= experts)
+    p.load(row + e0);
+  else
+    p.load_some(row + e0, experts - e0, kNegInf);
+#pragma unroll
+  for (int i = 0; i < NPL; ++i) l[i] = p.v[i] == p.v[i] ? p.v[i] : kNegInf;
+}
+
+// Softmax statistics of a token over its W lanes: the maximum (0 where every
+// logit is -Infinity) and the reciprocal of the sum of exponentials.
+template <int W, int NPL>
+__device__ __forceinline__ void softmax_stats(const float (&l)[NPL], float *m, float *inv) {
+  float mx = l[0];
+#pragma unroll
+  for (int i = 1; i < NPL; ++i) mx = fmaxf(mx, l[i]);
+  mx = group_max<W>(mx);
+  if (mx == kNegInf) mx = 0.f;
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < NPL; ++i) s += expf(l[i] - mx);
+  s = group_sum<W>(s);
+  *m = mx;
+  *inv = s > 0.f || s != s ? 1.f / s : 0.f;
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+
+template <typename T, int W, int NPL, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
+  const int sub = threadIdx.x % W, lane = threadIdx.x % 64;
+  const uint32_t t = blockIdx.x * (kThreads / W) + threadIdx.x / W;
+  const bool live = t < a.tokens;  // no early exit: the lanes of a wave work on several tokens together
+  const T *row = (const T *)a.logits + (uint64_t)(live ? t : 0) * a.ld;
+  const int e0 = sub * NPL;
+  float l[NPL], key[NPL];
+  load_logits<T, NPL, VEC>(row, e0, a.experts, l);
+#pragma unroll
+  for (int i = 0; i < NPL; ++i) {
+    float x = l[i];
+    if (a.bias != nullptr && e0 + i < a.experts) x += a.bias[e0 + i];
+    key[i] = x == x ? x : kNegInf;
+  }
+  float m = 0.f, inv = 0.f;
+  if (a.score == 0) softmax_stats<W, NPL>(l, &m, &inv);
+  int mine = -1;  // lane j keeps the j-th choice
+  for (int j = 0; j < a.k; ++j) {
+    float best = key[0];
+    int at = 0;
+#pragma unroll
+    for (int i = 1; i < NPL; ++i)
+      if (key[i] > best) {
+        best = key[i];
+        at = i;
+      }
+    const float top = group_max<W>(best);
+    uint64_t have = __ballot(best == top && top > kNegInf);
+    if constexpr (W == 16) have = (have >> (lane & 48)) & 0xFFFFull;
+    const int who = have == 0 ? -1 : __ffsll((unsigned long long)have) - 1;
+    const int won = __shfl(at, who < 0 ? 0 : who, W);
+    if (sub == j) mine = who < 0 ? -1 : who * NPL + won;
+    if (sub == who) {
+#pragma unroll
+      for (int i = 0; i < NPL; ++i)
+        if (i == at) key[i] = kNegInf;
+    }
+  }
+  float u = 0.f;
+  if (mine >= 0) {
+    const float x = Num<T>::get(row[mine]);
+    u = a.score == 0 ? expf(x - m) * inv : sigmoid(x);
+    if (x != x) u = 0.f;
+  }
+  if (a.normalise) {
+    const float tot = group_sum<W>(u);
+    u = tot > 0.f || tot != tot ? u / tot : 0.f;
+  }
+  if (live && sub < a.k) {
+    a.ids[(uint64_t)t * a.k + sub] = mine;
+    a.weights[(uint64_t)t * a.k + sub] = a.scale * u;
+  }
+}
+
+// The gradient recomputes the scores from the logits.  With u the chosen
+// scores, divided by their sum where normalised, and g = scale * dweights:
+//   softmax             dl_i = p_i (g_i - sum u g)        (g_i = 0 if not chosen)
+//   softmax, normalised dl_i = u_i (g_i - sum u g)        (chosen only)
+//   sigmoid             dl_i = g_i s_i (1 - s_i)          (chosen only)
+//   sigmoid, normalised dl_i = u_i (g_i - sum u g)(1 - s_i)
+template <typename T, int W, int NPL, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_route_grad(RouteArgs a) {
+  __shared__ float coef[kThreads * NPL];
+  const int sub = threadIdx.x % W;
+  const uint32_t t = blockIdx.x * (kThreads / W) + threadIdx.x / W;
+  const bool live = t < a.tokens;
+  const T *row = (const T *)a.logits + (uint64_t)(live ? t : 0) * a.ld;
+  const int e0 = sub * NPL;
+  float *mine = coef + (threadIdx.x / W) * (W * NPL);
+  float l[NPL];
+  load_logits<T, NPL, VEC>(row, e0, a.experts, l);
+#pragma unroll
+  for (int i = 0; i < NPL; ++i) mine[e0 + i] = 0.f;
+  int id = -1;
+  float g = 0.f;
+  if (live && sub < a.k) {
+    id = a.ids[(uint64_t)t * a.k + sub];
+    if (id < 0 || id >= a.experts) id = -1;
+    if (id >= 0) g = a.scale * a.dweights[(uint64_t)t * a.k + sub];
+  }
+  float m = 0.f, inv = 0.f;
+  if (a.score == 0) softmax_stats<W, NPL>(l, &m, &inv);
+  float p = 0.f;
+  if (id >= 0) {
+    const float x = Num<T>::get(row[id]);
+    p = a.score == 0 ? expf(x - m) * inv : sigmoid(x);
+    if (x != x) p = 0.f;
+  }
+  float u = p;
+  if (a.normalise) {
+    const float tot = group_sum<W>(p);
+    u = tot > 0.f || tot != tot ? p / tot : 0.f;
+  }
+  const float mean = group_sum<W>(u * g);
+  __syncthreads();
+  float c = 0.f;
+  if (id >= 0) {
+    if (a.score == 0)
+      c = a.normalise ? u * (g - mean) : p * g;
+    else
+      c = a.normalise ? u * (g - mean) * (1.f - p) : g * p * (1.f - p);
+    mine[id] = c;
+  }
+  __syncthreads();
+  Pack<T, NPL, VEC> out;
+  const bool all = a.score == 0 && !a.normalise;  // every expert's logit moves the softmax
+#pragma unroll
+  for (int i = 0; i < NPL; ++i) {
+    float d = mine[e0 + i];
+    if (all) d -= expf(l[i] - m) * inv * mean;
+    out.v[i] = d;
+  }
+  if (!live) return;
+  T *drow = (T *)a.dlogits + (uint64_t)t * a.ldd;
+  if (VEC && e0 + NPL <= a.experts)
+    out.store(drow + e0);
+  else
+    out.store_some(drow + e0, a.experts - e0);
+}
+
+// ---------------------------------------------------------------- sorting by expert
+//
+// A stable counting sort.  Each block takes `chunk` consecutive (token,
+// choice) pairs, each of its waves a consecutive quarter of them, and a wave
+// 64 at a time, so a pair's place is: the rows of smaller experts, the
+// expert's rows in earlier blocks, in earlier waves of this block, in earlier
+// batches of this wave, and among the lower lanes.
+struct SortArgs {
+  const int32_t *ids;
+  uint32_t pairs, chunk, blocks;
+  int first, experts, bits;
+  int32_t *offsets, *slots, *rows;
+  int32_t *hist;  // [blocks][experts]
+};
+
+__device__ __forceinline__ int local_expert(const SortArgs &a, uint32_t i) {
+  const int64_t e = (int64_t)a.ids[i] - a.first;
+  return e >= 0 && e < a.experts ? (int)e : -1;
+}
+
+// Counts of a wave's pairs [lo, hi) into cnt[experts] (zeroed, LDS).
+__device__ __forceinline__ void wave_count(const SortArgs &a, uint32_t lo, uint32_t hi, int *cnt) {
+  for (uint32_t i = lo + threadIdx.x % 64; i < hi; i += 64) {
+    const int e = local_expert(a, i);
+    if (e >= 0) atomicAdd(&cnt[e], 1);  // integers: the order does not matter
+  }
+}
+
+// Places of a wave's pairs [lo, hi), cnt[e] = the first place of expert e for
+// this wave (advanced).  put(i, place) is called for every pair, -1 where it
+// is not local.
+template <typename F>
+__device__ __forceinline__ void wave_place(const SortArgs &a, uint32_t lo, uint32_t hi, int *cnt, F put) {
+  const int lane = threadIdx.x % 64;
+  for (uint32_t base = lo; base < hi; base += 64) {
+    const uint32_t i = base + lane;
+    const int e = i < hi ? local_expert(a, i) : -1;
+    uint64_t same = __ballot(e >= 0);  // lanes with this lane's expert
+    for (int b = 0; b < a.bits; ++b) {
+      const uint64_t m = __ballot(e >= 0 && ((e >> b) & 1));
+      same &= ((e >> b) & 1) ? m : ~m;
+    }
+    const int before = __popcll(same & ((1ull << lane) - 1ull));
+    int place = -1;
+    if (e >= 0) place = cnt[e] + before;
+    __builtin_amdgcn_wave_barrier();
+    if (e >= 0 && before == 0) cnt[e] += __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    if (i < hi) put(i, place);
+  }
+}
+
+// base[e] <- sum of total[e'] for e' < e, by the block's first wave; returns
+// the sum of all through *sum (LDS).
+__device__ __forceinline__ void scan_experts(const int *total, int *base, int experts, int *sum) {
+  if (threadIdx.x < 64) {
+    int carry = 0;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+      const int e = e0 + threadIdx.x;
+      const int v = e < experts ? total[e] : 0;
+      int s = v;
+      for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(s, d);
+        if ((int)threadIdx.x >= d) s += up;
+      }
+      if (e < experts) base[e] = carry + s - v;
+      carry += __shfl(s, 63);
+    }
+    if (threadIdx.x == 0) *sum = carry;
+  }
+}
+
+constexpr int kWaves = kThreads / 64;
+
+// First launch of a large sort: each block's counts.
+static __global__ __launch_bounds__(kThreads) void k_sort_count(SortArgs a) {
+  extern __shared__ int cnt[];
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) cnt[e] = 0;
+  __syncthreads();
+  const uint32_t lo = blockIdx.x * a.chunk, hi = min(a.pairs, lo + a.chunk);
+  for (uint32_t i = lo + threadIdx.x; i < hi; i += kThreads) {
+    const int e = local_expert(a, i);
+    if (e >= 0) atomicAdd(&cnt[e], 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) a.hist[(uint64_t)blockIdx.x * a.experts + e] = cnt[e];
+}
+
+// Places of this block's pairs.  LDS: total[experts], base[experts],
+// cnt[kWaves][experts].  hist NULL: the block has every pair (blocks == 1).
+template <typename F>
+__device__ __forceinline__ void block_sort(const SortArgs &a, uint32_t block, int *lds, int *sum, F put) {
+  int *total = lds, *base = lds + a.experts, *cnt = lds + 2 * a.experts;
+  for (int i = threadIdx.x; i < kWaves * a.experts; i += kThreads) cnt[i] = 0;
+  __syncthreads();
+  const int wave = threadIdx.x / 64;
+  const uint32_t part = a.chunk / kWaves;
+  const uint32_t lo = min(a.pairs, block * a.chunk + wave * part);
+  const uint32_t hi = min(a.pairs, lo + part);
+  wave_count(a, lo, hi, cnt + wave * a.experts);
+  __syncthreads();
+  // per expert: rows of all blocks, and of the blocks before this one
+  int before[LL_MOE_MAX_EXPERTS / kThreads];
+#pragma unroll
+  for (int n = 0; n < LL_MOE_MAX_EXPERTS / kThreads; ++n) {
+    const int e = threadIdx.x + n * kThreads;
+    before[n] = 0;
+    if (e >= a.experts) continue;
+    int all = 0;
+    if (a.hist == nullptr) {
+      for (int w = 0; w < kWaves; ++w) all += cnt[w * a.experts + e];
+    } else {
+      for (uint32_t b = 0; b < a.blocks; ++b) {
+        const int v = a.hist[(uint64_t)b * a.experts + e];
+        if (b < block) before[n] += v;
+        all += v;
+      }
+    }
+    total[e] = all;
+  }
+  __syncthreads();
+  scan_experts(total, base, a.experts, sum);
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < LL_MOE_MAX_EXPERTS / kThreads; ++n) {
+    const int e = threadIdx.x + n * kThreads;
+    if (e >= a.experts) continue;
+    int at = base[e] + before[n];
+    for (int w = 0; w < kWaves; ++w) {
+      const int c = cnt[w * a.experts + e];
+      cnt[w * a.experts + e] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  wave_place(a, lo, hi, cnt + wave * a.experts, put);
+}
+
+__device__ __forceinline__ void write_offsets(const SortArgs &a, const int *base, int sum) {
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) a.offsets[e] = base[e];
+  if (threadIdx.x == 0) a.offsets[a.experts] = sum;
+}
+
+// Second launch: places, the sorted order and the offsets.
+static __global__ __launch_bounds__(kThreads) void k_sort_place(SortArgs a) {
+  extern __shared__ int lds[];
+  __shared__ int sum;
+  block_sort(a, blockIdx.x, lds, &sum, [&](uint32_t i, int place) {
+    a.rows[i] = place;
+    if (place >= 0) a.slots[place] = (int32_t)i;
+  });
+  if (blockIdx.x == 0) write_offsets(a, lds + a.experts, sum);
+  const uint32_t lo = blockIdx.x * a.chunk, hi = min(a.pairs, lo + a.chunk);
+  for (uint32_t i = lo + threadIdx.x; i < hi; i += kThreads)
+    if (i >= (uint32_t)sum) a.slots[i] = -1;
+}
+
+// ---------------------------------------------------------------- rows
+struct RowArgs {
+  const void *x;  // dispatch: token rows; combine: expert rows
+  uint64_t ldx;
+  const void *extra;  // combine: residual; combine_grad: dout
+  uint64_t lde;
+  void *out;
+  uint64_t ldo;
+  const int32_t *rows;
+  const float *weights;
+  float *dweights;
+  uint32_t tokens, nrows;
+  int k;
+  uint32_t features;
+};
+
+// A row is cut into chunks of 16 bytes (VEC) or single elements; TPR threads
+// (64 or 256) work on one token's row.
+template <typename T, bool VEC>
+constexpr int chunk_elems() {
+  return VEC ? Num<T>::kPer16 : 1;
+}
+
+// One token's row to each of its local sorted rows; read once, written up to
+// k times, so a token's row comes from memory once however many experts it
+// has here.
+template <typename T, bool VEC, int TPR>
+__device__ __forceinline__ void push_row(const RowArgs &a, uint32_t t, const int32_t *rows_of) {
+  constexpr int C = chunk_elems<T, VEC>();
+  typedef T vec __attribute__((ext_vector_type(C)));
+  bool any = false;
+  for (int j = 0; j < a.k; ++j) any = any || rows_of[j] >= 0;
+  if (!any) return;
+  const uint32_t chunks = a.features / C;
+  const vec *src = (const vec *)((const T *)a.x + (uint64_t)t * a.ldx);
+  for (uint32_t c = threadIdx.x % TPR; c < chunks; c += TPR) {
+    const vec v = src[c];
+    for (int j = 0; j < a.k; ++j) {
+      const int r = rows_of[j];
+      if (r >= 0) ((vec *)((T *)a.out + (uint64_t)(uint32_t)r * a.ldo))[c] = v;
+    }
+  }
+}
+
+template <typename T, bool VEC, int TPR>
+__global__ __launch_bounds__(kThreads) void k_push(RowArgs a) {
+  const uint32_t t = blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR;
+  if (t >= a.tokens) return;
+  push_row<T, VEC, TPR>(a, t, a.rows + (uint64_t)t * a.k);
+}
+
+// Few pairs: every block sorts all of them for itself and pushes its own
+// tokens, in one launch instead of two.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_dispatch_small(SortArgs s, RowArgs a) {
+  extern __shared__ int lds[];
+  __shared__ int sum;
+  int *mine = lds + (2 + kWaves) * s.experts;  // rows of this block's token
+  const uint32_t t = blockIdx.x;
+  const uint32_t lo = t * (uint32_t)a.k, hi = lo + (uint32_t)a.k;
+  const bool lead = blockIdx.x == 0;
+  block_sort(s, 0, lds, &sum, [&](uint32_t i, int place) {
+    if (i >= lo && i < hi) mine[i - lo] = place;
+    if (lead) {
+      s.rows[i] = place;
+      if (place >= 0) s.slots[place] = (int32_t)i;
+    }
+  });
+  __syncthreads();
+  if (lead) {
+    write_offsets(s, lds + s.experts, sum);
+    for (uint32_t i = threadIdx.x; i < s.pairs; i += kThreads)
+      if (i >= (uint32_t)sum) s.slots[i] = -1;
+  }
+  if (a.x != nullptr && t < a.tokens) push_row<T, VEC, kThreads>(a, t, mine);
+}
+
+// out[t] = sum_j w[t,j] y[rows[t,j]] (+ residual).  The loads of up to
+// kBatch expert rows are issued before the first of them is used.
+constexpr int kBatch = 8;
+
+template <typename T, bool VEC, int TPR>
+__global__ __launch_bounds__(kThreads) void k_combine(RowArgs a) {
+  constexpr int C = chunk_elems<T, VEC>();
+  const uint32_t t = blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR;
+  if (t >= a.tokens) return;
+  const int32_t *rows = a.rows + (uint64_t)t * a.k;
+  const float *w = a.weights == nullptr ? nullptr : a.weights + (uint64_t)t * a.k;
+  const uint32_t chunks = a.features / C;
+  for (uint32_t c = threadIdx.x % TPR; c < chunks; c += TPR) {
+    Pack<T, C, VEC> acc, res;
+#pragma unroll
+    for (int i = 0; i < C; ++i) acc.v[i] = 0.f;
+    if (a.extra != nullptr) res.load((const T *)a.extra + (uint64_t)t * a.lde + c * C);
+    for (int j0 = 0; j0 < a.k; j0 += kBatch) {
+      Pack<T, C, VEC> y[kBatch];
+      bool ok[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int r = j0 + j < a.k ? rows[j0 + j] : -1;
+        ok[j] = r >= 0 && (uint32_t)r < a.nrows;
+        if (ok[j]) y[j].load((const T *)a.x + (uint64_t)(uint32_t)r * a.ldx + c * C);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (!ok[j]) continue;
+        const float wj = w == nullptr ? 1.f : w[j0 + j];
+#pragma unroll
+        for (int i = 0; i < C; ++i) acc.v[i] = __builtin_fmaf(wj, y[j].v[i], acc.v[i]);
+      }
+    }
+    if (a.extra != nullptr) {
+#pragma unroll
+      for (int i = 0; i < C; ++i) acc.v[i] += res.v[i];
+    }
+    acc.store((T *)a.out + (uint64_t)t * a.ldo + c * C);
+  }
+}
+
+// dy[rows[t,j]] = w[t,j] dout[t], dw[t,j] = <dout[t], y[rows[t,j]]>.  A
+// thread's partial products of up to kBatch choices stay in registers; the
+// row's threads join them once a batch.
+template <typename T, bool VEC, int TPR>
+__global__ __launch_bounds__(kThreads) void k_combine_grad(RowArgs a) {
+  constexpr int C = chunk_elems<T, VEC>();
+  __shared__ float part[kWaves][kBatch];
+  const uint32_t t = blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR;
+  const bool live = t < a.tokens;
+  const uint64_t t0 = live ? t : 0;
+  const int32_t *rows = a.rows + t0 * a.k;
+  const float *w = a.weights == nullptr ? nullptr : a.weights + t0 * a.k;
+  const uint32_t chunks = live ? a.features / C : 0;
+  const int wave = threadIdx.x / 64;
+  for (int j0 = 0; j0 < a.k; j0 += kBatch) {
+    float dot[kBatch], wj[kBatch];
+    int r[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      dot[j] = 0.f;
+      r[j] = j0 + j < a.k ? rows[j0 + j] : -1;
+      if (r[j] >= 0 && (uint32_t)r[j] >= a.nrows) r[j] = -1;
+      wj[j] = w == nullptr || r[j] < 0 ? 1.f : w[j0 + j];
+    }
+    for (uint32_t c = threadIdx.x % TPR; c < chunks; c += TPR) {
+      Pack<T, C, VEC> d, y[kBatch], o;
+      d.load((const T *)a.extra + t0 * a.lde + c * C);
+      if (a.dweights != nullptr) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (r[j] >= 0) y[j].load((const T *)a.x + (uint64_t)r[j] * a.ldx + c * C);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (r[j] < 0) continue;
+#pragma unroll
+        for (int i = 0; i < C; ++i) o.v[i] = wj[j] * d.v[i];
+        o.store((T *)a.out + (uint64_t)r[j] * a.ldo + c * C);
+        if (a.dweights != nullptr) {
+#pragma unroll
+          for (int i = 0; i < C; ++i) dot[j] = __builtin_fmaf(d.v[i], y[j].v[i], dot[j]);
+        }
+      }
+    }
+    if (a.dweights == nullptr) continue;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) dot[j] = group_sum<64>(dot[j]);
+    if constexpr (TPR == 64) {
+      const int lane = threadIdx.x % 64;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (live && lane == j && j0 + j < a.k) a.dweights[t0 * a.k + j0 + j] = r[j] < 0 ? 0.f : dot[j];
+    } else {
+      __syncthreads();
+      if (threadIdx.x % 64 == 0) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) part[wave][j] = dot[j];
+      }
+      __syncthreads();
+      const int j = threadIdx.x;
+      if (live && j < kBatch && j0 + j < a.k) {
+        float s = 0.f;
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) s += part[v][j];
+        a.dweights[t0 * a.k + j0 + j] = s;
+      }
+    }
+  }
+}
+
+}  // namespace moe
+}  // namespace llc

@@ -1,0 +1,116 @@
+// Element types and small cross-lane helpers of the expert-layer kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ll_device.hpp"
+
+namespace llc {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Elements as they lie in memory.  Arithmetic is binary32; a store rounds once.
+template <typename T>
+struct Num;
+template <>
+struct Num<float> {
+  static constexpr int kPer16 = 4;
+  static __device__ __forceinline__ float get(float v) { return v; }
+  static __device__ __forceinline__ float put(float v) { return v; }
+};
+template <>
+struct Num<__bf16> {
+  static constexpr int kPer16 = 8;
+  static __device__ __forceinline__ float get(__bf16 v) { return (float)v; }
+  static __device__ __forceinline__ __bf16 put(float v) { return (__bf16)v; }
+};
+
+// N consecutive elements held as binary32.  VEC: the address is aligned to
+// min(16, N * sizeof(T)) bytes.
+template <typename T, int N, bool VEC>
+struct Pack {
+  float v[N];
+  __device__ __forceinline__ void load(const T *p) {
+    if constexpr (VEC) {
+      constexpr int kBytes = N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16;
+      constexpr int kEach = kBytes / (int)sizeof(T);
+      typedef T vec __attribute__((ext_vector_type(kEach)));
+#pragma unroll
+      for (int i = 0; i < N / kEach; ++i) {
+        const vec r = *reinterpret_cast<const vec *>(p + i * kEach);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) v[i * kEach + j] = Num<T>::get(r[j]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = Num<T>::get(p[i]);
+    }
+  }
+  __device__ __forceinline__ void store(T *p) const {
+    if constexpr (VEC) {
+      constexpr int kBytes = N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16;
+      constexpr int kEach = kBytes / (int)sizeof(T);
+      typedef T vec __attribute__((ext_vector_type(kEach)));
+#pragma unroll
+      for (int i = 0; i < N / kEach; ++i) {
+        vec r;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) r[j] = Num<T>::put(v[i * kEach + j]);
+        *reinterpret_cast<vec *>(p + i * kEach) = r;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = Num<T>::put(v[i]);
+    }
+  }
+  // The first n of the N elements (n may be 0 or less); the others read as `fill`.
+  __device__ __forceinline__ void load_some(const T *p, int n, float fill) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = i < n ? Num<T>::get(p[i]) : fill;
+  }
+  __device__ __forceinline__ void store_some(T *p, int n) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = Num<T>::put(v[i]);
+  }
+};
+
+template <int kCtrl>
+__device__ __forceinline__ float dpp_f32(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, true));
+}
+
+// Sum / maximum over each aligned group of W lanes (16 or 64); every lane gets
+// the same bits, since each step adds the same two partial results in both
+// lanes.  Within 16 lanes the partners come from the DPP controls xor 1, xor
+// 2, mirrored halves of 8, mirrored 16.
+template <int W>
+__device__ __forceinline__ float group_sum(float v) {
+  v += dpp_f32<0xB1>(v);
+  v += dpp_f32<0x4E>(v);
+  v += dpp_f32<0x141>(v);
+  v += dpp_f32<0x140>(v);
+  if constexpr (W == 64) {
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+  }
+  return v;
+}
+template <int W>
+__device__ __forceinline__ float group_max(float v) {
+  v = fmaxf(v, dpp_f32<0xB1>(v));
+  v = fmaxf(v, dpp_f32<0x4E>(v));
+  v = fmaxf(v, dpp_f32<0x141>(v));
+  v = fmaxf(v, dpp_f32<0x140>(v));
+  if constexpr (W == 64) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    v = fmaxf(v, __shfl_xor(v, 32));
+  }
+  return v;
+}
+
+}  // namespace llc

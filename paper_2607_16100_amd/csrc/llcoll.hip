@@ -17,6 +17,7 @@
 #include "../../include/lltune.h"
 #include "ll_device.hpp"
 #include "ll_fill.hpp"
+#include "ll_host.hpp"
 #include "ll_iter.hpp"
 #include "ll_layout.hpp"
 #include "ll_probe.hpp"
@@ -1019,6 +1020,27 @@ void plan_allreduce(Plan *pl, ll_algo algo, uint64_t count, int es, int nranks, 
 }  // namespace
 
 // =================================================================== C ABI
+namespace llc {
+
+int hip_failed(hipError_t e) {
+  t_last_hip = (int)e;
+  return LL_ERR_HIP;
+}
+
+int launch_status() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? LL_OK : hip_failed(e);
+}
+
+int device_cus(int *cus) {
+  DevInfo d;
+  const int st = device_info(&d);
+  *cus = d.cus;
+  return st;
+}
+
+}  // namespace llc
+
 extern "C" {
 
 int ll_options_init(ll_options *opt) {

@@ -1,0 +1,318 @@
+"""Expert-layer operators on torch tensors (``include/llmoe.h``).
+
+torch provides memory and the stream; every operator runs in the HIP library.
+A call checks its tensors, launches on the current stream (or ``stream``) and
+returns its outputs, which it allocates unless they are given.  Errors raise
+``llcoll.LLError`` with the C status, or ValueError for tensors that do not
+fit together.  Matrices have unit stride along their last dimension; their
+rows may lie further apart.
+
+What one rank of an expert-parallel layer does between its AllGather and its
+ReduceScatter:
+
+    ids, weights = moe.route(logits, k)
+    plan = moe.Dispatch(tokens, k, local_experts, hidden, dtype, first=first_local_expert)
+    plan.dispatch(ids, x)                                  # plan.x: rows sorted by expert
+    h = moe.linear(plan.x, w_up, act="swiglu", offsets=plan.offsets)
+    y = moe.linear(h, w_down, offsets=plan.offsets)
+    out = moe.combine(y, plan.rows, weights)
+
+``moe.linear`` without offsets is an ordinary dense layer.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import llcoll as ll
+from . import llmoe as lm
+
+_DT = {torch.float32: ll.LL_F32, torch.bfloat16: ll.LL_BF16}
+
+
+def _stream(stream) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _dt(t: torch.Tensor) -> int:
+    dt = _DT.get(t.dtype)
+    if dt is None:
+        raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(t.dtype))
+    return dt
+
+
+def _mat(t: torch.Tensor, name: str, rows=None, cols=None, dtype=None) -> int:
+    """Checks a matrix on the GPU; its leading dimension."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name}: a matrix on the GPU is needed")
+    n, c = t.shape
+    if (rows is not None and n != rows) or (cols is not None and c != cols):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ({rows}, {cols})")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
+    ld, unit = t.stride()
+    if c > 1 and unit != 1:
+        raise ValueError(f"{name}: the last dimension needs unit stride")
+    if n < 2:
+        return max(c, 1)
+    if ld < c:
+        raise ValueError(f"{name}: rows overlap")
+    return max(ld, 1)
+
+
+def _flat(t: torch.Tensor, name: str, numel: int, dtype) -> int:
+    """Checks a contiguous array on the GPU; its address."""
+    if t.numel() != numel or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} array of {numel} elements on the GPU is needed")
+    return t.data_ptr()
+
+
+# ---------------------------------------------------------------- routing
+def route(logits, k: int, *, bias=None, score: str = "softmax", normalise: bool = False, scale: float = 1.0, ids=None,
+          weights=None, stream=None):
+    """(ids int32 [tokens, k], weights float32 [tokens, k]) of the k largest
+    logits + bias a row; see ll_moe_route."""
+    ld = _mat(logits, "logits")
+    t, e = logits.shape
+    if ids is None:
+        ids = torch.empty(t, k, dtype=torch.int32, device=logits.device)
+    if weights is None:
+        weights = torch.empty(t, k, dtype=torch.float32, device=logits.device)
+    ll.check(lm.ll_moe_route(logits.data_ptr(), ld, t, e, k, _dt(logits),
+                             None if bias is None else _flat(bias, "bias", e, torch.float32), lm.SCORES[score],
+                             int(normalise), scale, _flat(ids, "ids", t * k, torch.int32),
+                             _flat(weights, "weights", t * k, torch.float32), _stream(stream)), "ll_moe_route")
+    return ids, weights
+
+
+def route_grad(logits, ids, dweights, *, score: str = "softmax", normalise: bool = False, scale: float = 1.0,
+               out=None, stream=None):
+    """The logits' gradient from the weights' gradient, for the ids that route returned."""
+    ld = _mat(logits, "logits")
+    t, e = logits.shape
+    k = ids.shape[-1]
+    if out is None:
+        out = torch.empty(t, e, dtype=logits.dtype, device=logits.device)
+    ldd = _mat(out, "out", t, e, logits.dtype)
+    ll.check(lm.ll_moe_route_grad(logits.data_ptr(), ld, t, e, k, _dt(logits), lm.SCORES[score], int(normalise),
+                                  scale, _flat(ids, "ids", t * k, torch.int32),
+                                  _flat(dweights, "dweights", t * k, torch.float32), out.data_ptr(), ldd,
+                                  _stream(stream)), "ll_moe_route_grad")
+    return out
+
+
+# ---------------------------------------------------------------- dispatch and combine
+class Dispatch:
+    """Buffers of a dispatch of up to ``tokens`` tokens with ``k`` choices each
+    to the experts [first, first + experts): ``offsets`` [experts + 1],
+    ``slots`` [tokens * k], ``rows`` [tokens, k] and the sorted rows ``x``
+    [tokens * k, features] (``features`` 0: sort only).  After ``dispatch`` of
+    fewer tokens the attributes are views of that many."""
+
+    def __init__(self, tokens: int, k: int, experts: int, features: int, dtype=torch.bfloat16, *, first: int = 0,
+                 device="cuda"):
+        self.capacity, self.k, self.experts, self.first, self.features = tokens, k, experts, first, features
+        st, need = lm.ll_moe_dispatch_bytes(tokens, k, experts)
+        ll.check(st, "ll_moe_dispatch_bytes")
+        n = tokens * k
+        self.offsets = torch.zeros(experts + 1, dtype=torch.int32, device=device)
+        self._slots = torch.empty(n, dtype=torch.int32, device=device)
+        self._rows = torch.empty(n, dtype=torch.int32, device=device)
+        self._x = torch.empty(n, features, dtype=dtype, device=device)
+        # fewer tokens may be cut into more blocks than the capacity is, but never into more than this
+        self._work = torch.empty(max(need, 128 * experts * 4), dtype=torch.uint8, device=device)
+        self._view(tokens)
+
+    def _view(self, tokens: int) -> None:
+        n = tokens * self.k
+        self.tokens = tokens
+        self.slots, self.rows, self.x = self._slots[:n], self._rows[:n].view(tokens, self.k), self._x[:n]
+
+    def dispatch(self, ids, x=None, stream=None):
+        """Sorts the (token, choice) pairs of ``ids`` [tokens, k] and, given the
+        tokens' rows ``x``, copies them in that order; see ll_moe_dispatch."""
+        t = ids.shape[0]
+        if ids.dim() != 2 or ids.shape[1] != self.k or t > self.capacity:
+            raise ValueError(f"ids: shape {tuple(ids.shape)}, expected at most ({self.capacity}, {self.k})")
+        if t != self.tokens:
+            self._view(t)
+        xp = ldx = 0
+        if x is not None:
+            ldx = _mat(x, "x", t, self.features, self._x.dtype)
+            xp = x.data_ptr()
+        ll.check(lm.ll_moe_dispatch(_flat(ids, "ids", t * self.k, torch.int32), t, self.k, self.first, self.experts,
+                                    xp, ldx, self.features, _DT[self._x.dtype], self.offsets.data_ptr(),
+                                    self._slots.data_ptr(), self._rows.data_ptr(), self._x.data_ptr() if xp else 0,
+                                    self.features, self._work.data_ptr(), self._work.numel(), _stream(stream)),
+                 "ll_moe_dispatch")
+        return self
+
+    def grad(self, dx, out=None, stream=None):
+        """The gradient of the tokens' rows from that of the sorted rows."""
+        return combine(dx, self.rows, out=out, stream=stream)
+
+
+def combine(y, rows, weights=None, *, residual=None, out=None, stream=None):
+    """out[t] = residual[t] + sum_j weights[t, j] * y[rows[t, j]]; see ll_moe_combine."""
+    ldy = _mat(y, "y")
+    n, h = y.shape
+    t, k = rows.shape
+    if out is None:
+        out = torch.empty(t, h, dtype=y.dtype, device=y.device)
+    ldo = _mat(out, "out", t, h, y.dtype)
+    rp = ldr = 0
+    if residual is not None:
+        ldr, rp = _mat(residual, "residual", t, h, y.dtype), residual.data_ptr()
+    ll.check(lm.ll_moe_combine(y.data_ptr(), ldy, n, _flat(rows, "rows", t * k, torch.int32),
+                               None if weights is None else _flat(weights, "weights", t * k, torch.float32), rp, ldr,
+                               t, k, h, _dt(y), out.data_ptr(), ldo, _stream(stream)), "ll_moe_combine")
+    return out
+
+
+def combine_grad(dout, y, rows, weights=None, *, dy=None, dweights=None, stream=None):
+    """(dy, dweights) of combine; dweights is None where weights is None.
+    Rows of dy that no token uses are left as they are (zeros in a new one)."""
+    ldd = _mat(dout, "dout")
+    ldy = _mat(y, "y", None, dout.shape[1], dout.dtype)
+    n, h = y.shape
+    t, k = rows.shape
+    if dout.shape[0] != t:
+        raise ValueError(f"dout: {dout.shape[0]} rows, expected {t}")
+    if dy is None:
+        dy = torch.zeros(n, h, dtype=y.dtype, device=y.device)
+    lddy = _mat(dy, "dy", n, h, y.dtype)
+    wp = wg = None
+    if weights is not None:
+        wp = _flat(weights, "weights", t * k, torch.float32)
+        if dweights is None:
+            dweights = torch.empty(t, k, dtype=torch.float32, device=y.device)
+        wg = _flat(dweights, "dweights", t * k, torch.float32)
+    ll.check(lm.ll_moe_combine_grad(dout.data_ptr(), ldd, y.data_ptr(), ldy, n,
+                                    _flat(rows, "rows", t * k, torch.int32), wp, t, k, h, _dt(y), dy.data_ptr(), lddy,
+                                    wg, _stream(stream)), "ll_moe_combine_grad")
+    return dy, dweights
+
+
+# ---------------------------------------------------------------- products
+def _weight(w, offsets, name="w"):
+    """(groups, out, in, leading dimension, group stride) of a weight [out, in] or [groups, out, in]."""
+    if w.dim() == 2:
+        ld = _mat(w, name)
+        return 1, w.shape[0], w.shape[1], ld, w.shape[0] * ld
+    if w.dim() != 3 or not w.is_cuda:
+        raise ValueError(f"{name}: [out, in] or [groups, out, in] on the GPU is needed")
+    g, o, i = w.shape
+    gs, ld, unit = w.stride()
+    if i > 1 and unit != 1:
+        raise ValueError(f"{name}: the last dimension needs unit stride")
+    if o < 2:
+        ld = i
+    if g < 2:
+        gs = o * ld
+    return g, o, i, ld, gs
+
+
+def _offsets(offsets, groups: int):
+    if offsets is None:
+        if groups != 1:
+            raise ValueError("offsets are needed for more than one group")
+        return None
+    return _flat(offsets, "offsets", groups + 1, torch.int32)
+
+
+def _work(d, which: int, device):
+    st, need = lm.ll_linear_bytes(d, which)
+    ll.check(st, "ll_linear_bytes")
+    return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+
+
+def linear(x, w, *, bias=None, act: str = "none", residual=None, offsets=None, out=None, z=None, stream=None):
+    """act(x w^T + bias) + residual, by groups of rows where ``offsets`` is
+    given.  ``z`` [rows, out]: receives the pre-activations.  See ll_linear."""
+    n = x.shape[0]
+    g, o, i, ldw, gs = _weight(w, offsets)
+    ldx = _mat(x, "x", n, i, w.dtype)
+    width = o // 2 if act in lm.GATED else o
+    if out is None:
+        out = torch.empty(n, width, dtype=x.dtype, device=x.device)
+    ldy = _mat(out, "out", n, width, x.dtype)
+    ldr = ldz = max(o, 1)
+    rp = zp = None
+    if residual is not None:
+        ldr, rp = _mat(residual, "residual", n, width, x.dtype), residual.data_ptr()
+    if z is not None:
+        ldz, zp = _mat(z, "z", n, o, x.dtype), z.data_ptr()
+    d = lm.desc(_dt(x), lm.ACTS[act], g, n, i, o, offsets=_offsets(offsets, g), ldx=ldx, ldw=ldw, wstride=gs, ldy=ldy,
+                ldz=ldz, ldr=ldr)
+    ws = _work(d, lm.LL_LINEAR_FORWARD, x.device)
+    ll.check(lm.ll_linear(d, x.data_ptr(), w.data_ptr(),
+                          None if bias is None else _flat(bias, "bias", g * o, x.dtype), rp, out.data_ptr(), zp,
+                          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream(stream)),
+             "ll_linear")
+    return out
+
+
+def linear_grad_x(dz, w, *, act: str = "none", z=None, offsets=None, out=None, stream=None):
+    """dz w, taken on through the activation of the layer below whose
+    pre-activations are ``z``; see ll_linear_grad_x."""
+    n = dz.shape[0]
+    g, o, i, ldw, gs = _weight(w, offsets)
+    ldy = _mat(dz, "dz", n, o, w.dtype)
+    width = 2 * i if act in lm.GATED else i
+    if out is None:
+        out = torch.empty(n, width, dtype=dz.dtype, device=dz.device)
+    ldx = _mat(out, "out", n, width, dz.dtype)
+    ldz, zp = width, None
+    if act != "none":
+        if z is None:
+            raise ValueError("z is needed to go through an activation")
+        ldz, zp = _mat(z, "z", n, width, dz.dtype), z.data_ptr()
+    d = lm.desc(_dt(dz), lm.ACTS[act], g, n, i, o, offsets=_offsets(offsets, g), ldx=ldx, ldw=ldw, wstride=gs,
+                ldy=ldy, ldz=ldz)
+    ws = _work(d, lm.LL_LINEAR_GRAD_X, dz.device)
+    ll.check(lm.ll_linear_grad_x(d, dz.data_ptr(), w.data_ptr(), zp, out.data_ptr(),
+                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                                 _stream(stream)), "ll_linear_grad_x")
+    return out
+
+
+def linear_grad_w(dz, x, *, offsets=None, out=None, bias_out=None, add: bool = False, stream=None):
+    """(dw, dbias): dw [out, in] (or [groups, out, in] with offsets) = dz^T x,
+    dbias its bias gradient where ``bias_out`` is given.  Their type is dz's
+    or float32; ``add`` adds to what they hold.  See ll_linear_grad_w."""
+    n, o = dz.shape
+    ldy = _mat(dz, "dz")
+    ldx = _mat(x, "x", n, None, dz.dtype)
+    i = x.shape[1]
+    groups = 1 if offsets is None else offsets.numel() - 1
+    if out is None:
+        shape = (o, i) if offsets is None else (groups, o, i)
+        out = torch.zeros(shape, dtype=dz.dtype, device=dz.device) if add else torch.empty(
+            shape, dtype=dz.dtype, device=dz.device)
+    g, o2, i2, ldw, gs = _weight(out, offsets, "out")
+    if (g, o2, i2) != (groups, o, i) or out.dtype not in (dz.dtype, torch.float32):
+        raise ValueError(f"out: {tuple(out.shape)} {out.dtype}, expected ({groups}, {o}, {i})")
+    flags = (lm.LL_GRAD_F32 if out.dtype == torch.float32 else 0) | (lm.LL_GRAD_ADD if add else 0)
+    bp = None if bias_out is None else _flat(bias_out, "bias_out", g * o, out.dtype)
+    d = lm.desc(_dt(dz), lm.LL_ACT_NONE, g, n, i, o, offsets=_offsets(offsets, g), ldx=ldx, ldw=ldw, wstride=gs,
+                ldy=ldy)
+    ws = _work(d, lm.LL_LINEAR_GRAD_W, dz.device)
+    ll.check(lm.ll_linear_grad_w(d, dz.data_ptr(), x.data_ptr(), out.data_ptr(), bp, flags,
+                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                                 _stream(stream)), "ll_linear_grad_w")
+    return out, bias_out
+
+
+def act_grad(dy, z, act: str, *, out=None, stream=None):
+    """The gradient of an activation's output taken to its pre-activations z."""
+    ldy = _mat(dy, "dy")
+    n, h = dy.shape
+    width = 2 * h if act in lm.GATED else h
+    ldz = _mat(z, "z", n, width, dy.dtype)
+    if out is None:
+        out = torch.empty(n, width, dtype=dy.dtype, device=dy.device)
+    ldo = _mat(out, "out", n, width, dy.dtype)
+    ll.check(lm.ll_act_grad(dy.data_ptr(), ldy, z.data_ptr(), ldz, n, h, _dt(dy), lm.ACTS[act], out.data_ptr(), ldo,
+                            _stream(stream)), "ll_act_grad")
+    return out

@@ -1,0 +1,305 @@
+"""Grouped matrix products and their gradients on the GPU against plain 64-bit forms."""
+from __future__ import annotations
+
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import moeref as ref  # noqa: E402
+from test_moe_gpu import gen, randn, strided  # noqa: E402
+
+if torch.cuda.is_available():
+    from paper_2607_16100_amd import moe  # noqa: E402
+else:  # pragma: no cover
+    pytest.skip("no GPU", allow_module_level=True)
+
+F32, BF16 = torch.float32, torch.bfloat16
+DEV = "cuda"
+
+# rows a group, or None for one group of `rows` without offsets; in, out
+SHAPES = {
+    "one": (None, 1, 1, 2),
+    "token": (None, 1, 512, 256),
+    "small": (None, 5, 72, 40),
+    "tile": (None, 128, 64, 128),
+    "dense": (None, 301, 264, 520),
+    "odd": (None, 33, 101, 66),
+    "deep": (None, 17, 4096, 64),
+    "groups": ([3, 0, 1, 0, 130, 64, 0], 0, 136, 144),
+    "decode": ([1, 0, 2, 0, 0, 1, 1, 3], 0, 1024, 384),
+    "sixteens": ([16, 17, 15, 32, 33, 48, 0, 1], 0, 320, 192),
+    "many": ([5] * 70 + [0] * 30 + [1] * 29, 0, 40, 24),
+    "skew": ([0, 600, 1], 0, 200, 72),
+    "oddgroups": ([7, 0, 90], 0, 51, 34),
+    "wide": ([2, 260], 0, 96, 1030),
+}
+
+
+def case(name, dtype, seed):
+    counts, rows, i, o = SHAPES[name]
+    g = gen(seed)
+    if counts is None:
+        offsets, n, groups, extra = None, rows, 1, 0
+    else:
+        extra = 3  # rows that belong to no group
+        n, groups = sum(counts) + extra, len(counts)
+        offsets = torch.tensor([sum(counts[:c]) for c in range(groups + 1)], dtype=torch.int32, device=DEV)
+    w = randn(g, groups, o, i, dtype=dtype) if offsets is not None else randn(g, o, i, dtype=dtype)
+    return g, n, groups, i, o, offsets, extra, w
+
+
+def weight(w, g):
+    return (w if w.dim() == 2 else w[g]).double()
+
+
+LAYOUTS = [(0, 0), (3, 1), (8, 0)]  # row padding, first element; NaN in the padding
+
+
+@pytest.mark.parametrize("name", list(SHAPES))
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act,bias,residual,save,layout", [
+    ("none", False, False, False, 0), ("relu", True, False, True, 1), ("gelu", True, True, False, 2),
+    ("silu", False, True, True, 0), ("swiglu", True, True, True, 0), ("geglu", False, False, True, 1)])
+def test_forward(name, dtype, act, bias, residual, save, layout):
+    g, n, groups, i, o, offsets, extra, w = case(name, dtype, 11)
+    pad, lead = LAYOUTS[layout]
+    x = strided(randn(g, n, i, dtype=dtype), pad, lead)
+    if extra:
+        x[-extra:] = math.nan  # of no group: must not reach any result
+    b = randn(g, groups, o, dtype=dtype) if bias else None
+    width = o // 2 if act in ref.GATED else o
+    res = strided(randn(g, n, width, dtype=dtype), pad, lead) if residual else None
+    out = torch.full((n, width), 9.0, dtype=dtype, device=DEV)
+    z = torch.full((n, o), 9.0, dtype=dtype, device=DEV) if save else None
+    moe.linear(x, w, bias=b, act=act, residual=res, offsets=offsets, out=out, z=z)
+    for gi, lo, hi in ref.spans(offsets, n):
+        zz, ez = ref.matmul(x[lo:hi].double(), weight(w, gi).t())
+        if bias:
+            zz = zz + b[gi].double()
+            ez = ez + ref.EPS * zz.abs()
+        want, err = ref.act(zz, act), ref.act_err(zz, ez, act)
+        if residual:
+            want = want + res[lo:hi].double()
+            err = err + ref.EPS * want.abs()
+        ref.close(out[lo:hi], want, err, dtype)
+        if save:
+            ref.close(z[lo:hi], zz, ez, dtype)
+    if extra:
+        assert bool((out[-extra:] == 9.0).all()) and (z is None or bool((z[-extra:] == 9.0).all()))
+
+
+@pytest.mark.parametrize("name", list(SHAPES))
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act,layout", [("none", 0), ("relu", 1), ("gelu", 2), ("silu", 0), ("swiglu", 0),
+                                        ("geglu", 1)])
+def test_grad_x(name, dtype, act, layout):
+    g, n, groups, i, o, offsets, extra, w = case(name, dtype, 12)
+    pad, lead = LAYOUTS[layout]
+    dz = strided(randn(g, n, o, dtype=dtype), pad, lead)
+    if extra:
+        dz[-extra:] = math.nan
+    width = 2 * i if act in ref.GATED else i
+    z = strided(randn(g, n, width, dtype=dtype), pad, lead) if act != "none" else None
+    out = torch.full((n, width), 9.0, dtype=dtype, device=DEV)
+    moe.linear_grad_x(dz, w, act=act, z=z, offsets=offsets, out=out)
+    for gi, lo, hi in ref.spans(offsets, n):
+        da, ea = ref.matmul(dz[lo:hi].double(), weight(w, gi))
+        if act == "none":
+            ref.close(out[lo:hi], da, ea, dtype)
+        else:
+            zz = z[lo:hi].double()
+            ref.close(out[lo:hi], ref.through(da, zz, act), ref.through_err(da, ea, zz, act), dtype)
+    if extra:
+        assert bool((out[-extra:] == 9.0).all())
+
+
+@pytest.mark.parametrize("name", list(SHAPES))
+@pytest.mark.parametrize("dtype,grad", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("add,bias,layout", [(False, True, 0), (True, True, 1), (False, False, 2), (True, False, 0)])
+def test_grad_w(name, dtype, grad, add, bias, layout):
+    g, n, groups, i, o, offsets, extra, _ = case(name, dtype, 13)
+    pad, lead = LAYOUTS[layout]
+    dz = strided(randn(g, n, o, dtype=dtype), pad, lead)
+    x = strided(randn(g, n, i, dtype=dtype), pad, lead)
+    if extra:
+        dz[-extra:] = math.nan
+        x[-extra:] = math.nan
+    shape = (o, i) if offsets is None else (groups, o, i)
+    dw = randn(g, *shape, dtype=grad) if add else torch.full(shape, math.nan, dtype=grad, device=DEV)
+    db = None
+    if bias:
+        db = randn(g, groups, o, dtype=grad) if add else torch.full((groups, o), math.nan, dtype=grad, device=DEV)
+    old_w, old_b = dw.clone(), None if db is None else db.clone()
+    moe.linear_grad_w(dz, x, offsets=offsets, out=dw, bias_out=db, add=add)
+    for gi, lo, hi in ref.spans(offsets, n):
+        want, err = ref.matmul(dz[lo:hi].double().t(), x[lo:hi].double())
+        got = dw if offsets is None else dw[gi]
+        if add:
+            want = want + (old_w if offsets is None else old_w[gi]).double()
+            err = err + ref.EPS * want.abs()
+        ref.close(got, want, err, grad)
+        if bias:
+            d = dz[lo:hi].double()
+            want, err = d.sum(0), (hi - lo + 2) * ref.EPS * d.abs().sum(0)
+            if add:
+                want = want + old_b[gi].double()
+                err = err + ref.EPS * want.abs()
+            ref.close(db[gi], want, err, grad)
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu", "swiglu", "geglu"])
+@pytest.mark.parametrize("dtype,h,pad", [(F32, 33, 0), (BF16, 64, 8), (F32, 8, 1)])
+def test_act_grad(act, dtype, h, pad):
+    g = gen(14)
+    dy = strided(randn(g, 37, h, dtype=dtype), pad)
+    z = strided(3 * randn(g, 37, 2 * h if act in ref.GATED else h, dtype=dtype), pad)
+    got = moe.act_grad(dy, z, act)
+    want = ref.through(dy.double(), z.double(), act)
+    ref.close(got, want, ref.through_err(dy.double(), torch.zeros_like(dy.double()), z.double(), act), dtype)
+    moe.act_grad(dy, z, act, out=z)
+    assert torch.equal(z, got)
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu", "swiglu", "geglu"])
+def test_gradients_against_differences(act):
+    """loss = sum(c * linear(act(z0), w)): grad_x and grad_w against central differences."""
+    g = gen(15)
+    n, i, o = 6, 12, 10
+    wide = 2 * i if act in ref.GATED else i
+    z0, w, c = randn(g, n, wide), randn(g, o, i), randn(g, n, o)
+    x = ref.act(z0.double(), act)
+    dx = moe.linear_grad_x(c, w, act=act, z=z0).double()
+    dw, _ = moe.linear_grad_w(c, x.float())
+
+    def loss(zz, ww):
+        return (c.double() * (ref.act(zz, act) @ ww.t())).sum()
+
+    h = 1e-5
+    size = float((c.double().abs() @ w.double().abs()).max()) * 4
+    for r, col in ((0, 0), (3, i - 1), (5, wide - 1), (2, wide // 2)):
+        e = torch.zeros_like(z0, dtype=torch.float64)
+        e[r, col] = h
+        num = (loss(z0.double() + e, w.double()) - loss(z0.double() - e, w.double())) / (2 * h)
+        assert abs(float(dx[r, col] - num)) <= 1e-7 + 200 * ref.EPS * size
+    for r, col in ((0, 0), (o - 1, i - 1)):
+        e = torch.zeros_like(w, dtype=torch.float64)
+        e[r, col] = h
+        num = (loss(z0.double(), w.double() + e) - loss(z0.double(), w.double() - e)) / (2 * h)
+        assert abs(float(dw[r, col] - num)) <= 1e-7 + 200 * ref.EPS * size
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_strided_weights_and_inplace_residual(dtype):
+    g = gen(16)
+    off = torch.tensor([0, 40, 40, 77], dtype=torch.int32, device=DEV)
+    buf = torch.full((3, 60, 144), math.nan, dtype=dtype, device=DEV)
+    w = buf[:, :56, :128]
+    w.copy_(randn(g, 3, 56, 128, dtype=dtype))
+    x, y = randn(g, 77, 128, dtype=dtype), randn(g, 77, 56, dtype=dtype)
+    want = moe.linear(x, w.contiguous(), residual=y, offsets=off)
+    moe.linear(x, w, residual=y, offsets=off, out=y)
+    assert torch.equal(y, want)
+    assert torch.equal(moe.linear_grad_x(y, w, offsets=off), moe.linear_grad_x(y, w.contiguous(), offsets=off))
+    dw, _ = moe.linear_grad_w(y, x, offsets=off)
+    out = buf.clone()
+    moe.linear_grad_w(y, x, offsets=off, out=out[:, :56, :128])
+    assert torch.equal(out[:, :56, :128], dw)
+    assert bool(torch.isnan(out[:, 56:]).all()) and bool(torch.isnan(out[:, :, 128:]).all())
+
+
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_nan_and_infinity_stay_in_their_rows(rows):
+    g = gen(17)
+    x, w = randn(g, rows, 200, dtype=BF16), randn(g, 96, 200, dtype=BF16)
+    clean = moe.linear(x, w)
+    x[rows // 2, 7] = math.nan
+    got = moe.linear(x, w)
+    bad = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    bad[rows // 2] = True
+    assert bool(torch.isnan(got[bad]).all()) and torch.equal(got[~bad], clean[~bad])
+    w[5, 3] = math.inf
+    got = moe.linear(x, w)
+    keep = [c for c in range(96) if c != 5]
+    assert torch.equal(got[~bad][:, keep], clean[~bad][:, keep])
+
+
+def test_rows_past_32_bit_offsets():
+    """A group whose rows lie past 2^32 bytes of x, y and z."""
+    n, i, o = (1 << 32) // 16384 + 300, 8192, 64
+    x = torch.zeros(n, i, dtype=BF16, device=DEV)
+    x[-200:] = randn(gen(18), 200, i, dtype=BF16)
+    w = randn(gen(19), 2, o, i, dtype=BF16)
+    off = torch.tensor([0, n - 150, n], dtype=torch.int32, device=DEV)
+    got = moe.linear(x, w, offsets=off)
+    small = torch.tensor([0, 50, 200], dtype=torch.int32, device=DEV)
+    want = moe.linear(x[-200:].clone(), w, offsets=small)
+    assert torch.equal(got[-200:], want) and not bool(got[:-200].any())
+    dw, _ = moe.linear_grad_w(got, x, offsets=off)
+    z, ez = ref.matmul(got[-150:].double().t(), x[-150:].double())
+    ref.close(dw[1], z, ez, BF16)
+    dx = moe.linear_grad_x(got, w, offsets=off)
+    z, ez = ref.matmul(got[-150:].double(), w[1].double())
+    ref.close(dx[-150:], z, ez, BF16)
+    assert not bool(dx[:-200].any())
+
+
+def test_results_do_not_depend_on_timing():
+    g = gen(20)
+    off = torch.tensor([0, 100, 130, 500], dtype=torch.int32, device=DEV)
+    x, w = randn(g, 500, 1024, dtype=BF16), randn(g, 3, 512, 1024, dtype=BF16)
+    first = moe.linear(x, w, act="swiglu", offsets=off)
+    dz = randn(g, 500, 512, dtype=BF16)
+    dw, _ = moe.linear_grad_w(dz, x, offsets=off)
+    for _ in range(5):
+        assert torch.equal(moe.linear(x, w, act="swiglu", offsets=off), first)
+        assert torch.equal(moe.linear_grad_w(dz, x, offsets=off)[0], dw)
+
+
+def test_on_another_stream_and_in_a_graph():
+    g = gen(21)
+    off = torch.tensor([0, 3, 3, 10], dtype=torch.int32, device=DEV)
+    x, w1, w2 = randn(g, 12, 256, dtype=BF16), randn(g, 3, 128, 256, dtype=BF16), randn(g, 3, 256, 64, dtype=BF16)
+    h, y = torch.zeros(12, 64, dtype=BF16, device=DEV), torch.zeros(12, 256, dtype=BF16, device=DEV)
+
+    def mlp():
+        moe.linear(x, w1, act="swiglu", offsets=off, out=h)
+        moe.linear(h, w2, offsets=off, out=y)
+
+    mlp()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        mlp()
+    for seed in range(3):
+        x.copy_(randn(gen(30 + seed), 12, 256, dtype=BF16))
+        off.copy_(torch.tensor([0, seed, 5, 9 + seed], dtype=torch.int32))
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        y.zero_()
+        mlp()
+        torch.cuda.synchronize()
+        assert torch.equal(got, y)
+
+
+def test_refusals():
+    x = torch.zeros(4, 8, device=DEV)
+    w = torch.zeros(2, 6, 8, device=DEV)
+    off = torch.tensor([0, 2, 4], dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError):
+        moe.linear(x, w)  # two groups need offsets
+    with pytest.raises(ValueError):
+        moe.linear(x, w, offsets=off[:2].contiguous())
+    with pytest.raises(ValueError):
+        moe.linear(x.bfloat16(), w, offsets=off)
+    with pytest.raises(ValueError):
+        moe.linear_grad_x(torch.zeros(4, 6, device=DEV), w, act="gelu", offsets=off)
+    with pytest.raises(KeyError):
+        moe.linear(x, w, offsets=off, act="tanh")
