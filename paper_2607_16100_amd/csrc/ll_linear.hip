@@ -51,38 +51,53 @@ int check_rows(const void *p, size_t ld, size_t len, int es, bool any) {
 
 using tile_fn = void (*)(Args);
 
-template <typename T, Pass PASS, int BM, int BN, int WM, int WN>
-tile_fn pick(bool gate, bool vec) {
+template <typename T, Pass PASS, int B, int WM, int WN, bool VEC>
+tile_fn pick(bool gate) {
   if constexpr (PASS == kForward) {
-    if (gate)
-      return vec ? k_tile<T, PASS, BM, BN, WM, WN, true, true> : k_tile<T, PASS, BM, BN, WM, WN, true, false>;
+    if (gate) return k_tile<T, PASS, B, B, WM, WN, true, VEC>;
   }
-  return vec ? k_tile<T, PASS, BM, BN, WM, WN, false, true> : k_tile<T, PASS, BM, BN, WM, WN, false, false>;
+  return k_tile<T, PASS, B, B, WM, WN, false, VEC>;
 }
 
-template <Pass PASS>
-int launch_tiles(Args &a, ll_dtype dt, bool gate, bool vec, void *stream) {
-  constexpr int kB = 128;
+template <typename T, Pass PASS, int B, int WM, int WN, bool VEC>
+int launch_tiles(Args &a, bool gate, void *stream) {
   const uint32_t width = gate ? a.n / 2 : a.n;
-  const uint32_t per_n = gate ? kB / 2 : kB;
+  const uint32_t per_n = gate ? B / 2 : B;
   a.tiles_n = (width + per_n - 1) / per_n;
   uint64_t tiles;
   if (PASS == kGradW) {
-    a.tiles_m = (a.m + kB - 1) / kB;
+    a.tiles_m = (a.m + B - 1) / B;
     tiles = (uint64_t)a.tiles_m * a.groups;
   } else {
     // every group with rows may add one partial tile
-    tiles = a.offsets == nullptr ? (a.rows + kB - 1) / kB : a.rows / kB + std::min<uint64_t>(a.groups, a.rows);
+    tiles = a.offsets == nullptr ? (a.rows + B - 1) / B : a.rows / B + std::min<uint64_t>(a.groups, a.rows);
   }
   const uint64_t grid = tiles * a.tiles_n;
-  if (grid * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
-  const tile_fn fn = dt == LL_F32 ? pick<float, PASS, kB, kB, 2, 2>(gate, vec) : pick<__bf16, PASS, kB, kB, 2, 2>(gate, vec);
-  hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
+  constexpr int kThreads = WM * WN * 64;
+  if (grid * kThreads >= 1ull << 32) return LL_ERR_UNSUPPORTED;
+  const tile_fn fn = pick<T, PASS, B, WM, WN, VEC>(gate);
+  hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)stream, a);
   return launch_status();
 }
 
-// Four consecutive elements at multiples of 4 are aligned in every row.
-bool four(const void *p, size_t ld, int es) { return p == nullptr || (aligned(p, 4 * es) && ld % 4 == 0); }
+template <Pass PASS>
+int launch_product(Args &a, ll_dtype dt, bool gate, bool vec, void *stream) {
+  // rows that are not whole 16-byte chunks pass through registers, which eight
+  // waves have enough of
+  if (!vec)
+    return dt == LL_F32 ? launch_tiles<float, PASS, 128, 2, 4, false>(a, gate, stream)
+                        : launch_tiles<__bf16, PASS, 128, 2, 4, false>(a, gate, stream);
+  if (dt == LL_F32) return launch_tiles<float, PASS, 128, 2, 2, true>(a, gate, stream);
+  // 256-wide tiles move half the operand bytes of 128-wide ones but need many
+  // tiles to fill the chip (binary32 is bound by its matrix instructions,
+  // which are 16 times slower, with either)
+  const uint64_t m256 = PASS == kGradW ? (uint64_t)((a.m + 255) / 256) * a.groups : (a.rows + 255) / 256;
+  if (m256 * ((a.n + 255) / 256) >= 256) return launch_tiles<__bf16, PASS, 256, 2, 4, true>(a, gate, stream);
+  return launch_tiles<__bf16, PASS, 128, 2, 2, true>(a, gate, stream);
+}
+
+// Every row starts at a 16-byte address.
+bool rows16(const void *p, size_t ld, int es) { return p == nullptr || (aligned(p, 16) && ld * es % 16 == 0); }
 bool chunked(const void *p, size_t ld, size_t len, int es) {
   return aligned(p, 16) && ld * es % 16 == 0 && len * es % 16 == 0;
 }
@@ -159,10 +174,11 @@ int ll_linear(const ll_linear_desc *d, const void *x, const void *w, const void 
   a.c = y;
   a.ldc = d->ldy;
   a.act = (int)d->act;
-  a.vec_c = four(y, d->ldy, es) && four(z, d->ldz, es) && four(residual, d->ldr, es);
+  a.vec_b = rows16(bias, d->out, es);
+  a.vec_c = rows16(y, d->ldy, es) && rows16(z, d->ldz, es) && rows16(residual, d->ldr, es);
   const bool vec = chunked(x, d->ldx, d->in, es) && chunked(w, d->ldw, d->in, es) && d->wstride * es % 16 == 0 &&
                    d->out * d->ldw * es < 0xF0000000ull;
-  return launch_tiles<kForward>(a, d->dt, gate, vec, stream);
+  return launch_product<kForward>(a, d->dt, gate, vec, stream);
 }
 
 int ll_linear_grad_x(const ll_linear_desc *d, const void *dz, const void *w, const void *z, void *dx, void *workspace,
@@ -199,9 +215,9 @@ int ll_linear_grad_x(const ll_linear_desc *d, const void *dz, const void *w, con
   a.c = dx;
   a.ldc = d->ldx;
   a.act = (int)d->act;
-  a.vec_c = four(dx, d->ldx, es) && four(z, d->ldz, es);
+  a.vec_c = rows16(dx, d->ldx, es) && rows16(z, d->ldz, es);
   const bool vec = chunked(dz, d->ldy, d->out, es) && chunked(w, d->ldw, d->in, es) && d->wstride * es % 16 == 0;
-  return launch_tiles<kGradX>(a, d->dt, false, vec, stream);
+  return launch_product<kGradX>(a, d->dt, false, vec, stream);
 }
 
 int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, void *dw, void *dbias, uint32_t flags,
@@ -238,10 +254,17 @@ int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, voi
   a.dbias = dbias;
   a.flags = flags;
   // the gradient's own element size decides its alignment
-  a.vec_c = four(dw, d->ldw, gs) && d->wstride % 4 == 0;
+  a.vec_c = rows16(dw, d->ldw, gs) && d->wstride * gs % 16 == 0;
   const bool vec = chunked(dz, d->ldy, d->out, es) && chunked(x, d->ldx, d->in, es);
   a.k = a.rows;
-  return launch_tiles<kGradW>(a, d->dt, false, vec, stream);
+  if (dbias != nullptr) {
+    const bool rows_vec = chunked(dz, d->ldy, d->out, es);
+    const auto fn = d->dt == LL_F32 ? (rows_vec ? k_bias_grad<float, true> : k_bias_grad<float, false>)
+                                    : (rows_vec ? k_bias_grad<__bf16, true> : k_bias_grad<__bf16, false>);
+    const unsigned cols = 16 * (rows_vec ? 16 / es : 1);
+    hipLaunchKernelGGL(fn, dim3((a.m + cols - 1) / cols, a.groups), dim3(1024), 0, (hipStream_t)stream, a);
+  }
+  return launch_product<kGradW>(a, d->dt, false, vec, stream);
 }
 
 int ll_act_grad(const void *dy, size_t lddy, const void *z, size_t ldz, size_t rows, size_t features, ll_dtype dt,

@@ -8,14 +8,15 @@
 // along m or n ("RM": a row is one k).
 //
 // A workgroup owns a BM x BN tile of C, in registers.  Both operands pass
-// through LDS in steps of 128 bytes of k (KM) or of BK rows (RM), loaded
-// straight from memory into LDS.  The matrix instruction takes Q as its first
-// operand, so a lane ends up with four consecutive n of one m: rows of C are
-// written 8 or 16 bytes at a time.
+// through LDS in stages of 32 (bf16) or 16 (binary32) k, loaded straight from
+// memory into LDS.  The matrix instruction takes Q as its first operand, so a
+// lane ends up with four consecutive n of one m.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "../../include/llmoe.h"
 #include "ll_num.hpp"
@@ -39,7 +40,8 @@ struct Args {
   void *c, *zout, *dbias;
   int act;
   uint32_t flags;  // LL_GRAD_*
-  bool vec_c;      // four consecutive elements of every epilogue row are aligned
+  bool vec_c;      // every epilogue row starts at a 16-byte address
+  bool vec_b;      // so does every group's bias
 };
 
 // ---------------------------------------------------------------- activations
@@ -75,65 +77,108 @@ __device__ __forceinline__ float slope1(float x, int act) {
 }
 __host__ __device__ constexpr bool gated(int act) { return act == LL_ACT_SWIGLU || act == LL_ACT_GEGLU; }
 
-// ---------------------------------------------------------------- groups
-// Row tile `rt` of the grouped rows: its group, its first row and the end of
-// the group's rows.  false: past the last tile.  Every lane of the calling
-// wave takes part; the offsets are clamped to the rows there are.
-__device__ __forceinline__ bool find_rows(const Args &a, uint32_t rt, uint32_t bm, int *group, uint32_t *row0,
-                                          uint32_t *row1) {
-  if (a.offsets == nullptr) {
-    *group = 0;
-    *row0 = rt * bm;
-    *row1 = a.rows;
-    return *row0 < a.rows;
-  }
+// ---------------------------------------------------------------- which tile
+//
+// Workgroups go to the 8 XCDs in turn, each with an L2 of its own, so XCD x
+// takes the x-th run of consecutive tiles.  Within a run tiles are numbered
+// in bands of kBand row tiles, column by column: the 32 workgroups an XCD
+// runs at a time then share a few panels of each operand.
+constexpr uint32_t kBand = 4;
+
+__device__ __forceinline__ bool tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t *tm, uint32_t *tn) {
+  const uint32_t total = tiles_m * tiles_n;
+  if (id >= total) return false;
+  const uint32_t x = id % 8, each = total / 8, more = total % 8;
+  const uint32_t t = x * each + min(x, more) + id / 8;
+  const uint32_t band = t / (kBand * tiles_n), in_band = t % (kBand * tiles_n);
+  const uint32_t high = min(kBand, tiles_m - band * kBand);
+  *tm = band * kBand + in_band % high;
+  *tn = in_band / high;
+  return true;
+}
+
+// Rows [lo, hi) of group g; clamped to the rows there are.
+__device__ __forceinline__ void group_rows(const Args &a, int g, uint32_t *lo, uint32_t *hi) {
+  *lo = 0;
+  *hi = a.rows;
+  if (a.offsets == nullptr) return;
+  *lo = (uint32_t)min(max(a.offsets[g], 0), (int)a.rows);
+  *hi = (uint32_t)min(max(a.offsets[g + 1], (int)*lo), (int)a.rows);
+}
+
+// Inclusive sums of the row tiles of groups g0 .. g0 + 63, one a lane.
+__device__ __forceinline__ uint32_t scan_tiles(const Args &a, int g0, uint32_t bm, uint32_t *lo, uint32_t *hi,
+                                               uint32_t *tiles) {
   const int lane = threadIdx.x % 64;
+  *lo = *hi = 0;
+  if (g0 + lane < a.groups) group_rows(a, g0 + lane, lo, hi);
+  *tiles = (*hi - *lo + bm - 1) / bm;
+  uint32_t incl = *tiles;
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t up = __shfl_up(incl, d);
+    if (lane >= d) incl += up;
+  }
+  return incl;
+}
+
+// The tile of workgroup `id` among the grouped rows: its group, first row, end
+// of the group's rows, and column tile.  false: there is none.  Every lane of
+// the calling wave takes part.
+__device__ __forceinline__ bool find_rows(const Args &a, uint32_t id, uint32_t bm, int *group, uint32_t *row0,
+                                          uint32_t *row1, uint32_t *tn) {
+  uint32_t tm;
+  if (a.offsets == nullptr) {
+    if (!tile_of(id, (a.rows + bm - 1) / bm, a.tiles_n, &tm, tn)) return false;
+    *group = 0;
+    *row0 = tm * bm;
+    *row1 = a.rows;
+    return true;
+  }
+  uint32_t lo, hi, tiles, incl = 0, total = 0;
+  for (int g0 = 0; g0 < a.groups; g0 += 64) {
+    incl = scan_tiles(a, g0, bm, &lo, &hi, &tiles);
+    total += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+  }
+  if (!tile_of(id, total, a.tiles_n, &tm, tn)) return false;
   uint32_t before = 0;
   for (int g0 = 0; g0 < a.groups; g0 += 64) {
-    const int g = g0 + lane;
-    uint32_t lo = 0, hi = 0;
-    if (g < a.groups) {
-      lo = (uint32_t)min(max(a.offsets[g], 0), (int)a.rows);
-      hi = (uint32_t)min(max(a.offsets[g + 1], (int)lo), (int)a.rows);
-    }
-    const uint32_t tiles = (hi - lo + bm - 1) / bm;
-    uint32_t incl = tiles;
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t up = __shfl_up(incl, d);
-      if (lane >= d) incl += up;
-    }
-    const uint64_t past = __ballot(before + incl > rt);
+    if (a.groups > 64) incl = scan_tiles(a, g0, bm, &lo, &hi, &tiles);
+    const uint64_t past = __ballot(before + incl > tm);
     if (past != 0) {
       const int who = __ffsll((unsigned long long)past) - 1;
-      const uint32_t first = __shfl(before + incl - tiles, who);
-      *group = __builtin_amdgcn_readfirstlane(g0 + who);
-      *row0 = __builtin_amdgcn_readfirstlane(__shfl(lo, who) + (rt - first) * bm);
-      *row1 = __builtin_amdgcn_readfirstlane(__shfl(hi, who));
+      const uint32_t first = before + __builtin_amdgcn_readlane((int)(incl - tiles), who);
+      *group = g0 + who;
+      *row0 = __builtin_amdgcn_readlane((int)lo, who) + (tm - first) * bm;
+      *row1 = __builtin_amdgcn_readlane((int)hi, who);
       return true;
     }
-    before += __shfl(incl, 63);
+    before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
   }
   return false;
 }
 
-// ---------------------------------------------------------------- operand tiles in LDS
+// ---------------------------------------------------------------- operand stages in LDS
 //
-// A tile holds R entries of m or n by BK of k in R * 128 bytes, as 16-byte
-// chunks.  KM: entry r's 8 chunks at r * 128, chunk c at position c ^ (r & 7),
-// so the 16 entries a fragment read touches spread over the banks.  RM: k row
-// r's chunks at r * R * sizeof(T), chunk c at position c ^ swz(r), which keeps
-// pairs (bf16) or fours (binary32) of chunks together, as one fragment reads
-// them, and spreads the k rows of a read over the banks.
+// A stage holds R entries of m or n by 128 bytes of k in R * 128 bytes, as
+// 16-byte chunks.  KM: entry r's 8 chunks at r * 128, chunk c at position c ^
+// (r & 7), so that 8 lanes that read one chunk of 8 entries touch 8 different
+// 16-byte columns.  128 bytes of k at a time, because a load of half a cache
+// line costs L2 as much as a whole one: with stages of 64 bytes the forward
+// product of 8192^3 took 892 us against 768 for grad_x, one of whose operands
+// is loaded in longer rows.  RM: k row r's chunks at r * R * sizeof(T), chunk c
+// at position c ^ swz(r), which keeps pairs (bf16) or fours (binary32) of
+// chunks together, as one fragment reads them, and spreads the k rows of a
+// read over the banks.
 template <typename T>
 struct Step;
 template <>
 struct Step<__bf16> {
-  static constexpr int kBK = 64, kPerMma = 32;
+  static constexpr int kBK = 64, kMma = 32;  // a 16x16x32 instruction per half of a stage
   typedef bf16x8 frag;
 };
 template <>
 struct Step<float> {
-  static constexpr int kBK = 32, kPerMma = 16;  // four 16x16x4 instructions
+  static constexpr int kBK = 32, kMma = 16;  // four 16x16x4 instructions
   typedef f32x4 frag;
 };
 
@@ -146,38 +191,44 @@ __device__ __forceinline__ uint32_t rm_swz(uint32_t krow) {
     return (((krow >> 2) & 3) << 2) & kMask;
 }
 
-typedef __attribute__((address_space(3))) char lds_char;
-
+// A fragment of half ks of a stage: lane (i, q) = (lane % 16, lane / 16) holds
+// entry dim0 + i at k = ks * kMma + q * kMma / 4 + 0 .. kMma / 4 - 1.  frag_off
+// is where a lane's part of it starts in an operand's stage; RM: the second
+// half lies kMma k rows further on, with the same swizzle.
 template <typename T, int R, bool KM>
-__device__ __forceinline__ typename Step<T>::frag read_frag(const char *tile, int dim0, int ks) {
-  const int lane = threadIdx.x % 64, i = lane % 16, q = lane / 16;
+__device__ __forceinline__ uint32_t frag_off(uint32_t dim0, int ks) {
+  const uint32_t lane = threadIdx.x % 64, i = lane % 16, q = lane / 16;
   if constexpr (KM) {
-    const int r = dim0 + i, chunk = ks * 4 + q;
-    return *reinterpret_cast<const typename Step<T>::frag *>(tile + r * 128 + ((chunk ^ (r & 7)) << 4));
+    const uint32_t r = dim0 + i, chunk = ks * 4 + q;
+    return r * 128 + ((chunk ^ (r & 7)) << 4);
+  } else if constexpr (sizeof(T) == 2) {
+    const uint32_t krow = q * 8 + i / 4, chunk = dim0 / 8 + (i % 4) / 2;
+    return (ks * 32 + krow) * (R * 2) + ((chunk ^ rm_swz<T, R>(krow)) << 4) + (i % 2) * 8;
+  } else {
+    const uint32_t krow = q * 4, col = dim0 + i;
+    return (ks * 16 + krow) * (R * 4) + (((col / 4) ^ rm_swz<T, R>(krow)) << 4) + (col % 4) * 4;
+  }
+}
+template <typename T, int R, bool KM>
+__device__ __forceinline__ typename Step<T>::frag read_frag(const char *at) {
+  if constexpr (KM) {
+    return *reinterpret_cast<const typename Step<T>::frag *>(at);
   } else if constexpr (sizeof(T) == 2) {
     // the transposing read: 16 lanes take 4 k rows of 16 columns, and lane i
-    // receives column i of the 4 rows
+    // receives column i of the 4 rows; 4 rows on, the swizzle is the same
     typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     union {
       s16x4 half[2];
       bf16x8 all;
     } u;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t krow = ks * 32 + q * 8 + h * 4 + i / 4;
-      const uint32_t chunk = dim0 / 8 + (i % 4) / 2;
-      const char *at = tile + krow * (R * 2) + ((chunk ^ rm_swz<T, R>(krow)) << 4) + (i % 2) * 8;
-      u.half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
-    }
+    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * R * 2));
     return u.all;
   } else {
     f32x4 v;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t krow = ks * 16 + q * 4 + j, col = dim0 + i;
-      v[j] = *reinterpret_cast<const float *>(tile + krow * (R * 4) + (((col / 4) ^ rm_swz<T, R>(krow)) << 4) +
-                                              (col % 4) * 4);
-    }
+    for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float *>(at + j * R * 4);
     return v;
   }
 }
@@ -191,9 +242,9 @@ __device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
-// Which row of an operand's matrix entry j of a tile is.  Gated: a wave's
-// first half of columns are activations, its second half the same columns of
-// the other half of the weight, so both halves of a column end up in one lane.
+// Which row of the weight entry j of a tile is.  Gated: a wave's first half of
+// columns are activations, its second half the same columns of the other half
+// of the weight, so both halves of a column end up in one lane.
 template <int WTN, bool GATED>
 __device__ __forceinline__ uint32_t q_row(uint32_t tile_n, uint32_t bn, uint32_t j, uint32_t n, bool *ok) {
   if constexpr (!GATED) {
@@ -208,311 +259,582 @@ __device__ __forceinline__ uint32_t q_row(uint32_t tile_n, uint32_t bn, uint32_t
   }
 }
 
-// Loads one operand's tiles.  VEC: 16-byte chunks straight into LDS through a
-// buffer resource; a chunk outside the matrix gets an offset outside the
-// resource, which reads as zero.  Otherwise single elements through registers.
+constexpr uint32_t kOutside = 0xFFFFFFF0u;  // a buffer offset past the resource: reads as zero
+
+// Loads one operand's stages, one after the other, kChunks chunks a thread.
+//   VEC: every row is whole 16-byte chunks at 16-byte addresses, so a chunk
+//   lies in the matrix or outside it.  Chunks go straight into LDS through a
+//   buffer resource; issue() leaves them in flight until the caller waits.
+//   Otherwise fetch() brings them to registers, 16 bytes at any alignment
+//   where they lie inside the matrix and single elements at its end, and
+//   commit() writes them to LDS.
 template <typename T, int R, int NW, bool KM, bool VEC>
 struct Loader {
   static constexpr int kEpc = 16 / (int)sizeof(T);
-  static constexpr int kChunks = R * 8 / (NW * 64);  // per thread
+  static constexpr int kBK = Step<T>::kBK;
+  static constexpr int kChunks = R * 8 / (NW * 64);
   static constexpr int kRowChunks = KM ? 8 : R / kEpc;
-  const T *base;       // VEC: of the tile's k position, advanced by load()
-  uint64_t ld, left;   // left: bytes from base to the end of the matrix
-  uint32_t off[kChunks];
-  uint32_t kk[kChunks];  // the chunk's first k (KM) or its k row (RM), within a step
-  uint32_t row[kChunks]; // !VEC: the chunk's matrix row (KM) or first column (RM)
-  uint32_t lim;          // !VEC, RM: columns of the matrix
+  static_assert(kChunks * NW * 64 == R * 8, "every thread loads the same number of chunks");
+  uint64_t base;  // of the stage to load next
+  uint64_t left;  // !VEC: bytes from base to the end of the matrix
+  uint64_t step;  // bytes from one stage to the next
+  uint32_t off[kChunks];  // of the chunk, from base; kOutside: not in the matrix
+  uint32_t kk0;
+  u32x4 raw[VEC ? 1 : kChunks];
 
-  // KM: matrix [rows..][k], entry j is row row_of(j).  RM: matrix [k][cols],
-  // the tile's first column is col0.
+  // KM: matrix [mat_rows][k], the tile's entry j is row row_of(j) >= first.
+  // RM: matrix [k][cols], the tile's first column is `first`.
   template <typename F>
-  __device__ __forceinline__ void init(const T *mat, uint64_t ld_, uint32_t k, uint32_t mat_rows, uint32_t cols,
+  __device__ __forceinline__ void init(const T *mat, uint64_t ld, uint32_t k, uint32_t mat_rows, uint32_t cols,
                                        uint32_t first, F row_of) {
-    ld = ld_;
-    lim = cols;
-    const uint32_t tid = threadIdx.x;
+    constexpr uint64_t kEs = sizeof(T);
     if constexpr (KM) {
-      base = mat + (uint64_t)first * ld;
-      left = mat_rows > first ? ((uint64_t)(mat_rows - 1 - first) * ld + k) * sizeof(T) : 0;
+      base = (uint64_t)(mat + (uint64_t)first * ld);
+      left = mat_rows > first ? ((uint64_t)(mat_rows - 1 - first) * ld + k) * kEs : 0;
+      step = kBK * kEs;
     } else {
-      base = mat + first;
-      left = k > 0 && cols > first ? ((uint64_t)(k - 1) * ld + cols - first) * sizeof(T) : 0;
+      base = (uint64_t)(mat + first);
+      left = k > 0 && cols > first ? ((uint64_t)(k - 1) * ld + cols - first) * kEs : 0;
+      step = kBK * ld * kEs;
     }
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
-      const uint32_t pos = (uint32_t)(tid / 64 * kChunks + c) * 64 + tid % 64;
+      const uint32_t pos = (uint32_t)(threadIdx.x / 64 * kChunks + c) * 64 + threadIdx.x % 64;
       if constexpr (KM) {
         const uint32_t r = pos / 8, chunk = (pos % 8) ^ (r & 7);
         bool ok;
         const uint32_t mr = row_of(r, &ok);
-        kk[c] = chunk * kEpc;
-        off[c] = ok ? (uint32_t)((uint64_t)(mr - first) * ld * sizeof(T)) + chunk * 16 : 0xFFFFFFF0u;
-        row[c] = ok ? mr : 0xFFFFFFFFu;
+        kk0 = chunk * kEpc;  // the same for every c: rows are 8 apart
+        off[c] = ok ? (uint32_t)((uint64_t)(mr - first) * ld * kEs) + chunk * 16 : kOutside;
       } else {
         const uint32_t krow = pos / kRowChunks, chunk = (pos % kRowChunks) ^ rm_swz<T, R>(krow);
-        kk[c] = krow;
-        off[c] = first + chunk * kEpc < cols ? (uint32_t)(krow * ld * sizeof(T)) + chunk * 16 : 0xFFFFFFF0u;
-        row[c] = first + chunk * kEpc;
+        if (c == 0) kk0 = krow;
+        off[c] = first + chunk * kEpc < cols ? (uint32_t)(krow * ld * kEs) + chunk * 16 : kOutside;
       }
     }
   }
 
-  // Issues the loads of the k step that starts at k0 (consecutive steps).
-  __device__ __forceinline__ void load(char *tile, uint32_t k0, uint32_t k) {
-    const uint32_t lane_chunk0 = threadIdx.x / 64 * kChunks;
-    if constexpr (VEC) {
-      const uint32_t records = left > 0xFFFFFFF0ull ? 0xFFFFFFF0u : (uint32_t)left;
-      const rsrc_t rs = make_rsrc(base, records);
-#pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
-        const uint32_t o = k0 + kk[c] < k ? off[c] : 0xFFFFFFF0u;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rs, (__attribute__((address_space(3))) void *)(tile + (lane_chunk0 + c) * 1024), 16, (int)o, 0, 0, 0);
-      }
-      const uint64_t step = KM ? 128 : (uint64_t)Step<T>::kBK * ld * sizeof(T);
-      base = reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + step);
-      left = left > step ? left - step : 0;
-    } else {
+  // chunk c's first k (KM) or its k row (RM) within a stage
+  __device__ __forceinline__ uint32_t kk(int c) const { return KM ? kk0 : kk0 + c * (64 / kRowChunks); }
+
+  __device__ __forceinline__ void advance() {
+    base += step;
+    if constexpr (!VEC) left = left > step ? left - step : 0;
+  }
+
+  // VEC: issues chunk c of a stage to LDS byte `at` (this wave's part of the
+  // operand's stage); whole: the stage has kBK k left, else `have` of them.
+  // In assembly so that the compiler does not wait for the load before the
+  // next LDS read, as it must where it sees a write to LDS; it has no result
+  // register, and the caller waits for it.
+  template <bool WHOLE>
+  __device__ __forceinline__ void issue(uint32_t at, int c, uint32_t have) {
+    // the base and the LDS address are the same in every lane
+    const u32x4 rs = {uniform_u32((uint32_t)base), uniform_u32((uint32_t)(base >> 32)), kOutside,
+                      (uint32_t)kRsrcWord3};
+    const uint32_t o = WHOLE || kk(c) < have ? off[c] : kOutside;
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %1, %2, 0 offen lds"
+        :
+        : "s"(uniform_u32(at + c * 1024)), "v"(o), "s"(rs)
+        : "memory");
+  }
+
+  // !VEC: the stage's chunks to registers; have: k left from the stage's
+  // first (may be 0 or less).
+  __device__ __forceinline__ void fetch(int have) {
+    if constexpr (!VEC) {
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
         union {
           T e[kEpc];
           u32x4 raw;
         } v;
-        const uint32_t kc = k0 + kk[c];
-#pragma unroll
-        for (int i = 0; i < kEpc; ++i) {
-          bool ok;
-          uint64_t at;
-          if constexpr (KM) {
-            ok = row[c] != 0xFFFFFFFFu && kc + i < k;
-            at = (uint64_t)row[c] * ld + kc + i;
+        v.raw = u32x4{0, 0, 0, 0};
+        if (off[c] != kOutside && (int)kk(c) < have) {
+          const char *p = reinterpret_cast<const char *>(base) + off[c];
+          if ((uint64_t)off[c] + 16 <= left) {
+            __builtin_memcpy(&v, p, 16);
           } else {
-            ok = kc < k && row[c] + i < lim;
-            at = (uint64_t)kc * ld + row[c] + i;
+#pragma unroll
+            for (int i = 0; i < kEpc; ++i)
+              if ((uint64_t)off[c] + (i + 1) * sizeof(T) <= left) v.e[i] = reinterpret_cast<const T *>(p)[i];
           }
-          v.e[i] = ok ? base[at] : (T)0.f;
+          if constexpr (KM) {
+            if ((int)kk(c) + kEpc > have) {  // the row ends inside the chunk
+#pragma unroll
+              for (int i = 0; i < kEpc; ++i)
+                if ((int)kk(c) + i >= have) v.e[i] = (T)0.f;
+            }
+          }
         }
-        *reinterpret_cast<u32x4 *>(tile + (lane_chunk0 + c) * 1024 + threadIdx.x % 64 * 16) = v.raw;
+        raw[c] = v.raw;
       }
+    }
+  }
+  __device__ __forceinline__ void commit(char *tile) {
+    if constexpr (!VEC) {
+      const uint32_t chunk0 = threadIdx.x / 64 * kChunks;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+        *reinterpret_cast<u32x4 *>(tile + (chunk0 + c) * 1024 + threadIdx.x % 64 * 16) = raw[c];
     }
   }
 };
 
 // ---------------------------------------------------------------- epilogues
+//
+// A wave's sums go through LDS, half of its rows at a time, so that each lane
+// finishes kEw consecutive columns of a row and rows are written whole lines
+// at a time.
+constexpr int kEw = 8;
+typedef Pack<float, kEw, true> Vals;
+
+// kEw values at p, of which the row has n; vec: p is aligned for 16 bytes (or
+// for all kEw elements, if they are fewer).
 template <typename T>
-__device__ __forceinline__ void put4(T *p, f32x4 v, uint32_t n, bool vec) {
-  Pack<T, 4, true> o;
+__device__ __forceinline__ void put8(T *p, const Vals &v, uint32_t n, bool vec) {
+  Pack<T, kEw, true> o;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o.v[i] = v[i];
-  if (vec && n >= 4)
+  for (int i = 0; i < kEw; ++i) o.v[i] = v.v[i];
+  if (vec && n >= kEw)
     o.store(p);
   else
     o.store_some(p, (int)n);
 }
 template <typename T>
-__device__ __forceinline__ f32x4 get4(const T *p, uint32_t n, bool vec) {
-  Pack<T, 4, true> o;
-  if (vec && n >= 4)
+__device__ __forceinline__ Vals get8(const T *p, uint32_t n, bool vec) {
+  Pack<T, kEw, true> o;
+  if (vec && n >= kEw)
     o.load(p);
   else
     o.load_some(p, (int)n, 0.f);
-  f32x4 v;
+  Vals v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = o.v[i];
+  for (int i = 0; i < kEw; ++i) v.v[i] = o.v[i];
   return v;
 }
+__device__ __forceinline__ void add8(Vals &v, const Vals &w) {
+#pragma unroll
+  for (int i = 0; i < kEw; ++i) v.v[i] += w.v[i];
+}
 
-// Writes y (and z) for four columns n0.. of row r, v the sums; gated: u the
+// f(z) of all kEw values, f the (ungated or first half's) activation; the
+// branch on it is taken once for all of them.
+__device__ __forceinline__ void act8(Vals &v, int act) {
+  switch (act) {
+    case LL_ACT_NONE: break;
+    case LL_ACT_RELU:
+#pragma unroll
+      for (int i = 0; i < kEw; ++i) v.v[i] = act1(v.v[i], LL_ACT_RELU);
+      break;
+    case LL_ACT_GELU:
+    case LL_ACT_GEGLU:
+#pragma unroll
+      for (int i = 0; i < kEw; ++i) v.v[i] = gelu(v.v[i]);
+      break;
+    default:
+#pragma unroll
+      for (int i = 0; i < kEw; ++i) v.v[i] = silu(v.v[i]);
+  }
+}
+__device__ __forceinline__ void slope8(Vals &v, int act) {
+  switch (act) {
+    case LL_ACT_RELU:
+#pragma unroll
+      for (int i = 0; i < kEw; ++i) v.v[i] = slope1(v.v[i], LL_ACT_RELU);
+      break;
+    case LL_ACT_GELU:
+    case LL_ACT_GEGLU:
+#pragma unroll
+      for (int i = 0; i < kEw; ++i) v.v[i] = gelu_slope(v.v[i]);
+      break;
+    default:
+#pragma unroll
+      for (int i = 0; i < kEw; ++i) v.v[i] = silu_slope(v.v[i]);
+  }
+}
+
+// Writes y (and z) for kEw columns n0.. of row r, v the sums; gated: u the
 // sums of the second half's columns.
 template <typename T, bool GATED>
-__device__ __forceinline__ void put_forward(const Args &a, int g, uint64_t r, uint32_t n0, f32x4 v, f32x4 u) {
+__device__ __forceinline__ void put_forward(const Args &a, int g, uint64_t r, uint32_t n0, Vals v, Vals u) {
   const uint32_t width = GATED ? a.n / 2 : a.n;
   if (n0 >= width) return;
   const uint32_t left = width - n0;
   if (a.bias != nullptr) {
     const T *b = (const T *)a.bias + (uint64_t)g * a.n + n0;
-    v += get4(b, left, false);
-    if constexpr (GATED) u += get4(b + width, left, false);
+    add8(v, get8(b, left, a.vec_b));
+    if constexpr (GATED) add8(u, get8(b + width, left, a.vec_b && width % kEw == 0));
   }
   if (a.zout != nullptr) {
     T *z = (T *)a.zout + r * a.ldz + n0;
-    put4(z, v, left, a.vec_c);
-    if constexpr (GATED) put4(z + width, u, left, a.vec_c && width % 4 == 0);
+    put8(z, v, left, a.vec_c);
+    if constexpr (GATED) put8(z + width, u, left, a.vec_c && width % kEw == 0);
   }
+  act8(v, a.act);
+  if constexpr (GATED) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = GATED ? act1(v[i], a.act) * u[i] : act1(v[i], a.act);
-  if (a.res != nullptr) v += get4((const T *)a.res + r * a.ldr + n0, left, a.vec_c);
-  put4((T *)a.c + r * a.ldc + n0, v, left, a.vec_c);
+    for (int i = 0; i < kEw; ++i) v.v[i] *= u.v[i];
+  }
+  if (a.res != nullptr) add8(v, get8((const T *)a.res + r * a.ldr + n0, left, a.vec_c));
+  put8((T *)a.c + r * a.ldc + n0, v, left, a.vec_c);
 }
 
-// dx for four columns, through the activation of the layer below.
+// dx for kEw columns, through the activation of the layer below.
 template <typename T>
-__device__ __forceinline__ void put_grad_x(const Args &a, uint64_t r, uint32_t n0, f32x4 v) {
+__device__ __forceinline__ void put_grad_x(const Args &a, uint64_t r, uint32_t n0, Vals v) {
   if (n0 >= a.n) return;
   const uint32_t left = a.n - n0;
   T *out = (T *)a.c + r * a.ldc + n0;
-  if (a.act == LL_ACT_NONE) {
-    put4(out, v, left, a.vec_c);
-    return;
-  }
-  const T *zp = (const T *)a.z + r * a.ldz + n0;
-  f32x4 z = get4(zp, left, a.vec_c), w;
-  if (gated(a.act)) {
-    const bool vec = a.vec_c && a.n % 4 == 0;
-    const f32x4 u = get4(zp + a.n, left, vec);
+  if (a.act != LL_ACT_NONE) {
+    const T *zp = (const T *)a.z + r * a.ldz + n0;
+    const Vals z = get8(zp, left, a.vec_c);
+    Vals s = z;
+    slope8(s, a.act);
+    if (gated(a.act)) {
+      const bool vec = a.vec_c && a.n % kEw == 0;
+      const Vals u = get8(zp + a.n, left, vec);
+      Vals w = z;
+      act8(w, a.act);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i] = v[i] * act1(z[i], a.act);
-      v[i] = v[i] * u[i] * slope1(z[i], a.act);
+      for (int i = 0; i < kEw; ++i) {
+        w.v[i] *= v.v[i];
+        v.v[i] *= u.v[i];
+      }
+      put8(out + a.n, w, left, vec);
     }
-    put4(out + a.n, w, left, vec);
-  } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= slope1(z[i], a.act);
+    for (int i = 0; i < kEw; ++i) v.v[i] *= s.v[i];
   }
-  put4(out, v, left, a.vec_c);
+  put8(out, v, left, a.vec_c);
 }
 
 template <typename G>
-__device__ __forceinline__ void put_grad_w(const Args &a, int g, uint32_t m, uint32_t n0, f32x4 v) {
+__device__ __forceinline__ void put_grad_w(const Args &a, int g, uint32_t m, uint32_t n0, Vals v) {
   if (n0 >= a.n) return;
   const uint32_t left = a.n - n0;
   G *out = (G *)a.c + (uint64_t)g * a.cstride + (uint64_t)m * a.ldc + n0;
-  if (a.flags & LL_GRAD_ADD) v += get4(out, left, a.vec_c);
-  put4(out, v, left, a.vec_c);
+  if (a.flags & LL_GRAD_ADD) add8(v, get8(out, left, a.vec_c));
+  put8(out, v, left, a.vec_c);
+}
+
+template <typename T>
+__device__ __forceinline__ void put_bias_grad(const Args &a, int g, uint32_t m, float b) {
+  const uint64_t at = (uint64_t)g * a.m + m;
+  if (a.flags & LL_GRAD_F32) {
+    float *o = (float *)a.dbias + at;
+    *o = (a.flags & LL_GRAD_ADD) ? *o + b : b;
+  } else {
+    T *o = (T *)a.dbias + at;
+    *o = Num<T>::put((a.flags & LL_GRAD_ADD) ? Num<T>::get(*o) + b : b);
+  }
 }
 
 // ---------------------------------------------------------------- the tile kernel
+//
+// Two stages of both operands lie in LDS.  A wave's rows are FM / 2 fragments
+// in the tile's upper half and as many in its lower half, and a stage is four
+// clusters of matrix instructions: upper and lower rows with the first half of
+// the stage's k, then with the second.  The fragments of a cluster are read
+// during the cluster before it, one LDS read between two matrix instructions.
+// After the third cluster every fragment of the stage is in registers: a
+// barrier there, the only one of a stage, frees its buffer, into which the
+// loads of the stage after next go out during the fourth cluster, and says
+// that the next stage has arrived (its loads went out a stage earlier), whose
+// first fragments are read meanwhile.
+//
+// A tile with no rows in its lower half (the last tile of a group, often)
+// leaves that half's work out.
+constexpr int kStages = 2;
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// This wave's LDS reads and writes are done; then everyone's.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 template <typename T, Pass PASS, int BM, int BN, int WM, int WN, bool GATED, bool VEC>
-__global__ __launch_bounds__(WM *WN * 64) void k_tile(Args a) {
+__global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
   constexpr bool kPkm = PASS != kGradW, kQkm = PASS == kForward;
-  constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, FM = WTM / 16, FN = WTN / 16;
-  constexpr int BK = Step<T>::kBK, KS = BK / Step<T>::kPerMma;
-  constexpr int kTile = (BM + BN) * 128;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kTile];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, FM = WTM / 16, FN = WTN / 16, FH = FM / 2;
+  constexpr int BK = Step<T>::kBK;
+  constexpr int kStage = (BM + BN) * 128;
+  constexpr int kPitch = WTN + 4;  // binary32 of an epilogue row: rows start in different banks
+  constexpr int kEpi = NW * (WTM / 2) * kPitch * 4;
+  constexpr int kLds = kStages * kStage > kEpi ? kStages * kStage : kEpi;
+  typedef typename Step<T>::frag frag;
+  __shared__ __attribute__((aligned(1024))) char lds[kLds];
+  const int lane = threadIdx.x % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int wm = wave / WN, wn = wave % WN;
 
-  const uint32_t tn = blockIdx.x % a.tiles_n, tm = blockIdx.x / a.tiles_n;
   int g = 0;
-  uint32_t m0 = 0, m_end = a.m, k = a.k;
+  uint32_t tn = 0, m0 = 0, m_end = a.m, k = a.k;
   const T *p = (const T *)a.p, *q = (const T *)a.q;
   if constexpr (PASS == kGradW) {
-    g = tm / a.tiles_m;
-    m0 = (tm % a.tiles_m) * BM;
-    uint32_t lo = 0, hi = a.rows;
-    if (a.offsets != nullptr) {
-      lo = (uint32_t)min(max(a.offsets[g], 0), (int)a.rows);
-      hi = (uint32_t)min(max(a.offsets[g + 1], (int)lo), (int)a.rows);
-    }
-    k = hi - lo;
+    const uint32_t per = a.tiles_m * a.tiles_n;
+    uint32_t tm, lo, hi;
+    g = blockIdx.x / per;
+    if (!tile_of(blockIdx.x % per, a.tiles_m, a.tiles_n, &tm, &tn)) return;
+    m0 = tm * BM;
+    group_rows(a, g, &lo, &hi);
+    lo = uniform_u32(lo);
+    k = uniform_u32(hi) - lo;
     p += (uint64_t)lo * a.ldp;
     q += (uint64_t)lo * a.ldq;
   } else {
-    if (!find_rows(a, tm, BM, &g, &m0, &m_end)) return;
+    if (!find_rows(a, blockIdx.x, BM, &g, &m0, &m_end, &tn)) return;
     q += (uint64_t)g * a.qstride;
   }
 
   Loader<T, BM, NW, kPkm, VEC> lp;
   Loader<T, BN, NW, kQkm, VEC> lq;
   if constexpr (kPkm)
-    lp.init(VEC ? p : p, a.ldp, k, m_end, 0, VEC ? m0 : 0, [&](uint32_t j, bool *ok) {
+    lp.init(p, a.ldp, k, m_end, 0, m0, [&](uint32_t j, bool *ok) {
       *ok = m0 + j < m_end;
       return m0 + j;
     });
   else
-    lp.init(p, a.ldp, k, 0, a.m, VEC ? m0 : 0, [](uint32_t, bool *) { return 0u; });
+    lp.init(p, a.ldp, k, 0, a.m, m0, [](uint32_t, bool *) { return 0u; });
   if constexpr (kQkm)
     lq.init(q, a.ldq, k, a.n, 0, 0, [&](uint32_t j, bool *ok) { return q_row<WTN, GATED>(tn, BN, j, a.n, ok); });
   else
-    lq.init(q, a.ldq, k, 0, a.n, VEC ? tn * BN : 0, [](uint32_t, bool *) { return 0u; });
-  if constexpr (!VEC && !kPkm) {
-    for (auto &c : lp.row) c += m0;
-  }
-  if constexpr (!VEC && !kQkm) {
-    for (auto &c : lq.row) c += tn * BN;
-  }
+    lq.init(q, a.ldq, k, 0, a.n, tn * BN, [](uint32_t, bool *) { return 0u; });
 
-  f32x4 acc[FN][FM], accb[FM];
+  f32x4 acc[FN][FM];
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
-    accb[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const bool want_bias = PASS == kGradW && a.dbias != nullptr && tn == 0 && wn == 0;
-  typename Step<T>::frag ones;
-#pragma unroll
-  for (int i = 0; i < (int)(sizeof(ones) / sizeof(T)); ++i) ones[i] = (T)1.f;
-
   const uint32_t steps = (k + BK - 1) / BK;
-  if (steps > 0) {
-    lp.load(lds, 0, k);
-    lq.load(lds + BM * 128, 0, k);
-  }
-  for (uint32_t s = 0; s < steps; ++s) {
-    __syncthreads();  // step s has arrived, and step s-1's reads are done
-    const char *tp = lds + (s & 1) * kTile, *tq = tp + BM * 128;
-    if (s + 1 < steps) {
-      char *next = lds + ((s + 1) & 1) * kTile;
-      lp.load(next, (s + 1) * BK, k);
-      lq.load(next + BM * 128, (s + 1) * BK, k);
+  constexpr int kLoads = lp.kChunks + lq.kChunks;  // of a thread, a stage
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+  const uint32_t at_p = lds0 + wave * lp.kChunks * 1024, at_q = lds0 + BM * 128 + wave * lq.kChunks * 1024;
+  // load n (of kLoads) of the stage that goes to buffer `into`
+  auto issue = [&](int into, int n, auto whole, uint32_t have) __attribute__((always_inline)) {
+    if (n < lp.kChunks)
+      lp.template issue<decltype(whole)::value>(at_p + into * kStage, n, have);
+    else
+      lq.template issue<decltype(whole)::value>(at_q + into * kStage, n - lp.kChunks, have);
+  };
+  // first entry of the wave's fragment i of P
+  auto dim_p = [&](int i) __attribute__((always_inline)) { return (i < FH ? 0 : BM / 2) + wm * (WTM / 2) + (i % FH) * 16; };
+  // Where the fragments lie in a stage, by half of its k (RM: a constant
+  // apart).  Those of P's lower half lie a constant further on where the
+  // swizzle does not reach that bit of the entry.
+  constexpr bool kSame = kPkm || BM / 2 * sizeof(T) % 256 == 0;
+  constexpr int kHalfOff = kPkm ? BM / 2 * 128 : BM / 2 * (int)sizeof(T);
+  constexpr int kKsP = Step<T>::kMma * BM * (int)sizeof(T), kKsQ = Step<T>::kMma * BN * (int)sizeof(T);
+  uint32_t off_q[2][FN], off_p[2][FM];
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      off_q[ks][j] = kQkm || ks == 0 ? BM * 128 + frag_off<T, BN, kQkm>(wn * WTN + j * 16, ks) : off_q[0][j] + kKsQ;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      if (i >= FH && kSame)
+        off_p[ks][i] = off_p[ks][i - FH] + kHalfOff;
+      else
+        off_p[ks][i] = kPkm || ks == 0 ? frag_off<T, BM, kPkm>(dim_p(i), ks) : off_p[0][i] + kKsP;
     }
+  }
+  const bool lower = m_end - m0 > BM / 2;  // the tile has rows in its lower half
+
+  if (steps > 0) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      typename Step<T>::frag fp[FM], fq[FN];
+    for (int s = 0; s < kStages; ++s) {
+      const int have = (int)k - s * BK;
+      if constexpr (VEC) {
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fp[i] = read_frag<T, BM, kPkm>(tp, wm * WTM + i * 16, ks);
+        for (int n = 0; n < kLoads; ++n) issue(s, n, std::false_type{}, have > 0 ? have : 0);
+      } else {
+        lp.fetch(have);
+        lq.fetch(have);
+        if (s == 0) {  // the second stage is committed during the first
+          lp.commit(lds);
+          lq.commit(lds + BM * 128);
+        }
+      }
+      lp.advance();
+      lq.advance();
+    }
+    wait_loads<VEC ? kLoads : 0>();
+    lds_barrier();
+    frag fq[2][FN], fu[2][FH], fl[2][FH];  // by half of k: Q, P's upper rows, P's lower rows
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fq[j] = read_frag<T, BN, kQkm>(tq, wn * WTN + j * 16, ks);
+    for (int j = 0; j < FN; ++j) fq[0][j] = read_frag<T, BN, kQkm>(lds + off_q[0][j]);
+#pragma unroll
+    for (int i = 0; i < FH; ++i) fu[0][i] = read_frag<T, BM, kPkm>(lds + off_p[0][i]);
+
+    // The matrix instruction t of a cluster (none past the last).
+    auto multiply = [&](int t, int ks, bool low) __attribute__((always_inline)) {
+      if (t >= FN * FH) return;
+      const int j = t / FH, i = t % FH;
+      if (low)
+        acc[j][FH + i] = mma(fq[ks][j], fl[ks][i], acc[j][FH + i]);
+      else
+        acc[j][i] = mma(fq[ks][j], fu[ks][i], acc[j][i]);
+    };
+    // One stage from LDS buffer b.  WHOLE: the stage after next has BK k, else
+    // `have` of them (none: zeros are written).
+    auto stage = [&](int b, auto lower_c, auto whole, int have) __attribute__((always_inline)) {
+      constexpr bool kLower = decltype(lower_c)::value;
+      constexpr int kMmas = FN * FH, kMmasL = kLower ? kMmas : 0;
+      const char *here = lds + b * kStage, *next = lds + (1 - b) * kStage;
+#pragma unroll
+      for (int t = 0; t < kMmas; ++t) {
+        if (kLower && t < FH) fl[0][t < FH ? t : 0] = read_frag<T, BM, kPkm>(here + off_p[0][FH + (t < FH ? t : 0)]);
+        multiply(t, 0, false);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int t = 0; t < FN + FH || t < kMmasL; ++t) {
+        if (t < FN)
+          fq[1][t < FN ? t : 0] = read_frag<T, BN, kQkm>(here + off_q[1][t < FN ? t : 0]);
+        else if (t < FN + FH)
+          fu[1][t - FN] = read_frag<T, BM, kPkm>(here + off_p[1][t - FN]);
+        if (kLower) multiply(t, 0, true);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int t = 0; t < kMmas; ++t) {
+        if (kLower && t < FH) fl[1][t < FH ? t : 0] = read_frag<T, BM, kPkm>(here + off_p[1][FH + (t < FH ? t : 0)]);
+        multiply(t, 1, false);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (!VEC) {
+        // the next stage's chunks, fetched a stage ago
+        lp.commit(const_cast<char *>(next));
+        lq.commit(const_cast<char *>(next) + BM * 128);
+      }
+      wait_loads<0>();
+      lds_barrier();
+      if constexpr (!VEC) {
+        lp.fetch(have);
+        lq.fetch(have);
+      }
+      constexpr int kReads = FN + FH, kAux = VEC && kLoads > kReads ? kLoads : kReads;
+#pragma unroll
+      for (int t = 0; t < kAux || t < kMmasL; ++t) {
+        if (VEC && t < kLoads) issue(b, t, whole, have > 0 ? have : 0);
+        if (t < FN)
+          fq[0][t < FN ? t : 0] = read_frag<T, BN, kQkm>(next + off_q[0][t < FN ? t : 0]);
+        else if (t < kReads)
+          fu[0][t - FN] = read_frag<T, BM, kPkm>(next + off_p[0][t - FN]);
+        if (kLower) multiply(t, 1, true);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      lp.advance();
+      lq.advance();
+    };
+    auto all = [&](auto lower_c) __attribute__((always_inline)) {
+      uint32_t s = 0;
+      if constexpr (VEC) {  // two stages at a time: LDS addresses are constants
+        for (; (s + 4) * BK <= k; s += 2) {
+          stage(0, lower_c, std::true_type{}, BK);
+          stage(1, lower_c, std::true_type{}, BK);
+        }
+      }
+      for (; s < steps; ++s) stage(s % kStages, lower_c, std::false_type{}, (int)k - (int)(s + kStages) * BK);
+    };
+    if (PASS == kGradW || lower)
+      all(std::true_type{});
+    else
+      all(std::false_type{});
+  }
+  wait_loads<0>();
+  lds_barrier();  // every wave is past its last stage, and no load is under way
+
+  float *mine = reinterpret_cast<float *>(lds) + wave * (WTM / 2) * kPitch;
+  auto finish = [&](auto half) __attribute__((always_inline)) {
+    constexpr int h = decltype(half)::value;
+#pragma unroll
+    for (int i = 0; i < FH; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int i = 0; i < FM; ++i) acc[j][i] = mma(fq[j], fp[i], acc[j][i]);
-      if constexpr (PASS == kGradW) {
-        if (want_bias) {
-#pragma unroll
-          for (int i = 0; i < FM; ++i) accb[i] = mma(ones, fp[i], accb[i]);
-        }
+        *reinterpret_cast<f32x4 *>(mine + (i * 16 + lane % 16) * kPitch + j * 16 + lane / 16 * 4) = acc[j][h * FH + i];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    constexpr int kWidth = GATED ? WTN / 2 : WTN;  // columns of C a wave has
+    constexpr int kLanes = kWidth / kEw;           // lanes a row
+    const int c = lane % kLanes * kEw;
+    const uint32_t n0 = (GATED ? tn * (BN / 2) + wn * kWidth : tn * BN + wn * WTN) + c;
+#pragma unroll 1
+    for (int r = lane / kLanes; r < WTM / 2; r += 64 / kLanes) {
+      const uint32_t m = m0 + h * (BM / 2) + wm * (WTM / 2) + r;
+      if (m >= m_end) break;
+      Pack<float, kEw, true> v, u;
+      v.load(mine + r * kPitch + c);
+      if constexpr (PASS == kForward) {
+        if constexpr (GATED) u.load(mine + r * kPitch + kWidth + c);
+        put_forward<T, GATED>(a, g, m, n0, v, u);
+      } else if constexpr (PASS == kGradX) {
+        put_grad_x<T>(a, m, n0, v);
+      } else {
+        if (a.flags & LL_GRAD_F32)
+          put_grad_w<float>(a, g, m, n0, v);
+        else
+          put_grad_w<T>(a, g, m, n0, v);
       }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  };
+  finish(std::integral_constant<int, 0>{});
+  if (PASS == kGradW || lower) finish(std::integral_constant<int, 1>{});
+}
+
+// ---------------------------------------------------------------- bias gradient
+//
+// dbias[g] = the sum of dz over the group's rows.  A launch of its own: inside
+// the weight gradient's kernel it took registers that kernel has not (its
+// loop's addresses went to memory, 765 -> 1860 us for 8192^3).  16 chunks of
+// columns a workgroup, the rows dealt to 64 threads a chunk, eight loads of a
+// thread under way at a time; the 64 parts are added in order.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(1024) void k_bias_grad(Args a) {
+  constexpr int C = VEC ? Num<T>::kPer16 : 1, kAhead = 8;
+  __shared__ float part[64][16 * C + 1];
+  const int g = blockIdx.y, c = threadIdx.x % 16, lane = threadIdx.x / 16;
+  const uint32_t col = (blockIdx.x * 16 + c) * C;
+  uint32_t lo, hi;
+  group_rows(a, g, &lo, &hi);
+  float sum[C];
+#pragma unroll
+  for (int i = 0; i < C; ++i) sum[i] = 0.f;
+  if (col < a.m) {
+    const T *p = (const T *)a.p + col;
+    uint32_t r = lo + lane;
+    for (; r + 64 * (kAhead - 1) < hi; r += 64 * kAhead) {
+      Pack<T, C, VEC> v[kAhead];
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) v[n].load(p + (uint64_t)(r + 64 * n) * a.ldp);
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n)
+#pragma unroll
+        for (int i = 0; i < C; ++i) sum[i] += v[n].v[i];
+    }
+    for (; r < hi; r += 64) {
+      Pack<T, C, VEC> v;
+      v.load(p + (uint64_t)r * a.ldp);
+#pragma unroll
+      for (int i = 0; i < C; ++i) sum[i] += v.v[i];
     }
   }
-
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const uint32_t m = m0 + wm * WTM + i * 16 + lane % 16;
-    if (m >= m_end) continue;
-    if constexpr (PASS == kForward) {
-#pragma unroll
-      for (int j = 0; j < (GATED ? FN / 2 : FN); ++j) {
-        const uint32_t n0 = GATED ? tn * (BN / 2) + wn * (WTN / 2) + j * 16 + lane / 16 * 4
-                                  : tn * BN + wn * WTN + j * 16 + lane / 16 * 4;
-        put_forward<T, GATED>(a, g, m, n0, acc[j][i], acc[GATED ? FN / 2 + j : j][i]);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const uint32_t n0 = tn * BN + wn * WTN + j * 16 + lane / 16 * 4;
-        if constexpr (PASS == kGradX)
-          put_grad_x<T>(a, m, n0, acc[j][i]);
-        else if (a.flags & LL_GRAD_F32)
-          put_grad_w<float>(a, g, m, n0, acc[j][i]);
-        else
-          put_grad_w<T>(a, g, m, n0, acc[j][i]);
-      }
-      if (want_bias && lane < 16) {
-        const uint64_t at = (uint64_t)g * a.m + m;
-        float b = accb[i][0];
-        if (a.flags & LL_GRAD_F32) {
-          float *o = (float *)a.dbias + at;
-          *o = (a.flags & LL_GRAD_ADD) ? *o + b : b;
-        } else {
-          T *o = (T *)a.dbias + at;
-          *o = Num<T>::put((a.flags & LL_GRAD_ADD) ? Num<T>::get(*o) + b : b);
-        }
-      }
-    }
+  for (int i = 0; i < C; ++i) part[lane][c * C + i] = sum[i];
+  __syncthreads();
+  const uint32_t m = blockIdx.x * 16 * C + threadIdx.x;
+  if (threadIdx.x < 16 * C && m < a.m) {
+    float b = 0.f;
+    for (int r = 0; r < 64; ++r) b += part[r][threadIdx.x];
+    put_bias_grad<T>(a, g, m, b);
   }
 }
 
