@@ -59,41 +59,115 @@ tile_fn pick(bool gate) {
   return k_tile<T, PASS, B, B, WM, WN, false, VEC>;
 }
 
+// Tiles of b x b that a product has at most: every group with rows may add one
+// partial row tile.
+uint64_t count_tiles(Pass pass, const Args &a, uint32_t b) {
+  const uint64_t n = (a.n + b - 1) / b;
+  if (pass == kGradW) return (uint64_t)((a.m + b - 1) / b) * a.groups * n;
+  return (a.offsets == nullptr ? (a.rows + b - 1) / b : a.rows / b + std::min<uint64_t>(a.groups, a.rows)) * n;
+}
+
+// How a product runs: the tile's edge and the splits of its sum.
+struct Plan {
+  uint32_t tile, splits;
+};
+
+constexpr uint32_t kFill = 256;            // workgroups that fill the chip
+constexpr uint64_t kMaxParts = 256 << 20;  // bytes of split sums
+
+Plan plan_of(Pass pass, const Args &a, ll_dtype dt, bool vec) {
+  Plan p{64, 1};
+  // Larger tiles move fewer operand bytes but need many tiles to fill the chip.
+  // 256: bfloat16 rows of whole 16-byte chunks only (binary32 is bound by its
+  // matrix instructions, which are 16 times slower, with any).
+  if (vec && dt == LL_BF16 && count_tiles(pass, a, 256) >= kFill)
+    p.tile = 256;
+  else if (count_tiles(pass, a, 128) >= kFill)
+    p.tile = 128;
+  const uint32_t bk = 128 / esize(dt);
+  const uint64_t tiles = count_tiles(pass, a, p.tile), steps = (a.k + bk - 1) / bk;
+  // Too few tiles: the sum is cut so that the chip is filled, into shares of
+  // eight stages or more (a stage is about 0.5 us when little else runs, the
+  // joining launch a few us).
+  if (tiles < kFill) {
+    uint64_t s = std::min<uint64_t>(kFill * 2 / std::max<uint64_t>(tiles, 1), steps / 8);
+    const uint64_t one = (uint64_t)a.rows_c * a.n * 4;
+    s = std::min(s, kMaxParts / std::max<uint64_t>(one, 1));
+    if (s >= 2) p.splits = (uint32_t)std::min<uint64_t>(s, 32);
+  }
+  return p;
+}
+
 template <typename T, Pass PASS, int B, int WM, int WN, bool VEC>
 int launch_tiles(Args &a, bool gate, void *stream) {
   const uint32_t width = gate ? a.n / 2 : a.n;
   const uint32_t per_n = gate ? B / 2 : B;
   a.tiles_n = (width + per_n - 1) / per_n;
-  uint64_t tiles;
-  if (PASS == kGradW) {
-    a.tiles_m = (a.m + B - 1) / B;
-    tiles = (uint64_t)a.tiles_m * a.groups;
-  } else {
-    // every group with rows may add one partial tile
-    tiles = a.offsets == nullptr ? (a.rows + B - 1) / B : a.rows / B + std::min<uint64_t>(a.groups, a.rows);
-  }
-  const uint64_t grid = tiles * a.tiles_n;
+  a.tiles_m = (a.m + B - 1) / B;
+  const uint64_t grid = count_tiles(PASS, a, B) / ((a.n + B - 1) / B) * a.tiles_n;
   constexpr int kThreads = WM * WN * 64;
   if (grid * kThreads >= 1ull << 32) return LL_ERR_UNSUPPORTED;
   const tile_fn fn = pick<T, PASS, B, WM, WN, VEC>(gate);
-  hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)stream, a);
+  hipLaunchKernelGGL(fn, dim3((unsigned)grid, a.splits), dim3(kThreads), 0, (hipStream_t)stream, a);
+  if (a.parts != nullptr) {
+    const uint64_t items = (uint64_t)a.rows_c * ((width + kEw - 1) / kEw);
+    if ((items + 255) / 256 * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
+    tile_fn join = k_join<T, PASS, false>;
+    if constexpr (PASS == kForward) {
+      if (gate) join = k_join<T, PASS, true>;
+    }
+    hipLaunchKernelGGL(join, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, (hipStream_t)stream, a);
+  }
   return launch_status();
 }
 
-template <Pass PASS>
-int launch_product(Args &a, ll_dtype dt, bool gate, bool vec, void *stream) {
+template <typename T, Pass PASS>
+int launch_plan(Args &a, const Plan &p, bool gate, bool vec, void *stream) {
+  if constexpr (sizeof(T) == 2) {
+    if (p.tile == 256) return launch_tiles<T, PASS, 256, 2, 4, true>(a, gate, stream);
+  }
   // rows that are not whole 16-byte chunks pass through registers, which eight
   // waves have enough of
-  if (!vec)
-    return dt == LL_F32 ? launch_tiles<float, PASS, 128, 2, 4, false>(a, gate, stream)
-                        : launch_tiles<__bf16, PASS, 128, 2, 4, false>(a, gate, stream);
-  if (dt == LL_F32) return launch_tiles<float, PASS, 128, 2, 2, true>(a, gate, stream);
-  // 256-wide tiles move half the operand bytes of 128-wide ones but need many
-  // tiles to fill the chip (binary32 is bound by its matrix instructions,
-  // which are 16 times slower, with either)
-  const uint64_t m256 = PASS == kGradW ? (uint64_t)((a.m + 255) / 256) * a.groups : (a.rows + 255) / 256;
-  if (m256 * ((a.n + 255) / 256) >= 256) return launch_tiles<__bf16, PASS, 256, 2, 4, true>(a, gate, stream);
-  return launch_tiles<__bf16, PASS, 128, 2, 2, true>(a, gate, stream);
+  if (p.tile == 128)
+    return vec ? launch_tiles<T, PASS, 128, 2, 2, true>(a, gate, stream)
+               : launch_tiles<T, PASS, 128, 2, 4, false>(a, gate, stream);
+  return vec ? launch_tiles<T, PASS, 64, 2, 2, true>(a, gate, stream)
+             : launch_tiles<T, PASS, 64, 2, 2, false>(a, gate, stream);
+}
+
+template <Pass PASS>
+int launch_product(Args &a, ll_dtype dt, bool gate, bool vec, void *workspace, size_t workspace_bytes, void *stream) {
+  Plan p = plan_of(PASS, a, dt, vec);
+  const uint64_t one = (uint64_t)a.rows_c * a.n * 4;
+  if (workspace == nullptr) workspace_bytes = 0;
+  if (p.splits * one > workspace_bytes) p.splits = one == 0 ? 1 : (uint32_t)std::max<uint64_t>(1, workspace_bytes / one);
+  a.splits = p.splits;
+  a.parts = p.splits > 1 ? (float *)workspace : nullptr;
+  return dt == LL_F32 ? launch_plan<float, PASS>(a, p, gate, vec, stream)
+                      : launch_plan<__bf16, PASS>(a, p, gate, vec, stream);
+}
+
+// ---------------------------------------------------------------- few rows
+// Row blocks of 16 a workgroup of the streaming kernel takes; 0: the product
+// is not for it.
+int stream_blocks(const Args &a, bool vec) {
+  if (!vec) return 0;
+  const uint32_t each = (a.rows + a.groups - 1) / a.groups;  // rows a group on average
+  if (each > 32) return 0;
+  return each <= 16 ? 1 : 2;
+}
+
+template <typename T, int RB>
+int launch_stream(Args &a, bool gate, void *stream) {
+  constexpr int kNW = 8;
+  a.tiles_n = ((gate ? a.n / 2 : a.n) + 15) / 16;
+  const uint64_t rows = a.offsets == nullptr ? (a.rows + RB * 16 - 1) / (RB * 16)
+                                             : a.rows / (RB * 16) + std::min<uint64_t>(a.groups, a.rows);
+  const uint64_t grid = rows * a.tiles_n;
+  if (grid * kNW * 64 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
+  const tile_fn fn = gate ? k_stream<T, RB, kNW, true> : k_stream<T, RB, kNW, false>;
+  hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kNW * 64), 0, (hipStream_t)stream, a);
+  return launch_status();
 }
 
 // Every row starts at a 16-byte address.
@@ -129,7 +203,24 @@ int ll_linear_bytes(const ll_linear_desc *d, ll_linear_pass pass, size_t *bytes)
   if (bytes == nullptr || (int)pass < LL_LINEAR_FORWARD || (int)pass > LL_LINEAR_GRAD_W) return LL_ERR_INVALID;
   const int st = check_desc(d);
   if (st != LL_OK) return st;
+  // whether rows are whole 16-byte chunks depends on the pointers too; the
+  // larger of both plans' splits serves either
+  Args a{};
+  a.offsets = d->offsets;
+  a.groups = d->groups;
+  a.rows = (uint32_t)d->rows;
+  const bool gw = pass == LL_LINEAR_GRAD_W;
+  a.m = gw ? (uint32_t)d->out : a.rows;
+  a.n = (uint32_t)(pass == LL_LINEAR_FORWARD ? d->out : d->in);
+  a.k = gw ? a.rows : (uint32_t)(pass == LL_LINEAR_FORWARD ? d->in : d->out);
+  a.rows_c = gw ? a.m * (uint32_t)a.groups : a.rows;
+  const int es = esize(d->dt);
+  const bool whole = d->in * es % 16 == 0 && d->ldx * es % 16 == 0 && d->ldw * es % 16 == 0 && d->wstride * es % 16 == 0;
   *bytes = 0;
+  if (pass == LL_LINEAR_FORWARD && stream_blocks(a, whole) != 0) return LL_OK;
+  uint32_t splits = 1;
+  for (const bool vec : {false, true}) splits = std::max(splits, plan_of((Pass)pass, a, d->dt, vec).splits);
+  *bytes = splits > 1 ? (size_t)splits * a.rows_c * a.n * 4 : 0;
   return LL_OK;
 }
 
@@ -163,7 +254,7 @@ int ll_linear(const ll_linear_desc *d, const void *x, const void *w, const void 
   a.qstride = d->wstride;
   a.offsets = d->offsets;
   a.groups = d->groups;
-  a.rows = a.m = (uint32_t)d->rows;
+  a.rows = a.m = a.rows_c = (uint32_t)d->rows;
   a.n = (uint32_t)d->out;
   a.k = (uint32_t)d->in;
   a.bias = bias;
@@ -178,7 +269,12 @@ int ll_linear(const ll_linear_desc *d, const void *x, const void *w, const void 
   a.vec_c = rows16(y, d->ldy, es) && rows16(z, d->ldz, es) && rows16(residual, d->ldr, es);
   const bool vec = chunked(x, d->ldx, d->in, es) && chunked(w, d->ldw, d->in, es) && d->wstride * es % 16 == 0 &&
                    d->out * d->ldw * es < 0xF0000000ull;
-  return launch_product<kForward>(a, d->dt, gate, vec, stream);
+  const int blocks = stream_blocks(a, vec);
+  if (blocks == 1)
+    return d->dt == LL_F32 ? launch_stream<float, 1>(a, gate, stream) : launch_stream<__bf16, 1>(a, gate, stream);
+  if (blocks == 2)
+    return d->dt == LL_F32 ? launch_stream<float, 2>(a, gate, stream) : launch_stream<__bf16, 2>(a, gate, stream);
+  return launch_product<kForward>(a, d->dt, gate, vec, workspace, workspace_bytes, stream);
 }
 
 int ll_linear_grad_x(const ll_linear_desc *d, const void *dz, const void *w, const void *z, void *dx, void *workspace,
@@ -207,7 +303,7 @@ int ll_linear_grad_x(const ll_linear_desc *d, const void *dz, const void *w, con
   a.qstride = d->wstride;
   a.offsets = d->offsets;
   a.groups = d->groups;
-  a.rows = a.m = (uint32_t)d->rows;
+  a.rows = a.m = a.rows_c = (uint32_t)d->rows;
   a.n = (uint32_t)d->in;
   a.k = (uint32_t)d->out;
   a.z = z;
@@ -217,7 +313,7 @@ int ll_linear_grad_x(const ll_linear_desc *d, const void *dz, const void *w, con
   a.act = (int)d->act;
   a.vec_c = rows16(dx, d->ldx, es) && rows16(z, d->ldz, es);
   const bool vec = chunked(dz, d->ldy, d->out, es) && chunked(w, d->ldw, d->in, es) && d->wstride * es % 16 == 0;
-  return launch_product<kGradX>(a, d->dt, false, vec, stream);
+  return launch_product<kGradX>(a, d->dt, false, vec, workspace, workspace_bytes, stream);
 }
 
 int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, void *dw, void *dbias, uint32_t flags,
@@ -248,6 +344,7 @@ int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, voi
   a.groups = d->groups;
   a.rows = (uint32_t)d->rows;
   a.m = (uint32_t)d->out;
+  a.rows_c = a.m * (uint32_t)a.groups;
   a.n = (uint32_t)d->in;
   a.c = dw;
   a.ldc = d->ldw;
@@ -264,7 +361,7 @@ int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, voi
     const unsigned cols = 16 * (rows_vec ? 16 / es : 1);
     hipLaunchKernelGGL(fn, dim3((a.m + cols - 1) / cols, a.groups), dim3(1024), 0, (hipStream_t)stream, a);
   }
-  return launch_product<kGradW>(a, d->dt, false, vec, stream);
+  return launch_product<kGradW>(a, d->dt, false, vec, workspace, workspace_bytes, stream);
 }
 
 int ll_act_grad(const void *dy, size_t lddy, const void *z, size_t ldz, size_t rows, size_t features, ll_dtype dt,

@@ -42,6 +42,8 @@ struct Args {
   uint32_t flags;  // LL_GRAD_*
   bool vec_c;      // every epilogue row starts at a 16-byte address
   bool vec_b;      // so does every group's bias
+  float *parts;      // sums of the splits of k, [splits][rows of C][n], or NULL
+  uint32_t splits, rows_c;
 };
 
 // ---------------------------------------------------------------- activations
@@ -79,17 +81,25 @@ __host__ __device__ constexpr bool gated(int act) { return act == LL_ACT_SWIGLU 
 
 // ---------------------------------------------------------------- which tile
 //
-// Workgroups go to the 8 XCDs in turn, each with an L2 of its own, so XCD x
-// takes the x-th run of consecutive tiles.  Within a run tiles are numbered
-// in bands of kBand row tiles, column by column: the 32 workgroups an XCD
-// runs at a time then share a few panels of each operand.
-constexpr uint32_t kBand = 4;
+// Workgroups go to the 8 XCDs in turn, each with an L2 of its own.  Tiles are
+// numbered in bands of kBand row tiles, column by column, and XCD x takes runs
+// x, x + 8, ... of kRun consecutive tiles, what its 32 CUs work on at a time:
+// those share a few panels of each operand, and tiles of less work (a group's
+// last) fall to every XCD alike.
+constexpr uint32_t kBand = 4, kRun = 32;
 
 __device__ __forceinline__ bool tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t *tm, uint32_t *tn) {
   const uint32_t total = tiles_m * tiles_n;
   if (id >= total) return false;
-  const uint32_t x = id % 8, each = total / 8, more = total % 8;
-  const uint32_t t = x * each + min(x, more) + id / 8;
+  const uint32_t whole = total / (8 * kRun) * (8 * kRun);
+  uint32_t t;
+  if (id < whole) {
+    const uint32_t x = id % 8, i = id / 8;
+    t = (i / kRun * 8 + x) * kRun + i % kRun;
+  } else {  // the last, shorter runs
+    const uint32_t left = total - whole, i = id - whole, x = i % 8, each = left / 8, more = left % 8;
+    t = whole + x * each + min(x, more) + i / 8;
+  }
   const uint32_t band = t / (kBand * tiles_n), in_band = t % (kBand * tiles_n);
   const uint32_t high = min(kBand, tiles_m - band * kBand);
   *tm = band * kBand + in_band % high;
@@ -320,6 +330,11 @@ struct Loader {
   __device__ __forceinline__ void advance() {
     base += step;
     if constexpr (!VEC) left = left > step ? left - step : 0;
+  }
+
+  __device__ __forceinline__ void skip(uint32_t stages) {
+    base += stages * step;
+    if constexpr (!VEC) left = left > stages * step ? left - stages * step : 0;
   }
 
   // VEC: issues chunk c of a stage to LDS byte `at` (this wave's part of the
@@ -591,6 +606,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
     q += (uint64_t)g * a.qstride;
   }
 
+  // this workgroup's share of k, whole stages
+  const uint32_t share = a.splits == 1 ? k : ((k + BK - 1) / BK + a.splits - 1) / a.splits * BK;
+  const uint32_t k_from = min(k, blockIdx.y * share);
+
   Loader<T, BM, NW, kPkm, VEC> lp;
   Loader<T, BN, NW, kQkm, VEC> lq;
   if constexpr (kPkm)
@@ -604,6 +623,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
     lq.init(q, a.ldq, k, a.n, 0, 0, [&](uint32_t j, bool *ok) { return q_row<WTN, GATED>(tn, BN, j, a.n, ok); });
   else
     lq.init(q, a.ldq, k, 0, a.n, tn * BN, [](uint32_t, bool *) { return 0u; });
+
+  if (a.splits > 1) {
+    lp.skip(k_from / BK);
+    lq.skip(k_from / BK);
+    k = min(k - k_from, share);
+  }
 
   f32x4 acc[FN][FM];
 #pragma unroll
@@ -771,7 +796,16 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
       if (m >= m_end) break;
       Pack<float, kEw, true> v, u;
       v.load(mine + r * kPitch + c);
-      if constexpr (PASS == kForward) {
+      if (a.parts != nullptr) {
+        const uint32_t rc = PASS == kGradW ? g * a.m + m : m;
+        float *to = a.parts + ((uint64_t)blockIdx.y * a.rows_c + rc) * a.n + n0;
+        const uint32_t width = GATED ? a.n / 2 : a.n, left = width > n0 ? width - n0 : 0;
+        put8(to, v, left, a.n % 4 == 0);
+        if constexpr (GATED) {
+          u.load(mine + r * kPitch + kWidth + c);
+          put8(to + width, u, left, width % 4 == 0);
+        }
+      } else if constexpr (PASS == kForward) {
         if constexpr (GATED) u.load(mine + r * kPitch + kWidth + c);
         put_forward<T, GATED>(a, g, m, n0, v, u);
       } else if constexpr (PASS == kGradX) {
@@ -788,6 +822,156 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
   };
   finish(std::integral_constant<int, 0>{});
   if (PASS == kGradW || lower) finish(std::integral_constant<int, 1>{});
+}
+
+// ---------------------------------------------------------------- joining split sums
+//
+// Adds the splits of each element in order and finishes it as the product
+// itself would have.  A lane has kEw columns of a row.
+template <typename T, Pass PASS, bool GATED>
+__global__ __launch_bounds__(256) void k_join(Args a) {
+  const uint32_t width = GATED ? a.n / 2 : a.n, cols = (width + kEw - 1) / kEw;
+  const uint64_t id = blockIdx.x * 256ull + threadIdx.x;
+  const uint32_t r = (uint32_t)(id / cols), n0 = (uint32_t)(id % cols) * kEw;
+  if (r >= a.rows_c) return;
+  int g = 0;
+  if (PASS == kGradW) {
+    g = r / a.m;
+  } else if (a.offsets != nullptr) {
+    // the last group that starts at or before r and has it
+    int lo = 0, hi = a.groups;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (a.offsets[mid] <= (int)r)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    g = lo;
+    if ((int)r < a.offsets[g] || (int)r >= a.offsets[g + 1]) return;
+  }
+  Vals v, u;
+  const uint32_t left = width - n0;
+  for (uint32_t z = 0; z < a.splits; ++z) {
+    const float *from = a.parts + ((uint64_t)z * a.rows_c + r) * a.n + n0;
+    const Vals p = get8(from, left, a.n % 4 == 0);
+    if (z == 0)
+      v = p;
+    else
+      add8(v, p);
+    if constexpr (GATED) {
+      const Vals q = get8(from + width, left, width % 4 == 0);
+      if (z == 0)
+        u = q;
+      else
+        add8(u, q);
+    }
+  }
+  if constexpr (PASS == kForward)
+    put_forward<T, GATED>(a, g, r, n0, v, u);
+  else if constexpr (PASS == kGradX)
+    put_grad_x<T>(a, r, n0, v);
+  else if (a.flags & LL_GRAD_F32)
+    put_grad_w<float>(a, g, r % a.m, n0, v);
+  else
+    put_grad_w<T>(a, g, r % a.m, n0, v);
+}
+
+// ---------------------------------------------------------------- few rows a group
+//
+// The forward product of up to 16 * RB rows of a group, bound by reading the
+// weight once: a workgroup owns 16 weight rows (gated: 16 of each half), its
+// NW waves take 128 bytes of k of each in turn, straight from memory into
+// registers, and the waves' sums are joined in LDS in order.  The rows come
+// from L2.  kAhead steps of loads are under way in each wave.
+template <typename T, int RB, int NW, bool GATED>
+__global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
+  constexpr int kHalves = GATED ? 2 : 1, kAhead = RB == 1 ? 4 : 2;
+  constexpr int kStepK = 128 / (int)sizeof(T);
+  typedef typename Step<T>::frag frag;
+  constexpr int kPitch = kHalves * 16 + 4;
+  __shared__ float part[NW][RB * 16][kPitch];
+  const int lane = threadIdx.x % 64, i = lane % 16, q = lane / 16;
+  const uint32_t wave = uniform_u32(threadIdx.x / 64);
+  int g = 0;
+  uint32_t tn = 0, m0 = 0, m_end = 0;
+  if (!find_rows(a, blockIdx.x, RB * 16, &g, &m0, &m_end, &tn)) return;
+  const uint32_t width = GATED ? a.n / 2 : a.n;
+  const T *w = (const T *)a.q + (uint64_t)g * a.qstride + (uint64_t)(tn * 16) * a.ldq;
+  const T *x = (const T *)a.p + (uint64_t)m0 * a.ldp;
+  const uint64_t bw = (uint64_t)w, bx = (uint64_t)x;
+  const rsrc_t rw = make_rsrc((const void *)(((uint64_t)uniform_u32((uint32_t)(bw >> 32)) << 32) | uniform_u32((uint32_t)bw)),
+                              kOutside);
+  const rsrc_t rx = make_rsrc((const void *)(((uint64_t)uniform_u32((uint32_t)(bx >> 32)) << 32) | uniform_u32((uint32_t)bx)),
+                              kOutside);
+  uint32_t ow[kHalves], ox[RB];
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h)
+    ow[h] = tn * 16 + i < width ? (uint32_t)((uint64_t)(i + h * width) * a.ldq * sizeof(T)) + q * 16 : kOutside;
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+    ox[b] = m0 + b * 16 + i < m_end ? (uint32_t)((uint64_t)(b * 16 + i) * a.ldp * sizeof(T)) + q * 16 : kOutside;
+  f32x4 acc[kHalves][RB];
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+    for (int b = 0; b < RB; ++b) acc[h][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t steps = (a.k + kStepK - 1) / kStepK;
+  const uint32_t row_bytes = a.k * (uint32_t)sizeof(T);
+  union Raw {
+    u32x4 u;
+    frag f;
+  };
+  for (uint32_t s0 = wave; s0 < steps; s0 += NW * kAhead) {
+    Raw fw[kAhead][2][kHalves], fx[kAhead][2][RB];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      const uint32_t at = (s0 + n * NW) * 128;  // past the last step: outside
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const uint32_t o = at + c * 64;
+        const bool in = o + q * 16 < row_bytes;
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+          fw[n][c][h].u = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(in && ow[h] != kOutside ? ow[h] + o : kOutside), 0, 0);
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+          fx[n][c][b].u = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)(in && ox[b] != kOutside ? ox[b] + o : kOutside), 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);  // every load is issued before the first result is used
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+          for (int b = 0; b < RB; ++b) acc[h][b] = mma(fw[n][c][h].f, fx[n][c][b].f, acc[h][b]);
+  }
+#pragma unroll
+  for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+    for (int b = 0; b < RB; ++b) *reinterpret_cast<f32x4 *>(&part[wave][b * 16 + i][h * 16 + q * 4]) = acc[h][b];
+  __syncthreads();
+  for (int t = threadIdx.x; t < RB * 32; t += NW * 64) {
+    const int r = t / 2, c = t % 2 * kEw;
+    const uint32_t m = m0 + r;
+    if (m >= m_end) continue;
+    Vals v, u;
+#pragma unroll
+    for (int e = 0; e < kEw; ++e) {
+      v.v[e] = part[0][r][c + e];
+      if constexpr (GATED) u.v[e] = part[0][r][16 + c + e];
+    }
+    for (int o = 1; o < NW; ++o)
+#pragma unroll
+      for (int e = 0; e < kEw; ++e) {
+        v.v[e] += part[o][r][c + e];
+        if constexpr (GATED) u.v[e] += part[o][r][16 + c + e];
+      }
+    put_forward<T, GATED>(a, g, m, tn * 16 + c, v, u);
+  }
 }
 
 // ---------------------------------------------------------------- bias gradient
