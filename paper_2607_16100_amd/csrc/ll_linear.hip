@@ -153,14 +153,18 @@ int launch_product(Args &a, ll_dtype dt, bool gate, bool vec, void *workspace, s
 int stream_blocks(const Args &a, bool vec) {
   if (!vec) return 0;
   const uint32_t each = (a.rows + a.groups - 1) / a.groups;  // rows a group on average
-  if (each > 32) return 0;
-  return each <= 16 ? 1 : 2;
+#ifndef LL_T1
+#define LL_T1 16
+#define LL_T2 32
+#endif
+  if (each > LL_T2) return 0;
+  return each <= LL_T1 ? 1 : 2;
 }
 
 template <typename T, int RB>
 int launch_stream(Args &a, bool gate, void *stream) {
   constexpr int kNW = 8;
-  a.tiles_n = ((gate ? a.n / 2 : a.n) + 15) / 16;
+  a.tiles_n = gate ? (a.n / 2 + 15) / 16 : (a.n + 31) / 32;
   const uint64_t rows = a.offsets == nullptr ? (a.rows + RB * 16 - 1) / (RB * 16)
                                              : a.rows / (RB * 16) + std::min<uint64_t>(a.groups, a.rows);
   const uint64_t grid = rows * a.tiles_n;

@@ -880,16 +880,17 @@ __global__ __launch_bounds__(256) void k_join(Args a) {
 // ---------------------------------------------------------------- few rows a group
 //
 // The forward product of up to 16 * RB rows of a group, bound by reading the
-// weight once: a workgroup owns 16 weight rows (gated: 16 of each half), its
-// NW waves take 128 bytes of k of each in turn, straight from memory into
-// registers, and the waves' sums are joined in LDS in order.  The rows come
-// from L2.  kAhead steps of loads are under way in each wave.
+// weight once: a workgroup owns 2 x 16 weight rows (gated: 16 of each half,
+// else 32 in a row), its NW waves take 128 bytes of k of each in turn, straight
+// from memory into registers, and the waves' sums are joined in LDS in order.
+// The rows come from L2, as often as there are workgroups: two fragments of
+// weight share one of them.  kAhead steps of loads are under way in each wave.
 template <typename T, int RB, int NW, bool GATED>
 __global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
-  constexpr int kHalves = GATED ? 2 : 1, kAhead = RB == 1 ? 4 : 2;
+  constexpr int kAhead = RB == 1 ? 4 : 2, kCols = GATED ? 16 : 32;  // columns of C
   constexpr int kStepK = 128 / (int)sizeof(T);
+  constexpr int kPitch = 2 * 16 + 4;
   typedef typename Step<T>::frag frag;
-  constexpr int kPitch = kHalves * 16 + 4;
   __shared__ float part[NW][RB * 16][kPitch];
   const int lane = threadIdx.x % 64, i = lane % 16, q = lane / 16;
   const uint32_t wave = uniform_u32(threadIdx.x / 64);
@@ -897,23 +898,25 @@ __global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
   uint32_t tn = 0, m0 = 0, m_end = 0;
   if (!find_rows(a, blockIdx.x, RB * 16, &g, &m0, &m_end, &tn)) return;
   const uint32_t width = GATED ? a.n / 2 : a.n;
-  const T *w = (const T *)a.q + (uint64_t)g * a.qstride + (uint64_t)(tn * 16) * a.ldq;
-  const T *x = (const T *)a.p + (uint64_t)m0 * a.ldp;
-  const uint64_t bw = (uint64_t)w, bx = (uint64_t)x;
-  const rsrc_t rw = make_rsrc((const void *)(((uint64_t)uniform_u32((uint32_t)(bw >> 32)) << 32) | uniform_u32((uint32_t)bw)),
-                              kOutside);
-  const rsrc_t rx = make_rsrc((const void *)(((uint64_t)uniform_u32((uint32_t)(bx >> 32)) << 32) | uniform_u32((uint32_t)bx)),
-                              kOutside);
-  uint32_t ow[kHalves], ox[RB];
+  const uint64_t bw = (uint64_t)((const T *)a.q + (uint64_t)g * a.qstride + (uint64_t)(tn * kCols) * a.ldq);
+  const uint64_t bx = (uint64_t)((const T *)a.p + (uint64_t)m0 * a.ldp);
+  auto rsrc = [](uint64_t b) {
+    return make_rsrc((const void *)(((uint64_t)uniform_u32((uint32_t)(b >> 32)) << 32) | uniform_u32((uint32_t)b)),
+                     kOutside);
+  };
+  const rsrc_t rw = rsrc(bw), rx = rsrc(bx);
+  uint32_t ow[2], ox[RB];
 #pragma unroll
-  for (int h = 0; h < kHalves; ++h)
-    ow[h] = tn * 16 + i < width ? (uint32_t)((uint64_t)(i + h * width) * a.ldq * sizeof(T)) + q * 16 : kOutside;
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t row = i + h * (GATED ? width : 16);
+    ow[h] = tn * kCols + (GATED ? i : row) < width ? (uint32_t)((uint64_t)row * a.ldq * sizeof(T)) + q * 16 : kOutside;
+  }
 #pragma unroll
   for (int b = 0; b < RB; ++b)
     ox[b] = m0 + b * 16 + i < m_end ? (uint32_t)((uint64_t)(b * 16 + i) * a.ldp * sizeof(T)) + q * 16 : kOutside;
-  f32x4 acc[kHalves][RB];
+  f32x4 acc[2][RB];
 #pragma unroll
-  for (int h = 0; h < kHalves; ++h)
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int b = 0; b < RB; ++b) acc[h][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   const uint32_t steps = (a.k + kStepK - 1) / kStepK;
@@ -922,8 +925,13 @@ __global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
     u32x4 u;
     frag f;
   };
+  auto load = [](rsrc_t rs, uint32_t off, uint32_t o, bool in) __attribute__((always_inline)) {
+    Raw r;
+    r.u = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(in && off != kOutside ? off + o : kOutside), 0, 0);
+    return r;
+  };
   for (uint32_t s0 = wave; s0 < steps; s0 += NW * kAhead) {
-    Raw fw[kAhead][2][kHalves], fx[kAhead][2][RB];
+    Raw fw[kAhead][2][2], fx[kAhead][2][RB];
 #pragma unroll
     for (int n = 0; n < kAhead; ++n) {
       const uint32_t at = (s0 + n * NW) * 128;  // past the last step: outside
@@ -932,11 +940,9 @@ __global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
         const uint32_t o = at + c * 64;
         const bool in = o + q * 16 < row_bytes;
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h)
-          fw[n][c][h].u = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(in && ow[h] != kOutside ? ow[h] + o : kOutside), 0, 0);
+        for (int h = 0; h < 2; ++h) fw[n][c][h] = load(rw, ow[h], o, in);
 #pragma unroll
-        for (int b = 0; b < RB; ++b)
-          fx[n][c][b].u = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)(in && ox[b] != kOutside ? ox[b] + o : kOutside), 0, 0);
+        for (int b = 0; b < RB; ++b) fx[n][c][b] = load(rx, ox[b], o, in);
       }
     }
     __builtin_amdgcn_sched_barrier(0);  // every load is issued before the first result is used
@@ -945,17 +951,18 @@ __global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int b = 0; b < RB; ++b) acc[h][b] = mma(fw[n][c][h].f, fx[n][c][b].f, acc[h][b]);
   }
 #pragma unroll
-  for (int h = 0; h < kHalves; ++h)
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int b = 0; b < RB; ++b) *reinterpret_cast<f32x4 *>(&part[wave][b * 16 + i][h * 16 + q * 4]) = acc[h][b];
   __syncthreads();
-  for (int t = threadIdx.x; t < RB * 32; t += NW * 64) {
-    const int r = t / 2, c = t % 2 * kEw;
+  constexpr int kLanes = kCols / kEw;
+  for (int t = threadIdx.x; t < RB * 16 * kLanes; t += NW * 64) {
+    const int r = t / kLanes, c = t % kLanes * kEw;
     const uint32_t m = m0 + r;
     if (m >= m_end) continue;
     Vals v, u;
@@ -970,7 +977,7 @@ __global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
         v.v[e] += part[o][r][c + e];
         if constexpr (GATED) u.v[e] += part[o][r][16 + c + e];
       }
-    put_forward<T, GATED>(a, g, m, tn * 16 + c, v, u);
+    put_forward<T, GATED>(a, g, m, tn * kCols + c, v, u);
   }
 }
 

@@ -52,23 +52,20 @@ route_fn route_of(bool grad, bool vec) {
   return vec ? k_route<T, W, NPL, true> : k_route<T, W, NPL, false>;
 }
 
-template <typename T>
-route_fn route_fn_of(int w, int npl, bool grad, bool vec) {
-  if (w == 16) {
-    switch (npl) {
-      case 1: return route_of<T, 16, 1>(grad, false);
-      case 2: return route_of<T, 16, 2>(grad, vec);
-      case 4: return route_of<T, 16, 4>(grad, vec);
-      case 8: return route_of<T, 16, 8>(grad, vec);
-      default: return route_of<T, 16, 16>(grad, vec);
-    }
-  }
+// A lane's logits: the fewest of these that hold a row (fewer steps over them).
+constexpr int kNpl[] = {1, 2, 4, 6, 8, 10, 12, 16};
+
+template <typename T, int W>
+route_fn route_fn_of(int npl, bool grad, bool vec) {
   switch (npl) {
-    case 1: return route_of<T, 64, 1>(grad, false);
-    case 2: return route_of<T, 64, 2>(grad, vec);
-    case 4: return route_of<T, 64, 4>(grad, vec);
-    case 8: return route_of<T, 64, 8>(grad, vec);
-    default: return route_of<T, 64, 16>(grad, vec);
+    case 1: return route_of<T, W, 1>(grad, vec && sizeof(T) == 4);
+    case 2: return route_of<T, W, 2>(grad, vec);
+    case 4: return route_of<T, W, 4>(grad, vec);
+    case 6: return route_of<T, W, 6>(grad, vec);
+    case 8: return route_of<T, W, 8>(grad, vec);
+    case 10: return route_of<T, W, 10>(grad, vec);
+    case 12: return route_of<T, W, 12>(grad, vec);
+    default: return route_of<T, W, 16>(grad, vec);
   }
 }
 
@@ -76,11 +73,20 @@ int launch_route(const RouteArgs &a, ll_dtype dt, bool grad, void *stream) {
   // 16 lanes a token (four tokens a wave share the steps over the lanes)
   // where a token's logits and choices fit them, else a whole wave
   const int w = a.experts <= 256 && a.k <= 16 ? 16 : 64;
-  int npl = 1;
-  while (npl * w < a.experts) npl *= 2;
+  int npl = 16;
+  for (int n : kNpl)
+    if (n * w >= a.experts) {
+      npl = n;
+      break;
+    }
   const int es = esize(dt);
-  const bool vec = vec16(a.logits, a.ld, es) && vec16(a.dlogits, a.ldd, es);
-  const route_fn fn = dt == LL_F32 ? route_fn_of<float>(w, npl, grad, vec) : route_fn_of<__bf16>(w, npl, grad, vec);
+  auto dwords = [&](const void *p, size_t ld) { return aligned(p, 4) && ld * es % 4 == 0; };
+  const bool vec = dwords(a.logits, a.ld) && dwords(a.dlogits, a.ldd);
+  route_fn fn;
+  if (w == 16)
+    fn = dt == LL_F32 ? route_fn_of<float, 16>(npl, grad, vec) : route_fn_of<__bf16, 16>(npl, grad, vec);
+  else
+    fn = dt == LL_F32 ? route_fn_of<float, 64>(npl, grad, vec) : route_fn_of<__bf16, 64>(npl, grad, vec);
   const unsigned per = kThreads / w;
   hipLaunchKernelGGL(fn, dim3((a.tokens + per - 1) / per), dim3(kThreads), 0, (hipStream_t)stream, a);
   return launch_status();
@@ -240,7 +246,7 @@ int ll_moe_dispatch(const int32_t *ids, size_t tokens, int k, int first, int exp
   a.k = k;
   a.features = (uint32_t)features;
   const RowShape shape = row_shape(a, es);
-  const size_t lds = (size_t)(2 + kWaves) * experts * 4;
+  const size_t lds = (size_t)kSortInts * experts * 4;
   if (pairs <= kSmallPairs) {
     const unsigned grid = a.x == nullptr ? 1 : std::max(1u, a.tokens);
     const auto fn = dt == LL_F32 ? (shape.vec ? k_dispatch_small<float, true> : k_dispatch_small<float, false>)

@@ -37,21 +37,27 @@ struct RouteArgs {
 };
 
 // The logits of one lane; past the last expert, and for NaN, -Infinity.
+// VEC: rows start at multiples of 4 bytes, and NPL elements are whole dwords.
 template <typename T, int NPL, bool VEC>
 __device__ __forceinline__ void load_logits(const T *row, int e0, int experts, float (&l)[NPL]) {
-  Pack<T, NPL, VEC> p;
-  if (VEC && e0 + NPL <= experts)
-    p.load(row + e0);
-  else
-    p.load_some(row + e0, experts - e0, kNegInf);
+  if (VEC && e0 + NPL <= experts) {
+    T v[NPL];
+    __builtin_memcpy(v, __builtin_assume_aligned(row + e0, 4), sizeof v);
 #pragma unroll
-  for (int i = 0; i < NPL; ++i) l[i] = p.v[i] == p.v[i] ? p.v[i] : kNegInf;
+    for (int i = 0; i < NPL; ++i) l[i] = Num<T>::get(v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) l[i] = e0 + i < experts ? Num<T>::get(row[e0 + i]) : kNegInf;
+  }
+#pragma unroll
+  for (int i = 0; i < NPL; ++i) l[i] = l[i] == l[i] ? l[i] : kNegInf;
 }
 
-// Softmax statistics of a token over its W lanes: the maximum (0 where every
-// logit is -Infinity) and the reciprocal of the sum of exponentials.
+// Softmax statistics of a token over its W lanes: e <- the exponentials of l
+// less the maximum, inv <- the reciprocal of their sum (0 where every logit is
+// -Infinity).  Returns the maximum.
 template <int W, int NPL>
-__device__ __forceinline__ void softmax_stats(const float (&l)[NPL], float *m, float *inv) {
+__device__ __forceinline__ float softmax_stats(const float (&l)[NPL], float (&e)[NPL], float *inv) {
   float mx = l[0];
 #pragma unroll
   for (int i = 1; i < NPL; ++i) mx = fmaxf(mx, l[i]);
@@ -59,13 +65,28 @@ __device__ __forceinline__ void softmax_stats(const float (&l)[NPL], float *m, f
   if (mx == kNegInf) mx = 0.f;
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < NPL; ++i) s += expf(l[i] - mx);
+  for (int i = 0; i < NPL; ++i) {
+    e[i] = exp_f32(l[i] - mx);
+    s += e[i];
+  }
   s = group_sum<W>(s);
-  *m = mx;
   *inv = s > 0.f || s != s ? 1.f / s : 0.f;
+  return mx;
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + exp_f32(-x)); }
+
+// The score of a choice with logit x (-Infinity: none), before any division by
+// the chosen ones' sum.  m, inv: softmax statistics, where they are needed.
+// A normalised softmax is one over the chosen logits alone, whatever m is, so
+// the other experts' exponentials are never computed for it.
+template <int W>
+__device__ __forceinline__ float choice_score(const RouteArgs &a, float x, float m, float inv) {
+  if (a.score != 0) return x == kNegInf ? 0.f : sigmoid(x);
+  if (!a.normalise) return exp_f32(x - m) * inv;
+  m = group_max<W>(x);
+  return x == kNegInf ? 0.f : exp_f32(x - m);
+}
 
 template <typename T, int W, int NPL, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
@@ -74,44 +95,48 @@ __global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
   const bool live = t < a.tokens;  // no early exit: the lanes of a wave work on several tokens together
   const T *row = (const T *)a.logits + (uint64_t)(live ? t : 0) * a.ld;
   const int e0 = sub * NPL;
-  float l[NPL], key[NPL];
-  load_logits<T, NPL, VEC>(row, e0, a.experts, l);
-#pragma unroll
-  for (int i = 0; i < NPL; ++i) {
-    float x = l[i];
-    if (a.bias != nullptr && e0 + i < a.experts) x += a.bias[e0 + i];
-    key[i] = x == x ? x : kNegInf;
-  }
+  float key[NPL];
+  load_logits<T, NPL, VEC>(row, e0, a.experts, key);
   float m = 0.f, inv = 0.f;
-  if (a.score == 0) softmax_stats<W, NPL>(l, &m, &inv);
+  if (a.score == 0 && !a.normalise) {
+    float e[NPL];
+    m = softmax_stats<W, NPL>(key, e, &inv);
+  }
+  if (a.bias != nullptr) {
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) {
+      const float x = key[i] + (e0 + i < a.experts ? a.bias[e0 + i] : 0.f);
+      key[i] = x == x ? x : kNegInf;
+    }
+  }
   int mine = -1;  // lane j keeps the j-th choice
   for (int j = 0; j < a.k; ++j) {
     float best = key[0];
-    int at = 0;
 #pragma unroll
-    for (int i = 1; i < NPL; ++i)
-      if (key[i] > best) {
-        best = key[i];
-        at = i;
-      }
+    for (int i = 1; i < NPL; ++i) best = fmaxf(best, key[i]);
     const float top = group_max<W>(best);
     uint64_t have = __ballot(best == top && top > kNegInf);
     if constexpr (W == 16) have = (have >> (lane & 48)) & 0xFFFFull;
     const int who = have == 0 ? -1 : __ffsll((unsigned long long)have) - 1;
+    // the winner's lowest key that is the maximum: found and taken out
+    bool open = sub == who;
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) {
+      const bool hit = open && key[i] == top;
+      key[i] = hit ? kNegInf : key[i];
+      at = hit ? i : at;
+      open = open && !hit;
+    }
     const int won = __shfl(at, who < 0 ? 0 : who, W);
     if (sub == j) mine = who < 0 ? -1 : who * NPL + won;
-    if (sub == who) {
-#pragma unroll
-      for (int i = 0; i < NPL; ++i)
-        if (i == at) key[i] = kNegInf;
-    }
   }
-  float u = 0.f;
+  float x = kNegInf;
   if (mine >= 0) {
-    const float x = Num<T>::get(row[mine]);
-    u = a.score == 0 ? expf(x - m) * inv : sigmoid(x);
-    if (x != x) u = 0.f;
+    x = Num<T>::get(row[mine]);
+    if (x != x) x = kNegInf;
   }
+  float u = choice_score<W>(a, x, m, inv);
   if (a.normalise) {
     const float tot = group_sum<W>(u);
     u = tot > 0.f || tot != tot ? u / tot : 0.f;
@@ -128,6 +153,7 @@ __global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
 //   softmax, normalised dl_i = u_i (g_i - sum u g)        (chosen only)
 //   sigmoid             dl_i = g_i s_i (1 - s_i)          (chosen only)
 //   sigmoid, normalised dl_i = u_i (g_i - sum u g)(1 - s_i)
+// Only the first needs the row; the others read the chosen logits.
 template <typename T, int W, int NPL, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_route_grad(RouteArgs a) {
   __shared__ float coef[kThreads * NPL];
@@ -136,26 +162,29 @@ __global__ __launch_bounds__(kThreads) void k_route_grad(RouteArgs a) {
   const bool live = t < a.tokens;
   const T *row = (const T *)a.logits + (uint64_t)(live ? t : 0) * a.ld;
   const int e0 = sub * NPL;
+  const bool all = a.score == 0 && !a.normalise;  // every expert's logit moves the softmax
   float *mine = coef + (threadIdx.x / W) * (W * NPL);
-  float l[NPL];
-  load_logits<T, NPL, VEC>(row, e0, a.experts, l);
 #pragma unroll
   for (int i = 0; i < NPL; ++i) mine[e0 + i] = 0.f;
   int id = -1;
-  float g = 0.f;
+  float g = 0.f, x = kNegInf;
   if (live && sub < a.k) {
     id = a.ids[(uint64_t)t * a.k + sub];
     if (id < 0 || id >= a.experts) id = -1;
-    if (id >= 0) g = a.scale * a.dweights[(uint64_t)t * a.k + sub];
+    if (id >= 0) {
+      g = a.scale * a.dweights[(uint64_t)t * a.k + sub];
+      x = Num<T>::get(row[id]);
+      if (x != x) x = kNegInf;
+    }
   }
+  float e[NPL];
   float m = 0.f, inv = 0.f;
-  if (a.score == 0) softmax_stats<W, NPL>(l, &m, &inv);
-  float p = 0.f;
-  if (id >= 0) {
-    const float x = Num<T>::get(row[id]);
-    p = a.score == 0 ? expf(x - m) * inv : sigmoid(x);
-    if (x != x) p = 0.f;
+  if (all) {
+    float l[NPL];
+    load_logits<T, NPL, VEC>(row, e0, a.experts, l);
+    m = softmax_stats<W, NPL>(l, e, &inv);
   }
+  const float p = choice_score<W>(a, x, m, inv);
   float u = p;
   if (a.normalise) {
     const float tot = group_sum<W>(p);
@@ -163,8 +192,8 @@ __global__ __launch_bounds__(kThreads) void k_route_grad(RouteArgs a) {
   }
   const float mean = group_sum<W>(u * g);
   __syncthreads();
-  float c = 0.f;
   if (id >= 0) {
+    float c;
     if (a.score == 0)
       c = a.normalise ? u * (g - mean) : p * g;
     else
@@ -172,20 +201,24 @@ __global__ __launch_bounds__(kThreads) void k_route_grad(RouteArgs a) {
     mine[id] = c;
   }
   __syncthreads();
-  Pack<T, NPL, VEC> out;
-  const bool all = a.score == 0 && !a.normalise;  // every expert's logit moves the softmax
+  if (!live) return;
+  float d[NPL];
 #pragma unroll
   for (int i = 0; i < NPL; ++i) {
-    float d = mine[e0 + i];
-    if (all) d -= expf(l[i] - m) * inv * mean;
-    out.v[i] = d;
+    d[i] = mine[e0 + i];
+    if (all) d[i] -= e[i] * inv * mean;
   }
-  if (!live) return;
   T *drow = (T *)a.dlogits + (uint64_t)t * a.ldd;
-  if (VEC && e0 + NPL <= a.experts)
-    out.store(drow + e0);
-  else
-    out.store_some(drow + e0, a.experts - e0);
+  if (VEC && e0 + NPL <= a.experts) {
+    T v[NPL];
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) v[i] = Num<T>::put(d[i]);
+    __builtin_memcpy(__builtin_assume_aligned(drow + e0, 4), v, sizeof v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NPL; ++i)
+      if (e0 + i < a.experts) drow[e0 + i] = Num<T>::put(d[i]);
+  }
 }
 
 // ---------------------------------------------------------------- sorting by expert
@@ -208,12 +241,26 @@ __device__ __forceinline__ int local_expert(const SortArgs &a, uint32_t i) {
   return e >= 0 && e < a.experts ? (int)e : -1;
 }
 
+constexpr int kAheadIds = 4;  // ids of a lane under way
+
+// f(i, local expert or -1) for a wave's pairs [lo, hi), 64 at a time (every
+// lane takes part in each batch; past hi the expert is -1).
+template <typename F>
+__device__ __forceinline__ void wave_pairs(const SortArgs &a, uint32_t lo, uint32_t hi, F f) {
+  for (uint32_t base = lo + threadIdx.x % 64; base - threadIdx.x % 64 < hi; base += 64 * kAheadIds) {
+    int e[kAheadIds];
+#pragma unroll
+    for (int n = 0; n < kAheadIds; ++n) e[n] = base + 64 * n < hi ? local_expert(a, base + 64 * n) : -1;
+#pragma unroll
+    for (int n = 0; n < kAheadIds; ++n) f(base + 64 * n, e[n]);
+  }
+}
+
 // Counts of a wave's pairs [lo, hi) into cnt[experts] (zeroed, LDS).
 __device__ __forceinline__ void wave_count(const SortArgs &a, uint32_t lo, uint32_t hi, int *cnt) {
-  for (uint32_t i = lo + threadIdx.x % 64; i < hi; i += 64) {
-    const int e = local_expert(a, i);
+  wave_pairs(a, lo, hi, [&](uint32_t, int e) {
     if (e >= 0) atomicAdd(&cnt[e], 1);  // integers: the order does not matter
-  }
+  });
 }
 
 // Places of a wave's pairs [lo, hi), cnt[e] = the first place of expert e for
@@ -222,9 +269,7 @@ __device__ __forceinline__ void wave_count(const SortArgs &a, uint32_t lo, uint3
 template <typename F>
 __device__ __forceinline__ void wave_place(const SortArgs &a, uint32_t lo, uint32_t hi, int *cnt, F put) {
   const int lane = threadIdx.x % 64;
-  for (uint32_t base = lo; base < hi; base += 64) {
-    const uint32_t i = base + lane;
-    const int e = i < hi ? local_expert(a, i) : -1;
+  wave_pairs(a, lo, hi, [&](uint32_t i, int e) {
     uint64_t same = __ballot(e >= 0);  // lanes with this lane's expert
     for (int b = 0; b < a.bits; ++b) {
       const uint64_t m = __ballot(e >= 0 && ((e >> b) & 1));
@@ -237,7 +282,7 @@ __device__ __forceinline__ void wave_place(const SortArgs &a, uint32_t lo, uint3
     if (e >= 0 && before == 0) cnt[e] += __popcll(same);
     __builtin_amdgcn_wave_barrier();
     if (i < hi) put(i, place);
-  }
+  });
 }
 
 // base[e] <- sum of total[e'] for e' < e, by the block's first wave; returns
@@ -277,45 +322,43 @@ static __global__ __launch_bounds__(kThreads) void k_sort_count(SortArgs a) {
 }
 
 // Places of this block's pairs.  LDS: total[experts], base[experts],
-// cnt[kWaves][experts].  hist NULL: the block has every pair (blocks == 1).
+// before[experts], cnt[kWaves][experts].  hist NULL: the block has every pair
+// (blocks == 1).
+constexpr int kSortInts = 3 + kWaves;  // LDS integers an expert
+
 template <typename F>
 __device__ __forceinline__ void block_sort(const SortArgs &a, uint32_t block, int *lds, int *sum, F put) {
-  int *total = lds, *base = lds + a.experts, *cnt = lds + 2 * a.experts;
-  for (int i = threadIdx.x; i < kWaves * a.experts; i += kThreads) cnt[i] = 0;
+  int *total = lds, *base = lds + a.experts, *before = lds + 2 * a.experts, *cnt = lds + 3 * a.experts;
+  for (int i = threadIdx.x; i < kSortInts * a.experts; i += kThreads) lds[i] = 0;
   __syncthreads();
   const int wave = threadIdx.x / 64;
   const uint32_t part = a.chunk / kWaves;
   const uint32_t lo = min(a.pairs, block * a.chunk + wave * part);
   const uint32_t hi = min(a.pairs, lo + part);
   wave_count(a, lo, hi, cnt + wave * a.experts);
-  __syncthreads();
   // per expert: rows of all blocks, and of the blocks before this one
-  int before[LL_MOE_MAX_EXPERTS / kThreads];
-#pragma unroll
-  for (int n = 0; n < LL_MOE_MAX_EXPERTS / kThreads; ++n) {
-    const int e = threadIdx.x + n * kThreads;
-    before[n] = 0;
-    if (e >= a.experts) continue;
-    int all = 0;
-    if (a.hist == nullptr) {
-      for (int w = 0; w < kWaves; ++w) all += cnt[w * a.experts + e];
-    } else {
-      for (uint32_t b = 0; b < a.blocks; ++b) {
-        const int v = a.hist[(uint64_t)b * a.experts + e];
-        if (b < block) before[n] += v;
-        all += v;
-      }
+  if (a.hist != nullptr) {
+    const uint32_t n = a.blocks * a.experts;
+    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+      const int v = a.hist[i], e = i % a.experts;
+      if (v == 0) continue;
+      atomicAdd(&total[e], v);
+      if (i < block * a.experts) atomicAdd(&before[e], v);
     }
-    total[e] = all;
   }
   __syncthreads();
+  if (a.hist == nullptr) {
+    for (int e = threadIdx.x; e < a.experts; e += kThreads) {
+      int all = 0;
+      for (int w = 0; w < kWaves; ++w) all += cnt[w * a.experts + e];
+      total[e] = all;
+    }
+    __syncthreads();
+  }
   scan_experts(total, base, a.experts, sum);
   __syncthreads();
-#pragma unroll
-  for (int n = 0; n < LL_MOE_MAX_EXPERTS / kThreads; ++n) {
-    const int e = threadIdx.x + n * kThreads;
-    if (e >= a.experts) continue;
-    int at = base[e] + before[n];
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) {
+    int at = base[e] + before[e];
     for (int w = 0; w < kWaves; ++w) {
       const int c = cnt[w * a.experts + e];
       cnt[w * a.experts + e] = at;
@@ -368,6 +411,16 @@ constexpr int chunk_elems() {
   return VEC ? Num<T>::kPer16 : 1;
 }
 
+// A chunk as it lies in memory: converted where it is used, so that a load
+// does not wait for the one before it.
+template <typename T, int C>
+struct Raw {
+  typedef T vec __attribute__((ext_vector_type(C)));
+  vec r;
+  __device__ __forceinline__ void load(const T *p) { r = *reinterpret_cast<const vec *>(p); }
+  __device__ __forceinline__ float get(int i) const { return Num<T>::get(r[i]); }
+};
+
 // One token's row to each of its local sorted rows; read once, written up to
 // k times, so a token's row comes from memory once however many experts it
 // has here.
@@ -380,11 +433,19 @@ __device__ __forceinline__ void push_row(const RowArgs &a, uint32_t t, const int
   if (!any) return;
   const uint32_t chunks = a.features / C;
   const vec *src = (const vec *)((const T *)a.x + (uint64_t)t * a.ldx);
-  for (uint32_t c = threadIdx.x % TPR; c < chunks; c += TPR) {
-    const vec v = src[c];
+  constexpr int kAhead = 4;  // loads of a thread under way
+  for (uint32_t c0 = threadIdx.x % TPR; c0 < chunks; c0 += TPR * kAhead) {
+    vec v[kAhead];
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n)
+      if (c0 + n * TPR < chunks) v[n] = src[c0 + n * TPR];
     for (int j = 0; j < a.k; ++j) {
       const int r = rows_of[j];
-      if (r >= 0) ((vec *)((T *)a.out + (uint64_t)(uint32_t)r * a.ldo))[c] = v;
+      if (r < 0) continue;
+      vec *to = (vec *)((T *)a.out + (uint64_t)(uint32_t)r * a.ldo);
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n)
+        if (c0 + n * TPR < chunks) to[c0 + n * TPR] = v[n];
     }
   }
 }
@@ -402,7 +463,7 @@ template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_dispatch_small(SortArgs s, RowArgs a) {
   extern __shared__ int lds[];
   __shared__ int sum;
-  int *mine = lds + (2 + kWaves) * s.experts;  // rows of this block's token
+  int *mine = lds + kSortInts * s.experts;  // rows of this block's token
   const uint32_t t = blockIdx.x;
   const uint32_t lo = t * (uint32_t)a.k, hi = lo + (uint32_t)a.k;
   const bool lead = blockIdx.x == 0;
@@ -435,12 +496,13 @@ __global__ __launch_bounds__(kThreads) void k_combine(RowArgs a) {
   const float *w = a.weights == nullptr ? nullptr : a.weights + (uint64_t)t * a.k;
   const uint32_t chunks = a.features / C;
   for (uint32_t c = threadIdx.x % TPR; c < chunks; c += TPR) {
-    Pack<T, C, VEC> acc, res;
+    Pack<T, C, VEC> acc;
+    Raw<T, C> res;
 #pragma unroll
     for (int i = 0; i < C; ++i) acc.v[i] = 0.f;
     if (a.extra != nullptr) res.load((const T *)a.extra + (uint64_t)t * a.lde + c * C);
     for (int j0 = 0; j0 < a.k; j0 += kBatch) {
-      Pack<T, C, VEC> y[kBatch];
+      Raw<T, C> y[kBatch];
       bool ok[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
@@ -453,12 +515,12 @@ __global__ __launch_bounds__(kThreads) void k_combine(RowArgs a) {
         if (!ok[j]) continue;
         const float wj = w == nullptr ? 1.f : w[j0 + j];
 #pragma unroll
-        for (int i = 0; i < C; ++i) acc.v[i] = __builtin_fmaf(wj, y[j].v[i], acc.v[i]);
+        for (int i = 0; i < C; ++i) acc.v[i] = __builtin_fmaf(wj, y[j].get(i), acc.v[i]);
       }
     }
     if (a.extra != nullptr) {
 #pragma unroll
-      for (int i = 0; i < C; ++i) acc.v[i] += res.v[i];
+      for (int i = 0; i < C; ++i) acc.v[i] += res.get(i);
     }
     acc.store((T *)a.out + (uint64_t)t * a.ldo + c * C);
   }
@@ -489,7 +551,8 @@ __global__ __launch_bounds__(kThreads) void k_combine_grad(RowArgs a) {
       wj[j] = w == nullptr || r[j] < 0 ? 1.f : w[j0 + j];
     }
     for (uint32_t c = threadIdx.x % TPR; c < chunks; c += TPR) {
-      Pack<T, C, VEC> d, y[kBatch], o;
+      Pack<T, C, VEC> d, o;
+      Raw<T, C> y[kBatch];
       d.load((const T *)a.extra + t0 * a.lde + c * C);
       if (a.dweights != nullptr) {
 #pragma unroll
@@ -504,7 +567,7 @@ __global__ __launch_bounds__(kThreads) void k_combine_grad(RowArgs a) {
         o.store((T *)a.out + (uint64_t)r[j] * a.ldo + c * C);
         if (a.dweights != nullptr) {
 #pragma unroll
-          for (int i = 0; i < C; ++i) dot[j] = __builtin_fmaf(d.v[i], y[j].v[i], dot[j]);
+          for (int i = 0; i < C; ++i) dot[j] = __builtin_fmaf(d.v[i], y[j].get(i), dot[j]);
         }
       }
     }

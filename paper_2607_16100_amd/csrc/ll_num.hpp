@@ -79,6 +79,18 @@ struct Pack {
   }
 };
 
+// e^x to about two units in the last place: 2^t with t = x log2(e) rounded,
+// times 1 + the first-order correction for that rounding.  Results below
+// 2^-126 are 0; NaN stays NaN.
+__device__ __forceinline__ float exp_f32(float x) {
+  x = x < -150.f ? -150.f : x;  // keeps the correction finite at the infinities
+  x = x > 150.f ? 150.f : x;
+  const float t = x * 1.44269502162933349609375f;
+  float r = __builtin_fmaf(x, 1.44269502162933349609375f, -t);
+  r = __builtin_fmaf(x, 1.92596299112661746887e-8f, r);
+  return __builtin_amdgcn_exp2f(t) * __builtin_fmaf(r, 0.693147180559945309417f, 1.f);
+}
+
 template <int kCtrl>
 __device__ __forceinline__ float dpp_f32(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, true));

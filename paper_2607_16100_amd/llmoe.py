@@ -32,6 +32,7 @@ class LLLinearDesc(ctypes.Structure):
                 ("ldr", _sz)]
 
 
+DESC_SIZE = ctypes.sizeof(LLLinearDesc)
 _D = ctypes.POINTER(LLLinearDesc)
 
 # name -> argtypes (every function returns a status)

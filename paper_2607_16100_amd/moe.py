@@ -21,18 +21,21 @@ ReduceScatter:
 """
 from __future__ import annotations
 
+from functools import lru_cache
+
 import torch
 
 from . import llcoll as ll
 from . import llmoe as lm
 
 _DT = {torch.float32: ll.LL_F32, torch.bfloat16: ll.LL_BF16}
+_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 def _stream(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return _raw_stream(_device())
 
 
 def _dt(t: torch.Tensor) -> int:
@@ -44,26 +47,27 @@ def _dt(t: torch.Tensor) -> int:
 
 def _mat(t: torch.Tensor, name: str, rows=None, cols=None, dtype=None) -> int:
     """Checks a matrix on the GPU; its leading dimension."""
-    if t.dim() != 2 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{name}: a matrix on the GPU is needed")
-    n, c = t.shape
+    n, c = shape
     if (rows is not None and n != rows) or (cols is not None and c != cols):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected ({rows}, {cols})")
-    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected ({rows}, {cols})")
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
     ld, unit = t.stride()
-    if c > 1 and unit != 1:
+    if unit != 1 and c > 1:
         raise ValueError(f"{name}: the last dimension needs unit stride")
     if n < 2:
-        return max(c, 1)
+        return c or 1
     if ld < c:
         raise ValueError(f"{name}: rows overlap")
-    return max(ld, 1)
+    return ld or 1
 
 
 def _flat(t: torch.Tensor, name: str, numel: int, dtype) -> int:
     """Checks a contiguous array on the GPU; its address."""
-    if t.numel() != numel or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != numel or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} array of {numel} elements on the GPU is needed")
     return t.data_ptr()
 
@@ -221,10 +225,24 @@ def _offsets(offsets, groups: int):
     return _flat(offsets, "offsets", groups + 1, torch.int32)
 
 
-def _work(d, which: int, device):
-    st, need = lm.ll_linear_bytes(d, which)
+@lru_cache(maxsize=4096)
+def _bytes(which: int, *fields) -> int:
+    """Workspace of a product of this shape (host arithmetic only)."""
+    st, need = lm.ll_linear_bytes(lm.LLLinearDesc(*fields), which)
     ll.check(st, "ll_linear_bytes")
-    return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    return need
+
+
+def _plan(which: int, device, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz=0, ldr=0):
+    """(descriptor, workspace address, its bytes, the workspace)."""
+    # the address of the offsets is no part of the shape; whether there are any is
+    need = _bytes(which, lm.DESC_SIZE, dt, act, groups, rows, in_, out, None if offsets is None else 16, ldx, ldw,
+                  wstride, ldy, ldz, ldr)
+    d = lm.LLLinearDesc(lm.DESC_SIZE, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz, ldr)
+    if not need:
+        return d, None, 0, None
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    return d, ws.data_ptr(), need, ws
 
 
 def linear(x, w, *, bias=None, act: str = "none", residual=None, offsets=None, out=None, z=None, stream=None):
@@ -243,13 +261,11 @@ def linear(x, w, *, bias=None, act: str = "none", residual=None, offsets=None, o
         ldr, rp = _mat(residual, "residual", n, width, x.dtype), residual.data_ptr()
     if z is not None:
         ldz, zp = _mat(z, "z", n, o, x.dtype), z.data_ptr()
-    d = lm.desc(_dt(x), lm.ACTS[act], g, n, i, o, offsets=_offsets(offsets, g), ldx=ldx, ldw=ldw, wstride=gs, ldy=ldy,
-                ldz=ldz, ldr=ldr)
-    ws = _work(d, lm.LL_LINEAR_FORWARD, x.device)
+    d, wp, wn, _ws = _plan(lm.LL_LINEAR_FORWARD, x.device, _dt(x), lm.ACTS[act], g, n, i, o, _offsets(offsets, g), ldx,
+                           ldw, gs, ldy, ldz, ldr)
     ll.check(lm.ll_linear(d, x.data_ptr(), w.data_ptr(),
-                          None if bias is None else _flat(bias, "bias", g * o, x.dtype), rp, out.data_ptr(), zp,
-                          None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream(stream)),
-             "ll_linear")
+                          None if bias is None else _flat(bias, "bias", g * o, x.dtype), rp, out.data_ptr(), zp, wp,
+                          wn, _stream(stream)), "ll_linear")
     return out
 
 
@@ -268,12 +284,10 @@ def linear_grad_x(dz, w, *, act: str = "none", z=None, offsets=None, out=None, s
         if z is None:
             raise ValueError("z is needed to go through an activation")
         ldz, zp = _mat(z, "z", n, width, dz.dtype), z.data_ptr()
-    d = lm.desc(_dt(dz), lm.ACTS[act], g, n, i, o, offsets=_offsets(offsets, g), ldx=ldx, ldw=ldw, wstride=gs,
-                ldy=ldy, ldz=ldz)
-    ws = _work(d, lm.LL_LINEAR_GRAD_X, dz.device)
-    ll.check(lm.ll_linear_grad_x(d, dz.data_ptr(), w.data_ptr(), zp, out.data_ptr(),
-                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
-                                 _stream(stream)), "ll_linear_grad_x")
+    d, wp, wn, _ws = _plan(lm.LL_LINEAR_GRAD_X, dz.device, _dt(dz), lm.ACTS[act], g, n, i, o, _offsets(offsets, g), ldx,
+                           ldw, gs, ldy, ldz)
+    ll.check(lm.ll_linear_grad_x(d, dz.data_ptr(), w.data_ptr(), zp, out.data_ptr(), wp, wn, _stream(stream)),
+             "ll_linear_grad_x")
     return out
 
 
@@ -295,12 +309,10 @@ def linear_grad_w(dz, x, *, offsets=None, out=None, bias_out=None, add: bool = F
         raise ValueError(f"out: {tuple(out.shape)} {out.dtype}, expected ({groups}, {o}, {i})")
     flags = (lm.LL_GRAD_F32 if out.dtype == torch.float32 else 0) | (lm.LL_GRAD_ADD if add else 0)
     bp = None if bias_out is None else _flat(bias_out, "bias_out", g * o, out.dtype)
-    d = lm.desc(_dt(dz), lm.LL_ACT_NONE, g, n, i, o, offsets=_offsets(offsets, g), ldx=ldx, ldw=ldw, wstride=gs,
-                ldy=ldy)
-    ws = _work(d, lm.LL_LINEAR_GRAD_W, dz.device)
-    ll.check(lm.ll_linear_grad_w(d, dz.data_ptr(), x.data_ptr(), out.data_ptr(), bp, flags,
-                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
-                                 _stream(stream)), "ll_linear_grad_w")
+    d, wp, wn, _ws = _plan(lm.LL_LINEAR_GRAD_W, dz.device, _dt(dz), lm.LL_ACT_NONE, g, n, i, o, _offsets(offsets, g),
+                           ldx, ldw, gs, ldy)
+    ll.check(lm.ll_linear_grad_w(d, dz.data_ptr(), x.data_ptr(), out.data_ptr(), bp, flags, wp, wn, _stream(stream)),
+             "ll_linear_grad_w")
     return out, bias_out
 
 
