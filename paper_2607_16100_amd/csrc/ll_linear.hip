@@ -31,13 +31,23 @@ int check_desc(const ll_linear_desc *d) {
   if (d->groups < 1 || (d->offsets == nullptr && d->groups != 1) || !aligned(d->offsets, 4)) return LL_ERR_INVALID;
   if (d->in < 1 || d->out < 1) return LL_ERR_INVALID;
   if (d->groups > LL_MOE_MAX_EXPERTS || d->rows > kMaxExtent) return LL_ERR_UNSUPPORTED;
-  // a tile's rows lie within 2^31 bytes of its first one
+  // a tile's rows, and a group's weight, lie within 32 bits of bytes
   constexpr size_t kMaxFeatures = 1u << 20;
   if (d->in > kMaxFeatures || d->out > kMaxFeatures) return LL_ERR_UNSUPPORTED;
   for (size_t ld : {d->ldx, d->ldw, d->ldy, d->ldz, d->ldr})
     if (ld > 2 * kMaxFeatures) return LL_ERR_UNSUPPORTED;
+  if (d->out * d->ldw > 0xF0000000ull / esize(d->dt)) return LL_ERR_UNSUPPORTED;
   if (d->ldw < d->in || (d->groups > 1 && d->wstride < (d->out - 1) * d->ldw + d->in)) return LL_ERR_INVALID;
   return LL_OK;
+}
+
+Rows rows_of(const void *p, size_t ld, size_t len, int es);
+
+// The same of every group's weight.
+Rows weight_rows(const ll_linear_desc *d, const void *w, int es) {
+  const Rows r = rows_of(w, d->ldw, d->in, es);
+  if (d->groups == 1) return r;
+  return std::min(r, d->wstride * es % 16 == 0 ? kChunkRows : d->wstride * es % 4 == 0 ? kDwordRows : kAnyRows);
 }
 
 size_t weight_span(const ll_linear_desc *d, int es) {
@@ -51,12 +61,12 @@ int check_rows(const void *p, size_t ld, size_t len, int es, bool any) {
 
 using tile_fn = void (*)(Args);
 
-template <typename T, Pass PASS, int B, int WM, int WN, bool VEC>
+template <typename T, Pass PASS, int B, int WM, int WN, int ST, Rows ROWS>
 tile_fn pick(bool gate) {
   if constexpr (PASS == kForward) {
-    if (gate) return k_tile<T, PASS, B, B, WM, WN, true, VEC>;
+    if (gate) return k_tile<T, PASS, B, B, WM, WN, ST, true, ROWS>;
   }
-  return k_tile<T, PASS, B, B, WM, WN, false, VEC>;
+  return k_tile<T, PASS, B, B, WM, WN, ST, false, ROWS>;
 }
 
 // Tiles of b x b that a product has at most: every group with rows may add one
@@ -73,14 +83,22 @@ struct Plan {
 };
 
 constexpr uint32_t kFill = 256;            // workgroups that fill the chip
+
+// Sizes the rows of split sums; bytes of one split.
+uint64_t size_parts(Args &a, bool gate) {
+  const uint32_t width = gate ? a.n / 2 : a.n;
+  a.part_half = (width + kEw - 1) / kEw * kEw;
+  a.part_row = gate ? 2 * a.part_half : a.part_half;
+  return (uint64_t)a.rows_c * a.part_row * 4;
+}
 constexpr uint64_t kMaxParts = 256 << 20;  // bytes of split sums
 
-Plan plan_of(Pass pass, const Args &a, ll_dtype dt, bool vec) {
+Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows) {
   Plan p{64, 1};
   // Larger tiles move fewer operand bytes but need many tiles to fill the chip.
-  // 256: bfloat16 rows of whole 16-byte chunks only (binary32 is bound by its
-  // matrix instructions, which are 16 times slower, with any).
-  if (vec && dt == LL_BF16 && count_tiles(pass, a, 256) >= kFill)
+  // 256 is for bfloat16 only: binary32 is bound by its matrix instructions,
+  // which are 16 times slower, with any.
+  if (rows != kAnyRows && dt == LL_BF16 && count_tiles(pass, a, 256) >= kFill)
     p.tile = 256;
   else if (count_tiles(pass, a, 128) >= kFill)
     p.tile = 128;
@@ -91,14 +109,14 @@ Plan plan_of(Pass pass, const Args &a, ll_dtype dt, bool vec) {
   // joining launch a few us).
   if (tiles < kFill) {
     uint64_t s = std::min<uint64_t>(kFill * 2 / std::max<uint64_t>(tiles, 1), steps / 8);
-    const uint64_t one = (uint64_t)a.rows_c * a.n * 4;
+    const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
     s = std::min(s, kMaxParts / std::max<uint64_t>(one, 1));
     if (s >= 2) p.splits = (uint32_t)std::min<uint64_t>(s, 32);
   }
   return p;
 }
 
-template <typename T, Pass PASS, int B, int WM, int WN, bool VEC>
+template <typename T, Pass PASS, int B, int WM, int WN, int ST, Rows ROWS>
 int launch_tiles(Args &a, bool gate, void *stream) {
   const uint32_t width = gate ? a.n / 2 : a.n;
   const uint32_t per_n = gate ? B / 2 : B;
@@ -107,7 +125,7 @@ int launch_tiles(Args &a, bool gate, void *stream) {
   const uint64_t grid = count_tiles(PASS, a, B) / ((a.n + B - 1) / B) * a.tiles_n;
   constexpr int kThreads = WM * WN * 64;
   if (grid * kThreads >= 1ull << 32) return LL_ERR_UNSUPPORTED;
-  const tile_fn fn = pick<T, PASS, B, WM, WN, VEC>(gate);
+  const tile_fn fn = pick<T, PASS, B, WM, WN, ST, ROWS>(gate);
   hipLaunchKernelGGL(fn, dim3((unsigned)grid, a.splits), dim3(kThreads), 0, (hipStream_t)stream, a);
   if (a.parts != nullptr) {
     const uint64_t items = (uint64_t)a.rows_c * ((width + kEw - 1) / kEw);
@@ -121,44 +139,52 @@ int launch_tiles(Args &a, bool gate, void *stream) {
   return launch_status();
 }
 
-template <typename T, Pass PASS>
-int launch_plan(Args &a, const Plan &p, bool gate, bool vec, void *stream) {
-  if constexpr (sizeof(T) == 2) {
-    if (p.tile == 256) return launch_tiles<T, PASS, 256, 2, 4, true>(a, gate, stream);
+template <typename T, Pass PASS, Rows ROWS>
+int launch_plan(Args &a, const Plan &p, bool gate, void *stream) {
+  if constexpr (sizeof(T) == 2 && ROWS != kAnyRows) {
+    if (p.tile == 256) return launch_tiles<T, PASS, 256, 2, 4, 2, ROWS>(a, gate, stream);
   }
-  // rows that are not whole 16-byte chunks pass through registers, which eight
-  // waves have enough of
-  if (p.tile == 128)
-    return vec ? launch_tiles<T, PASS, 128, 2, 2, true>(a, gate, stream)
-               : launch_tiles<T, PASS, 128, 2, 4, false>(a, gate, stream);
-  return vec ? launch_tiles<T, PASS, 64, 2, 2, true>(a, gate, stream)
-             : launch_tiles<T, PASS, 64, 2, 2, false>(a, gate, stream);
+  if constexpr (ROWS == kAnyRows) {
+    // eight waves: a stage of a thread's chunks lies in registers meanwhile
+    if (p.tile == 128) return launch_tiles<T, PASS, 128, 2, 4, 2, ROWS>(a, gate, stream);
+    return launch_tiles<T, PASS, 64, 2, 2, 2, ROWS>(a, gate, stream);
+  } else {
+    if (p.tile == 128) return launch_tiles<T, PASS, 128, 2, 2, 2, ROWS>(a, gate, stream);
+    return launch_tiles<T, PASS, 64, 2, 2, 4, ROWS>(a, gate, stream);
+  }
+}
+
+template <typename T, Pass PASS>
+int launch_rows(Args &a, const Plan &p, Rows rows, bool gate, void *stream) {
+  if (rows == kChunkRows) return launch_plan<T, PASS, kChunkRows>(a, p, gate, stream);
+  if constexpr (sizeof(T) == 2) {  // binary32 rows are always whole dwords
+    if (rows == kAnyRows) return launch_plan<T, PASS, kAnyRows>(a, p, gate, stream);
+  }
+  return launch_plan<T, PASS, kDwordRows>(a, p, gate, stream);
 }
 
 template <Pass PASS>
-int launch_product(Args &a, ll_dtype dt, bool gate, bool vec, void *workspace, size_t workspace_bytes, void *stream) {
-  Plan p = plan_of(PASS, a, dt, vec);
-  const uint64_t one = (uint64_t)a.rows_c * a.n * 4;
+int launch_product(Args &a, ll_dtype dt, bool gate, Rows rows, void *workspace, size_t workspace_bytes, void *stream) {
+  const uint64_t one = size_parts(a, gate);
+  Plan p = plan_of(PASS, a, dt, rows);
   if (workspace == nullptr) workspace_bytes = 0;
   if (p.splits * one > workspace_bytes) p.splits = one == 0 ? 1 : (uint32_t)std::max<uint64_t>(1, workspace_bytes / one);
   a.splits = p.splits;
   a.parts = p.splits > 1 ? (float *)workspace : nullptr;
-  return dt == LL_F32 ? launch_plan<float, PASS>(a, p, gate, vec, stream)
-                      : launch_plan<__bf16, PASS>(a, p, gate, vec, stream);
+  return dt == LL_F32 ? launch_rows<float, PASS>(a, p, rows, gate, stream)
+                      : launch_rows<__bf16, PASS>(a, p, rows, gate, stream);
 }
 
 // ---------------------------------------------------------------- few rows
 // Row blocks of 16 a workgroup of the streaming kernel takes; 0: the product
 // is not for it.
-int stream_blocks(const Args &a, bool vec) {
-  if (!vec) return 0;
-  const uint32_t each = (a.rows + a.groups - 1) / a.groups;  // rows a group on average
-#ifndef LL_T1
-#define LL_T1 16
-#define LL_T2 32
-#endif
-  if (each > LL_T2) return 0;
-  return each <= LL_T1 ? 1 : 2;
+int stream_blocks(const Args &a, Rows rows) {
+  if (rows != kChunkRows) return 0;
+  // One group: its rows are known.  Several: their sizes are not, and one of
+  // more than the workgroup's rows reads its weight twice (32 groups of 7168 ->
+  // 2 x 2048, 32 rows each on average: 667 us here, 372 with tiles).
+  const uint32_t each = a.groups == 1 ? a.rows : 2 * ((a.rows + a.groups - 1) / a.groups);
+  return each <= 16 ? 1 : each <= 32 ? 2 : 0;
 }
 
 template <typename T, int RB>
@@ -176,9 +202,11 @@ int launch_stream(Args &a, bool gate, void *stream) {
 
 // Every row starts at a 16-byte address.
 bool rows16(const void *p, size_t ld, int es) { return p == nullptr || (aligned(p, 16) && ld * es % 16 == 0); }
-bool chunked(const void *p, size_t ld, size_t len, int es) {
-  return aligned(p, 16) && ld * es % 16 == 0 && len * es % 16 == 0;
+Rows rows_of(const void *p, size_t ld, size_t len, int es) {
+  if (aligned(p, 16) && ld * es % 16 == 0 && len * es % 16 == 0) return kChunkRows;
+  return aligned(p, 4) && ld * es % 4 == 0 ? kDwordRows : kAnyRows;
 }
+bool chunked(const void *p, size_t ld, size_t len, int es) { return rows_of(p, ld, len, es) == kChunkRows; }
 
 }  // namespace
 
@@ -221,10 +249,11 @@ int ll_linear_bytes(const ll_linear_desc *d, ll_linear_pass pass, size_t *bytes)
   const int es = esize(d->dt);
   const bool whole = d->in * es % 16 == 0 && d->ldx * es % 16 == 0 && d->ldw * es % 16 == 0 && d->wstride * es % 16 == 0;
   *bytes = 0;
-  if (pass == LL_LINEAR_FORWARD && stream_blocks(a, whole) != 0) return LL_OK;
+  if (pass == LL_LINEAR_FORWARD && stream_blocks(a, whole ? kChunkRows : kDwordRows) != 0) return LL_OK;
+  const uint64_t one = size_parts(a, pass == LL_LINEAR_FORWARD && gated((int)d->act));
   uint32_t splits = 1;
-  for (const bool vec : {false, true}) splits = std::max(splits, plan_of((Pass)pass, a, d->dt, vec).splits);
-  *bytes = splits > 1 ? (size_t)splits * a.rows_c * a.n * 4 : 0;
+  for (const Rows rows : {kAnyRows, kChunkRows}) splits = std::max(splits, plan_of((Pass)pass, a, d->dt, rows).splits);
+  *bytes = splits > 1 ? (size_t)splits * one : 0;
   return LL_OK;
 }
 
@@ -271,14 +300,14 @@ int ll_linear(const ll_linear_desc *d, const void *x, const void *w, const void 
   a.act = (int)d->act;
   a.vec_b = rows16(bias, d->out, es);
   a.vec_c = rows16(y, d->ldy, es) && rows16(z, d->ldz, es) && rows16(residual, d->ldr, es);
-  const bool vec = chunked(x, d->ldx, d->in, es) && chunked(w, d->ldw, d->in, es) && d->wstride * es % 16 == 0 &&
-                   d->out * d->ldw * es < 0xF0000000ull;
-  const int blocks = stream_blocks(a, vec);
+  Rows rows = std::min(rows_of(x, d->ldx, d->in, es), weight_rows(d, w, es));
+
+  const int blocks = stream_blocks(a, rows);
   if (blocks == 1)
     return d->dt == LL_F32 ? launch_stream<float, 1>(a, gate, stream) : launch_stream<__bf16, 1>(a, gate, stream);
   if (blocks == 2)
     return d->dt == LL_F32 ? launch_stream<float, 2>(a, gate, stream) : launch_stream<__bf16, 2>(a, gate, stream);
-  return launch_product<kForward>(a, d->dt, gate, vec, workspace, workspace_bytes, stream);
+  return launch_product<kForward>(a, d->dt, gate, rows, workspace, workspace_bytes, stream);
 }
 
 int ll_linear_grad_x(const ll_linear_desc *d, const void *dz, const void *w, const void *z, void *dx, void *workspace,
@@ -316,8 +345,8 @@ int ll_linear_grad_x(const ll_linear_desc *d, const void *dz, const void *w, con
   a.ldc = d->ldx;
   a.act = (int)d->act;
   a.vec_c = rows16(dx, d->ldx, es) && rows16(z, d->ldz, es);
-  const bool vec = chunked(dz, d->ldy, d->out, es) && chunked(w, d->ldw, d->in, es) && d->wstride * es % 16 == 0;
-  return launch_product<kGradX>(a, d->dt, false, vec, workspace, workspace_bytes, stream);
+  const Rows rows = std::min(rows_of(dz, d->ldy, d->out, es), weight_rows(d, w, es));
+  return launch_product<kGradX>(a, d->dt, false, rows, workspace, workspace_bytes, stream);
 }
 
 int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, void *dw, void *dbias, uint32_t flags,
@@ -356,7 +385,7 @@ int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, voi
   a.flags = flags;
   // the gradient's own element size decides its alignment
   a.vec_c = rows16(dw, d->ldw, gs) && d->wstride * gs % 16 == 0;
-  const bool vec = chunked(dz, d->ldy, d->out, es) && chunked(x, d->ldx, d->in, es);
+  const Rows rows = std::min(rows_of(dz, d->ldy, d->out, es), rows_of(x, d->ldx, d->in, es));
   a.k = a.rows;
   if (dbias != nullptr) {
     const bool rows_vec = chunked(dz, d->ldy, d->out, es);
@@ -365,7 +394,7 @@ int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, voi
     const unsigned cols = 16 * (rows_vec ? 16 / es : 1);
     hipLaunchKernelGGL(fn, dim3((a.m + cols - 1) / cols, a.groups), dim3(1024), 0, (hipStream_t)stream, a);
   }
-  return launch_product<kGradW>(a, d->dt, false, vec, workspace, workspace_bytes, stream);
+  return launch_product<kGradW>(a, d->dt, false, rows, workspace, workspace_bytes, stream);
 }
 
 int ll_act_grad(const void *dy, size_t lddy, const void *z, size_t ldz, size_t rows, size_t features, ll_dtype dt,

@@ -42,8 +42,9 @@ struct Args {
   uint32_t flags;  // LL_GRAD_*
   bool vec_c;      // every epilogue row starts at a 16-byte address
   bool vec_b;      // so does every group's bias
-  float *parts;      // sums of the splits of k, [splits][rows of C][n], or NULL
+  float *parts;      // sums of the splits of k, [splits][rows of C][part_row], or NULL
   uint32_t splits, rows_c;
+  uint32_t part_half, part_row;  // columns of a (gated: half a) row of parts, multiples of kEw
 };
 
 // ---------------------------------------------------------------- activations
@@ -271,14 +272,23 @@ __device__ __forceinline__ uint32_t q_row(uint32_t tile_n, uint32_t bn, uint32_t
 
 constexpr uint32_t kOutside = 0xFFFFFFF0u;  // a buffer offset past the resource: reads as zero
 
+// How an operand's rows lie in memory.
+enum Rows {
+  kAnyRows = 0,    // 2-byte aligned (bf16): through registers
+  kDwordRows = 1,  // every row at a multiple of 4 bytes
+  kChunkRows = 2   // every row at a multiple of 16 bytes and whole 16-byte chunks long
+};
+
 // Loads one operand's stages, one after the other, kChunks chunks a thread.
-//   VEC: every row is whole 16-byte chunks at 16-byte addresses, so a chunk
-//   lies in the matrix or outside it.  Chunks go straight into LDS through a
-//   buffer resource; issue() leaves them in flight until the caller waits.
-//   Otherwise fetch() brings them to registers, 16 bytes at any alignment
-//   where they lie inside the matrix and single elements at its end, and
-//   commit() writes them to LDS.
-template <typename T, int R, int NW, bool KM, bool VEC>
+//   kChunkRows, kDwordRows: chunks go straight into LDS through a buffer
+//   resource; issue() leaves them in flight until the caller waits.  A chunk
+//   of kChunkRows lies in the matrix or outside it.  One of kDwordRows may
+//   reach past the end of its row: along m or n that touches columns nobody
+//   stores, along k clear_tail() writes zeros over it once it has arrived.
+//   kAnyRows: fetch() brings them to registers, 16 bytes at any alignment where
+//   they lie inside the matrix and single elements at its end, and commit()
+//   writes them to LDS.
+template <typename T, int R, int NW, bool KM, Rows ROWS>
 struct Loader {
   static constexpr int kEpc = 16 / (int)sizeof(T);
   static constexpr int kBK = Step<T>::kBK;
@@ -286,11 +296,11 @@ struct Loader {
   static constexpr int kRowChunks = KM ? 8 : R / kEpc;
   static_assert(kChunks * NW * 64 == R * 8, "every thread loads the same number of chunks");
   uint64_t base;  // of the stage to load next
-  uint64_t left;  // !VEC: bytes from base to the end of the matrix
+  uint64_t left;  // not kChunkRows: bytes from base to the end of the matrix
   uint64_t step;  // bytes from one stage to the next
   uint32_t off[kChunks];  // of the chunk, from base; kOutside: not in the matrix
   uint32_t kk0;
-  u32x4 raw[VEC ? 1 : kChunks];
+  u32x4 raw[ROWS == kAnyRows ? kChunks : 1];
 
   // KM: matrix [mat_rows][k], the tile's entry j is row row_of(j) >= first.
   // RM: matrix [k][cols], the tile's first column is `first`.
@@ -329,15 +339,15 @@ struct Loader {
 
   __device__ __forceinline__ void advance() {
     base += step;
-    if constexpr (!VEC) left = left > step ? left - step : 0;
+    if constexpr (ROWS != kChunkRows) left = left > step ? left - step : 0;
   }
 
   __device__ __forceinline__ void skip(uint32_t stages) {
     base += stages * step;
-    if constexpr (!VEC) left = left > stages * step ? left - stages * step : 0;
+    if constexpr (ROWS != kChunkRows) left = left > stages * step ? left - stages * step : 0;
   }
 
-  // VEC: issues chunk c of a stage to LDS byte `at` (this wave's part of the
+  // Issues chunk c of a stage to LDS byte `at` (this wave's part of the
   // operand's stage); whole: the stage has kBK k left, else `have` of them.
   // In assembly so that the compiler does not wait for the load before the
   // next LDS read, as it must where it sees a write to LDS; it has no result
@@ -345,7 +355,9 @@ struct Loader {
   template <bool WHOLE>
   __device__ __forceinline__ void issue(uint32_t at, int c, uint32_t have) {
     // the base and the LDS address are the same in every lane
-    const u32x4 rs = {uniform_u32((uint32_t)base), uniform_u32((uint32_t)(base >> 32)), kOutside,
+    // (the last dword of a matrix of bfloat16 may be half outside it)
+    const uint32_t records = ROWS == kChunkRows || left > kOutside - 4 ? kOutside : ((uint32_t)left + 3) & ~3u;
+    const u32x4 rs = {uniform_u32((uint32_t)base), uniform_u32((uint32_t)(base >> 32)), uniform_u32(records),
                       (uint32_t)kRsrcWord3};
     const uint32_t o = WHOLE || kk(c) < have ? off[c] : kOutside;
     asm volatile(
@@ -357,10 +369,25 @@ struct Loader {
         : "memory");
   }
 
-  // !VEC: the stage's chunks to registers; have: k left from the stage's
+  // kDwordRows along k: zeros over what this thread's chunks of a stage with
+  // `have` k hold past them.  After the thread's loads have arrived.
+  __device__ __forceinline__ void clear_tail(char *tile, int have) const {
+    if constexpr (KM && ROWS == kDwordRows) {
+      const int from = have - (int)kk0;
+      if (from <= 0 || from >= kEpc) return;
+      const uint32_t chunk0 = threadIdx.x / 64 * kChunks;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        T *e = reinterpret_cast<T *>(tile + (chunk0 + c) * 1024 + threadIdx.x % 64 * 16);
+        for (int i = from; i < kEpc; ++i) e[i] = (T)0.f;
+      }
+    }
+  }
+
+  // kAnyRows: the stage's chunks to registers; have: k left from the stage's
   // first (may be 0 or less).
   __device__ __forceinline__ void fetch(int have) {
-    if constexpr (!VEC) {
+    if constexpr (ROWS == kAnyRows) {
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
         union {
@@ -369,13 +396,14 @@ struct Loader {
         } v;
         v.raw = u32x4{0, 0, 0, 0};
         if (off[c] != kOutside && (int)kk(c) < have) {
-          const char *p = reinterpret_cast<const char *>(base) + off[c];
+          typedef const __attribute__((address_space(1))) T *global;
+          const global p = (global)(base + off[c]);
           if ((uint64_t)off[c] + 16 <= left) {
             __builtin_memcpy(&v, p, 16);
           } else {
 #pragma unroll
             for (int i = 0; i < kEpc; ++i)
-              if ((uint64_t)off[c] + (i + 1) * sizeof(T) <= left) v.e[i] = reinterpret_cast<const T *>(p)[i];
+              if ((uint64_t)off[c] + (i + 1) * sizeof(T) <= left) v.e[i] = p[i];
           }
           if constexpr (KM) {
             if ((int)kk(c) + kEpc > have) {  // the row ends inside the chunk
@@ -390,7 +418,7 @@ struct Loader {
     }
   }
   __device__ __forceinline__ void commit(char *tile) {
-    if constexpr (!VEC) {
+    if constexpr (ROWS == kAnyRows) {
       const uint32_t chunk0 = threadIdx.x / 64 * kChunks;
 #pragma unroll
       for (int c = 0; c < kChunks; ++c)
@@ -550,21 +578,24 @@ __device__ __forceinline__ void put_bias_grad(const Args &a, int g, uint32_t m, 
 
 // ---------------------------------------------------------------- the tile kernel
 //
-// Two stages of both operands lie in LDS.  A wave's rows are FM / 2 fragments
+// ST stages of both operands lie in LDS.  A wave's rows are FM / 2 fragments
 // in the tile's upper half and as many in its lower half, and a stage is four
 // clusters of matrix instructions: upper and lower rows with the first half of
 // the stage's k, then with the second.  The fragments of a cluster are read
 // during the cluster before it, one LDS read between two matrix instructions.
 // After the third cluster every fragment of the stage is in registers: a
 // barrier there, the only one of a stage, frees its buffer, into which the
-// loads of the stage after next go out during the fourth cluster, and says
-// that the next stage has arrived (its loads went out a stage earlier), whose
-// first fragments are read meanwhile.
+// loads of the stage ST further on go out during the fourth cluster, and says
+// that the next stage has arrived (its loads went out ST - 1 stages earlier),
+// whose first fragments are read meanwhile.  Large tiles have two stages;
+// small ones four, since a stage of theirs is shorter than a load takes.
+//
+// Tiles of 64 have few matrix instructions between one LDS read and the next
+// cluster that waits for it (0.5 us a stage with one wave a SIMD): they read
+// the whole next stage's fragments at once, for which they have registers.
 //
 // A tile with no rows in its lower half (the last tile of a group, often)
 // leaves that half's work out.
-constexpr int kStages = 2;
-
 template <int N>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -572,15 +603,18 @@ __device__ __forceinline__ void wait_loads() {
 // This wave's LDS reads and writes are done; then everyone's.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-template <typename T, Pass PASS, int BM, int BN, int WM, int WN, bool GATED, bool VEC>
+template <typename T, Pass PASS, int BM, int BN, int WM, int WN, int ST, bool GATED, Rows ROWS>
 __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
   constexpr bool kPkm = PASS != kGradW, kQkm = PASS == kForward;
+  constexpr bool VEC = ROWS != kAnyRows;  // loads go straight into LDS
+  constexpr bool kFlat = BM == 64;        // all fragments of a stage at once
+  static_assert(VEC || ST == 2, "a stage in registers at a time");
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, FM = WTM / 16, FN = WTN / 16, FH = FM / 2;
   constexpr int BK = Step<T>::kBK;
   constexpr int kStage = (BM + BN) * 128;
   constexpr int kPitch = WTN + 4;  // binary32 of an epilogue row: rows start in different banks
   constexpr int kEpi = NW * (WTM / 2) * kPitch * 4;
-  constexpr int kLds = kStages * kStage > kEpi ? kStages * kStage : kEpi;
+  constexpr int kLds = ST * kStage > kEpi ? ST * kStage : kEpi;
   typedef typename Step<T>::frag frag;
   __shared__ __attribute__((aligned(1024))) char lds[kLds];
   const int lane = threadIdx.x % 64;
@@ -610,8 +644,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
   const uint32_t share = a.splits == 1 ? k : ((k + BK - 1) / BK + a.splits - 1) / a.splits * BK;
   const uint32_t k_from = min(k, blockIdx.y * share);
 
-  Loader<T, BM, NW, kPkm, VEC> lp;
-  Loader<T, BN, NW, kQkm, VEC> lq;
+  Loader<T, BM, NW, kPkm, ROWS> lp;
+  Loader<T, BN, NW, kQkm, ROWS> lq;
   if constexpr (kPkm)
     lp.init(p, a.ldp, k, m_end, 0, m0, [&](uint32_t j, bool *ok) {
       *ok = m0 + j < m_end;
@@ -673,7 +707,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
 
   if (steps > 0) {
 #pragma unroll
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < ST; ++s) {
       const int have = (int)k - s * BK;
       if constexpr (VEC) {
 #pragma unroll
@@ -689,8 +723,60 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
       lp.advance();
       lq.advance();
     }
-    wait_loads<VEC ? kLoads : 0>();
+    wait_loads<VEC ? (ST - 1) * kLoads : 0>();
+    lp.clear_tail(lds, (int)k);
+    lq.clear_tail(lds + BM * 128, (int)k);
     lds_barrier();
+    if constexpr (kFlat) {
+      frag fq[2][2][FN], fp[2][2][FM];  // of two stages, by half of k
+      auto read_all = [&](auto set_c, const char *from) __attribute__((always_inline)) {
+        constexpr int set = decltype(set_c)::value;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+          for (int j = 0; j < FN; ++j) fq[set][ks][j] = read_frag<T, BN, kQkm>(from + off_q[ks][j]);
+#pragma unroll
+          for (int i = 0; i < FM; ++i) fp[set][ks][i] = read_frag<T, BM, kPkm>(from + off_p[ks][i]);
+        }
+      };
+      read_all(std::integral_constant<int, 0>{}, lds);
+      // One stage, its fragments in set `now`, from LDS buffer b.
+      auto flat = [&](int b, auto now_c, int have, int next_has) __attribute__((always_inline)) {
+        constexpr int now = decltype(now_c)::value;
+        char *next = lds + (b + 1) % ST * kStage;
+        lp.commit(next);
+        lq.commit(next + BM * 128);
+        wait_loads<VEC ? (ST - 2) * kLoads : 0>();
+        if (ROWS == kDwordRows && next_has < BK) {
+          lp.clear_tail(next, next_has);
+          lq.clear_tail(next + BM * 128, next_has);
+        }
+        lds_barrier();
+        if constexpr (VEC) {
+#pragma unroll
+          for (int n = 0; n < kLoads; ++n) issue(b, n, std::false_type{}, have > 0 ? have : 0);
+        } else {
+          lp.fetch(have);
+          lq.fetch(have);
+        }
+        read_all(std::integral_constant<int, 1 - now>{}, next);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) acc[j][i] = mma(fq[now][ks][j], fp[now][ks][i], acc[j][i]);
+        lp.advance();
+        lq.advance();
+      };
+      for (uint32_t s = 0;;) {
+        flat(s % ST, std::integral_constant<int, 0>{}, (int)k - (int)(s + ST) * BK, (int)k - (int)(s + 1) * BK);
+        if (++s >= steps) break;
+        flat(s % ST, std::integral_constant<int, 1>{}, (int)k - (int)(s + ST) * BK, (int)k - (int)(s + 1) * BK);
+        if (++s >= steps) break;
+      }
+    } else {
     frag fq[2][FN], fu[2][FH], fl[2][FH];  // by half of k: Q, P's upper rows, P's lower rows
 #pragma unroll
     for (int j = 0; j < FN; ++j) fq[0][j] = read_frag<T, BN, kQkm>(lds + off_q[0][j]);
@@ -706,12 +792,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
       else
         acc[j][i] = mma(fq[ks][j], fu[ks][i], acc[j][i]);
     };
-    // One stage from LDS buffer b.  WHOLE: the stage after next has BK k, else
-    // `have` of them (none: zeros are written).
-    auto stage = [&](int b, auto lower_c, auto whole, int have) __attribute__((always_inline)) {
+    // One stage from LDS buffer b.  WHOLE: the stage loaded meanwhile has BK k,
+    // else `have` of them (none: zeros are written).  next_has: k of the next one.
+    auto stage = [&](int b, auto lower_c, auto whole, int have, int next_has) __attribute__((always_inline)) {
       constexpr bool kLower = decltype(lower_c)::value;
       constexpr int kMmas = FN * FH, kMmasL = kLower ? kMmas : 0;
-      const char *here = lds + b * kStage, *next = lds + (1 - b) * kStage;
+      const char *here = lds + b * kStage, *next = lds + (b + 1) % ST * kStage;
 #pragma unroll
       for (int t = 0; t < kMmas; ++t) {
         if (kLower && t < FH) fl[0][t < FH ? t : 0] = read_frag<T, BM, kPkm>(here + off_p[0][FH + (t < FH ? t : 0)]);
@@ -738,7 +824,11 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
         lp.commit(const_cast<char *>(next));
         lq.commit(const_cast<char *>(next) + BM * 128);
       }
-      wait_loads<0>();
+      wait_loads<VEC ? (ST - 2) * kLoads : 0>();
+      if (ROWS == kDwordRows && next_has < BK) {
+        lp.clear_tail(const_cast<char *>(next), next_has);
+        lq.clear_tail(const_cast<char *>(next) + BM * 128, next_has);
+      }
       lds_barrier();
       if constexpr (!VEC) {
         lp.fetch(have);
@@ -760,18 +850,24 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
     };
     auto all = [&](auto lower_c) __attribute__((always_inline)) {
       uint32_t s = 0;
-      if constexpr (VEC) {  // two stages at a time: LDS addresses are constants
-        for (; (s + 4) * BK <= k; s += 2) {
-          stage(0, lower_c, std::true_type{}, BK);
-          stage(1, lower_c, std::true_type{}, BK);
+      if constexpr (VEC) {  // ST stages at a time: LDS addresses are constants
+        for (; (s + 2 * ST) * BK <= k; s += ST) {
+          stage(0, lower_c, std::true_type{}, BK, BK);
+          stage(1, lower_c, std::true_type{}, BK, BK);
+          if constexpr (ST > 2) {
+            stage(2, lower_c, std::true_type{}, BK, BK);
+            stage(3, lower_c, std::true_type{}, BK, BK);
+          }
         }
       }
-      for (; s < steps; ++s) stage(s % kStages, lower_c, std::false_type{}, (int)k - (int)(s + kStages) * BK);
+      for (; s < steps; ++s)
+        stage(s % ST, lower_c, std::false_type{}, (int)k - (int)(s + ST) * BK, (int)k - (int)(s + 1) * BK);
     };
     if (PASS == kGradW || lower)
       all(std::true_type{});
     else
       all(std::false_type{});
+    }
   }
   wait_loads<0>();
   lds_barrier();  // every wave is past its last stage, and no load is under way
@@ -798,12 +894,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
       v.load(mine + r * kPitch + c);
       if (a.parts != nullptr) {
         const uint32_t rc = PASS == kGradW ? g * a.m + m : m;
-        float *to = a.parts + ((uint64_t)blockIdx.y * a.rows_c + rc) * a.n + n0;
-        const uint32_t width = GATED ? a.n / 2 : a.n, left = width > n0 ? width - n0 : 0;
-        put8(to, v, left, a.n % 4 == 0);
-        if constexpr (GATED) {
-          u.load(mine + r * kPitch + kWidth + c);
-          put8(to + width, u, left, width % 4 == 0);
+        if (n0 < a.part_half) {
+          float *to = a.parts + ((uint64_t)blockIdx.y * a.rows_c + rc) * a.part_row + n0;
+          v.store(to);
+          if constexpr (GATED) {
+            u.load(mine + r * kPitch + kWidth + c);
+            u.store(to + a.part_half);
+          }
         }
       } else if constexpr (PASS == kForward) {
         if constexpr (GATED) u.load(mine + r * kPitch + kWidth + c);
@@ -850,21 +947,20 @@ __global__ __launch_bounds__(256) void k_join(Args a) {
     g = lo;
     if ((int)r < a.offsets[g] || (int)r >= a.offsets[g + 1]) return;
   }
+  const uint64_t next = (uint64_t)a.rows_c * a.part_row;
+  const float *from = a.parts + (uint64_t)r * a.part_row + n0;
   Vals v, u;
-  const uint32_t left = width - n0;
-  for (uint32_t z = 0; z < a.splits; ++z) {
-    const float *from = a.parts + ((uint64_t)z * a.rows_c + r) * a.n + n0;
-    const Vals p = get8(from, left, a.n % 4 == 0);
-    if (z == 0)
-      v = p;
-    else
-      add8(v, p);
+  v.load(from);
+  if constexpr (GATED) u.load(from + a.part_half);
+#pragma unroll 4
+  for (uint32_t z = 1; z < a.splits; ++z) {
+    from += next;
+    Vals p;
+    p.load(from);
+    add8(v, p);
     if constexpr (GATED) {
-      const Vals q = get8(from + width, left, width % 4 == 0);
-      if (z == 0)
-        u = q;
-      else
-        add8(u, q);
+      p.load(from + a.part_half);
+      add8(u, p);
     }
   }
   if constexpr (PASS == kForward)
