@@ -77,9 +77,9 @@ uint64_t count_tiles(Pass pass, const Args &a, uint32_t b) {
   return (a.offsets == nullptr ? (a.rows + b - 1) / b : a.rows / b + std::min<uint64_t>(a.groups, a.rows)) * n;
 }
 
-// How a product runs: the tile's edge and the splits of its sum.
+// How a product runs: the tile's edge, its stages in LDS, the splits of its sum.
 struct Plan {
-  uint32_t tile, splits;
+  uint32_t tile, stages, splits;
 };
 
 constexpr uint32_t kFill = 256;            // workgroups that fill the chip
@@ -93,26 +93,39 @@ uint64_t size_parts(Args &a, bool gate) {
 }
 constexpr uint64_t kMaxParts = 256 << 20;  // bytes of split sums
 
+// Larger tiles move fewer operand bytes but need many tiles to fill the chip.
+// Measured, bfloat16, us with tiles of 256 / 128 (2 and 4 stages) / 64 (2 and 4):
+//   8192 x 2048 x 7168   grad_x  168 / 194, 228 / -       (256 tiles of 256)
+//   2048 x 2048 x 2048           46 / 25.8, 24.0 / 28.9, 30.8 (256 of 128)
+//   1024 x 4096 x 4096           78 / 44, 39 / 49, 52     (256 of 128)
+//   1024 x 1032 -> 2056          29 / 14.7, 15.7 / 16.2, 18.3 (136 of 128)
+//    512 x 2048 -> 2048          43 / 17.6, 19.9 / 11.5, 11.0 (64 of 128)
+//    128 x 4096 -> 4096          58 / 41, 32 / 31, 17.3; 4 splits 16.4 (128 of 64)
+//    301 x 8192 -> 1024         144 / 72, 56 / 58, 36; 3 splits 19.7  (80 of 64)
+// 256 is for bfloat16 only: binary32 is bound by its matrix instructions, which
+// are 16 times slower (1024^3: 62 us with 128, 23 us with 64).
 Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows) {
-  Plan p{64, 1};
-  // Larger tiles move fewer operand bytes but need many tiles to fill the chip.
-  // 256 is for bfloat16 only: binary32 is bound by its matrix instructions,
-  // which are 16 times slower, with any.
-  if (rows != kAnyRows && dt == LL_BF16 && count_tiles(pass, a, 256) >= kFill)
-    p.tile = 256;
-  else if (count_tiles(pass, a, 128) >= kFill)
-    p.tile = 128;
+  Plan p{64, 2, 1};
   const uint32_t bk = 128 / esize(dt);
-  const uint64_t tiles = count_tiles(pass, a, p.tile), steps = (a.k + bk - 1) / bk;
-  // Too few tiles: the sum is cut so that the chip is filled, into shares of
-  // eight stages or more (a stage is about 0.5 us when little else runs, the
-  // joining launch a few us).
-  if (tiles < kFill) {
-    uint64_t s = std::min<uint64_t>(kFill * 2 / std::max<uint64_t>(tiles, 1), steps / 8);
-    const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
-    s = std::min(s, kMaxParts / std::max<uint64_t>(one, 1));
-    if (s >= 2) p.splits = (uint32_t)std::min<uint64_t>(s, 32);
+  const uint64_t steps = (a.k + bk - 1) / bk;
+  const uint64_t t128 = count_tiles(pass, a, 128), t64 = count_tiles(pass, a, 64);
+  if (rows != kAnyRows && dt == LL_BF16 && count_tiles(pass, a, 256) >= kFill) {
+    p.tile = 256;
+  } else if (t128 >= (dt == LL_BF16 ? kFill / 2 : 4 * kFill)) {
+    p.tile = 128;
+    // one workgroup a CU: four stages of it hide what two workgroups hide from each other
+    if (t128 <= kFill && steps >= 24) p.stages = 4;
+  } else {
+    if (t64 <= 2 * kFill) p.stages = 4;
+    // too few tiles: the sum is cut into shares of 16 stages or more
+    if (t64 < kFill) {
+      uint64_t s = std::min<uint64_t>((kFill + t64 - 1) / std::max<uint64_t>(t64, 1), steps / 16);
+      const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
+      s = std::min(s, kMaxParts / std::max<uint64_t>(one, 1));
+      if (s >= 2) p.splits = (uint32_t)std::min<uint64_t>(s, 32);
+    }
   }
+  if (rows == kAnyRows) p.stages = 2;
   return p;
 }
 
@@ -126,7 +139,18 @@ int launch_tiles(Args &a, bool gate, void *stream) {
   constexpr int kThreads = WM * WN * 64;
   if (grid * kThreads >= 1ull << 32) return LL_ERR_UNSUPPORTED;
   const tile_fn fn = pick<T, PASS, B, WM, WN, ST, ROWS>(gate);
+  // more tiles than one round of the chip: a short last round is left to the
+  // 128-wide kernel, four of whose tiles make one of these
+  const bool tail = B == 256 && PASS != kGradW && grid > kRound;
+  if (tail) a.tail = 1;
   hipLaunchKernelGGL(fn, dim3((unsigned)grid, a.splits), dim3(kThreads), 0, (hipStream_t)stream, a);
+  if constexpr (B == 256 && PASS != kGradW) {
+    if (tail) {
+      a.tail = 2;
+      const tile_fn rest = pick<T, PASS, 128, 2, 2, 4, ROWS>(gate);
+      hipLaunchKernelGGL(rest, dim3(4 * kMaxTail), dim3(256), 0, (hipStream_t)stream, a);
+    }
+  }
   if (a.parts != nullptr) {
     const uint64_t items = (uint64_t)a.rows_c * ((width + kEw - 1) / kEw);
     if ((items + 255) / 256 * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
@@ -149,8 +173,11 @@ int launch_plan(Args &a, const Plan &p, bool gate, void *stream) {
     if (p.tile == 128) return launch_tiles<T, PASS, 128, 2, 4, 2, ROWS>(a, gate, stream);
     return launch_tiles<T, PASS, 64, 2, 2, 2, ROWS>(a, gate, stream);
   } else {
-    if (p.tile == 128) return launch_tiles<T, PASS, 128, 2, 2, 2, ROWS>(a, gate, stream);
-    return launch_tiles<T, PASS, 64, 2, 2, 4, ROWS>(a, gate, stream);
+    if (p.tile == 128)
+      return p.stages == 4 ? launch_tiles<T, PASS, 128, 2, 2, 4, ROWS>(a, gate, stream)
+                           : launch_tiles<T, PASS, 128, 2, 2, 2, ROWS>(a, gate, stream);
+    return p.stages == 4 ? launch_tiles<T, PASS, 64, 2, 2, 4, ROWS>(a, gate, stream)
+                         : launch_tiles<T, PASS, 64, 2, 2, 2, ROWS>(a, gate, stream);
   }
 }
 

@@ -44,6 +44,7 @@ struct Args {
   bool vec_b;      // so does every group's bias
   float *parts;      // sums of the splits of k, [splits][rows of C][part_row], or NULL
   uint32_t splits, rows_c;
+  uint32_t tail;  // 1: leaves a short last round of tiles out; 2: runs that round, in quarters
   uint32_t part_half, part_row;  // columns of a (gated: half a) row of parts, multiples of kEw
 };
 
@@ -89,8 +90,17 @@ __host__ __device__ constexpr bool gated(int act) { return act == LL_ACT_SWIGLU 
 // last) fall to every XCD alike.
 constexpr uint32_t kBand = 4, kRun = 32;
 
-__device__ __forceinline__ bool tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t *tm, uint32_t *tn) {
-  const uint32_t total = tiles_m * tiles_n;
+// Tile number t, in bands.
+__device__ __forceinline__ void number_of(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, uint32_t *tm, uint32_t *tn) {
+  const uint32_t band = t / (kBand * tiles_n), in_band = t % (kBand * tiles_n);
+  const uint32_t high = min(kBand, tiles_m - band * kBand);
+  *tm = band * kBand + in_band % high;
+  *tn = in_band / high;
+}
+
+// Workgroup `id`'s tile among the first `total` of tiles_m x tiles_n.
+__device__ __forceinline__ bool tile_of(uint32_t id, uint32_t total, uint32_t tiles_m, uint32_t tiles_n, uint32_t *tm,
+                                        uint32_t *tn) {
   if (id >= total) return false;
   const uint32_t whole = total / (8 * kRun) * (8 * kRun);
   uint32_t t;
@@ -101,10 +111,7 @@ __device__ __forceinline__ bool tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
     const uint32_t left = total - whole, i = id - whole, x = i % 8, each = left / 8, more = left % 8;
     t = whole + x * each + min(x, more) + i / 8;
   }
-  const uint32_t band = t / (kBand * tiles_n), in_band = t % (kBand * tiles_n);
-  const uint32_t high = min(kBand, tiles_m - band * kBand);
-  *tm = band * kBand + in_band % high;
-  *tn = in_band / high;
+  number_of(t, tiles_m, tiles_n, tm, tn);
   return true;
 }
 
@@ -132,25 +139,60 @@ __device__ __forceinline__ uint32_t scan_tiles(const Args &a, int g0, uint32_t b
   return incl;
 }
 
+// A round is what the chip's 256 CUs work on at a time, one 256-wide tile each.
+// A last round of at most kMaxTail tiles takes as long as a whole one, so the
+// launch leaves it out and another runs it in 128-wide quarters: gradient of 8
+// groups of about 1024 rows, 288 tiles: 400 -> see the table of the plans.
+constexpr uint32_t kRound = 256, kMaxTail = 128;
+
+__device__ __forceinline__ uint32_t tail_tiles(uint32_t total) {
+  const uint32_t rest = total % kRound;
+  return total > kRound && rest <= kMaxTail ? rest : 0;
+}
+
+// Workgroup `id`'s tile among tiles_m x tiles_n of edge bm.  Quarters (tail 2):
+// the tiles are twice as wide as the workgroup's, whose edge is bm / 2, and
+// *quarter is which of the four.
+__device__ __forceinline__ bool pick_tile(const Args &a, uint32_t id, uint32_t tiles_m, uint32_t *tm, uint32_t *tn,
+                                          uint32_t *quarter) {
+  const uint32_t total = tiles_m * a.tiles_n;
+  *quarter = 0;
+  if (a.tail == 0) return tile_of(id, total, tiles_m, a.tiles_n, tm, tn);
+  const uint32_t rest = tail_tiles(total);
+  if (a.tail == 1) return tile_of(id, total - rest, tiles_m, a.tiles_n, tm, tn);
+  if (id >= 4 * rest) return false;
+  *quarter = id / rest;
+  number_of(total - rest + id % rest, tiles_m, a.tiles_n, tm, tn);
+  return true;
+}
+
 // The tile of workgroup `id` among the grouped rows: its group, first row, end
 // of the group's rows, and column tile.  false: there is none.  Every lane of
 // the calling wave takes part.
-__device__ __forceinline__ bool find_rows(const Args &a, uint32_t id, uint32_t bm, int *group, uint32_t *row0,
+__device__ __forceinline__ bool find_rows(const Args &a, uint32_t id, uint32_t edge, int *group, uint32_t *row0,
                                           uint32_t *row1, uint32_t *tn) {
-  uint32_t tm;
+  const uint32_t bm = a.tail == 2 ? 2 * edge : edge;
+  uint32_t tm, quarter;
+  auto place = [&]() {
+    if (a.tail == 2) {
+      *row0 += quarter / 2 * edge;
+      *tn = *tn * 2 + quarter % 2;
+    }
+    return *row0 < *row1;
+  };
   if (a.offsets == nullptr) {
-    if (!tile_of(id, (a.rows + bm - 1) / bm, a.tiles_n, &tm, tn)) return false;
+    if (!pick_tile(a, id, (a.rows + bm - 1) / bm, &tm, tn, &quarter)) return false;
     *group = 0;
     *row0 = tm * bm;
     *row1 = a.rows;
-    return true;
+    return place();
   }
   uint32_t lo, hi, tiles, incl = 0, total = 0;
   for (int g0 = 0; g0 < a.groups; g0 += 64) {
     incl = scan_tiles(a, g0, bm, &lo, &hi, &tiles);
     total += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
   }
-  if (!tile_of(id, total, a.tiles_n, &tm, tn)) return false;
+  if (!pick_tile(a, id, total, &tm, tn, &quarter)) return false;
   uint32_t before = 0;
   for (int g0 = 0; g0 < a.groups; g0 += 64) {
     if (a.groups > 64) incl = scan_tiles(a, g0, bm, &lo, &hi, &tiles);
@@ -161,7 +203,7 @@ __device__ __forceinline__ bool find_rows(const Args &a, uint32_t id, uint32_t b
       *group = g0 + who;
       *row0 = __builtin_amdgcn_readlane((int)lo, who) + (tm - first) * bm;
       *row1 = __builtin_amdgcn_readlane((int)hi, who);
-      return true;
+      return place();
     }
     before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
   }
@@ -628,7 +670,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
     const uint32_t per = a.tiles_m * a.tiles_n;
     uint32_t tm, lo, hi;
     g = blockIdx.x / per;
-    if (!tile_of(blockIdx.x % per, a.tiles_m, a.tiles_n, &tm, &tn)) return;
+    if (!tile_of(blockIdx.x % per, per, a.tiles_m, a.tiles_n, &tm, &tn)) return;
     m0 = tm * BM;
     group_rows(a, g, &lo, &hi);
     lo = uniform_u32(lo);
