@@ -94,32 +94,36 @@ uint64_t size_parts(Args &a, bool gate) {
 constexpr uint64_t kMaxParts = 256 << 20;  // bytes of split sums
 
 // Larger tiles move fewer operand bytes but need many tiles to fill the chip.
-// Measured, bfloat16, us with tiles of 256 / 128 (2 and 4 stages) / 64 (2 and 4):
-//   8192 x 2048 x 7168   grad_x  168 / 194, 228 / -       (256 tiles of 256)
-//   2048 x 2048 x 2048           46 / 25.8, 24.0 / 28.9, 30.8 (256 of 128)
-//   1024 x 4096 x 4096           78 / 44, 39 / 49, 52     (256 of 128)
-//   1024 x 1032 -> 2056          29 / 14.7, 15.7 / 16.2, 18.3 (136 of 128)
-//    512 x 2048 -> 2048          43 / 17.6, 19.9 / 11.5, 11.0 (64 of 128)
-//    128 x 4096 -> 4096          58 / 41, 32 / 31, 17.3; 4 splits 16.4 (128 of 64)
-//    301 x 8192 -> 1024         144 / 72, 56 / 58, 36; 3 splits 19.7  (80 of 64)
+// Measured with cold caches, bfloat16, us with tiles of 256 / 128 with 2 and 4
+// stages / 64 with 2 and 4, and the number of tiles:
+//   1024 x 4096 -> 4096   111 / 68, 54 / 70, 73      256 of 128
+//   2048 x 2048 -> 2048    61 / 39, 32 / 40, 42      256 of 128
+//    301 x 1024 -> 8192    38 / 23.7, 21.8 / 22.0, 23.2   192 of 128 (with bias and
+//      residual, call after call: - / 19.6, 18.6 / 14.7, 16.9)
+//   1024 x 1032 -> 2056    44 / 25.4, 24.4 / 22.8, 25.6   136 of 128, 528 of 64
+//    512 x 2048 -> 2048    60 / 38, 32 / 29, 17.8    256 of 64
+//    128 x 4096 -> 4096    98 / 69, 54 / 56, 31; 4 splits 26     128 of 64
+//   1000 x 7000 -> 200    237 / 127, 94 / 82, 51; 4 splits 25     64 of 64
+//     64 x 1024 -> 1024    30 / 22, 17 / 19, 14.8; 4 splits 11.9  16 of 64
+//   weight gradient of 301 rows, 1024 x 8192  22 / 17.7, 24 / 23, 27  512 of 128
 // 256 is for bfloat16 only: binary32 is bound by its matrix instructions, which
-// are 16 times slower (1024^3: 62 us with 128, 23 us with 64).
+// are 16 times slower (1024^3: 68 us with 128, 28 us with 64).
 Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows) {
   Plan p{64, 2, 1};
   const uint32_t bk = 128 / esize(dt);
-  const uint64_t steps = (a.k + bk - 1) / bk;
+  const uint64_t k = pass == kGradW ? a.k / a.groups : a.k, steps = (k + bk - 1) / bk;
   const uint64_t t128 = count_tiles(pass, a, 128), t64 = count_tiles(pass, a, 64);
   if (rows != kAnyRows && dt == LL_BF16 && count_tiles(pass, a, 256) >= kFill) {
     p.tile = 256;
-  } else if (t128 >= (dt == LL_BF16 ? kFill / 2 : 4 * kFill)) {
+  } else if (t128 >= (dt == LL_BF16 ? kFill : 4 * kFill)) {
     p.tile = 128;
     // one workgroup a CU: four stages of it hide what two workgroups hide from each other
-    if (t128 <= kFill && steps >= 24) p.stages = 4;
+    if (t128 == kFill && steps >= 12) p.stages = 4;
   } else {
     if (t64 <= 2 * kFill) p.stages = 4;
-    // too few tiles: the sum is cut into shares of 16 stages or more
-    if (t64 < kFill) {
-      uint64_t s = std::min<uint64_t>((kFill + t64 - 1) / std::max<uint64_t>(t64, 1), steps / 16);
+    // too few tiles: the sum is cut into shares of four stages or more
+    if (t64 < 200) {
+      uint64_t s = std::min<uint64_t>((320 + t64 - 1) / std::max<uint64_t>(t64, 1), steps / 4);
       const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
       s = std::min(s, kMaxParts / std::max<uint64_t>(one, 1));
       if (s >= 2) p.splits = (uint32_t)std::min<uint64_t>(s, 32);
@@ -418,7 +422,7 @@ int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, voi
     const bool rows_vec = chunked(dz, d->ldy, d->out, es);
     const auto fn = d->dt == LL_F32 ? (rows_vec ? k_bias_grad<float, true> : k_bias_grad<float, false>)
                                     : (rows_vec ? k_bias_grad<__bf16, true> : k_bias_grad<__bf16, false>);
-    const unsigned cols = 16 * (rows_vec ? 16 / es : 1);
+    const unsigned cols = kBiasChunks * (rows_vec ? 16 / es : 1);
     hipLaunchKernelGGL(fn, dim3((a.m + cols - 1) / cols, a.groups), dim3(1024), 0, (hipStream_t)stream, a);
   }
   return launch_product<kGradW>(a, d->dt, false, rows, workspace, workspace_bytes, stream);

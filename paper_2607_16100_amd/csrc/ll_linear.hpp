@@ -1123,15 +1123,18 @@ __global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
 //
 // dbias[g] = the sum of dz over the group's rows.  A launch of its own: inside
 // the weight gradient's kernel it took registers that kernel has not (its
-// loop's addresses went to memory, 765 -> 1860 us for 8192^3).  16 chunks of
-// columns a workgroup, the rows dealt to 64 threads a chunk, eight loads of a
-// thread under way at a time; the 64 parts are added in order.
+// loop's addresses went to memory, 765 -> 1860 us for 8192^3).  kBiasChunks
+// chunks of columns a workgroup (a cache line), the rows dealt to kBiasLanes
+// threads a chunk, eight loads of a thread under way at a time; the threads'
+// parts are added in order.
+constexpr int kBiasChunks = 8, kBiasLanes = 128;
+
 template <typename T, bool VEC>
-__global__ __launch_bounds__(1024) void k_bias_grad(Args a) {
-  constexpr int C = VEC ? Num<T>::kPer16 : 1, kAhead = 8;
-  __shared__ float part[64][16 * C + 1];
-  const int g = blockIdx.y, c = threadIdx.x % 16, lane = threadIdx.x / 16;
-  const uint32_t col = (blockIdx.x * 16 + c) * C;
+__global__ __launch_bounds__(kBiasChunks *kBiasLanes) void k_bias_grad(Args a) {
+  constexpr int C = VEC ? Num<T>::kPer16 : 1, kAhead = 8, kCols = kBiasChunks * C;
+  __shared__ float part[kBiasLanes][kCols + 1];
+  const int g = blockIdx.y, c = threadIdx.x % kBiasChunks, lane = threadIdx.x / kBiasChunks;
+  const uint32_t col = (blockIdx.x * kBiasChunks + c) * C;
   uint32_t lo, hi;
   group_rows(a, g, &lo, &hi);
   float sum[C];
@@ -1140,16 +1143,17 @@ __global__ __launch_bounds__(1024) void k_bias_grad(Args a) {
   if (col < a.m) {
     const T *p = (const T *)a.p + col;
     uint32_t r = lo + lane;
-    for (; r + 64 * (kAhead - 1) < hi; r += 64 * kAhead) {
+    for (; r + kBiasLanes * (kAhead - 1) < hi; r += kBiasLanes * kAhead) {
       Pack<T, C, VEC> v[kAhead];
 #pragma unroll
-      for (int n = 0; n < kAhead; ++n) v[n].load(p + (uint64_t)(r + 64 * n) * a.ldp);
+      for (int n = 0; n < kAhead; ++n) v[n].load(p + (uint64_t)(r + kBiasLanes * n) * a.ldp);
 #pragma unroll
       for (int n = 0; n < kAhead; ++n)
 #pragma unroll
         for (int i = 0; i < C; ++i) sum[i] += v[n].v[i];
     }
-    for (; r < hi; r += 64) {
+#pragma unroll 4
+    for (; r < hi; r += kBiasLanes) {
       Pack<T, C, VEC> v;
       v.load(p + (uint64_t)r * a.ldp);
 #pragma unroll
@@ -1159,10 +1163,11 @@ __global__ __launch_bounds__(1024) void k_bias_grad(Args a) {
 #pragma unroll
   for (int i = 0; i < C; ++i) part[lane][c * C + i] = sum[i];
   __syncthreads();
-  const uint32_t m = blockIdx.x * 16 * C + threadIdx.x;
-  if (threadIdx.x < 16 * C && m < a.m) {
+  const uint32_t m = blockIdx.x * kCols + threadIdx.x;
+  if (threadIdx.x < kCols && m < a.m) {
     float b = 0.f;
-    for (int r = 0; r < 64; ++r) b += part[r][threadIdx.x];
+#pragma unroll 8
+    for (int r = 0; r < kBiasLanes; ++r) b += part[r][threadIdx.x];
     put_bias_grad<T>(a, g, m, b);
   }
 }

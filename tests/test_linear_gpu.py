@@ -151,6 +151,67 @@ def test_grad_w(name, dtype, grad, add, bias, layout):
             ref.close(db[gi], want, err, grad)
 
 
+# Products large enough for each tile edge, stage count and last round, whole
+# and odd rows alike: (counts or rows, in, out), as forward, grad_x and grad_w.
+LARGE = [
+    # 256-wide tiles: several groups with half-empty tiles and a short last round of them
+    ("forward", BF16, [900, 1300, 0, 40, 2100], 200, 4096), ("forward", BF16, 4100, 130, 4100),
+    ("forward", BF16, [4300, 1], 72, 8192), ("grad_x", BF16, [100, 257, 4000], 4096, 136),
+    ("grad_x", BF16, 4096, 4098, 70), ("grad_w", BF16, 100, 4096, 4096), ("grad_w", BF16, [70, 0, 3], 2310, 2306),
+    # 128-wide tiles, 4 and 2 stages, and odd rows of bfloat16
+    ("forward", BF16, 2048, 800, 2048), ("forward", BF16, [1000, 0, 1100], 640, 2200),
+    ("forward", BF16, 2100, 333, 2047), ("grad_x", BF16, 2100, 2047, 333), ("grad_w", BF16, 333, 2047, 2100),
+    ("grad_w", BF16, 800, 2048, 2048), ("forward", F32, 4100, 100, 4097), ("grad_x", F32, 4096, 4096, 67),
+    ("grad_w", F32, 67, 4096, 4100),
+    # split sums, and the streaming kernel's 16 and 32 rows
+    ("forward", BF16, 200, 4100, 136), ("forward", BF16, [30, 90, 0, 7], 2051, 66), ("grad_x", BF16, 100, 136, 4096),
+    ("grad_w", BF16, 5000, 136, 72), ("grad_w", F32, [3000, 5], 100, 130), ("forward", F32, 20, 1100, 300),
+    ("forward", BF16, 20, 7176, 1000), ("forward", BF16, [5, 40, 0, 11, 16, 17, 2, 3], 1032, 500),
+]
+
+
+@pytest.mark.parametrize("what,dtype,counts,i,o", LARGE)
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+def test_large(what, dtype, counts, i, o, act):
+    g = gen(22)
+    if isinstance(counts, int):
+        offsets, n, groups = None, counts, 1
+        w = randn(g, o, i, dtype=dtype)
+    else:
+        n, groups = sum(counts), len(counts)
+        offsets = torch.tensor([sum(counts[:c]) for c in range(groups + 1)], dtype=torch.int32, device=DEV)
+        w = randn(g, groups, o, i, dtype=dtype)
+    if what == "forward":
+        if act == "swiglu" and o % 2:
+            o -= 1
+            w = w[..., :o, :].contiguous()
+        x, b = randn(g, n, i, dtype=dtype), randn(g, groups, o, dtype=dtype)
+        z = torch.empty(n, o, dtype=dtype, device=DEV)
+        out = moe.linear(x, w, bias=b, act=act, offsets=offsets, z=z)
+        for gi, lo, hi in ref.spans(offsets, n):
+            zz, ez = ref.matmul(x[lo:hi].double(), weight(w, gi).t())
+            zz = zz + b[gi].double()
+            ez = ez + ref.EPS * zz.abs()
+            ref.close(out[lo:hi], ref.act(zz, act), ref.act_err(zz, ez, act), dtype)
+            ref.close(z[lo:hi], zz, ez, dtype)
+    elif what == "grad_x":
+        dz, z = randn(g, n, o, dtype=dtype), randn(g, n, 2 * i if act == "swiglu" else i, dtype=dtype)
+        out = moe.linear_grad_x(dz, w, act=act, z=None if act == "none" else z, offsets=offsets)
+        for gi, lo, hi in ref.spans(offsets, n):
+            da, ea = ref.matmul(dz[lo:hi].double(), weight(w, gi))
+            zz = z[lo:hi].double()
+            ref.close(out[lo:hi], ref.through(da, zz, act), ref.through_err(da, ea, zz, act), dtype)
+    else:
+        dz, x = randn(g, n, o, dtype=dtype), randn(g, n, i, dtype=dtype)
+        db = torch.empty(groups, o, dtype=dtype, device=DEV)
+        dw, _ = moe.linear_grad_w(dz, x, offsets=offsets, bias_out=db)
+        for gi, lo, hi in ref.spans(offsets, n):
+            want, err = ref.matmul(dz[lo:hi].double().t(), x[lo:hi].double())
+            ref.close(dw if offsets is None else dw[gi], want, err, dtype)
+            d = dz[lo:hi].double()
+            ref.close(db[gi], d.sum(0), (hi - lo + 2) * ref.EPS * d.abs().sum(0), dtype)
+
+
 @pytest.mark.parametrize("act", ["relu", "gelu", "silu", "swiglu", "geglu"])
 @pytest.mark.parametrize("dtype,h,pad", [(F32, 33, 0), (BF16, 64, 8), (F32, 8, 1)])
 def test_act_grad(act, dtype, h, pad):
