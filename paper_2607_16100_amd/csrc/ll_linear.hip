@@ -41,7 +41,13 @@ int check_desc(const ll_linear_desc *d) {
   return LL_OK;
 }
 
-Rows rows_of(const void *p, size_t ld, size_t len, int es);
+// Every row starts at a 16-byte address.
+bool rows16(const void *p, size_t ld, int es) { return p == nullptr || (aligned(p, 16) && ld * es % 16 == 0); }
+Rows rows_of(const void *p, size_t ld, size_t len, int es) {
+  if (aligned(p, 16) && ld * es % 16 == 0 && len * es % 16 == 0) return kChunkRows;
+  return aligned(p, 4) && ld * es % 4 == 0 ? kDwordRows : kAnyRows;
+}
+bool chunked(const void *p, size_t ld, size_t len, int es) { return rows_of(p, ld, len, es) == kChunkRows; }
 
 // The same of every group's weight.
 Rows weight_rows(const ll_linear_desc *d, const void *w, int es) {
@@ -194,6 +200,16 @@ int launch_rows(Args &a, const Plan &p, Rows rows, bool gate, void *stream) {
   return launch_plan<T, PASS, kDwordRows>(a, p, gate, stream);
 }
 
+void launch_bias_grad(const Args &a, ll_dtype dt, void *stream) {
+  const int es = esize(dt);
+  const bool vec = chunked(a.p, a.ldp, a.m, es);
+  const auto fn = dt == LL_F32 ? (vec ? k_bias_grad<float, true> : k_bias_grad<float, false>)
+                               : (vec ? k_bias_grad<__bf16, true> : k_bias_grad<__bf16, false>);
+  const unsigned cols = kBiasChunks * (vec ? 16 / es : 1);
+  hipLaunchKernelGGL(fn, dim3((a.m + cols - 1) / cols, a.groups), dim3(kBiasChunks * kBiasLanes), 0,
+                     (hipStream_t)stream, a);
+}
+
 template <Pass PASS>
 int launch_product(Args &a, ll_dtype dt, bool gate, Rows rows, void *workspace, size_t workspace_bytes, void *stream) {
   const uint64_t one = size_parts(a, gate);
@@ -202,6 +218,10 @@ int launch_product(Args &a, ll_dtype dt, bool gate, Rows rows, void *workspace, 
   if (p.splits * one > workspace_bytes) p.splits = one == 0 ? 1 : (uint32_t)std::max<uint64_t>(1, workspace_bytes / one);
   a.splits = p.splits;
   a.parts = p.splits > 1 ? (float *)workspace : nullptr;
+  if (PASS == kGradW && a.dbias != nullptr) {
+    a.sum_bias = p.tile == 64 && p.splits == 1;
+    if (!a.sum_bias) launch_bias_grad(a, dt, stream);
+  }
   return dt == LL_F32 ? launch_rows<float, PASS>(a, p, rows, gate, stream)
                       : launch_rows<__bf16, PASS>(a, p, rows, gate, stream);
 }
@@ -230,14 +250,6 @@ int launch_stream(Args &a, bool gate, void *stream) {
   hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(kNW * 64), 0, (hipStream_t)stream, a);
   return launch_status();
 }
-
-// Every row starts at a 16-byte address.
-bool rows16(const void *p, size_t ld, int es) { return p == nullptr || (aligned(p, 16) && ld * es % 16 == 0); }
-Rows rows_of(const void *p, size_t ld, size_t len, int es) {
-  if (aligned(p, 16) && ld * es % 16 == 0 && len * es % 16 == 0) return kChunkRows;
-  return aligned(p, 4) && ld * es % 4 == 0 ? kDwordRows : kAnyRows;
-}
-bool chunked(const void *p, size_t ld, size_t len, int es) { return rows_of(p, ld, len, es) == kChunkRows; }
 
 }  // namespace
 
@@ -418,13 +430,6 @@ int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, voi
   a.vec_c = rows16(dw, d->ldw, gs) && d->wstride * gs % 16 == 0;
   const Rows rows = std::min(rows_of(dz, d->ldy, d->out, es), rows_of(x, d->ldx, d->in, es));
   a.k = a.rows;
-  if (dbias != nullptr) {
-    const bool rows_vec = chunked(dz, d->ldy, d->out, es);
-    const auto fn = d->dt == LL_F32 ? (rows_vec ? k_bias_grad<float, true> : k_bias_grad<float, false>)
-                                    : (rows_vec ? k_bias_grad<__bf16, true> : k_bias_grad<__bf16, false>);
-    const unsigned cols = kBiasChunks * (rows_vec ? 16 / es : 1);
-    hipLaunchKernelGGL(fn, dim3((a.m + cols - 1) / cols, a.groups), dim3(1024), 0, (hipStream_t)stream, a);
-  }
   return launch_product<kGradW>(a, d->dt, false, rows, workspace, workspace_bytes, stream);
 }
 

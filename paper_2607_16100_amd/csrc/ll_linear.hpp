@@ -44,6 +44,7 @@ struct Args {
   bool vec_b;      // so does every group's bias
   float *parts;      // sums of the splits of k, [splits][rows of C][part_row], or NULL
   uint32_t splits, rows_c;
+  bool sum_bias;  // grad_w: the tile kernel computes dbias too
   uint32_t tail;  // 1: leaves a short last round of tiles out; 2: runs that round, in quarters
   uint32_t part_half, part_row;  // columns of a (gated: half a) row of parts, multiples of kEw
 };
@@ -712,6 +713,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  f32x4 accb[kFlat ? FM : 1];  // grad_w: the bias gradient's sums
+  frag ones;
+#pragma unroll
+  for (auto &v : accb) v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(ones) / sizeof(T)); ++i) ones[i] = (T)1.f;
+
   const uint32_t steps = (k + BK - 1) / BK;
   constexpr int kLoads = lp.kChunks + lq.kChunks;  // of a thread, a stage
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
@@ -771,6 +779,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
     lds_barrier();
     if constexpr (kFlat) {
       frag fq[2][2][FN], fp[2][2][FM];  // of two stages, by half of k
+      const bool want_bias = PASS == kGradW && a.sum_bias && tn == 0 && wn == 0;
       auto read_all = [&](auto set_c, const char *from) __attribute__((always_inline)) {
         constexpr int set = decltype(set_c)::value;
 #pragma unroll
@@ -809,6 +818,14 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
           for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int i = 0; i < FM; ++i) acc[j][i] = mma(fq[now][ks][j], fp[now][ks][i], acc[j][i]);
+        if constexpr (PASS == kGradW) {
+          if (want_bias) {  // the product with a column of ones
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+              for (int i = 0; i < FM; ++i) accb[i] = mma(ones, fp[now][ks][i], accb[i]);
+          }
+        }
         lp.advance();
         lq.advance();
       };
@@ -914,6 +931,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
   wait_loads<0>();
   lds_barrier();  // every wave is past its last stage, and no load is under way
 
+  if constexpr (PASS == kGradW && kFlat) {
+    if (a.sum_bias && tn == 0 && wn == 0 && lane < 16) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+        if (m0 + dim_p(i) + lane < m_end) put_bias_grad<T>(a, g, m0 + dim_p(i) + lane, accb[i][0]);
+    }
+  }
   float *mine = reinterpret_cast<float *>(lds) + wave * (WTM / 2) * kPitch;
   auto finish = [&](auto half) __attribute__((always_inline)) {
     constexpr int h = decltype(half)::value;
@@ -1121,9 +1145,10 @@ __global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
 
 // ---------------------------------------------------------------- bias gradient
 //
-// dbias[g] = the sum of dz over the group's rows.  A launch of its own: inside
-// the weight gradient's kernel it took registers that kernel has not (its
-// loop's addresses went to memory, 765 -> 1860 us for 8192^3).  kBiasChunks
+// dbias[g] = the sum of dz over the group's rows.  The 64-wide tile kernel has
+// the registers to sum it along.  With larger tiles or split sums it is a
+// launch of its own: in the 256-wide kernel the sums sent its loop's addresses
+// to memory (765 -> 1860 us for 8192^3).  kBiasChunks
 // chunks of columns a workgroup (a cache line), the rows dealt to kBiasLanes
 // threads a chunk, eight loads of a thread under way at a time; the threads'
 // parts are added in order.

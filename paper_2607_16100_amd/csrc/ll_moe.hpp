@@ -88,6 +88,28 @@ __device__ __forceinline__ float choice_score(const RouteArgs &a, float x, float
   return x == kNegInf ? 0.f : exp_f32(x - m);
 }
 
+// Keys as integers of the same order (-0 made +0 first, as they compare equal),
+// which compare and reduce without the care NaN takes.
+__device__ __forceinline__ int sort_key(float x) {
+  const int i = __float_as_int(x + 0.f);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float key_value(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
+constexpr int kNoKey = (int)0x807fffff;  // of -Infinity
+
+template <int W>
+__device__ __forceinline__ int group_max_key(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0xB1, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x4E, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x141, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x140, 0xF, 0xF, false));
+  if constexpr (W == 64) {
+    v = max(v, __shfl_xor(v, 16));
+    v = max(v, __shfl_xor(v, 32));
+  }
+  return v;
+}
+
 template <typename T, int W, int NPL, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
   const int sub = threadIdx.x % W, lane = threadIdx.x % 64;
@@ -95,44 +117,73 @@ __global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
   const bool live = t < a.tokens;  // no early exit: the lanes of a wave work on several tokens together
   const T *row = (const T *)a.logits + (uint64_t)(live ? t : 0) * a.ld;
   const int e0 = sub * NPL;
-  float key[NPL];
-  load_logits<T, NPL, VEC>(row, e0, a.experts, key);
+  float l[NPL], bias[NPL];
+  if (a.bias != nullptr) {  // under way together with the logits
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) bias[i] = e0 + i < a.experts ? a.bias[e0 + i] : 0.f;
+  }
+  load_logits<T, NPL, VEC>(row, e0, a.experts, l);
   float m = 0.f, inv = 0.f;
   if (a.score == 0 && !a.normalise) {
     float e[NPL];
-    m = softmax_stats<W, NPL>(key, e, &inv);
+    m = softmax_stats<W, NPL>(l, e, &inv);
   }
   if (a.bias != nullptr) {
 #pragma unroll
     for (int i = 0; i < NPL; ++i) {
-      const float x = key[i] + (e0 + i < a.experts ? a.bias[e0 + i] : 0.f);
-      key[i] = x == x ? x : kNegInf;
+      const float x = l[i] + bias[i];
+      l[i] = x == x ? x : kNegInf;
     }
   }
-  int mine = -1;  // lane j keeps the j-th choice
-  for (int j = 0; j < a.k; ++j) {
-    float best = key[0];
+  int key[NPL];
 #pragma unroll
-    for (int i = 1; i < NPL; ++i) best = fmaxf(best, key[i]);
-    const float top = group_max<W>(best);
-    uint64_t have = __ballot(best == top && top > kNegInf);
-    if constexpr (W == 16) have = (have >> (lane & 48)) & 0xFFFFull;
-    const int who = have == 0 ? -1 : __ffsll((unsigned long long)have) - 1;
-    // the winner's lowest key that is the maximum: found and taken out
-    bool open = sub == who;
-    int at = 0;
-#pragma unroll
-    for (int i = 0; i < NPL; ++i) {
-      const bool hit = open && key[i] == top;
-      key[i] = hit ? kNegInf : key[i];
-      at = hit ? i : at;
-      open = open && !hit;
-    }
-    const int won = __shfl(at, who < 0 ? 0 : who, W);
-    if (sub == j) mine = who < 0 ? -1 : who * NPL + won;
-  }
+  for (int i = 0; i < NPL; ++i) key[i] = sort_key(l[i]);
+  int mine = -1;  // lane j keeps the j-th choice and its key
   float x = kNegInf;
-  if (mine >= 0) {
+  auto lane_best = [&]() __attribute__((always_inline)) {
+    int best = key[0];
+#pragma unroll
+    for (int i = 1; i + 1 < NPL; i += 2) best = max(max(best, key[i]), key[i + 1]);
+    return NPL % 2 == 0 ? max(best, key[NPL - 1]) : best;
+  };
+  if (sizeof(T) == 2 && a.bias == nullptr) {
+    // bfloat16 logits leave room for the index below the key's 16 bits, high
+    // for low indices: keys are unique and say which expert they are
+#pragma unroll
+    for (int i = 0; i < NPL; ++i) key[i] = (key[i] & (int)0xffff0000) | (0xffff - (e0 + i));
+    for (int j = 0; j < a.k; ++j) {
+      const int top = group_max_key<W>(lane_best());
+#pragma unroll
+      for (int i = 0; i < NPL; ++i) key[i] = key[i] == top ? kNoKey : key[i];
+      if (sub == j && top > (kNoKey | 0xffff)) {
+        mine = 0xffff - (top & 0xffff);
+        x = key_value((top & (int)0xffff0000) | (top < 0 ? 0xffff : 0));
+      }
+    }
+  } else {
+    for (int j = 0; j < a.k; ++j) {
+      const int best = lane_best(), top = group_max_key<W>(best);
+      uint64_t have = __ballot(best == top && top > kNoKey);
+      if constexpr (W == 16) have = (have >> (lane & 48)) & 0xFFFFull;
+      const int who = have == 0 ? -1 : __ffsll((unsigned long long)have) - 1;
+      // the winner's lowest key that is the maximum: found and taken out
+      bool open = sub == who;
+      int at = 0;
+#pragma unroll
+      for (int i = 0; i < NPL; ++i) {
+        const bool hit = open && key[i] == top;
+        key[i] = hit ? kNoKey : key[i];
+        at = hit ? i : at;
+        open = open && !hit;
+      }
+      const int won = __shfl(at, who < 0 ? 0 : who, W);
+      if (sub == j) {
+        mine = who < 0 ? -1 : who * NPL + won;
+        x = who < 0 ? kNegInf : key_value(top);
+      }
+    }
+  }
+  if (a.bias != nullptr && mine >= 0) {  // the key is not the logit
     x = Num<T>::get(row[mine]);
     if (x != x) x = kNegInf;
   }

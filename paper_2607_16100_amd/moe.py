@@ -21,8 +21,6 @@ ReduceScatter:
 """
 from __future__ import annotations
 
-from functools import lru_cache
-
 import torch
 
 from . import llcoll as ll
@@ -225,20 +223,21 @@ def _offsets(offsets, groups: int):
     return _flat(offsets, "offsets", groups + 1, torch.int32)
 
 
-@lru_cache(maxsize=4096)
-def _bytes(which: int, *fields) -> int:
-    """Workspace of a product of this shape (host arithmetic only)."""
-    st, need = lm.ll_linear_bytes(lm.LLLinearDesc(*fields), which)
-    ll.check(st, "ll_linear_bytes")
-    return need
+_needs: dict = {}  # workspace bytes by shape (host arithmetic only)
 
 
 def _plan(which: int, device, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz=0, ldr=0):
     """(descriptor, workspace address, its bytes, the workspace)."""
-    # the address of the offsets is no part of the shape; whether there are any is
-    need = _bytes(which, lm.DESC_SIZE, dt, act, groups, rows, in_, out, None if offsets is None else 16, ldx, ldw,
-                  wstride, ldy, ldz, ldr)
     d = lm.LLLinearDesc(lm.DESC_SIZE, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz, ldr)
+    # what a plan depends on: the shape, whether there are offsets, and how rows are aligned
+    key = (which, dt, act, groups, rows, in_, out, offsets is None, (ldx | ldw | wstride) & 7)
+    need = _needs.get(key)
+    if need is None:
+        st, need = lm.ll_linear_bytes(d, which)
+        ll.check(st, "ll_linear_bytes")
+        if len(_needs) >= 4096:
+            _needs.clear()
+        _needs[key] = need
     if not need:
         return d, None, 0, None
     ws = torch.empty(need, dtype=torch.uint8, device=device)
