@@ -394,7 +394,10 @@ struct Loader {
   // operand's stage); whole: the stage has kBK k left, else `have` of them.
   // In assembly so that the compiler does not wait for the load before the
   // next LDS read, as it must where it sees a write to LDS; it has no result
-  // register, and the caller waits for it.
+  // register, and the caller waits for it.  The compiler does not know that
+  // this reads scalar registers from the vector memory unit either, which
+  // must come five wait states after a vector instruction (v_readfirstlane)
+  // wrote them: they are inside the block.
   template <bool WHOLE>
   __device__ __forceinline__ void issue(uint32_t at, int c, uint32_t have) {
     // the base and the LDS address are the same in every lane
@@ -405,7 +408,7 @@ struct Loader {
     const uint32_t o = WHOLE || kk(c) < have ? off[c] : kOutside;
     asm volatile(
         "s_mov_b32 m0, %0\n\t"
-        "s_nop 0\n\t"
+        "s_nop 3\n\t"
         "buffer_load_dwordx4 %1, %2, 0 offen lds"
         :
         : "s"(uniform_u32(at + c * 1024)), "v"(o), "s"(rs)
@@ -647,7 +650,7 @@ __device__ __forceinline__ void wait_loads() {
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <typename T, Pass PASS, int BM, int BN, int WM, int WN, int ST, bool GATED, Rows ROWS>
-__global__ __launch_bounds__(WM *WN * 64, 2) void k_tile(Args a) {
+__global__ __launch_bounds__(WM *WN * 64, ST *(BM + BN) > 640 && WM * WN == 4 ? 1 : 2) void k_tile(Args a) {
   constexpr bool kPkm = PASS != kGradW, kQkm = PASS == kForward;
   constexpr bool VEC = ROWS != kAnyRows;  // loads go straight into LDS
   constexpr bool kFlat = BM == 64;        // all fragments of a stage at once
