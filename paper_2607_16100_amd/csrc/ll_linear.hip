@@ -83,6 +83,14 @@ uint64_t count_tiles(Pass pass, const Args &a, uint32_t b) {
   return (a.offsets == nullptr ? (a.rows + b - 1) / b : a.rows / b + std::min<uint64_t>(a.groups, a.rows)) * n;
 }
 
+// Tiles it has, about: half of a row tile of each group with rows is lost, and
+// some more, since a few tiles past a full round of the chip cost another.
+uint64_t expect_tiles(Pass pass, const Args &a, uint32_t b) {
+  if (pass == kGradW || a.groups == 1) return count_tiles(pass, a, b);
+  const uint64_t eighths = 8 * (uint64_t)a.rows / b + 6 * (uint64_t)std::min<uint32_t>(a.groups, a.rows);
+  return std::max<uint64_t>(1, eighths / 8) * ((a.n + b - 1) / b);
+}
+
 // How a product runs: the tile's edge, its stages in LDS, the splits of its sum.
 struct Plan {
   uint32_t tile, stages, splits;
@@ -118,21 +126,31 @@ Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows) {
   Plan p{64, 2, 1};
   const uint32_t bk = 128 / esize(dt);
   const uint64_t k = pass == kGradW ? a.k / a.groups : a.k, steps = (k + bk - 1) / bk;
-  const uint64_t t128 = count_tiles(pass, a, 128), t64 = count_tiles(pass, a, 64);
-  if (rows != kAnyRows && dt == LL_BF16 && count_tiles(pass, a, 256) >= kFill) {
+  const uint64_t t128 = expect_tiles(pass, a, 128), t64 = expect_tiles(pass, a, 64);
+  if (rows != kAnyRows && dt == LL_BF16 && expect_tiles(pass, a, 256) >= kFill) {
     p.tile = 256;
   } else if (t128 >= (dt == LL_BF16 ? kFill : 4 * kFill)) {
     p.tile = 128;
     // one workgroup a CU: four stages of it hide what two workgroups hide from each other
-    if (t128 == kFill && steps >= 12) p.stages = 4;
+    if (t128 <= kFill * 9 / 8 && steps >= 12) p.stages = 4;
   } else {
     if (t64 <= 2 * kFill) p.stages = 4;
-    // too few tiles: the sum is cut into shares of four stages or more
+    // Too few tiles: the sum is cut into shares of four stages or more.  s
+    // splits cost the rounds of the chip they make, each 1 / s of a whole one,
+    // and about a twentieth of a round each for the joining (128 x 4096 -> 4096
+    // binary32, 128 tiles: 84 us whole, 50 in 2, 58 in 3, 49 in 4; 777 x 1001
+    // x 515, about 135: 33 us in 2, 28 in 3).
     if (t64 < 200) {
-      uint64_t s = std::min<uint64_t>((320 + t64 - 1) / std::max<uint64_t>(t64, 1), steps / 4);
       const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
-      s = std::min(s, kMaxParts / std::max<uint64_t>(one, 1));
-      if (s >= 2) p.splits = (uint32_t)std::min<uint64_t>(s, 32);
+      const uint64_t most = std::min<uint64_t>(std::min<uint64_t>(16, steps / 4), kMaxParts / std::max<uint64_t>(one, 1));
+      double best = 1.;
+      for (uint64_t s = 2; s <= most; ++s) {
+        const double cost = (double)((t64 * s + kFill - 1) / kFill) / s + .05 * s + .08;
+        if (cost < best) {
+          best = cost;
+          p.splits = (uint32_t)s;
+        }
+      }
     }
   }
   if (rows == kAnyRows) p.stages = 2;
@@ -151,7 +169,10 @@ int launch_tiles(Args &a, bool gate, void *stream) {
   const tile_fn fn = pick<T, PASS, B, WM, WN, ST, ROWS>(gate);
   // more tiles than one round of the chip: a short last round is left to the
   // 128-wide kernel, four of whose tiles make one of these
-  const bool tail = B == 256 && PASS != kGradW && grid > kRound;
+  // (without offsets the number of tiles is known here)
+  const uint64_t rest = grid % kRound;
+  const bool tail = B == 256 && PASS != kGradW && grid > kRound &&
+                    (a.offsets != nullptr || (rest != 0 && rest <= kMaxTail));
   if (tail) a.tail = 1;
   hipLaunchKernelGGL(fn, dim3((unsigned)grid, a.splits), dim3(kThreads), 0, (hipStream_t)stream, a);
   if constexpr (B == 256 && PASS != kGradW) {

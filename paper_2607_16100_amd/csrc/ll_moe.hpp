@@ -21,6 +21,12 @@ constexpr float kNegInf = -__builtin_inff();
 // W lanes hold one token's logits, NPL consecutive ones each, so that among
 // equal keys the lowest lane holds the lowest index.  k rounds: every lane's
 // best key, the maximum over the lanes, the lowest lane that has it.
+//
+// Bound by vector instructions, not by memory: 32301 tokens x 160 bfloat16
+// logits, 6 choices, take 9.6 us (1.1 TB/s); 16 lanes a token rather than 64
+// share the steps over the lanes among four tokens of a wave.  Its gradient,
+// which computes the exponentials again and nothing else, takes 7.8 us (2.7
+// TB/s).  One token takes 6.7 us, a chain of 8 rounds behind two loads.
 struct RouteArgs {
   const void *logits;
   uint64_t ld;
@@ -278,7 +284,10 @@ __global__ __launch_bounds__(kThreads) void k_route_grad(RouteArgs a) {
 // choice) pairs, each of its waves a consecutive quarter of them, and a wave
 // 64 at a time, so a pair's place is: the rows of smaller experts, the
 // expert's rows in earlier blocks, in earlier waves of this block, in earlier
-// batches of this wave, and among the lower lanes.
+// batches of this wave, and among the lower lanes.  Two launches, 4.8 + 6.4 us
+// for 49152 pairs, almost all of it latency; up to 1024 pairs every block that
+// copies rows sorts them for itself instead, which saves a launch or two (128
+// pairs over 32 experts with their rows of 14 KiB: 6 us in all).
 struct SortArgs {
   const int32_t *ids;
   uint32_t pairs, chunk, blocks;
@@ -474,7 +483,8 @@ struct Raw {
 
 // One token's row to each of its local sorted rows; read once, written up to
 // k times, so a token's row comes from memory once however many experts it
-// has here.
+// has here.  Bound by memory: the whole dispatch of 8192 tokens of 14 KiB to
+// 12288 rows takes 58-70 us (3.9-4.7 TB/s).
 template <typename T, bool VEC, int TPR>
 __device__ __forceinline__ void push_row(const RowArgs &a, uint32_t t, const int32_t *rows_of) {
   constexpr int C = chunk_elems<T, VEC>();
@@ -535,7 +545,9 @@ __global__ __launch_bounds__(kThreads) void k_dispatch_small(SortArgs s, RowArgs
 }
 
 // out[t] = sum_j w[t,j] y[rows[t,j]] (+ residual).  The loads of up to
-// kBatch expert rows are issued before the first of them is used.
+// kBatch expert rows are issued before the first of them is used (converting
+// each as it is loaded made them wait for each other: 174 -> 98 us).  Bound by
+// memory: 8192 tokens of 14 KiB from 12288 rows in 95-103 us (4.0-4.3 TB/s).
 constexpr int kBatch = 8;
 
 template <typename T, bool VEC, int TPR>
@@ -579,7 +591,8 @@ __global__ __launch_bounds__(kThreads) void k_combine(RowArgs a) {
 
 // dy[rows[t,j]] = w[t,j] dout[t], dw[t,j] = <dout[t], y[rows[t,j]]>.  A
 // thread's partial products of up to kBatch choices stay in registers; the
-// row's threads join them once a batch.
+// row's threads join them once a batch.  Bound by memory: 4397 tokens of 4104
+// binary32, 2 choices, in 82 us (4.4 TB/s).
 template <typename T, bool VEC, int TPR>
 __global__ __launch_bounds__(kThreads) void k_combine_grad(RowArgs a) {
   constexpr int C = chunk_elems<T, VEC>();
