@@ -505,6 +505,22 @@ __device__ __forceinline__ Vals get8(const T *p, uint32_t n, bool vec) {
   for (int i = 0; i < kEw; ++i) v.v[i] = o.v[i];
   return v;
 }
+// kEw elements as they lie in memory, converted where they are used.
+template <typename T>
+struct Held {
+  typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+  vec r[kEw * sizeof(T) / 16];
+  __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+    for (int i = 0; i < (int)(kEw * sizeof(T) / 16); ++i) r[i] = reinterpret_cast<const vec *>(p)[i];
+  }
+  __device__ __forceinline__ Vals vals() const {
+    Vals v;
+#pragma unroll
+    for (int i = 0; i < kEw; ++i) v.v[i] = Num<T>::get(r[i * sizeof(T) / 16][i % (16 / sizeof(T))]);
+    return v;
+  }
+};
 __device__ __forceinline__ void add8(Vals &v, const Vals &w) {
 #pragma unroll
   for (int i = 0; i < kEw; ++i) v.v[i] += w.v[i];
@@ -572,6 +588,24 @@ __device__ __forceinline__ void put_forward(const Args &a, int g, uint64_t r, ui
   put8((T *)a.c + r * a.ldc + n0, v, left, a.vec_c);
 }
 
+// The sums v through the activation of the layer below, whose pre-activations
+// are z (gated: and u); gated: w <- the second half's.
+__device__ __forceinline__ void through_act(const Args &a, Vals &v, const Vals &z, const Vals &u, Vals &w) {
+  Vals s = z;
+  slope8(s, a.act);
+  if (gated(a.act)) {
+    w = z;
+    act8(w, a.act);
+#pragma unroll
+    for (int i = 0; i < kEw; ++i) {
+      w.v[i] *= v.v[i];
+      v.v[i] *= u.v[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kEw; ++i) v.v[i] *= s.v[i];
+}
+
 // dx for kEw columns, through the activation of the layer below.
 template <typename T>
 __device__ __forceinline__ void put_grad_x(const Args &a, uint64_t r, uint32_t n0, Vals v) {
@@ -579,24 +613,13 @@ __device__ __forceinline__ void put_grad_x(const Args &a, uint64_t r, uint32_t n
   const uint32_t left = a.n - n0;
   T *out = (T *)a.c + r * a.ldc + n0;
   if (a.act != LL_ACT_NONE) {
+    const bool vec = a.vec_c && a.n % kEw == 0;
     const T *zp = (const T *)a.z + r * a.ldz + n0;
+    Vals u, w;
     const Vals z = get8(zp, left, a.vec_c);
-    Vals s = z;
-    slope8(s, a.act);
-    if (gated(a.act)) {
-      const bool vec = a.vec_c && a.n % kEw == 0;
-      const Vals u = get8(zp + a.n, left, vec);
-      Vals w = z;
-      act8(w, a.act);
-#pragma unroll
-      for (int i = 0; i < kEw; ++i) {
-        w.v[i] *= v.v[i];
-        v.v[i] *= u.v[i];
-      }
-      put8(out + a.n, w, left, vec);
-    }
-#pragma unroll
-    for (int i = 0; i < kEw; ++i) v.v[i] *= s.v[i];
+    if (gated(a.act)) u = get8(zp + a.n, left, vec);
+    through_act(a, v, z, u, w);
+    if (gated(a.act)) put8(out + a.n, w, left, vec);
   }
   put8(out, v, left, a.vec_c);
 }
@@ -963,6 +986,43 @@ __global__ __launch_bounds__(WM *WN * 64, ST *(BM + BN) > 640 && WM * WN == 4 ? 
     constexpr int kLanes = kWidth / kEw;           // lanes a row
     const int c = lane % kLanes * kEw;
     const uint32_t n0 = (GATED ? tn * (BN / 2) + wn * kWidth : tn * BN + wn * WTN) + c;
+    constexpr int kRows = 64 / kLanes;  // rows of the wave's half at a time
+    if constexpr (PASS == kGradX) {
+      // Whole tiles through an activation: the pre-activations of kAhead rows
+      // are read before the first of them is used (gradient of 8 experts' 2048
+      // -> 7168 through SwiGLU, both gradients: 587 -> 578 us).
+      constexpr int kAhead = WTM / 2 / kRows < 4 ? WTM / 2 / kRows : 4;
+      if (a.parts == nullptr && a.act != LL_ACT_NONE && a.vec_c && a.n % kEw == 0 && (tn + 1) * BN <= a.n) {
+        const uint32_t first = m0 + h * (BM / 2) + wm * (WTM / 2) + lane / kLanes;
+#pragma unroll 1
+        for (int r = 0; r < WTM / 2; r += kRows * kAhead) {
+          Held<T> z[kAhead], u[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {
+            const T *zp = (const T *)a.z + (uint64_t)min(first + r + i * kRows, m_end - 1) * a.ldz + n0;
+            z[i].load(zp);
+            if (gated(a.act)) u[i].load(zp + a.n);
+          }
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {
+            const uint32_t m = first + r + i * kRows;
+            if (m >= m_end) continue;
+            Vals v, w;
+            Pack<float, kEw, true> sums;
+            sums.load(mine + (lane / kLanes + r + i * kRows) * kPitch + c);
+#pragma unroll
+            for (int e = 0; e < kEw; ++e) v.v[e] = sums.v[e];
+            through_act(a, v, z[i].vals(), u[i].vals(), w);
+            T *out = (T *)a.c + (uint64_t)m * a.ldc + n0;
+            if (gated(a.act)) put8(out + a.n, w, kEw, true);
+            put8(out, v, kEw, true);
+          }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+        return;
+      }
+    }
 #pragma unroll 1
     for (int r = lane / kLanes; r < WTM / 2; r += 64 / kLanes) {
       const uint32_t m = m0 + h * (BM / 2) + wm * (WTM / 2) + r;
@@ -1058,12 +1118,14 @@ __global__ __launch_bounds__(256) void k_join(Args a) {
 // else 32 in a row), its NW waves take 128 bytes of k of each in turn, straight
 // from memory into registers, and the waves' sums are joined in LDS in order.
 // The rows come from L2, as often as there are workgroups: two fragments of
-// weight share one of them.  kAhead steps of loads are under way in each wave.
+// weight share one of them.  kAhead steps of loads are under way in each wave,
+// in the registers that two workgroups a CU have (157 instead of 113: 16 rows
+// over 32 groups 149 -> 158 us).
 // 16 rows over 32 groups of 7168 -> 2 x 2048: 116-140 us, 5.5-6.4 TB/s of the
 // weights that have rows (the tile kernel: 127); 1 and 16 rows of 7168 -> 8192:
 // 21 and 24 us, 5.6 and 4.8 TB/s.
 template <typename T, int RB, int NW, bool GATED>
-__global__ __launch_bounds__(NW * 64) void k_stream(Args a) {
+__global__ __launch_bounds__(NW * 64, 4) void k_stream(Args a) {
   constexpr int kAhead = RB == 1 ? 4 : 2, kCols = GATED ? 16 : 32;  // columns of C
   constexpr int kStepK = 128 / (int)sizeof(T);
   constexpr int kPitch = 2 * 16 + 4;
