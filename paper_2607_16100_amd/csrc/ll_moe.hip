@@ -70,9 +70,12 @@ route_fn route_fn_of(int npl, bool grad, bool vec) {
 }
 
 int launch_route(const RouteArgs &a, ll_dtype dt, bool grad, void *stream) {
-  // 16 lanes a token (four tokens a wave share the steps over the lanes)
-  // where a token's logits and choices fit them, else a whole wave
-  const int w = a.experts <= 256 && a.k <= 16 ? 16 : 64;
+  // Many tokens: 16 lanes a token where its logits and choices fit them, so
+  // that four tokens of a wave share the steps over the lanes (32301 x 160
+  // bfloat16: 8.5 us, with 64 lanes 19.3).  Few: a wave a token, whose lanes
+  // have fewer logits to go through one after the other (1 x 256: 3.5 us, with
+  // 16 lanes 6.5; 2048 x 256: 4.4 and 7.0; at 8192 x 256 they meet).
+  const int w = a.experts <= 256 && a.k <= 16 && a.tokens > 4096 ? 16 : 64;
   int npl = 16;
   for (int n : kNpl)
     if (n * w >= a.experts) {

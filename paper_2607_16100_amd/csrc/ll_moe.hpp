@@ -23,10 +23,9 @@ constexpr float kNegInf = -__builtin_inff();
 // best key, the maximum over the lanes, the lowest lane that has it.
 //
 // Bound by vector instructions, not by memory: 32301 tokens x 160 bfloat16
-// logits, 6 choices, take 9.6 us (1.1 TB/s); 16 lanes a token rather than 64
-// share the steps over the lanes among four tokens of a wave.  Its gradient,
-// which computes the exponentials again and nothing else, takes 7.8 us (2.7
-// TB/s).  One token takes 6.7 us, a chain of 8 rounds behind two loads.
+// logits, 6 choices, take 8.5 us (1.2 TB/s), and their gradient, which computes
+// the exponentials again and nothing else, 6.5 us (3.2 TB/s).  One token takes
+// 3.5 us, a chain of 8 rounds behind two loads.
 struct RouteArgs {
   const void *logits;
   uint64_t ld;
@@ -110,8 +109,8 @@ __device__ __forceinline__ int group_max_key(int v) {
   v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x141, 0xF, 0xF, false));
   v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x140, 0xF, 0xF, false));
   if constexpr (W == 64) {
-    v = max(v, __shfl_xor(v, 16));
-    v = max(v, __shfl_xor(v, 32));
+    v = max_halves<16>(v);
+    v = max_halves<32>(v);
   }
   return v;
 }

@@ -96,6 +96,35 @@ __device__ __forceinline__ float dpp_f32(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xF, 0xF, true));
 }
 
+// The partner's value for the steps over 16 and 32 lanes: the two results of a
+// lane swap with itself are the value of the even and of the odd half.
+typedef uint32_t u32pair __attribute__((ext_vector_type(2)));
+template <int kDist>
+__device__ __forceinline__ u32pair lane_halves(uint32_t v) {
+  if constexpr (kDist == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return u32pair{r[0], r[1]};
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return u32pair{r[0], r[1]};
+  }
+}
+template <int kDist>
+__device__ __forceinline__ float add_halves(float v) {
+  const u32pair r = lane_halves<kDist>((uint32_t)__float_as_int(v));
+  return __int_as_float((int)r[0]) + __int_as_float((int)r[1]);
+}
+template <int kDist>
+__device__ __forceinline__ float max_halves(float v) {
+  const u32pair r = lane_halves<kDist>((uint32_t)__float_as_int(v));
+  return fmaxf(__int_as_float((int)r[0]), __int_as_float((int)r[1]));
+}
+template <int kDist>
+__device__ __forceinline__ int max_halves(int v) {
+  const u32pair r = lane_halves<kDist>((uint32_t)v);
+  return max((int)r[0], (int)r[1]);
+}
+
 // Sum / maximum over each aligned group of W lanes (16 or 64); every lane gets
 // the same bits, since each step adds the same two partial results in both
 // lanes.  Within 16 lanes the partners come from the DPP controls xor 1, xor
@@ -107,8 +136,8 @@ __device__ __forceinline__ float group_sum(float v) {
   v += dpp_f32<0x141>(v);
   v += dpp_f32<0x140>(v);
   if constexpr (W == 64) {
-    v += __shfl_xor(v, 16);
-    v += __shfl_xor(v, 32);
+    v = add_halves<16>(v);
+    v = add_halves<32>(v);
   }
   return v;
 }
@@ -119,8 +148,8 @@ __device__ __forceinline__ float group_max(float v) {
   v = fmaxf(v, dpp_f32<0x141>(v));
   v = fmaxf(v, dpp_f32<0x140>(v));
   if constexpr (W == 64) {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    v = fmaxf(v, __shfl_xor(v, 32));
+    v = max_halves<16>(v);
+    v = max_halves<32>(v);
   }
   return v;
 }

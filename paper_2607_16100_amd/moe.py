@@ -27,6 +27,8 @@ from . import llcoll as ll
 from . import llmoe as lm
 
 _DT = {torch.float32: ll.LL_F32, torch.bfloat16: ll.LL_BF16}
+# the C functions themselves: llmoe's wrappers add a call and nothing else here
+_c = ll.library()
 _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
@@ -81,7 +83,7 @@ def route(logits, k: int, *, bias=None, score: str = "softmax", normalise: bool 
         ids = torch.empty(t, k, dtype=torch.int32, device=logits.device)
     if weights is None:
         weights = torch.empty(t, k, dtype=torch.float32, device=logits.device)
-    ll.check(lm.ll_moe_route(logits.data_ptr(), ld, t, e, k, _dt(logits),
+    ll.check(_c.ll_moe_route(logits.data_ptr(), ld, t, e, k, _dt(logits),
                              None if bias is None else _flat(bias, "bias", e, torch.float32), lm.SCORES[score],
                              int(normalise), scale, _flat(ids, "ids", t * k, torch.int32),
                              _flat(weights, "weights", t * k, torch.float32), _stream(stream)), "ll_moe_route")
@@ -97,7 +99,7 @@ def route_grad(logits, ids, dweights, *, score: str = "softmax", normalise: bool
     if out is None:
         out = torch.empty(t, e, dtype=logits.dtype, device=logits.device)
     ldd = _mat(out, "out", t, e, logits.dtype)
-    ll.check(lm.ll_moe_route_grad(logits.data_ptr(), ld, t, e, k, _dt(logits), lm.SCORES[score], int(normalise),
+    ll.check(_c.ll_moe_route_grad(logits.data_ptr(), ld, t, e, k, _dt(logits), lm.SCORES[score], int(normalise),
                                   scale, _flat(ids, "ids", t * k, torch.int32),
                                   _flat(dweights, "dweights", t * k, torch.float32), out.data_ptr(), ldd,
                                   _stream(stream)), "ll_moe_route_grad")
@@ -143,7 +145,7 @@ class Dispatch:
         if x is not None:
             ldx = _mat(x, "x", t, self.features, self._x.dtype)
             xp = x.data_ptr()
-        ll.check(lm.ll_moe_dispatch(_flat(ids, "ids", t * self.k, torch.int32), t, self.k, self.first, self.experts,
+        ll.check(_c.ll_moe_dispatch(_flat(ids, "ids", t * self.k, torch.int32), t, self.k, self.first, self.experts,
                                     xp, ldx, self.features, _DT[self._x.dtype], self.offsets.data_ptr(),
                                     self._slots.data_ptr(), self._rows.data_ptr(), self._x.data_ptr() if xp else 0,
                                     self.features, self._work.data_ptr(), self._work.numel(), _stream(stream)),
@@ -166,7 +168,7 @@ def combine(y, rows, weights=None, *, residual=None, out=None, stream=None):
     rp = ldr = 0
     if residual is not None:
         ldr, rp = _mat(residual, "residual", t, h, y.dtype), residual.data_ptr()
-    ll.check(lm.ll_moe_combine(y.data_ptr(), ldy, n, _flat(rows, "rows", t * k, torch.int32),
+    ll.check(_c.ll_moe_combine(y.data_ptr(), ldy, n, _flat(rows, "rows", t * k, torch.int32),
                                None if weights is None else _flat(weights, "weights", t * k, torch.float32), rp, ldr,
                                t, k, h, _dt(y), out.data_ptr(), ldo, _stream(stream)), "ll_moe_combine")
     return out
@@ -190,7 +192,7 @@ def combine_grad(dout, y, rows, weights=None, *, dy=None, dweights=None, stream=
         if dweights is None:
             dweights = torch.empty(t, k, dtype=torch.float32, device=y.device)
         wg = _flat(dweights, "dweights", t * k, torch.float32)
-    ll.check(lm.ll_moe_combine_grad(dout.data_ptr(), ldd, y.data_ptr(), ldy, n,
+    ll.check(_c.ll_moe_combine_grad(dout.data_ptr(), ldd, y.data_ptr(), ldy, n,
                                     _flat(rows, "rows", t * k, torch.int32), wp, t, k, h, _dt(y), dy.data_ptr(), lddy,
                                     wg, _stream(stream)), "ll_moe_combine_grad")
     return dy, dweights
@@ -262,7 +264,7 @@ def linear(x, w, *, bias=None, act: str = "none", residual=None, offsets=None, o
         ldz, zp = _mat(z, "z", n, o, x.dtype), z.data_ptr()
     d, wp, wn, _ws = _plan(lm.LL_LINEAR_FORWARD, x.device, _dt(x), lm.ACTS[act], g, n, i, o, _offsets(offsets, g), ldx,
                            ldw, gs, ldy, ldz, ldr)
-    ll.check(lm.ll_linear(d, x.data_ptr(), w.data_ptr(),
+    ll.check(_c.ll_linear(d, x.data_ptr(), w.data_ptr(),
                           None if bias is None else _flat(bias, "bias", g * o, x.dtype), rp, out.data_ptr(), zp, wp,
                           wn, _stream(stream)), "ll_linear")
     return out
@@ -285,7 +287,7 @@ def linear_grad_x(dz, w, *, act: str = "none", z=None, offsets=None, out=None, s
         ldz, zp = _mat(z, "z", n, width, dz.dtype), z.data_ptr()
     d, wp, wn, _ws = _plan(lm.LL_LINEAR_GRAD_X, dz.device, _dt(dz), lm.ACTS[act], g, n, i, o, _offsets(offsets, g), ldx,
                            ldw, gs, ldy, ldz)
-    ll.check(lm.ll_linear_grad_x(d, dz.data_ptr(), w.data_ptr(), zp, out.data_ptr(), wp, wn, _stream(stream)),
+    ll.check(_c.ll_linear_grad_x(d, dz.data_ptr(), w.data_ptr(), zp, out.data_ptr(), wp, wn, _stream(stream)),
              "ll_linear_grad_x")
     return out
 
@@ -310,7 +312,7 @@ def linear_grad_w(dz, x, *, offsets=None, out=None, bias_out=None, add: bool = F
     bp = None if bias_out is None else _flat(bias_out, "bias_out", g * o, out.dtype)
     d, wp, wn, _ws = _plan(lm.LL_LINEAR_GRAD_W, dz.device, _dt(dz), lm.LL_ACT_NONE, g, n, i, o, _offsets(offsets, g),
                            ldx, ldw, gs, ldy)
-    ll.check(lm.ll_linear_grad_w(d, dz.data_ptr(), x.data_ptr(), out.data_ptr(), bp, flags, wp, wn, _stream(stream)),
+    ll.check(_c.ll_linear_grad_w(d, dz.data_ptr(), x.data_ptr(), out.data_ptr(), bp, flags, wp, wn, _stream(stream)),
              "ll_linear_grad_w")
     return out, bias_out
 
@@ -324,6 +326,6 @@ def act_grad(dy, z, act: str, *, out=None, stream=None):
     if out is None:
         out = torch.empty(n, width, dtype=dy.dtype, device=dy.device)
     ldo = _mat(out, "out", n, width, dy.dtype)
-    ll.check(lm.ll_act_grad(dy.data_ptr(), ldy, z.data_ptr(), ldz, n, h, _dt(dy), lm.ACTS[act], out.data_ptr(), ldo,
+    ll.check(_c.ll_act_grad(dy.data_ptr(), ldy, z.data_ptr(), ldz, n, h, _dt(dy), lm.ACTS[act], out.data_ptr(), ldo,
                             _stream(stream)), "ll_act_grad")
     return out
