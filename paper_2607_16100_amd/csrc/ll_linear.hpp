@@ -766,7 +766,9 @@ __global__ __launch_bounds__(WM *WN * 64, ST *(BM + BN) > 640 && WM * WN == 4 ? 
       lq.template issue<decltype(whole)::value>(at_q + into * kStage, n - lp.kChunks, have);
   };
   // first entry of the wave's fragment i of P
-  auto dim_p = [&](int i) __attribute__((always_inline)) { return (i < FH ? 0 : BM / 2) + wm * (WTM / 2) + (i % FH) * 16; };
+  auto dim_p = [&](int i) __attribute__((always_inline)) {
+    return (i < FH ? 0 : BM / 2) + wm * (WTM / 2) + (i % FH) * 16;
+  };
   // Where the fragments lie in a stage, by half of its k (RM: a constant
   // apart).  Those of P's lower half lie a constant further on where the
   // swizzle does not reach that bit of the entry.
@@ -870,96 +872,96 @@ __global__ __launch_bounds__(WM *WN * 64, ST *(BM + BN) > 640 && WM * WN == 4 ? 
         if (++s >= steps) break;
       }
     } else {
-    frag fq[2][FN], fu[2][FH], fl[2][FH];  // by half of k: Q, P's upper rows, P's lower rows
+      frag fq[2][FN], fu[2][FH], fl[2][FH];  // by half of k: Q, P's upper rows, P's lower rows
 #pragma unroll
-    for (int j = 0; j < FN; ++j) fq[0][j] = read_frag<T, BN, kQkm>(lds + off_q[0][j]);
+      for (int j = 0; j < FN; ++j) fq[0][j] = read_frag<T, BN, kQkm>(lds + off_q[0][j]);
 #pragma unroll
-    for (int i = 0; i < FH; ++i) fu[0][i] = read_frag<T, BM, kPkm>(lds + off_p[0][i]);
+      for (int i = 0; i < FH; ++i) fu[0][i] = read_frag<T, BM, kPkm>(lds + off_p[0][i]);
 
-    // The matrix instruction t of a cluster (none past the last).
-    auto multiply = [&](int t, int ks, bool low) __attribute__((always_inline)) {
-      if (t >= FN * FH) return;
-      const int j = t / FH, i = t % FH;
-      if (low)
-        acc[j][FH + i] = mma(fq[ks][j], fl[ks][i], acc[j][FH + i]);
-      else
-        acc[j][i] = mma(fq[ks][j], fu[ks][i], acc[j][i]);
-    };
-    // One stage from LDS buffer b.  WHOLE: the stage loaded meanwhile has BK k,
-    // else `have` of them (none: zeros are written).  next_has: k of the next one.
-    auto stage = [&](int b, auto lower_c, auto whole, int have, int next_has) __attribute__((always_inline)) {
-      constexpr bool kLower = decltype(lower_c)::value;
-      constexpr int kMmas = FN * FH, kMmasL = kLower ? kMmas : 0;
-      const char *here = lds + b * kStage, *next = lds + (b + 1) % ST * kStage;
+      // The matrix instruction t of a cluster (none past the last).
+      auto multiply = [&](int t, int ks, bool low) __attribute__((always_inline)) {
+        if (t >= FN * FH) return;
+        const int j = t / FH, i = t % FH;
+        if (low)
+          acc[j][FH + i] = mma(fq[ks][j], fl[ks][i], acc[j][FH + i]);
+        else
+          acc[j][i] = mma(fq[ks][j], fu[ks][i], acc[j][i]);
+      };
+      // One stage from LDS buffer b.  WHOLE: the stage loaded meanwhile has BK k,
+      // else `have` of them (none: zeros are written).  next_has: k of the next one.
+      auto stage = [&](int b, auto lower_c, auto whole, int have, int next_has) __attribute__((always_inline)) {
+        constexpr bool kLower = decltype(lower_c)::value;
+        constexpr int kMmas = FN * FH, kMmasL = kLower ? kMmas : 0;
+        const char *here = lds + b * kStage, *next = lds + (b + 1) % ST * kStage;
 #pragma unroll
-      for (int t = 0; t < kMmas; ++t) {
-        if (kLower && t < FH) fl[0][t < FH ? t : 0] = read_frag<T, BM, kPkm>(here + off_p[0][FH + (t < FH ? t : 0)]);
-        multiply(t, 0, false);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+        for (int t = 0; t < kMmas; ++t) {
+          if (kLower && t < FH) fl[0][t < FH ? t : 0] = read_frag<T, BM, kPkm>(here + off_p[0][FH + (t < FH ? t : 0)]);
+          multiply(t, 0, false);
+          __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-      for (int t = 0; t < FN + FH || t < kMmasL; ++t) {
-        if (t < FN)
-          fq[1][t < FN ? t : 0] = read_frag<T, BN, kQkm>(here + off_q[1][t < FN ? t : 0]);
-        else if (t < FN + FH)
-          fu[1][t - FN] = read_frag<T, BM, kPkm>(here + off_p[1][t - FN]);
-        if (kLower) multiply(t, 0, true);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+        for (int t = 0; t < FN + FH || t < kMmasL; ++t) {
+          if (t < FN)
+            fq[1][t < FN ? t : 0] = read_frag<T, BN, kQkm>(here + off_q[1][t < FN ? t : 0]);
+          else if (t < FN + FH)
+            fu[1][t - FN] = read_frag<T, BM, kPkm>(here + off_p[1][t - FN]);
+          if (kLower) multiply(t, 0, true);
+          __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-      for (int t = 0; t < kMmas; ++t) {
-        if (kLower && t < FH) fl[1][t < FH ? t : 0] = read_frag<T, BM, kPkm>(here + off_p[1][FH + (t < FH ? t : 0)]);
-        multiply(t, 1, false);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if constexpr (!VEC) {
-        // the next stage's chunks, fetched a stage ago
-        lp.commit(const_cast<char *>(next));
-        lq.commit(const_cast<char *>(next) + BM * 128);
-      }
-      wait_loads<VEC ? (ST - 2) * kLoads : 0>();
-      if (ROWS == kDwordRows && next_has < BK) {
-        lp.clear_tail(const_cast<char *>(next), next_has);
-        lq.clear_tail(const_cast<char *>(next) + BM * 128, next_has);
-      }
-      lds_barrier();
-      if constexpr (!VEC) {
-        lp.fetch(have);
-        lq.fetch(have);
-      }
-      constexpr int kReads = FN + FH, kAux = VEC && kLoads > kReads ? kLoads : kReads;
+        for (int t = 0; t < kMmas; ++t) {
+          if (kLower && t < FH) fl[1][t < FH ? t : 0] = read_frag<T, BM, kPkm>(here + off_p[1][FH + (t < FH ? t : 0)]);
+          multiply(t, 1, false);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (!VEC) {
+          // the next stage's chunks, fetched a stage ago
+          lp.commit(const_cast<char *>(next));
+          lq.commit(const_cast<char *>(next) + BM * 128);
+        }
+        wait_loads<VEC ? (ST - 2) * kLoads : 0>();
+        if (ROWS == kDwordRows && next_has < BK) {
+          lp.clear_tail(const_cast<char *>(next), next_has);
+          lq.clear_tail(const_cast<char *>(next) + BM * 128, next_has);
+        }
+        lds_barrier();
+        if constexpr (!VEC) {
+          lp.fetch(have);
+          lq.fetch(have);
+        }
+        constexpr int kReads = FN + FH, kAux = VEC && kLoads > kReads ? kLoads : kReads;
 #pragma unroll
-      for (int t = 0; t < kAux || t < kMmasL; ++t) {
-        if (VEC && t < kLoads) issue(b, t, whole, have > 0 ? have : 0);
-        if (t < FN)
-          fq[0][t < FN ? t : 0] = read_frag<T, BN, kQkm>(next + off_q[0][t < FN ? t : 0]);
-        else if (t < kReads)
-          fu[0][t - FN] = read_frag<T, BM, kPkm>(next + off_p[0][t - FN]);
-        if (kLower) multiply(t, 1, true);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      lp.advance();
-      lq.advance();
-    };
-    auto all = [&](auto lower_c) __attribute__((always_inline)) {
-      uint32_t s = 0;
-      if constexpr (VEC) {  // ST stages at a time: LDS addresses are constants
-        for (; (s + 2 * ST) * BK <= k; s += ST) {
-          stage(0, lower_c, std::true_type{}, BK, BK);
-          stage(1, lower_c, std::true_type{}, BK, BK);
-          if constexpr (ST > 2) {
-            stage(2, lower_c, std::true_type{}, BK, BK);
-            stage(3, lower_c, std::true_type{}, BK, BK);
+        for (int t = 0; t < kAux || t < kMmasL; ++t) {
+          if (VEC && t < kLoads) issue(b, t, whole, have > 0 ? have : 0);
+          if (t < FN)
+            fq[0][t < FN ? t : 0] = read_frag<T, BN, kQkm>(next + off_q[0][t < FN ? t : 0]);
+          else if (t < kReads)
+            fu[0][t - FN] = read_frag<T, BM, kPkm>(next + off_p[0][t - FN]);
+          if (kLower) multiply(t, 1, true);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        lp.advance();
+        lq.advance();
+      };
+      auto all = [&](auto lower_c) __attribute__((always_inline)) {
+        uint32_t s = 0;
+        if constexpr (VEC) {  // ST stages at a time: LDS addresses are constants
+          for (; (s + 2 * ST) * BK <= k; s += ST) {
+            stage(0, lower_c, std::true_type{}, BK, BK);
+            stage(1, lower_c, std::true_type{}, BK, BK);
+            if constexpr (ST > 2) {
+              stage(2, lower_c, std::true_type{}, BK, BK);
+              stage(3, lower_c, std::true_type{}, BK, BK);
+            }
           }
         }
-      }
-      for (; s < steps; ++s)
-        stage(s % ST, lower_c, std::false_type{}, (int)k - (int)(s + ST) * BK, (int)k - (int)(s + 1) * BK);
-    };
-    if (PASS == kGradW || lower)
-      all(std::true_type{});
-    else
-      all(std::false_type{});
+        for (; s < steps; ++s)
+          stage(s % ST, lower_c, std::false_type{}, (int)k - (int)(s + ST) * BK, (int)k - (int)(s + 1) * BK);
+      };
+      if (PASS == kGradW || lower)
+        all(std::true_type{});
+      else
+        all(std::false_type{});
     }
   }
   wait_loads<0>();

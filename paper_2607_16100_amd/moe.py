@@ -38,6 +38,15 @@ def _stream(stream) -> int:
     return _raw_stream(_device())
 
 
+def _new(stream, *shape, dtype, device, make=torch.empty) -> torch.Tensor:
+    """Memory of the stream the call runs on: it may be reused there as soon as
+    it is released, and nowhere else."""
+    if stream is None:
+        return make(*shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return make(*shape, dtype=dtype, device=device)
+
+
 def _dt(t: torch.Tensor) -> int:
     dt = _DT.get(t.dtype)
     if dt is None:
@@ -80,9 +89,9 @@ def route(logits, k: int, *, bias=None, score: str = "softmax", normalise: bool 
     ld = _mat(logits, "logits")
     t, e = logits.shape
     if ids is None:
-        ids = torch.empty(t, k, dtype=torch.int32, device=logits.device)
+        ids = _new(stream, t, k, dtype=torch.int32, device=logits.device)
     if weights is None:
-        weights = torch.empty(t, k, dtype=torch.float32, device=logits.device)
+        weights = _new(stream, t, k, dtype=torch.float32, device=logits.device)
     ll.check(_c.ll_moe_route(logits.data_ptr(), ld, t, e, k, _dt(logits),
                              None if bias is None else _flat(bias, "bias", e, torch.float32), lm.SCORES[score],
                              int(normalise), scale, _flat(ids, "ids", t * k, torch.int32),
@@ -97,7 +106,7 @@ def route_grad(logits, ids, dweights, *, score: str = "softmax", normalise: bool
     t, e = logits.shape
     k = ids.shape[-1]
     if out is None:
-        out = torch.empty(t, e, dtype=logits.dtype, device=logits.device)
+        out = _new(stream, t, e, dtype=logits.dtype, device=logits.device)
     ldd = _mat(out, "out", t, e, logits.dtype)
     ll.check(_c.ll_moe_route_grad(logits.data_ptr(), ld, t, e, k, _dt(logits), lm.SCORES[score], int(normalise),
                                   scale, _flat(ids, "ids", t * k, torch.int32),
@@ -163,7 +172,7 @@ def combine(y, rows, weights=None, *, residual=None, out=None, stream=None):
     n, h = y.shape
     t, k = rows.shape
     if out is None:
-        out = torch.empty(t, h, dtype=y.dtype, device=y.device)
+        out = _new(stream, t, h, dtype=y.dtype, device=y.device)
     ldo = _mat(out, "out", t, h, y.dtype)
     rp = ldr = 0
     if residual is not None:
@@ -184,13 +193,13 @@ def combine_grad(dout, y, rows, weights=None, *, dy=None, dweights=None, stream=
     if dout.shape[0] != t:
         raise ValueError(f"dout: {dout.shape[0]} rows, expected {t}")
     if dy is None:
-        dy = torch.zeros(n, h, dtype=y.dtype, device=y.device)
+        dy = _new(stream, n, h, dtype=y.dtype, device=y.device, make=torch.zeros)
     lddy = _mat(dy, "dy", n, h, y.dtype)
     wp = wg = None
     if weights is not None:
         wp = _flat(weights, "weights", t * k, torch.float32)
         if dweights is None:
-            dweights = torch.empty(t, k, dtype=torch.float32, device=y.device)
+            dweights = _new(stream, t, k, dtype=torch.float32, device=y.device)
         wg = _flat(dweights, "dweights", t * k, torch.float32)
     ll.check(_c.ll_moe_combine_grad(dout.data_ptr(), ldd, y.data_ptr(), ldy, n,
                                     _flat(rows, "rows", t * k, torch.int32), wp, t, k, h, _dt(y), dy.data_ptr(), lddy,
@@ -228,7 +237,7 @@ def _offsets(offsets, groups: int):
 _needs: dict = {}  # workspace bytes by shape (host arithmetic only)
 
 
-def _plan(which: int, device, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz=0, ldr=0):
+def _plan(which: int, stream, device, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz=0, ldr=0):
     """(descriptor, workspace address, its bytes, the workspace)."""
     d = lm.LLLinearDesc(lm.DESC_SIZE, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz, ldr)
     # what a plan depends on: the shape, whether there are offsets, and how rows are aligned
@@ -242,7 +251,7 @@ def _plan(which: int, device, dt, act, groups, rows, in_, out, offsets, ldx, ldw
         _needs[key] = need
     if not need:
         return d, None, 0, None
-    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    ws = _new(stream, need, dtype=torch.uint8, device=device)
     return d, ws.data_ptr(), need, ws
 
 
@@ -254,7 +263,7 @@ def linear(x, w, *, bias=None, act: str = "none", residual=None, offsets=None, o
     ldx = _mat(x, "x", n, i, w.dtype)
     width = o // 2 if act in lm.GATED else o
     if out is None:
-        out = torch.empty(n, width, dtype=x.dtype, device=x.device)
+        out = _new(stream, n, width, dtype=x.dtype, device=x.device)
     ldy = _mat(out, "out", n, width, x.dtype)
     ldr = ldz = max(o, 1)
     rp = zp = None
@@ -262,8 +271,8 @@ def linear(x, w, *, bias=None, act: str = "none", residual=None, offsets=None, o
         ldr, rp = _mat(residual, "residual", n, width, x.dtype), residual.data_ptr()
     if z is not None:
         ldz, zp = _mat(z, "z", n, o, x.dtype), z.data_ptr()
-    d, wp, wn, _ws = _plan(lm.LL_LINEAR_FORWARD, x.device, _dt(x), lm.ACTS[act], g, n, i, o, _offsets(offsets, g), ldx,
-                           ldw, gs, ldy, ldz, ldr)
+    d, wp, wn, _ws = _plan(lm.LL_LINEAR_FORWARD, stream, x.device, _dt(x), lm.ACTS[act], g, n, i, o,
+                           _offsets(offsets, g), ldx, ldw, gs, ldy, ldz, ldr)
     ll.check(_c.ll_linear(d, x.data_ptr(), w.data_ptr(),
                           None if bias is None else _flat(bias, "bias", g * o, x.dtype), rp, out.data_ptr(), zp, wp,
                           wn, _stream(stream)), "ll_linear")
@@ -278,15 +287,15 @@ def linear_grad_x(dz, w, *, act: str = "none", z=None, offsets=None, out=None, s
     ldy = _mat(dz, "dz", n, o, w.dtype)
     width = 2 * i if act in lm.GATED else i
     if out is None:
-        out = torch.empty(n, width, dtype=dz.dtype, device=dz.device)
+        out = _new(stream, n, width, dtype=dz.dtype, device=dz.device)
     ldx = _mat(out, "out", n, width, dz.dtype)
     ldz, zp = width, None
     if act != "none":
         if z is None:
             raise ValueError("z is needed to go through an activation")
         ldz, zp = _mat(z, "z", n, width, dz.dtype), z.data_ptr()
-    d, wp, wn, _ws = _plan(lm.LL_LINEAR_GRAD_X, dz.device, _dt(dz), lm.ACTS[act], g, n, i, o, _offsets(offsets, g), ldx,
-                           ldw, gs, ldy, ldz)
+    d, wp, wn, _ws = _plan(lm.LL_LINEAR_GRAD_X, stream, dz.device, _dt(dz), lm.ACTS[act], g, n, i, o,
+                           _offsets(offsets, g), ldx, ldw, gs, ldy, ldz)
     ll.check(_c.ll_linear_grad_x(d, dz.data_ptr(), w.data_ptr(), zp, out.data_ptr(), wp, wn, _stream(stream)),
              "ll_linear_grad_x")
     return out
@@ -303,15 +312,14 @@ def linear_grad_w(dz, x, *, offsets=None, out=None, bias_out=None, add: bool = F
     groups = 1 if offsets is None else offsets.numel() - 1
     if out is None:
         shape = (o, i) if offsets is None else (groups, o, i)
-        out = torch.zeros(shape, dtype=dz.dtype, device=dz.device) if add else torch.empty(
-            shape, dtype=dz.dtype, device=dz.device)
+        out = _new(stream, *shape, dtype=dz.dtype, device=dz.device, make=torch.zeros if add else torch.empty)
     g, o2, i2, ldw, gs = _weight(out, offsets, "out")
     if (g, o2, i2) != (groups, o, i) or out.dtype not in (dz.dtype, torch.float32):
         raise ValueError(f"out: {tuple(out.shape)} {out.dtype}, expected ({groups}, {o}, {i})")
     flags = (lm.LL_GRAD_F32 if out.dtype == torch.float32 else 0) | (lm.LL_GRAD_ADD if add else 0)
     bp = None if bias_out is None else _flat(bias_out, "bias_out", g * o, out.dtype)
-    d, wp, wn, _ws = _plan(lm.LL_LINEAR_GRAD_W, dz.device, _dt(dz), lm.LL_ACT_NONE, g, n, i, o, _offsets(offsets, g),
-                           ldx, ldw, gs, ldy)
+    d, wp, wn, _ws = _plan(lm.LL_LINEAR_GRAD_W, stream, dz.device, _dt(dz), lm.LL_ACT_NONE, g, n, i, o,
+                           _offsets(offsets, g), ldx, ldw, gs, ldy)
     ll.check(_c.ll_linear_grad_w(d, dz.data_ptr(), x.data_ptr(), out.data_ptr(), bp, flags, wp, wn, _stream(stream)),
              "ll_linear_grad_w")
     return out, bias_out
@@ -324,7 +332,7 @@ def act_grad(dy, z, act: str, *, out=None, stream=None):
     width = 2 * h if act in lm.GATED else h
     ldz = _mat(z, "z", n, width, dy.dtype)
     if out is None:
-        out = torch.empty(n, width, dtype=dy.dtype, device=dy.device)
+        out = _new(stream, n, width, dtype=dy.dtype, device=dy.device)
     ldo = _mat(out, "out", n, width, dy.dtype)
     ll.check(_c.ll_act_grad(dy.data_ptr(), ldy, z.data_ptr(), ldz, n, h, _dt(dy), lm.ACTS[act], out.data_ptr(), ldo,
                             _stream(stream)), "ll_act_grad")

@@ -351,6 +351,23 @@ def test_on_another_stream_and_in_a_graph():
         assert torch.equal(got, y)
 
 
+def test_memory_of_a_call_belongs_to_its_stream():
+    """Split sums and outputs made for a call on another stream are not handed
+    to the current stream's tensors while that call runs."""
+    g = gen(23)
+    x, w = randn(g, 48, 8192, dtype=BF16), randn(g, 192, 8192, dtype=BF16)
+    want = moe.linear(x, w)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    outs = []
+    for _ in range(30):
+        outs.append(moe.linear(x, w, stream=side))
+        for n in (48 * 192 * 4 * 16, 48 * 192 * 4 * 8, 48 * 192 * 2):
+            torch.empty(n, dtype=torch.uint8, device=DEV).fill_(0xFF)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+
+
 def test_refusals():
     x = torch.zeros(4, 8, device=DEV)
     w = torch.zeros(2, 6, 8, device=DEV)
