@@ -143,7 +143,7 @@ __device__ __forceinline__ uint32_t scan_tiles(const Args &a, int g0, uint32_t b
 // A round is what the chip's 256 CUs work on at a time, one 256-wide tile each.
 // A last round of at most kMaxTail tiles takes as long as a whole one, so the
 // launch leaves it out and another runs it in 128-wide quarters (grad_x of 8
-// groups of about 1024 rows, 7168 -> 2048, 288 tiles: 400 -> 305-330 us).
+// groups of about 1024 rows, 7168 -> 2048, 288 tiles: 400 -> 300-315 us).
 constexpr uint32_t kRound = 256, kMaxTail = 128;
 
 __device__ __forceinline__ uint32_t tail_tiles(uint32_t total) {
@@ -1123,7 +1123,7 @@ __global__ __launch_bounds__(256) void k_join(Args a) {
 // weight share one of them.  kAhead steps of loads are under way in each wave,
 // in the registers that two workgroups a CU have (157 instead of 113: 16 rows
 // over 32 groups 149 -> 158 us).
-// 16 rows over 32 groups of 7168 -> 2 x 2048: 116-140 us, 5.5-6.4 TB/s of the
+// 16 rows over 32 groups of 7168 -> 2 x 2048: 116-150 us, 5.0-6.5 TB/s of the
 // weights that have rows (the tile kernel: 127); 1 and 16 rows of 7168 -> 8192:
 // 21 and 24 us, 5.6 and 4.8 TB/s.
 template <typename T, int RB, int NW, bool GATED>
