@@ -122,17 +122,61 @@ constexpr uint64_t kMaxParts = 256 << 20;  // bytes of split sums
 //   weight gradient of 301 rows, 1024 x 8192  22 / 17.7, 24 / 23, 27  512 of 128
 // 256 is for bfloat16 only: binary32 is bound by its matrix instructions, which
 // are 16 times slower (1024^3: 68 us with 128, 28 us with 64).
-Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows) {
+//
+// Up to 128 tiles of 128, and a long sum: s = 256 / tiles splits of them fill
+// the chip in one round and read a quarter to a half of the operands that tiles
+// of 64 do, for the cost of the joining.  us with 64-wide tiles / these:
+//   bfloat16  640 x 2048 -> 2048  23.3 / 24.4   8192 -> 2048  67.8 / 45.6  3 splits
+//             512 x 2048 -> 4096  26.7 / 28.8   8192 -> 4096  79.3 / 63.0  2 splits
+//             weight gradient of 2300 rows, 1024 x 1024  18.7 / 24.9, of 8192 rows  51.5 / 39.5  4 splits
+//             512 x 3584 -> 1024  20.8 / 23.1   8192 -> 1024  33.2 / 30.5  8 splits
+//   binary32  640 x 1024 -> 2048  43.6 / 38.4   4096 -> 2048   148 / 99.7  3 splits
+//             512 x 1024 -> 4096  44.3 / 49.3   4096 -> 4096   154 / 137   2 splits
+// The lines through these times decide.  Returns the splits, or 0 where tiles of
+// 64 are faster or `room` bytes do not hold the parts.  Groups of less
+// than a tile of rows on average keep tiles of 64, since the larger ones are
+// fewer than expected (8 groups of 100, 4096 -> 1024: 37 us, split 47), and so
+// does a weight gradient with a bias, which tiles of 64 sum along (8192 rows,
+// 1024 x 1024: 50 us, split and summed apart 72).
+uint32_t wide_splits(const Args &a, ll_dtype dt, uint64_t steps, uint64_t t128, uint64_t t64, uint64_t room) {
+  if (t128 < 32 || t128 > kFill / 2 || (dt == LL_F32 && t64 <= kFill)) return 0;
+  const uint64_t s = kFill / t128;
+  if (s * a.rows_c * a.part_row * 4 > std::min(room, kMaxParts)) return 0;
+  const double n = (double)steps;
+  double narrow, wide;
+  if (dt == LL_F32) {
+    narrow = 8. + 1.1 * n;
+    wide = 18. + 1.87 * n / s;
+  } else {
+    narrow = t64 < 200 ? 12. + .0013 * t64 * n : 7. + (t64 <= kFill ? .34 : .51) * n;
+    wide = 18. + .66 * n / s;
+  }
+  return wide < narrow ? (uint32_t)s : 0;
+}
+
+Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
   Plan p{64, 2, 1};
   const uint32_t bk = 128 / esize(dt);
   const uint64_t k = pass == kGradW ? a.k / a.groups : a.k, steps = (k + bk - 1) / bk;
   const uint64_t t128 = expect_tiles(pass, a, 128), t64 = expect_tiles(pass, a, 64);
+  // tiles of 128 are about a quarter of those of 64, and may replace them
+  const bool full = rows != kAnyRows && (pass == kGradW ? a.dbias == nullptr : a.rows / a.groups >= 128);
   if (rows != kAnyRows && dt == LL_BF16 && expect_tiles(pass, a, 256) >= kFill) {
     p.tile = 256;
   } else if (t128 >= (dt == LL_BF16 ? kFill : 4 * kFill)) {
     p.tile = 128;
     // one workgroup a CU: four stages of it hide what two workgroups hide from each other
     if (t128 <= kFill * 9 / 8 && steps >= 12) p.stages = 4;
+  } else if (const uint32_t s = full ? wide_splits(a, dt, steps, t128, t64, room) : 0) {
+    p.tile = 128;
+    p.stages = dt == LL_BF16 ? 4 : 2;
+    p.splits = s;
+  } else if (full && dt == LL_BF16 && t128 > 160 && steps >= 24) {
+    // a round of 128 that is not quite full, and a sum long enough to pay for
+    // its start (184 tiles: 1000 x 1024 -> 2944 19.4 us with 64, 19.8 with 128;
+    // 2048 -> 2944 32.6 and 30.4; 8192 -> 2944 101 and 86)
+    p.tile = 128;
+    p.stages = 4;
   } else {
     if (t64 <= 2 * kFill) p.stages = 4;
     // Too few tiles: the sum is cut into shares of four stages or more.  s
@@ -234,8 +278,8 @@ void launch_bias_grad(const Args &a, ll_dtype dt, void *stream) {
 template <Pass PASS>
 int launch_product(Args &a, ll_dtype dt, bool gate, Rows rows, void *workspace, size_t workspace_bytes, void *stream) {
   const uint64_t one = size_parts(a, gate);
-  Plan p = plan_of(PASS, a, dt, rows);
   if (workspace == nullptr) workspace_bytes = 0;
+  Plan p = plan_of(PASS, a, dt, rows, workspace_bytes);
   if (p.splits * one > workspace_bytes) p.splits = one == 0 ? 1 : (uint32_t)std::max<uint64_t>(1, workspace_bytes / one);
   a.splits = p.splits;
   a.parts = p.splits > 1 ? (float *)workspace : nullptr;
@@ -316,7 +360,7 @@ int ll_linear_bytes(const ll_linear_desc *d, ll_linear_pass pass, size_t *bytes)
   if (pass == LL_LINEAR_FORWARD && stream_blocks(a, whole ? kChunkRows : kDwordRows) != 0) return LL_OK;
   const uint64_t one = size_parts(a, pass == LL_LINEAR_FORWARD && gated((int)d->act));
   uint32_t splits = 1;
-  for (const Rows rows : {kAnyRows, kChunkRows}) splits = std::max(splits, plan_of((Pass)pass, a, d->dt, rows).splits);
+  for (const Rows rows : {kAnyRows, kChunkRows}) splits = std::max(splits, plan_of((Pass)pass, a, d->dt, rows, ~0ull).splits);
   *bytes = splits > 1 ? (size_t)splits * one : 0;
   return LL_OK;
 }

@@ -212,6 +212,22 @@ def test_large(what, dtype, counts, i, o, act):
             ref.close(db[gi], d.sum(0), (hi - lo + 2) * ref.EPS * d.abs().sum(0), dtype)
 
 
+# Long sums of 32 to 128 tiles of 128, which run split, and of a round of them
+# that is not quite full, which do not.
+WIDE = [
+    ("forward", BF16, 640, 4104, 2048), ("forward", BF16, [300, 0, 341], 5002, 2046),
+    ("grad_x", BF16, 500, 1030, 8192), ("grad_w", BF16, 8193, 1024, 1024), ("grad_w", BF16, 8200, 518, 1030),
+    ("forward", F32, 640, 2050, 2048), ("grad_x", F32, 1000, 1030, 2048), ("grad_w", F32, 2500, 1033, 1100),
+    ("forward", BF16, 1000, 2052, 2944), ("grad_x", BF16, 999, 2944, 2050),
+]
+
+
+@pytest.mark.parametrize("what,dtype,counts,i,o", WIDE)
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+def test_long_sums(what, dtype, counts, i, o, act):
+    test_large(what, dtype, counts, i, o, act)
+
+
 @pytest.mark.parametrize("act", ["relu", "gelu", "silu", "swiglu", "geglu"])
 @pytest.mark.parametrize("dtype,h,pad", [(F32, 33, 0), (BF16, 64, 8), (F32, 8, 1)])
 def test_act_grad(act, dtype, h, pad):
