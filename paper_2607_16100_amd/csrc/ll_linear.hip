@@ -180,16 +180,20 @@ Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
   } else {
     if (t64 <= 2 * kFill) p.stages = 4;
     // Too few tiles: the sum is cut into shares of four stages or more.  s
-    // splits cost the rounds of the chip they make, each 1 / s of a whole one,
-    // and about a twentieth of a round each for the joining (128 x 4096 -> 4096
-    // binary32, 128 tiles: 84 us whole, 50 in 2, 58 in 3, 49 in 4; 777 x 1001
-    // x 515, about 135: 33 us in 2, 28 in 3).
+    // splits cost the rounds of the chip they make, each 1 / s of a whole one
+    // of .33 us a stage (binary32 .62), and the joining (bfloat16, us whole /
+    // 2 / 3 / 4 splits: 16 tiles, 16 stages 11.2 / 11.6 / 11.4 / 11.2 and 64
+    // stages 25.8 / 19.7 / 17.1 / 15.5; 64 tiles, 16 stages 11.6 / 12.8 / 13.2 /
+    // 13.4 and 64 stages 26.2 / 21.2 / 18.6 / 17.7; 160 tiles, 16 stages 11.6 /
+    // 16.9 / 17.5 / 20.5 and 64 stages 28.0 / 30.8 / 25.8 / 28.6).
     if (t64 < 200) {
       const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
       const uint64_t most = std::min<uint64_t>(std::min<uint64_t>(16, steps / 4), kMaxParts / std::max<uint64_t>(one, 1));
-      double best = 1.;
+      const double whole = (dt == LL_BF16 ? .33 : .62) * (double)steps;
+      double best = whole;
       for (uint64_t s = 2; s <= most; ++s) {
-        const double cost = (double)((t64 * s + kFill - 1) / kFill) / s + .05 * s + .08;
+        const double rounds = (double)((t64 * s + kFill - 1) / kFill);
+        const double cost = whole * rounds / (double)s + 3. + .009 * (double)(t64 * s);
         if (cost < best) {
           best = cost;
           p.splits = (uint32_t)s;
