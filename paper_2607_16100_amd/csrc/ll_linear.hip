@@ -185,11 +185,13 @@ Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
     // 2 / 3 / 4 splits: 16 tiles, 16 stages 11.2 / 11.6 / 11.4 / 11.2 and 64
     // stages 25.8 / 19.7 / 17.1 / 15.5; 64 tiles, 16 stages 11.6 / 12.8 / 13.2 /
     // 13.4 and 64 stages 26.2 / 21.2 / 18.6 / 17.7; 160 tiles, 16 stages 11.6 /
-    // 16.9 / 17.5 / 20.5 and 64 stages 28.0 / 30.8 / 25.8 / 28.6).
+    // 16.9 / 17.5 / 20.5 and 64 stages 28.0 / 30.8 / 25.8 / 28.6).  A stage of
+    // rows that are not whole chunks takes about a fifth longer (777 rows in 5
+    // groups, 1001 -> 515 binary32: 32.2 whole, 28.2 in 3).
     if (t64 < 200) {
       const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
       const uint64_t most = std::min<uint64_t>(std::min<uint64_t>(16, steps / 4), kMaxParts / std::max<uint64_t>(one, 1));
-      const double whole = (dt == LL_BF16 ? .33 : .62) * (double)steps;
+      const double whole = (dt == LL_BF16 ? .33 : .62) * (rows == kChunkRows ? 1. : 1.2) * (double)steps;
       double best = whole;
       for (uint64_t s = 2; s <= most; ++s) {
         const double rounds = (double)((t64 * s + kFill - 1) / kFill);
