@@ -72,3 +72,53 @@ def test_every_rank_gathers_and_scatters_the_same_layer_in_bfloat16():
 def test_experts_must_divide():
     with pytest.raises(ValueError):
         ExpertLayer(4, 8, 64, 32, 6, 2)
+
+
+def in_bfloat16(p, tokens, hidden, ffn, experts, k):
+    """A bfloat16 layer, its inputs, and the same layer in 64 bits on the experts it chose."""
+    layer = ExpertLayer(p, tokens, hidden, ffn, experts, k, seed=5)
+    g = gen(p + 40)
+    x, dout = (randn(g, p, tokens, hidden, dtype=torch.bfloat16) for _ in range(2))
+    out = layer.forward(x)
+    ids = layer._saved[0][1].long()
+    leaves = [x.double().reshape(-1, hidden), layer.router.double(), torch.cat(layer.up).double(),
+              torch.cat(layer.down).double()]
+    for leaf in leaves:
+        leaf.requires_grad_(True)
+    xs, router, up, down = leaves
+    w = torch.softmax(xs @ router.t(), 1).gather(1, ids)
+    w = w / w.sum(1, keepdim=True)
+    want = torch.zeros_like(xs)
+    for e in range(experts):
+        t, j = (ids == e).nonzero(as_tuple=True)
+        gate, u = (xs[t] @ up[e].t()).chunk(2, 1)
+        want = want.index_add(0, t, w[t, j, None] * ((gate * torch.sigmoid(gate) * u) @ down[e].t()))
+    want.backward(dout.double().reshape(-1, hidden))
+    return layer, x, dout, out, want, leaves
+
+
+@pytest.mark.parametrize("p,tokens,hidden,ffn,experts,k", [(8, 16, 256, 64, 32, 4), (4, 50, 200, 96, 8, 2)])
+def test_bfloat16_layer_and_gradients(p, tokens, hidden, ffn, experts, k):
+    """Relative in the Frobenius norm.  A value rounded to bfloat16 is off by at
+    most 2^-9 of itself, and the matrices pass a rounding on with at most twice
+    the gain (spectral over root-mean-square gain of a random matrix) that the
+    values themselves have; what goes through two of them, four times."""
+    layer, x, dout, out, want, leaves = in_bfloat16(p, tokens, hidden, ffn, experts, k)
+    dx, drouter, dup, ddown = layer.backward(dout)
+    assert ll.ll_check(SymRegion.stream_handle()) == ll.LL_OK
+    unit = 2.0 ** -9
+    # out: h (through one product), y, the ranks' parts, their sum
+    # ddown: dy and h.  dup: dy (through one product), the saved z (through the
+    # slopes, at most twice), dz.  dx: dup's and the product's own result, the
+    # router's share, the ranks' parts and their sum, all but the last two through
+    # one product more.  drouter: dweights from y's rounding and h's behind it;
+    # the differences g - <u, g> of those are smaller than they are, by up to the
+    # two terms' ratio of size, taken as 4.
+    for name, got, exact, roundings in (
+            ("out", out, want, 2 + 1 + 1 + 1), ("ddown", torch.cat(ddown), leaves[3].grad, 1 + 1),
+            ("dup", torch.cat(dup), leaves[2].grad, 2 + 2 + 1),
+            ("dx", dx, leaves[0].grad, 4 + 4 + 2 + 1 + 1 + 1 + 1),
+            ("drouter", drouter, leaves[1].grad, 4 * (1 + 2) + 1)):
+        exact = exact.detach().reshape(got.shape)
+        err = float((got.double() - exact).norm() / exact.norm())
+        assert err <= roundings * unit, (name, err / unit)

@@ -13,6 +13,8 @@ import moeref as ref  # noqa: E402
 from test_moe_gpu import gen, randn, strided  # noqa: E402
 
 if torch.cuda.is_available():
+    from paper_2607_16100_amd import llcoll as ll  # noqa: E402
+    from paper_2607_16100_amd import llmoe as lm  # noqa: E402
     from paper_2607_16100_amd import moe  # noqa: E402
 else:  # pragma: no cover
     pytest.skip("no GPU", allow_module_level=True)
@@ -398,3 +400,90 @@ def test_refusals():
         moe.linear_grad_x(torch.zeros(4, 6, device=DEV), w, act="gelu", offsets=off)
     with pytest.raises(KeyError):
         moe.linear(x, w, offsets=off, act="tanh")
+
+
+# Weight gradients without a bias whose sums run split over 128-wide tiles:
+# (dtype, counts or rows, in, out, splits).  A bias keeps them off that path.
+WIDE_GRAD_W = [
+    (BF16, 8193, 1024, 1024, 4), (BF16, 8200, 1022, 1030, 3), (BF16, [5000, 0, 4000], 640, 640, 3),
+    (BF16, [9000, 0, 6001], 638, 642, 2), (F32, 2501, 1100, 1033, 3), (F32, [6000, 1, 0, 4999], 513, 515, 2),
+]
+
+
+@pytest.mark.parametrize("dtype,counts,i,o,splits", WIDE_GRAD_W)
+@pytest.mark.parametrize("grad32,add", [(False, False), (True, True), (True, False), (False, True)])
+def test_weight_gradients_in_splits_of_wide_tiles(dtype, counts, i, o, splits, grad32, add):
+    g = gen(24)
+    if isinstance(counts, int):
+        offsets, n, groups = None, counts, 1
+    else:
+        n, groups = sum(counts), len(counts)
+        offsets = torch.tensor([sum(counts[:c]) for c in range(groups + 1)], dtype=torch.int32, device=DEV)
+    # the plan, from the workspace it asks for: rows of binary32 parts, whole
+    # eights of columns; more tiles of 64 than are ever split leave only this one
+    assert groups * (-(-i // 64)) * (-(-o // 64)) >= 200
+    need = lm.ll_linear_bytes(lm.desc(ll.DTYPES["f32" if dtype is F32 else "bf16"], lm.LL_ACT_NONE, groups, n, i, o,
+                                      offsets=None if offsets is None else offsets.data_ptr()), lm.LL_LINEAR_GRAD_W)
+    assert need == (ll.LL_OK, splits * groups * o * (-(-i // 8) * 8) * 4)
+    dz, x = randn(g, n, o, dtype=dtype), randn(g, n, i, dtype=dtype)
+    grad = F32 if grad32 else dtype
+    shape = (o, i) if offsets is None else (groups, o, i)
+    dw = randn(g, *shape, dtype=grad) if add else torch.full(shape, math.nan, dtype=grad, device=DEV)
+    old = dw.clone()
+    moe.linear_grad_w(dz, x, offsets=offsets, out=dw, add=add)
+    for gi, lo, hi in ref.spans(offsets, n):
+        want, err = ref.matmul(dz[lo:hi].double().t(), x[lo:hi].double())
+        if add:
+            want = want + (old if offsets is None else old[gi]).double()
+            err = err + ref.EPS * want.abs()
+        ref.close(dw if offsets is None else dw[gi], want, err, grad)
+
+
+# A row buffer several times as long as its groups' rows, as the sorted rows of
+# one of several ranks are: (counts, rows of the buffer, in, out).
+ROOMY = [([5, 0, 40, 19], 512, 1032, 520), ([130, 3, 0, 0, 77, 1], 2048, 640, 1030), ([300, 412], 6144, 2048, 1024),
+         ([1, 0, 2, 1], 4096, 7168, 512), ([0, 0, 0], 900, 72, 40), ([700, 20, 0, 48], 7000, 333, 515)]
+
+
+@pytest.mark.parametrize("counts,n,i,o", ROOMY)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+def test_more_rows_than_the_groups_hold(counts, n, i, o, dtype, act):
+    g = gen(25)
+    if act == "swiglu":
+        o -= o % 2
+    groups, used = len(counts), sum(counts)
+    offsets = torch.tensor([sum(counts[:c]) for c in range(groups + 1)], dtype=torch.int32, device=DEV)
+    w, b = randn(g, groups, o, i, dtype=dtype), randn(g, groups, o, dtype=dtype)
+
+    def rows(c):
+        t = torch.full((n, c), math.nan, dtype=dtype, device=DEV)
+        t[:used] = randn(g, used, c, dtype=dtype)
+        return t
+
+    def kept(c):
+        return torch.full((n, c), 9.0, dtype=dtype, device=DEV)
+
+    x, dz, zl = rows(i), rows(o), rows(2 * i if act == "swiglu" else i)
+    y, z, dx = kept(o // 2 if act == "swiglu" else o), kept(o), kept(zl.shape[1])
+    moe.linear(x, w, bias=b, act=act, offsets=offsets, out=y, z=z)
+    moe.linear_grad_x(dz, w, act=act, z=zl if act != "none" else None, offsets=offsets, out=dx)
+    dw, _ = moe.linear_grad_w(dz, x, offsets=offsets)
+    db = torch.empty(groups, o, dtype=dtype, device=DEV)
+    dwb, _ = moe.linear_grad_w(dz, x, offsets=offsets, bias_out=db)
+    for gi, lo, hi in ref.spans(offsets, n):
+        zz, ez = ref.matmul(x[lo:hi].double(), w[gi].double().t())
+        zz = zz + b[gi].double()
+        ez = ez + ref.EPS * zz.abs()
+        ref.close(y[lo:hi], ref.act(zz, act), ref.act_err(zz, ez, act), dtype)
+        ref.close(z[lo:hi], zz, ez, dtype)
+        da, ea = ref.matmul(dz[lo:hi].double(), w[gi].double())
+        zl64 = zl[lo:hi].double()
+        ref.close(dx[lo:hi], ref.through(da, zl64, act), ref.through_err(da, ea, zl64, act), dtype)
+        want, err = ref.matmul(dz[lo:hi].double().t(), x[lo:hi].double())
+        ref.close(dw[gi], want, err, dtype)
+        ref.close(dwb[gi], want, err, dtype)
+        d = dz[lo:hi].double()
+        ref.close(db[gi], d.sum(0), (hi - lo + 2) * ref.EPS * d.abs().sum(0), dtype)
+    for t in (y, z, dx):
+        assert bool((t[used:] == 9.0).all())

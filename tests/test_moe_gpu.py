@@ -348,3 +348,73 @@ def test_errors_are_raised():
         moe.Dispatch(3, 2, 4, 8, F32).dispatch(torch.zeros(4, 2, dtype=torch.int32, device=DEV), x)
     with pytest.raises(ValueError):
         moe.combine(x, torch.zeros(2, 2, dtype=torch.int64, device=DEV))
+
+
+# ---------------------------------------------------------------- routing of many tokens
+# More than 4096 tokens of up to 256 experts and 16 choices take 16 lanes a
+# token; one size for each number of logits a lane can hold, and one that does
+# not fit them.
+ROUTE_MANY = [(4097, 5, 2), (4098, 20, 3), (5003, 60, 8), (4099, 90, 6), (4100, 128, 8), (4097, 160, 6),
+              (4101, 190, 16), (4099, 256, 16), (4097, 8, 8), (4111, 16, 1), (4097, 257, 4), (4097, 40, 17)]
+
+
+def choose(logits, bias, k):
+    """The k largest binary32 keys a row, ties to the lowest index, on the CPU."""
+    key = (logits.float() if bias is None else logits.float() + bias).cpu()
+    key = torch.where(torch.isnan(key), torch.full_like(key, -math.inf), key)
+    val, idx = torch.sort(key, dim=1, descending=True, stable=True)
+    return torch.where(val[:, :k] > -math.inf, idx[:, :k], -1).to(logits.device)
+
+
+def check_route(t, e, k, dtype, score, normalise, biased, masked, pad):
+    x = route_inputs(t, e, dtype, t + e, masked)
+    bias = 0.3 * randn(gen(e), e) if biased else None
+    v = strided(x, pad)
+    ids, w = moe.route(v, k, bias=bias, score=score, normalise=normalise, scale=2.5)
+    want_ids = choose(x, bias, k)
+    assert torch.equal(ids.long(), want_ids)
+    rel = (e + k + 48) * ref.EPS  # as in test_route_and_gradient
+    want_w = route_weights64(x.double(), want_ids, score, normalise, 2.5)
+    ref.close(w, want_w, want_w.abs() * rel, F32)
+    g = randn(gen(3), t, k)
+    got = moe.route_grad(v, ids, g, score=score, normalise=normalise, scale=2.5)
+    want = route_grad64(x.double(), want_ids, g.double(), score, normalise, 2.5)
+    size = 2.5 * (g.abs() * (want_ids >= 0)).sum(1, keepdim=True).double()
+    ref.close(got, want, size * rel * torch.ones_like(want), dtype)
+
+
+@pytest.mark.parametrize("t,e,k", ROUTE_MANY)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("score,normalise,biased,masked,pad", [
+    ("softmax", False, False, True, 0), ("softmax", False, True, True, 3), ("softmax", True, True, False, 0),
+    ("sigmoid", False, False, True, 1), ("sigmoid", True, True, False, 8)])
+def test_route_of_many_tokens(t, e, k, dtype, score, normalise, biased, masked, pad):
+    check_route(t, e, k, dtype, score, normalise, biased, masked, pad)
+
+
+@pytest.mark.parametrize("t,e,k", [(1, 8, 8), (33, 64, 8), (7, 257, 4), (3, 1000, 32), (130, 160, 6)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("score,masked,pad", [("softmax", False, 0), ("softmax", True, 3), ("sigmoid", True, 0)])
+def test_biased_route_without_normalisation(t, e, k, dtype, score, masked, pad):
+    """Keys have the bias; the softmax is that of the logits alone."""
+    check_route(t, e, k, dtype, score, False, True, masked, pad)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_ties_of_many_tokens_go_to_the_lowest_index(dtype):
+    t = 5000
+    for e in (16, 60, 256):
+        x = torch.zeros(t, e, device=DEV)
+        x[1::5, e // 2:] = 1.0
+        x[2::5] = -0.0
+        x[2::5, 3] = 0.0  # equal to -0
+        x[3::5, 1::2] = -math.inf
+        x[4::5] = math.inf
+        want = torch.zeros(t, 4, dtype=torch.int32)
+        for r, row in enumerate(([0, 1, 2, 3], [e // 2 + i for i in range(4)], [0, 1, 2, 3], [0, 2, 4, 6],
+                                 [0, 1, 2, 3])):
+            want[r::5] = torch.tensor(row, dtype=torch.int32)
+        ids, _ = moe.route(x.to(dtype), 4)
+        assert torch.equal(ids.cpu(), want)
+        ids, _ = moe.route(x.to(dtype), 4, bias=torch.zeros(e, device=DEV))
+        assert torch.equal(ids.cpu(), want)
