@@ -106,8 +106,9 @@ int ll_moe_combine_grad(const void *dout, size_t ldd, const void *y, size_t ldy,
 
 /* ---- grouped matrix products ---- */
 
-/* Activations.  GELU is the exact one (erf).  The gated ones take pre-
- * activations of two halves [a, u] and return silu(a) * u, gelu(a) * u. */
+/* Activations.  GELU is the exact one, x Phi(x), relatively accurate far below
+ * zero too.  The gated ones take pre-activations of two halves [a, u] and
+ * return silu(a) * u, gelu(a) * u. */
 typedef enum {
   LL_ACT_NONE = 0,
   LL_ACT_RELU = 1,

@@ -50,10 +50,39 @@ struct Args {
 };
 
 // ---------------------------------------------------------------- activations
-__device__ __forceinline__ float gelu(float x) { return 0.5f * x * (1.f + erff(x * 0.70710678118654752f)); }
+//
+// GELU is x Phi(x), Phi the normal distribution function.  As (1 + erf) / 2 it
+// cancels below zero (x = -5: 4 % of the result, x = -5.6: all of it), so it is
+// Phi(-z) = e^(-z^2 / 2) M(z) for z >= 0, and 1 less that above.  M, Mills'
+// ratio over sqrt(2 pi), falls like 1 / z and is smooth in u = 1 / (1 + .34 z):
+// u times a polynomial of degree 8 in u, fitted to erfcx by least squares
+// weighted towards the largest relative error (3e-8; 3.1e-7 as computed here,
+// z up to 13).  The slope shares the exponential.  Gradient of 8192 x 4096
+// bfloat16 through GELU: 36.9 us, 5.4 TB/s; with erf 41.5, with erfc 54.0.
+__device__ __forceinline__ float normal_cdf(float x, float *bell) {
+  const float z = fabsf(x), u = __builtin_amdgcn_rcpf(__builtin_fmaf(0.34f, z, 1.f));
+  float m = -0.02612048014998436f;
+  m = __builtin_fmaf(m, u, 0.1394995152950287f);
+  m = __builtin_fmaf(m, u, -0.2731328010559082f);
+  m = __builtin_fmaf(m, u, 0.20218272507190704f);
+  m = __builtin_fmaf(m, u, -0.044718485325574875f);
+  m = __builtin_fmaf(m, u, 0.11535917222499847f);
+  m = __builtin_fmaf(m, u, 0.11519765853881836f);
+  m = __builtin_fmaf(m, u, 0.13611219823360443f);
+  m = __builtin_fmaf(m, u, 0.13562050461769104f);
+  *bell = exp_f32(-0.5f * x * x);
+  const float tail = *bell * (m * u);
+  return x < 0.f ? tail : 1.f - tail;
+}
+__device__ __forceinline__ float gelu(float x) {
+  float bell;
+  return x * normal_cdf(x, &bell);
+}
 __device__ __forceinline__ float silu(float x) { return x / (1.f + expf(-x)); }
 __device__ __forceinline__ float gelu_slope(float x) {
-  return 0.5f * (1.f + erff(x * 0.70710678118654752f)) + x * expf(-0.5f * x * x) * 0.39894228040143268f;
+  float bell;
+  const float phi = normal_cdf(x, &bell);
+  return phi + x * bell * 0.39894228040143268f;
 }
 __device__ __forceinline__ float silu_slope(float x) {
   const float s = 1.f / (1.f + expf(-x));

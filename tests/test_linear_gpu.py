@@ -487,3 +487,30 @@ def test_more_rows_than_the_groups_hold(counts, n, i, o, dtype, act):
         ref.close(db[gi], d.sum(0), (hi - lo + 2) * ref.EPS * d.abs().sum(0), dtype)
     for t in (y, z, dx):
         assert bool((t[used:] == 9.0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["gelu", "geglu"])
+def test_gelu_keeps_its_relative_accuracy_far_below_zero(act, dtype):
+    """x Phi(x) is tiny there, but a value like any other: Phi comes from a
+    complementary error function (good to 16 units) of x / sqrt 2, whose two
+    roundings it magnifies by x^2 + 1; exp(-x^2 / 2) does as much."""
+    a = torch.cat([torch.linspace(-9, -2, 1500), torch.linspace(-2, 9, 500)]).to(dtype).to(DEV)[:, None]
+    u = 3 * randn(gen(26), 2000, 1, dtype=dtype)
+    x = torch.cat([a, u], 1) if act == "geglu" else a
+    a64, u64 = a.double(), u.double()
+    phi = 0.5 * torch.special.erfc(-a64 / math.sqrt(2.0))
+    bell = torch.exp(-a64 * a64 / 2) / math.sqrt(2 * math.pi)
+    rel = (a64 * a64 + 32) * ref.EPS
+    other = u64 if act == "geglu" else 1.0
+    for rows in (2000, 7):  # tiles, and the streaming kernel
+        got = moe.linear(x[:rows].contiguous(), torch.eye(x.shape[1], dtype=dtype, device=DEV), act=act)
+        want = (a64 * phi * other)[:rows]
+        ref.close(got, want, want.abs() * rel[:rows], dtype)
+    got = moe.act_grad(torch.ones_like(a), x, act)
+    want, size = phi + a64 * bell, phi + (a64 * bell).abs()
+    if act == "geglu":
+        want, size = torch.cat([want * u64, a64 * phi], 1), torch.cat([size * u64.abs(), (a64 * phi).abs()], 1)
+    ref.close(got, want, size * rel, dtype)
+    one = torch.eye(1, dtype=dtype, device=DEV)
+    ref.close(moe.linear_grad_x(torch.ones_like(a), one, act=act, z=x), want, size * rel, dtype)
