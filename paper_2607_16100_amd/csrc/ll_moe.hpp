@@ -209,7 +209,8 @@ __global__ __launch_bounds__(kThreads) void k_route(RouteArgs a) {
 //   softmax, normalised dl_i = u_i (g_i - sum u g)        (chosen only)
 //   sigmoid             dl_i = g_i s_i (1 - s_i)          (chosen only)
 //   sigmoid, normalised dl_i = u_i (g_i - sum u g)(1 - s_i)
-// Only the first needs the row; the others read the chosen logits.
+// 1 - s is the sigmoid of -l: the difference would be a rounding error where s
+// is near 1.  Only the first needs the row; the others read the chosen logits.
 template <typename T, int W, int NPL, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_route_grad(RouteArgs a) {
   __shared__ float coef[kThreads * NPL];
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void k_route_grad(RouteArgs a) {
     if (a.score == 0)
       c = a.normalise ? u * (g - mean) : p * g;
     else
-      c = a.normalise ? u * (g - mean) * (1.f - p) : g * p * (1.f - p);
+      c = (a.normalise ? u * (g - mean) : g * p) * sigmoid(-x);
     mine[id] = c;
   }
   __syncthreads();

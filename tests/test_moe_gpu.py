@@ -418,3 +418,28 @@ def test_ties_of_many_tokens_go_to_the_lowest_index(dtype):
         assert torch.equal(ids.cpu(), want)
         ids, _ = moe.route(x.to(dtype), 4, bias=torch.zeros(e, device=DEV))
         assert torch.equal(ids.cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("normalise", [False, True])
+def test_sigmoid_gradient_keeps_its_relative_accuracy(normalise, dtype):
+    """1 - sigmoid(x) of a large x is a small value like any other, not the
+    rounding error of a subtraction.  A few exponentials, sums of two positive
+    terms and quotients, each good to a few units."""
+    x = torch.linspace(-30, 60, 400).to(dtype).to(DEV)[:, None].repeat(1, 3)
+    x[:, 1] -= 1.0
+    x[:, 2] = -math.inf
+    g = torch.zeros(400, 2, device=DEV)
+    g[:, 0] = 1.0
+    ids = torch.tensor([[0, 1]], dtype=torch.int32, device=DEV).repeat(400, 1)
+    got = moe.route_grad(x, ids, g, score="sigmoid", normalise=normalise)
+    l = x.double()
+    p, q = torch.sigmoid(l), torch.sigmoid(-l)
+    want = torch.zeros(400, 3, dtype=torch.float64, device=DEV)
+    if normalise:  # u (g - sum u g) (1 - p), and g - sum u g = 1 - u0 = u1
+        u0 = p[:, 0] / (p[:, 0] + p[:, 1])
+        u1 = p[:, 1] / (p[:, 0] + p[:, 1])
+        want[:, 0], want[:, 1] = u0 * u1 * q[:, 0], -u1 * u0 * q[:, 1]
+    else:
+        want[:, 0] = p[:, 0] * q[:, 0]
+    ref.close(got, want, want.abs() * 64 * ref.EPS, dtype)
