@@ -58,7 +58,8 @@ typedef enum { LL_SCORE_SOFTMAX = 0, LL_SCORE_SIGMOID = 1 } ll_score;
  * of an expert is the softmax of the logits over all experts, or their
  * sigmoid (without the bias; a NaN logit counts as -Infinity).  weights[t, j]
  * = scale * score, divided by the sum of the row's chosen scores when
- * normalise is not 0 (0 if that sum is 0).  ids, weights: [tokens, k]. */
+ * normalise is not 0 (0 if that sum is 0; scores too small for binary32 but
+ * not for binary64 have their shares).  ids, weights: [tokens, k]. */
 int ll_moe_route(const void *logits, size_t ld, size_t tokens, int experts, int k, ll_dtype dt, const float *bias,
                  ll_score score, int normalise, float scale, int32_t *ids, float *weights, void *stream);
 

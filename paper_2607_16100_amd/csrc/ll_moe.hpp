@@ -84,10 +84,19 @@ __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + exp_f32(
 // The score of a choice with logit x (-Infinity: none), before any division by
 // the chosen ones' sum.  m, inv: softmax statistics, where they are needed.
 // A normalised softmax is one over the chosen logits alone, whatever m is, so
-// the other experts' exponentials are never computed for it.
+// the other experts' exponentials are never computed for it.  A normalised
+// sigmoid is e^x / (1 + e^x) times e^-m, m the row's largest chosen logit but at
+// most 0: the factor leaves the shares as they are and keeps the scores of a row
+// of small logits inside binary32.  m ends at -700, where binary64 ends too, so
+// that masks of the type's lowest value have no share.  Only a wave that has
+// such a logit takes m (all of them: 32768 x 64, 6 choices 7.1 -> 7.4 us).
 template <int W>
 __device__ __forceinline__ float choice_score(const RouteArgs &a, float x, float m, float inv) {
-  if (a.score != 0) return x == kNegInf ? 0.f : sigmoid(x);
+  if (a.score != 0) {
+    if (!a.normalise || __ballot(x < -64.f && x > kNegInf) == 0) return x == kNegInf ? 0.f : sigmoid(x);
+    m = fminf(fmaxf(group_max<W>(x), -700.f), 0.f);
+    return x == kNegInf ? 0.f : (x > 0.f ? 1.f : exp_f32(x - m)) / (1.f + exp_f32(-fabsf(x)));
+  }
   if (!a.normalise) return exp_f32(x - m) * inv;
   m = group_max<W>(x);
   return x == kNegInf ? 0.f : exp_f32(x - m);

@@ -443,3 +443,32 @@ def test_sigmoid_gradient_keeps_its_relative_accuracy(normalise, dtype):
     else:
         want[:, 0] = p[:, 0] * q[:, 0]
     ref.close(got, want, want.abs() * 64 * ref.EPS, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("top", [-60.0, -95.0, -300.0, -600.0])
+@pytest.mark.parametrize("tokens", [9, 4200])
+def test_normalised_sigmoid_of_small_scores(top, dtype, tokens):
+    """Scores below binary32's range still have their shares of the sum; those
+    below binary64's, as of masks of the type's lowest value, have none."""
+    e, k = 20, 5
+    x = (top - 12 * torch.rand(tokens, e, generator=gen(7), device=DEV)).to(dtype)
+    x[1::3, ::2] = torch.finfo(dtype).min
+    x[2::3] = torch.finfo(dtype).min
+    ids, w = moe.route(x, k, score="sigmoid", normalise=True, scale=2.5)
+    want_ids = choose(x, None, k)
+    assert torch.equal(ids.long(), want_ids)
+    want = route_weights64(x.double(), want_ids, "sigmoid", True, 2.5)
+    # differences of logits below 16 rounded once, and the exponentials' few units of them
+    rel = (k + 48 + 16) * ref.EPS
+    ref.close(w, want, want.abs() * rel, F32)
+    assert bool((w[2::3] == 0).all()) and bool((w[::3].sum(1) > 2.4).all())
+    g = randn(gen(8), tokens, k)
+    got = moe.route_grad(x, ids, g, score="sigmoid", normalise=True, scale=2.5)
+    p = torch.sigmoid(x.double())
+    u = want / 2.5
+    gg = 2.5 * g.double()
+    c = u * (gg - (u * gg).sum(1, keepdim=True)) * (1 - p.gather(1, want_ids))
+    full = torch.zeros(tokens, e, dtype=torch.float64, device=DEV).scatter_(1, want_ids, c)
+    size = 2.5 * g.abs().sum(1, keepdim=True).double()
+    ref.close(got, full, size * rel * torch.ones_like(full), dtype)
