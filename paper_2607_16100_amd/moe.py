@@ -184,8 +184,9 @@ def combine(y, rows, weights=None, *, residual=None, out=None, stream=None):
 
 
 def combine_grad(dout, y, rows, weights=None, *, dy=None, dweights=None, stream=None):
-    """(dy, dweights) of combine; dweights is None where weights is None.
-    Rows of dy that no token uses are left as they are (zeros in a new one)."""
+    """(dy, dweights) of combine; without weights, dweights is computed only
+    where its memory is given, and else None.  Rows of dy that no token uses
+    are left as they are (zeros in a new one)."""
     ldd = _mat(dout, "dout")
     ldy = _mat(y, "y", None, dout.shape[1], dout.dtype)
     n, h = y.shape
@@ -200,6 +201,7 @@ def combine_grad(dout, y, rows, weights=None, *, dy=None, dweights=None, stream=
         wp = _flat(weights, "weights", t * k, torch.float32)
         if dweights is None:
             dweights = _new(stream, t, k, dtype=torch.float32, device=y.device)
+    if dweights is not None:
         wg = _flat(dweights, "dweights", t * k, torch.float32)
     ll.check(_c.ll_moe_combine_grad(dout.data_ptr(), ldd, y.data_ptr(), ldy, n,
                                     _flat(rows, "rows", t * k, torch.int32), wp, t, k, h, _dt(y), dy.data_ptr(), lddy,

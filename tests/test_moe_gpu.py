@@ -472,3 +472,17 @@ def test_normalised_sigmoid_of_small_scores(top, dtype, tokens):
     full = torch.zeros(tokens, e, dtype=torch.float64, device=DEV).scatter_(1, want_ids, c)
     size = 2.5 * g.abs().sum(1, keepdim=True).double()
     ref.close(got, full, size * rel * torch.ones_like(full), dtype)
+
+
+def test_weight_gradient_of_an_unweighted_combine():
+    """Asked for by giving its memory; weights of 1 have a gradient too."""
+    g = gen(27)
+    y, dout = randn(g, 12, 40), randn(g, 5, 40)
+    rows = some_rows(g, 5, 2, 10)
+    dw = torch.full((5, 2), math.nan, device=DEV)
+    dy, got = moe.combine_grad(dout, y, rows, dweights=dw)
+    assert got is dw
+    prod = dout.double()[:, None] * torch.where((rows >= 0)[..., None], y.double()[rows.clamp(min=0).long()], 0.0)
+    ref.close(dw, prod.sum(2), 42 * ref.EPS * prod.abs().sum(2), F32)
+    assert torch.equal(dy, moe.combine_grad(dout, y, rows, torch.ones(5, 2, device=DEV))[0])
+    assert moe.combine_grad(dout, y, rows)[1] is None
