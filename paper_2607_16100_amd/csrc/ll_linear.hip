@@ -512,14 +512,15 @@ int ll_act_grad(const void *dy, size_t lddy, const void *z, size_t ldz, size_t r
   const int es = esize(dt);
   const bool gate = gated((int)act);
   const size_t width = gate ? 2 * features : features;
-  int st = check_rows(dy, lddy, features, es, true);
-  if (st == LL_OK) st = check_rows(z, ldz, width, es, true);
-  if (st == LL_OK) st = check_rows(dz, lddz, width, es, true);
+  const bool any = rows != 0 && features != 0;
+  int st = check_rows(dy, lddy, features, es, any);
+  if (st == LL_OK) st = check_rows(z, ldz, width, es, any);
+  if (st == LL_OK) st = check_rows(dz, lddz, width, es, any);
   if (st != LL_OK) return st;
   const size_t ob = span(rows, lddz, width, es);
   if (overlap(dy, span(rows, lddy, features, es), dz, ob) && !(!gate && dy == dz && lddy == lddz)) return LL_ERR_INVALID;
   if (overlap(z, span(rows, ldz, width, es), dz, ob) && !(z == dz && ldz == lddz)) return LL_ERR_INVALID;
-  if (rows == 0 || features == 0) return LL_OK;
+  if (!any) return LL_OK;
   ActArgs a{dy, z, dz, lddy, ldz, lddz, (uint32_t)rows, (uint32_t)features, (int)act};
   const bool vec = chunked(dy, lddy, features, es) && chunked(z, ldz, features, es) && chunked(dz, lddz, features, es);
   int cus = 0;

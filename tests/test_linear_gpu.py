@@ -514,3 +514,11 @@ def test_gelu_keeps_its_relative_accuracy_far_below_zero(act, dtype):
     ref.close(got, want, size * rel, dtype)
     one = torch.eye(1, dtype=dtype, device=DEV)
     ref.close(moe.linear_grad_x(torch.ones_like(a), one, act=act, z=x), want, size * rel, dtype)
+
+
+def test_act_grad_of_nothing():
+    for act in ("silu", "swiglu"):
+        wide = 16 if act == "swiglu" else 8
+        dz = moe.act_grad(torch.zeros(0, 8, device=DEV), torch.zeros(0, wide, device=DEV), act)
+        assert dz.shape == (0, wide)
+        assert moe.act_grad(torch.zeros(5, 0, device=DEV), torch.zeros(5, 0, device=DEV), act).shape == (5, 0)

@@ -200,3 +200,10 @@ def test_extents_of_zero():
     assert route_grad(tokens=0, logits=0, ids=0, dweights=0, dlogits=0) == ll.LL_OK
     assert combine(tokens=0, y=0, rows=0, out=0) == combine_grad(tokens=0, dout=0, rows=0) == ll.LL_OK
     assert dispatch(tokens=0, offsets=0) == ll.LL_ERR_INVALID  # offsets are written all the same
+
+
+def test_act_grad_of_nothing():
+    for act, wide in ((lm.LL_ACT_SILU, 8), (lm.LL_ACT_SWIGLU, 16)):
+        assert act_grad(dy=0, z=0, dz=0, rows=0, act=act, ldz=wide, lddz=wide) == ll.LL_OK
+        assert act_grad(dy=0, z=0, dz=0, features=0, act=act) == ll.LL_OK
+        assert act_grad(dy=0, rows=1, act=act) == ll.LL_ERR_INVALID
