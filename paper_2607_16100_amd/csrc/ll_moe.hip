@@ -312,15 +312,18 @@ int ll_moe_combine_grad(const void *dout, size_t ldd, const void *y, size_t ldy,
   if (features > kMaxExtent || nrows > kMaxExtent) return LL_ERR_UNSUPPORTED;
   if (tokens == 0) return LL_OK;
   const int es = esize(dt);
-  st = check_rows(dout, ldd, features, es);
-  if (st == LL_OK && nrows != 0) st = check_rows(dy, lddy, features, es);
-  if (st == LL_OK && nrows != 0 && dweights != nullptr) st = check_rows(y, ldy, features, es);
-  if (st != LL_OK) return st;
+  if (features != 0) {  // else the weights' gradient alone is left, zeros
+    st = check_rows(dout, ldd, features, es);
+    if (st == LL_OK && nrows != 0) st = check_rows(dy, lddy, features, es);
+    if (st == LL_OK && nrows != 0 && dweights != nullptr) st = check_rows(y, ldy, features, es);
+    if (st != LL_OK) return st;
+    const size_t dy_bytes = span(nrows, lddy, features, es);
+    if (overlap(dout, span(tokens, ldd, features, es), dy, dy_bytes) ||
+        (dweights != nullptr && overlap(y, span(nrows, ldy, features, es), dy, dy_bytes)))
+      return LL_ERR_INVALID;
+  }
   if (rows == nullptr || !aligned(rows, 4) || !aligned(weights, 4) || !aligned(dweights, 4)) return LL_ERR_INVALID;
-  const size_t dy_bytes = span(nrows, lddy, features, es);
-  if (overlap(dout, span(tokens, ldd, features, es), dy, dy_bytes) ||
-      (dweights != nullptr && overlap(y, span(nrows, ldy, features, es), dy, dy_bytes)))
-    return LL_ERR_INVALID;
+  if (features == 0 && dweights == nullptr) return LL_OK;
   RowArgs a{};
   a.x = dweights == nullptr ? nullptr : y;
   a.ldx = ldy;

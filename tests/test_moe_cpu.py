@@ -207,3 +207,9 @@ def test_act_grad_of_nothing():
         assert act_grad(dy=0, z=0, dz=0, rows=0, act=act, ldz=wide, lddz=wide) == ll.LL_OK
         assert act_grad(dy=0, z=0, dz=0, features=0, act=act) == ll.LL_OK
         assert act_grad(dy=0, rows=1, act=act) == ll.LL_ERR_INVALID
+
+
+def test_combine_gradient_without_features_needs_no_rows():
+    assert combine_grad(features=0, dout=0, y=0, dy=0, dweights=0) == ll.LL_OK
+    assert combine_grad(features=0, dout=0, y=0, dy=0, rows=0) == ll.LL_ERR_INVALID
+    assert combine(features=0, y=0, out=0, rows=0) == ll.LL_OK

@@ -486,3 +486,11 @@ def test_weight_gradient_of_an_unweighted_combine():
     ref.close(dw, prod.sum(2), 42 * ref.EPS * prod.abs().sum(2), F32)
     assert torch.equal(dy, moe.combine_grad(dout, y, rows, torch.ones(5, 2, device=DEV))[0])
     assert moe.combine_grad(dout, y, rows)[1] is None
+
+
+def test_combine_and_gradient_of_rows_without_features():
+    y, rows = torch.zeros(4, 0, device=DEV), torch.tensor([[0, 1], [2, -1]], dtype=torch.int32, device=DEV)
+    assert moe.combine(y, rows).shape == (2, 0)
+    dy, dw = moe.combine_grad(torch.zeros(2, 0, device=DEV), y, rows, torch.ones(2, 2, device=DEV),
+                              dweights=torch.full((2, 2), math.nan, device=DEV))
+    assert dy.shape == (4, 0) and dw.tolist() == [[0.0, 0.0], [0.0, 0.0]]
