@@ -82,8 +82,9 @@ int ll_moe_dispatch_bytes(size_t tokens, int k, int experts, size_t *bytes);
  * -1 for i >= offsets[experts]; rows[token*k + choice] = the sorted row, or
  * -1 if the choice is not local.  y[i] = x[slots[i] / k] for i <
  * offsets[experts]; the remaining rows of y (it has tokens*k) are left as
- * they are.  x NULL (then y NULL): sort only.  The gradient of y with respect
- * to x is ll_moe_combine with weights NULL. */
+ * they are.  x NULL (then y NULL): sort only.  No array may overlap another
+ * (LL_ERR_INVALID).  The gradient of y with respect to x is ll_moe_combine
+ * with weights NULL. */
 int ll_moe_dispatch(const int32_t *ids, size_t tokens, int k, int first, int experts, const void *x, size_t ldx,
                     size_t features, ll_dtype dt, int32_t *offsets, int32_t *slots, int32_t *rows, void *y, size_t ldy,
                     void *workspace, size_t workspace_bytes, void *stream);

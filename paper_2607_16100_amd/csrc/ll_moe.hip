@@ -29,7 +29,7 @@ bool overlap(const void *a, size_t an, const void *b, size_t bn) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return a != nullptr && b != nullptr && an != 0 && bn != 0 && x < y + bn && y < x + an;
 }
-size_t span(size_t rows, size_t ld, size_t len, int es) { return rows == 0 ? 0 : ((rows - 1) * ld + len) * es; }
+size_t span(size_t rows, size_t ld, size_t len, int es) { return rows == 0 || len == 0 ? 0 : ((rows - 1) * ld + len) * es; }
 
 // A matrix argument: not NULL, aligned to its element, rows no longer than ld.
 int check_rows(const void *p, size_t ld, size_t len, int es) {
@@ -221,12 +221,26 @@ int ll_moe_dispatch(const int32_t *ids, size_t tokens, int k, int first, int exp
     st = check_rows(x, ldx, features, es);
     if (st == LL_OK) st = check_rows(y, ldy, features, es);
     if (st != LL_OK) return st;
-    if (overlap(x, span(tokens, ldx, features, es), y, span(pairs, ldy, features, es))) return LL_ERR_INVALID;
   }
   if (need != 0) {
     if (workspace == nullptr || !aligned(workspace, 4)) return LL_ERR_INVALID;
     if (workspace_bytes < need) return LL_ERR_SCRATCH;
   }
+  // Places come from ids that are read twice, and rows of y from places: an
+  // array written over another could send rows anywhere.
+  const struct {
+    const void *p;
+    size_t bytes;
+  } arrays[] = {{ids, pairs * 4},
+                {x, span(tokens, ldx, features, es)},  // the inputs first, then what is written
+                {y, span(pairs, ldy, features, es)},
+                {offsets, ((size_t)experts + 1) * 4},
+                {slots, pairs * 4},
+                {rows, pairs * 4},
+                {workspace, need}};
+  for (int i = 2; i < 7; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(arrays[i].p, arrays[i].bytes, arrays[j].p, arrays[j].bytes)) return LL_ERR_INVALID;
   SortArgs s{};
   s.ids = ids;
   s.pairs = (uint32_t)pairs;

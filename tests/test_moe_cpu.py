@@ -213,3 +213,21 @@ def test_combine_gradient_without_features_needs_no_rows():
     assert combine_grad(features=0, dout=0, y=0, dy=0, dweights=0) == ll.LL_OK
     assert combine_grad(features=0, dout=0, y=0, dy=0, rows=0) == ll.LL_ERR_INVALID
     assert combine(features=0, y=0, out=0, rows=0) == ll.LL_OK
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rows=A), dict(slots=A + 16), dict(offsets=A + 28), dict(slots=C + 32), dict(rows=C + 4096 + 28),
+    dict(y=C + 8192), dict(slots=D + 128), dict(x=C + 16), dict(offsets=B + 4),
+    # 40000 bytes of ids, slots and rows each, and a workspace
+    dict(tokens=5000, slots=E, rows=F, ws=A + 39996, ws_bytes=1 << 20),
+    dict(tokens=5000, slots=E, rows=F, ws=C + 32, ws_bytes=1 << 20),
+    dict(tokens=5000, slots=E, rows=E + 39996, ws=F, ws_bytes=1 << 20),
+])
+def test_dispatch_refuses_outputs_over_its_other_arrays(kw):
+    """Places come from ids that are read twice, and rows of y from places: an
+    output over them would send rows anywhere."""
+    assert dispatch(**kw) == ll.LL_ERR_INVALID
+
+
+def test_rows_without_features_overlap_nothing():
+    assert combine_grad(features=0, dout=A, y=A, dy=A, dweights=0) == ll.LL_OK
