@@ -148,8 +148,6 @@ class Dispatch:
         t = ids.shape[0]
         if ids.dim() != 2 or ids.shape[1] != self.k or t > self.capacity:
             raise ValueError(f"ids: shape {tuple(ids.shape)}, expected at most ({self.capacity}, {self.k})")
-        if t != self.tokens:
-            self._view(t)
         xp = ldx = 0
         if x is not None:
             ldx = _mat(x, "x", t, self.features, self._x.dtype)
@@ -159,6 +157,8 @@ class Dispatch:
                                     self._slots.data_ptr(), self._rows.data_ptr(), self._x.data_ptr() if xp else 0,
                                     self.features, self._work.data_ptr(), self._work.numel(), _stream(stream)),
                  "ll_moe_dispatch")
+        if t != self.tokens:
+            self._view(t)
         return self
 
     def grad(self, dx, out=None, stream=None):

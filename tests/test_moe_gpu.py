@@ -494,3 +494,16 @@ def test_combine_and_gradient_of_rows_without_features():
     dy, dw = moe.combine_grad(torch.zeros(2, 0, device=DEV), y, rows, torch.ones(2, 2, device=DEV),
                               dweights=torch.full((2, 2), math.nan, device=DEV))
     assert dy.shape == (4, 0) and dw.tolist() == [[0.0, 0.0], [0.0, 0.0]]
+
+
+def test_a_refused_dispatch_leaves_the_plan_as_it_was():
+    ids = torch.randint(0, 8, (6, 2), generator=gen(28), device=DEV, dtype=torch.int32)
+    x = randn(gen(29), 6, 16)
+    plan = moe.Dispatch(10, 2, 8, 16, F32).dispatch(ids, x)
+    kept = plan.rows.clone()
+    for bad_ids, bad_x in ((ids[:4], x), (ids[:4].long(), x[:4]), (ids[:4], x[:4].bfloat16())):
+        with pytest.raises(ValueError):
+            plan.dispatch(bad_ids, bad_x)
+        assert plan.tokens == 6 and plan.rows.shape == (6, 2) and plan.x.shape == (12, 16)
+        assert torch.equal(plan.rows, kept)
+    assert plan.dispatch(ids[:4], x[:4]).tokens == 4
