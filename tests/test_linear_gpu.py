@@ -522,3 +522,18 @@ def test_act_grad_of_nothing():
         dz = moe.act_grad(torch.zeros(0, 8, device=DEV), torch.zeros(0, wide, device=DEV), act)
         assert dz.shape == (0, wide)
         assert moe.act_grad(torch.zeros(5, 0, device=DEV), torch.zeros(5, 0, device=DEV), act).shape == (5, 0)
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch):
+    """One GPU here: the current device is said to be another one, and no call gets as far as a launch."""
+    x, w = randn(gen(32), 4, 8), randn(gen(33), 6, 8)
+    ids, weights = moe.route(x, 2)
+    plan = moe.Dispatch(4, 2, 8, 8, F32).dispatch(ids, x)
+    w3, off = w[None], torch.tensor([0, 4], dtype=torch.int32, device=DEV)
+    monkeypatch.setattr(moe, "_device", lambda: 1)
+    for call in (lambda: moe.linear(x, w), lambda: moe.linear(x, w3, offsets=off), lambda: moe.route(x, 2),
+                 lambda: moe.route_grad(x, ids, weights), lambda: plan.dispatch(ids, x), lambda: plan.dispatch(ids),
+                 lambda: moe.combine(plan.x, plan.rows), lambda: moe.combine_grad(x, plan.x, plan.rows),
+                 lambda: moe.act_grad(x, x, "silu")):
+        with pytest.raises(ValueError):
+            call()
