@@ -78,6 +78,8 @@ class ExpertLayer:
         return region.out[r * nbytes:(r + 1) * nbytes].view(_TORCH[region.dtype]).view(rows, cols)
 
     def _all_gather(self, shards: torch.Tensor) -> list:
+        if shards.requires_grad:
+            moe._no_grad("the layer's input")
         for r in range(self.nranks):
             self._slice(self._gather, r, self.tokens, self.hidden).copy_(shards[r])
         ll.check(self._gather.allgather(self.tokens * self.hidden), "ll_allgather")

@@ -5,7 +5,9 @@ A call checks its tensors, launches on the current stream (or ``stream``) and
 returns its outputs, which it allocates unless they are given.  Errors raise
 ``llcoll.LLError`` with the C status, or ValueError for tensors that do not
 fit together or lie on another GPU than the current one.  Matrices have unit
-stride along their last dimension; their rows may lie further apart.
+stride along their last dimension; their rows may lie further apart.  Nothing
+is recorded for autograd: each operator's gradient is a call of its own, and
+inputs that require gradients are refused while gradients are enabled.
 
 What one rank of an expert-parallel layer does between its AllGather and its
 ReduceScatter:
@@ -83,6 +85,13 @@ def _flat(t: torch.Tensor, name: str, dev: int, numel: int, dtype) -> int:
     return t.data_ptr()
 
 
+def _no_grad(name: str) -> None:
+    """For an input that requires a gradient, which would be lost silently."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which is not recorded: call under torch.no_grad() or in an "
+                         "autograd.Function, and the gradient's own call for the way back")
+
+
 # ---------------------------------------------------------------- routing
 def route(logits, k: int, *, bias=None, score: str = "softmax", normalise: bool = False, scale: float = 1.0, ids=None,
           weights=None, stream=None):
@@ -90,6 +99,8 @@ def route(logits, k: int, *, bias=None, score: str = "softmax", normalise: bool 
     logits + bias a row; see ll_moe_route."""
     dev = _device()
     ld = _mat(logits, "logits", dev)
+    if logits.requires_grad:
+        _no_grad("logits")
     t, e = logits.shape
     if ids is None:
         ids = _new(stream, t, k, dtype=torch.int32, device=logits.device)
@@ -157,6 +168,8 @@ class Dispatch:
         xp = ldx = 0
         if x is not None:
             ldx = _mat(x, "x", dev, t, self.features, self._x.dtype)
+            if x.requires_grad:
+                _no_grad("x")
             xp = x.data_ptr()
         if self.offsets.get_device() != dev:
             raise ValueError("the plan's buffers are not on the current GPU")
@@ -178,6 +191,8 @@ def combine(y, rows, weights=None, *, residual=None, out=None, stream=None):
     """out[t] = residual[t] + sum_j weights[t, j] * y[rows[t, j]]; see ll_moe_combine."""
     dev = _device()
     ldy = _mat(y, "y", dev)
+    if y.requires_grad or (weights is not None and weights.requires_grad):
+        _no_grad("y or weights")
     n, h = y.shape
     t, k = rows.shape
     if out is None:
@@ -186,6 +201,8 @@ def combine(y, rows, weights=None, *, residual=None, out=None, stream=None):
     rp = ldr = 0
     if residual is not None:
         ldr, rp = _mat(residual, "residual", dev, t, h, y.dtype), residual.data_ptr()
+        if residual.requires_grad:
+            _no_grad("residual")
     ll.check(_c.ll_moe_combine(y.data_ptr(), ldy, n, _flat(rows, "rows", dev, t * k, torch.int32),
                                None if weights is None else _flat(weights, "weights", dev, t * k, torch.float32), rp,
                                ldr, t, k, h, _dt(y), out.data_ptr(), ldo, _stream(stream, dev)), "ll_moe_combine")
@@ -274,6 +291,8 @@ def linear(x, w, *, bias=None, act: str = "none", residual=None, offsets=None, o
     n = x.shape[0]
     g, o, i, ldw, gs = _weight(w, dev)
     ldx = _mat(x, "x", dev, n, i, w.dtype)
+    if x.requires_grad or w.requires_grad or (bias is not None and bias.requires_grad):
+        _no_grad("x, w or bias")
     width = o // 2 if act in lm.GATED else o
     if out is None:
         out = _new(stream, n, width, dtype=x.dtype, device=x.device)
@@ -282,6 +301,8 @@ def linear(x, w, *, bias=None, act: str = "none", residual=None, offsets=None, o
     rp = zp = None
     if residual is not None:
         ldr, rp = _mat(residual, "residual", dev, n, width, x.dtype), residual.data_ptr()
+        if residual.requires_grad:
+            _no_grad("residual")
     if z is not None:
         ldz, zp = _mat(z, "z", dev, n, o, x.dtype), z.data_ptr()
     d, wp, wn, _ws = _plan(lm.LL_LINEAR_FORWARD, stream, x.device, _dt(x), lm.ACTS[act], g, n, i, o,

@@ -122,3 +122,14 @@ def test_bfloat16_layer_and_gradients(p, tokens, hidden, ffn, experts, k):
         exact = exact.detach().reshape(got.shape)
         err = float((got.double() - exact).norm() / exact.norm())
         assert err <= roundings * unit, (name, err / unit)
+
+
+def test_inputs_that_require_gradients_are_refused():
+    layer = ExpertLayer(2, 4, 16, 8, 4, 2, dtype="f32")
+    x = randn(gen(2), 2, 4, 16)
+    want = layer.forward(x)
+    x.requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        layer.forward(x)
+    with torch.no_grad():
+        assert torch.equal(layer.forward(x), want)

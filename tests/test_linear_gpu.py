@@ -537,3 +537,25 @@ def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch)
                  lambda: moe.act_grad(x, x, "silu")):
         with pytest.raises(ValueError):
             call()
+
+
+def test_inputs_that_require_gradients_are_refused_unless_gradients_are_off():
+    x, w = randn(gen(30), 4, 8), randn(gen(31), 6, 8)
+    want = moe.linear(x, w)
+    ids, weights = moe.route(x, 2)
+    plan = moe.Dispatch(4, 2, 8, 8, F32).dispatch(ids, x)
+    off = torch.tensor([0, 4], dtype=torch.int32, device=DEV)
+    xg, wg, pg, sg = (t.clone().requires_grad_() for t in (x, w, plan.x, weights))
+    bias, res = torch.zeros(6, device=DEV, requires_grad=True), torch.zeros(4, 6, device=DEV, requires_grad=True)
+    for call in (lambda: moe.linear(xg, w), lambda: moe.linear(x, wg), lambda: moe.linear(x, wg[None], offsets=off),
+                 lambda: moe.linear(x, w, bias=bias), lambda: moe.linear(x, w, residual=res),
+                 lambda: moe.route(xg, 2), lambda: plan.dispatch(ids, xg), lambda: moe.combine(pg, plan.rows),
+                 lambda: moe.combine(plan.x, plan.rows, sg), lambda: moe.combine(plan.x, plan.rows, residual=xg)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    with torch.no_grad():
+        assert torch.equal(moe.linear(xg, wg), want)
+    # the gradients' own calls take parameters as they are
+    assert torch.equal(moe.linear_grad_x(want, wg), moe.linear_grad_x(want, w))
