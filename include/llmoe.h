@@ -29,9 +29,10 @@
  * Errors: LL_ERR_INVALID (a null or misaligned pointer, a leading dimension
  * below the row's length, a bad enum value, k outside [1, 32] or above
  * experts), LL_ERR_UNSUPPORTED (unknown dtype, experts or groups above 1024,
- * 2^24 tokens or more, features of a product above 2^20, other extents past
- * 2^31 - 1), LL_ERR_SCRATCH (workspace too small),
- * LL_ERR_HIP.
+ * 2^24 tokens or more, features of a product above 2^20, its leading dimensions
+ * above 2^21, a gated ll_linear with a weight of more than 0xF0000000 bytes
+ * (out * ldw) a group, other extents past 2^31 - 1), LL_ERR_SCRATCH (workspace
+ * too small), LL_ERR_HIP.
  */
 #ifndef LLMOE_H
 #define LLMOE_H

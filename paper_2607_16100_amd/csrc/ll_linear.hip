@@ -31,15 +31,18 @@ int check_desc(const ll_linear_desc *d) {
   if (d->groups < 1 || (d->offsets == nullptr && d->groups != 1) || !aligned(d->offsets, 4)) return LL_ERR_INVALID;
   if (d->in < 1 || d->out < 1) return LL_ERR_INVALID;
   if (d->groups > LL_MOE_MAX_EXPERTS || d->rows > kMaxExtent) return LL_ERR_UNSUPPORTED;
-  // a tile's rows, and a group's weight, lie within 32 bits of bytes
+  // a tile's rows lie within 32 bits of bytes
   constexpr size_t kMaxFeatures = 1u << 20;
   if (d->in > kMaxFeatures || d->out > kMaxFeatures) return LL_ERR_UNSUPPORTED;
   for (size_t ld : {d->ldx, d->ldw, d->ldy, d->ldz, d->ldr})
     if (ld > 2 * kMaxFeatures) return LL_ERR_UNSUPPORTED;
-  if (d->out * d->ldw > 0xF0000000ull / esize(d->dt)) return LL_ERR_UNSUPPORTED;
   if (d->ldw < d->in || (d->groups > 1 && d->wstride < (d->out - 1) * d->ldw + d->in)) return LL_ERR_INVALID;
   return LL_OK;
 }
+
+// Both halves of a gated weight are read from one base, so that a group's lies
+// within 32 bits of bytes.
+bool gate_fits(const ll_linear_desc *d) { return d->out * d->ldw <= 0xF0000000ull / esize(d->dt); }
 
 // Every row starts at a 16-byte address.
 bool rows16(const void *p, size_t ld, int es) { return p == nullptr || (aligned(p, 16) && ld * es % 16 == 0); }
@@ -349,6 +352,7 @@ int ll_linear_bytes(const ll_linear_desc *d, ll_linear_pass pass, size_t *bytes)
   if (bytes == nullptr || (int)pass < LL_LINEAR_FORWARD || (int)pass > LL_LINEAR_GRAD_W) return LL_ERR_INVALID;
   const int st = check_desc(d);
   if (st != LL_OK) return st;
+  if (pass == LL_LINEAR_FORWARD && gated((int)d->act) && !gate_fits(d)) return LL_ERR_UNSUPPORTED;
   // whether rows are whole 16-byte chunks depends on the pointers too; the
   // larger of both plans' splits serves either
   Args a{};
@@ -378,6 +382,7 @@ int ll_linear(const ll_linear_desc *d, const void *x, const void *w, const void 
   const int es = esize(d->dt);
   const bool gate = gated((int)d->act), any = d->rows != 0;
   if (gate && d->out % 2 != 0) return LL_ERR_INVALID;
+  if (gate && !gate_fits(d)) return LL_ERR_UNSUPPORTED;
   const size_t width = gate ? d->out / 2 : d->out;
   st = check_rows(x, d->ldx, d->in, es, any);
   if (st == LL_OK) st = check_rows(w, d->ldw, d->in, es, any);

@@ -760,7 +760,8 @@ __global__ __launch_bounds__(WM *WN * 64, ST *(BM + BN) > 640 && WM * WN == 4 ? 
   else
     lp.init(p, a.ldp, k, 0, a.m, m0, [](uint32_t, bool *) { return 0u; });
   if constexpr (kQkm)
-    lq.init(q, a.ldq, k, a.n, 0, 0, [&](uint32_t j, bool *ok) { return q_row<WTN, GATED>(tn, BN, j, a.n, ok); });
+    lq.init(q, a.ldq, k, a.n, 0, GATED ? 0 : tn * BN,
+            [&](uint32_t j, bool *ok) { return q_row<WTN, GATED>(tn, BN, j, a.n, ok); });
   else
     lq.init(q, a.ldq, k, 0, a.n, tn * BN, [](uint32_t, bool *) { return 0u; });
 

@@ -559,3 +559,30 @@ def test_inputs_that_require_gradients_are_refused_unless_gradients_are_off():
         assert torch.equal(moe.linear(xg, wg), want)
     # the gradients' own calls take parameters as they are
     assert torch.equal(moe.linear_grad_x(want, wg), moe.linear_grad_x(want, w))
+
+
+@pytest.mark.parametrize("dtype,o,i", [(BF16, 70001, 32768), (BF16, 70001, 32770), (BF16, 70001, 32769),
+                                       (F32, 33003, 32772)])
+def test_weights_past_32_bit_offsets(dtype, o, i):
+    """One group's weight of more than 4 GiB, as a projection to a vocabulary is."""
+    g = gen(34)
+    w = torch.empty(o, i, dtype=dtype, device=DEV)
+    for lo in range(0, o, 4096):
+        w[lo:lo + 4096] = randn(g, min(4096, o - lo), i, dtype=dtype)
+    assert w.numel() * w.element_size() > 1 << 32
+    edge = (1 << 32) // (i * w.element_size())  # the row that lies on 4 GiB
+    cols = torch.cat([torch.arange(0, 40), torch.arange(edge - 40, edge + 40), torch.arange(o - 40, o)]).to(DEV)
+    for rows in (3, 150):  # the streaming kernel and tiles
+        x, dz = randn(g, rows, i, dtype=dtype), torch.zeros(rows, o, dtype=dtype, device=DEV)
+        y = moe.linear(x, w)
+        z, ez = ref.matmul(x.double(), w[cols].double().t())
+        ref.close(y[:, cols], z, ez, dtype)
+        dz[:, cols] = randn(g, rows, len(cols), dtype=dtype)
+        dx = moe.linear_grad_x(dz, w)
+        z, ez = ref.matmul(dz[:, cols].double(), w[cols].double())
+        ref.close(dx, z, ez, dtype)
+    dw, _ = moe.linear_grad_w(dz, x)
+    z, ez = ref.matmul(dz[:, cols].double().t(), x.double())
+    ref.close(dw[cols], z, ez, dtype)
+    dw[cols] = 0
+    assert not bool(dw.any())

@@ -231,3 +231,19 @@ def test_dispatch_refuses_outputs_over_its_other_arrays(kw):
 
 def test_rows_without_features_overlap_nothing():
     assert combine_grad(features=0, dout=A, y=A, dy=A, dweights=0) == ll.LL_OK
+
+
+def test_limits_of_a_products_weight():
+    """No rows: nothing is launched, but the shape is checked.  128256 x 16384 bfloat16 is 4.2 GB."""
+    for dt, in_ in ((BF16, 16384), (F32, 8192)):
+        big = dict(rows=0, in_=in_, out=128256, dt=dt)
+        assert lm.ll_linear(d(**big), 0, 0, 0, 0, 0, 0, 0, 0, 0) == ll.LL_OK
+        assert lm.ll_linear_grad_x(d(**big), 0, 0, 0, 0, 0, 0, 0) == ll.LL_OK
+        for which in range(3):
+            assert lm.ll_linear_bytes(d(**big), which)[0] == ll.LL_OK
+        gated = d(act=lm.LL_ACT_SWIGLU, **big)
+        assert lm.ll_linear(gated, 0, 0, 0, 0, 0, 0, 0, 0, 0) == ll.LL_ERR_UNSUPPORTED
+        assert [lm.ll_linear_bytes(gated, which)[0] for which in range(3)] == [ll.LL_ERR_UNSUPPORTED, ll.LL_OK, ll.LL_OK]
+    for ld in ("ldx", "ldw", "ldy"):
+        assert three(d(**{ld: 1 << 21}, rows=0))[:2] == (ll.LL_OK,) * 2
+        assert three(d(**{ld: (1 << 21) + 1}, rows=0)) == (ll.LL_ERR_UNSUPPORTED,) * 3
