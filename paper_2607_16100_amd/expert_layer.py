@@ -3,7 +3,9 @@
 program.
 
 Rank r holds ``tokens`` of the batch and experts [r * E / P, (r + 1) * E / P);
-the router's weight is on every rank.  Forward, on each rank:
+the router's weight is on every rank.  The router runs in binary32 whatever the
+layer's type: logits rounded to bfloat16 would tie, and choose other experts.
+Forward, on each rank:
 
     x    = AllGather of the ranks' tokens
     ids, weights = route(x w_router^T)
@@ -33,8 +35,8 @@ _TORCH = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 class ExpertLayer:
     """``tokens``: per rank.  Weights are random, scaled by the square root of
-    the fan-in; assign ``router`` [E, H], ``up`` [P][E/P, 2F, H] and ``down``
-    [P][E/P, H, F] to use others."""
+    the fan-in; assign ``router`` [E, H] (binary32), ``up`` [P][E/P, 2F, H] and
+    ``down`` [P][E/P, H, F] to use others."""
 
     def __init__(self, nranks: int, tokens: int, hidden: int, ffn: int, experts: int, k: int, dtype: str = "bf16",
                  seed: int = 0, device="cuda"):
@@ -52,10 +54,10 @@ class ExpertLayer:
         g = torch.Generator(device=device)
         g.manual_seed(seed)
 
-        def weight(*shape):
-            return (torch.randn(*shape, generator=g, device=device) * shape[-1] ** -0.5).to(self.dtype)
+        def weight(*shape, dtype=self.dtype):
+            return (torch.randn(*shape, generator=g, device=device) * shape[-1] ** -0.5).to(dtype)
 
-        self.router = weight(experts, hidden)
+        self.router = weight(experts, hidden, dtype=torch.float32)
         self.up = [weight(self.local, 2 * ffn, hidden) for _ in range(nranks)]
         self.down = [weight(self.local, hidden, ffn) for _ in range(nranks)]
         self.plans = [moe.Dispatch(n, k, self.local, hidden, self.dtype, first=r * self.local, device=device)
@@ -95,7 +97,7 @@ class ExpertLayer:
         """[P, tokens, hidden] -> the same shape."""
         n = self.nranks * self.tokens
         for r, xs in enumerate(self._all_gather(x)):
-            logits = moe.linear(xs, self.router)
+            logits = moe.linear(xs.float(), self.router.float())
             ids, weights = moe.route(logits, self.k, normalise=True)
             plan = self.plans[r].dispatch(ids, xs)
             moe.linear(plan.x, self.up[r], act="swiglu", offsets=plan.offsets, out=self._h[r], z=self._z[r])
@@ -125,8 +127,8 @@ class ExpertLayer:
             # a rank has the weights' gradient of its own experts' choices only,
             # and the routing gradient is linear in it: the ranks' parts add up
             dlogits = moe.route_grad(logits, ids, dweights, normalise=True)
-            moe.linear_grad_w(dlogits, xs, out=self._slice(self._sum, r, *self.router.shape))
-            through = moe.linear_grad_x(dlogits, self.router)
+            moe.linear_grad_w(dlogits, xs.float(), out=self._slice(self._sum, r, *self.router.shape))
+            through = moe.linear_grad_x(dlogits, self.router.float()).to(self.dtype)
             moe.combine(moe.linear_grad_x(dz, self.up[r], offsets=off), plan.rows, residual=through,
                         out=self._slice(self._scatter, r, n, self.hidden))
             ups.append(dup)

@@ -133,3 +133,23 @@ def test_inputs_that_require_gradients_are_refused():
         layer.forward(x)
     with torch.no_grad():
         assert torch.equal(layer.forward(x), want)
+
+
+@pytest.mark.parametrize("p,tokens,hidden,ffn,experts,k", [(8, 16, 256, 64, 32, 4), (4, 50, 200, 96, 8, 2)])
+def test_router_of_a_bfloat16_layer_is_binary32(p, tokens, hidden, ffn, experts, k):
+    """Logits, choice, weights and the router's gradient are not rounded to bfloat16."""
+    layer = ExpertLayer(p, tokens, hidden, ffn, experts, k, seed=6)
+    assert layer.router.dtype is torch.float32
+    x = randn(gen(41), p, tokens, hidden, dtype=torch.bfloat16)
+    layer.forward(x)
+    xs = x.double().reshape(-1, hidden)
+    z, ez = ref.matmul(xs, layer.router.double().t())
+    for logits, ids, weights in layer._saved:
+        ref.close(logits, z, ez, torch.float32)
+        u = torch.softmax(z, 1).gather(1, ids.long())
+        # an exponential of a logit that is off by ez, shared by a sum of k
+        rel = 2 * ez.max() + (k + 48) * ref.EPS
+        ref.close(weights, u / u.sum(1, keepdim=True), rel * torch.ones_like(u), torch.float32)
+        # no expert left out has a larger logit than one chosen, but for its error
+        rest = z.scatter(1, ids.long(), float("-inf")).max(1).values
+        assert bool((z.gather(1, ids.long()).min(1).values >= rest - 2 * ez.max()).all())
