@@ -189,12 +189,17 @@ Plan plan_of(Pass pass, const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
     // stages 25.8 / 19.7 / 17.1 / 15.5; 64 tiles, 16 stages 11.6 / 12.8 / 13.2 /
     // 13.4 and 64 stages 26.2 / 21.2 / 18.6 / 17.7; 160 tiles, 16 stages 11.6 /
     // 16.9 / 17.5 / 20.5 and 64 stages 28.0 / 30.8 / 25.8 / 28.6).  A stage of
-    // rows that are not whole chunks takes about a fifth longer (777 rows in 5
-    // groups, 1001 -> 515 binary32: 32.2 whole, 28.2 in 3).
+    // rows that are not whole chunks takes longer: of dwords 1.08-1.17 times as
+    // long in binary32 and 1.2-1.7 in bfloat16, through registers 2.3-3.6 times.
+    // Over 7 shapes of 16 to 176 tiles, 4 lengths and the three products the
+    // splits chosen so are 0.6 %, 0.4 % and 9 % slower than the best of 1 to 6 and
+    // 8 on average (caches warm 0.7 %, 0.4 %, 3.5 %); without the factors 0.8 %,
+    // 0.9 % and 21 % (1.2 %, 0.6 %, 11 %).
     if (t64 < 200) {
       const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
       const uint64_t most = std::min<uint64_t>(std::min<uint64_t>(16, steps / 4), kMaxParts / std::max<uint64_t>(one, 1));
-      const double whole = (dt == LL_BF16 ? .33 : .62) * (rows == kChunkRows ? 1. : 1.2) * (double)steps;
+      const double slower = rows == kChunkRows ? 1. : dt == LL_F32 ? 1.15 : rows == kDwordRows ? 1.4 : 2.4;
+      const double whole = (dt == LL_BF16 ? .33 : .62) * slower * (double)steps;
       double best = whole;
       for (uint64_t s = 2; s <= most; ++s) {
         const double rounds = (double)((t64 * s + kFill - 1) / kFill);
@@ -353,8 +358,6 @@ int ll_linear_bytes(const ll_linear_desc *d, ll_linear_pass pass, size_t *bytes)
   const int st = check_desc(d);
   if (st != LL_OK) return st;
   if (pass == LL_LINEAR_FORWARD && gated((int)d->act) && !gate_fits(d)) return LL_ERR_UNSUPPORTED;
-  // whether rows are whole 16-byte chunks depends on the pointers too; the
-  // larger of both plans' splits serves either
   Args a{};
   a.offsets = d->offsets;
   a.groups = d->groups;
@@ -365,12 +368,19 @@ int ll_linear_bytes(const ll_linear_desc *d, ll_linear_pass pass, size_t *bytes)
   a.k = gw ? a.rows : (uint32_t)(pass == LL_LINEAR_FORWARD ? d->in : d->out);
   a.rows_c = gw ? a.m * (uint32_t)a.groups : a.rows;
   const int es = esize(d->dt);
-  const bool whole = d->in * es % 16 == 0 && d->ldx * es % 16 == 0 && d->ldw * es % 16 == 0 && d->wstride * es % 16 == 0;
+  // the alignment that the leading dimensions allow; pointers that allow less
+  // get no more splits than this
+  const Rows rx = rows_of(nullptr, d->ldx, d->in, es), rz = rows_of(nullptr, d->ldy, d->out, es);
+  const Rows rw = weight_rows(d, nullptr, es);
+  const Rows rows = gw ? std::min(rx, rz) : std::min(rw, pass == LL_LINEAR_FORWARD ? rx : rz);
   *bytes = 0;
-  if (pass == LL_LINEAR_FORWARD && stream_blocks(a, whole ? kChunkRows : kDwordRows) != 0) return LL_OK;
+  if (pass == LL_LINEAR_FORWARD && stream_blocks(a, rows) != 0) return LL_OK;
   const uint64_t one = size_parts(a, pass == LL_LINEAR_FORWARD && gated((int)d->act));
-  uint32_t splits = 1;
-  for (const Rows rows : {kAnyRows, kChunkRows}) splits = std::max(splits, plan_of((Pass)pass, a, d->dt, rows, ~0ull).splits);
+  uint32_t splits = plan_of((Pass)pass, a, d->dt, rows, ~0ull).splits;
+  if (gw) {  // a bias gradient may change the plan
+    a.dbias = &a;
+    splits = std::max(splits, plan_of(kGradW, a, d->dt, rows, ~0ull).splits);
+  }
   *bytes = splits > 1 ? (size_t)splits * one : 0;
   return LL_OK;
 }

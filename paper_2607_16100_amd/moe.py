@@ -269,8 +269,9 @@ _needs: dict = {}  # workspace bytes by shape (host arithmetic only)
 def _plan(which: int, stream, device, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz=0, ldr=0):
     """(descriptor, workspace address, its bytes, the workspace)."""
     d = lm.LLLinearDesc(lm.DESC_SIZE, dt, act, groups, rows, in_, out, offsets, ldx, ldw, wstride, ldy, ldz, ldr)
-    # what a plan depends on: the shape, whether there are offsets, and how rows are aligned
-    key = (which, dt, act, groups, rows, in_, out, offsets is None, (ldx | ldw | wstride) & 7)
+    # what a plan depends on: the shape, whether there are offsets, and how the operands' rows are aligned
+    lds = ldx | ldy if which == lm.LL_LINEAR_GRAD_W else ldw | wstride | (ldy if which else ldx)
+    key = (which, dt, act, groups, rows, in_, out, offsets is None, lds & 7)
     need = _needs.get(key)
     if need is None:
         st, need = lm.ll_linear_bytes(d, which)

@@ -586,3 +586,24 @@ def test_weights_past_32_bit_offsets(dtype, o, i):
     ref.close(dw[cols], z, ez, dtype)
     dw[cols] = 0
     assert not bool(dw.any())
+
+
+# Split sums of rows that are not whole 16-byte chunks: dwords, and bfloat16
+# through registers.
+ODD_SPLITS = [
+    ("forward", BF16, 256, 1025, 256), ("forward", BF16, 777, 2051, 514), ("forward", BF16, 640, 4099, 1024),
+    ("forward", BF16, [90, 0, 210], 4099, 260), ("forward", BF16, 320, 2054, 1024), ("grad_x", BF16, 512, 513, 2050),
+    ("grad_x", BF16, 200, 1501, 1025), ("grad_w", BF16, 2050, 511, 513), ("grad_w", BF16, 2500, 502, 706),
+    ("forward", F32, 500, 2049, 516), ("grad_x", F32, [100, 156], 255, 1027), ("grad_w", F32, 1200, 321, 1025),
+]
+
+
+@pytest.mark.parametrize("what,dtype,counts,i,o", ODD_SPLITS)
+@pytest.mark.parametrize("act", ["none", "swiglu"])
+def test_split_sums_of_odd_rows(what, dtype, counts, i, o, act):
+    n, groups = (counts, 1) if isinstance(counts, int) else (sum(counts), len(counts))
+    st, need = lm.ll_linear_bytes(lm.desc(ll.DTYPES["f32" if dtype is F32 else "bf16"], lm.LL_ACT_NONE, groups, n, i, o,
+                                          offsets=None if groups == 1 else 256),
+                                  ["forward", "grad_x", "grad_w"].index(what))
+    assert st == ll.LL_OK and need > 0
+    test_large(what, dtype, counts, i, o, act)
