@@ -60,7 +60,13 @@ typedef enum { LL_SCORE_SOFTMAX = 0, LL_SCORE_SIGMOID = 1 } ll_score;
  * sigmoid (without the bias; a NaN logit counts as -Infinity).  weights[t, j]
  * = scale * score, divided by the sum of the row's chosen scores when
  * normalise is not 0 (0 if that sum is 0; scores too small for binary32 but
- * not for binary64 have their shares).  ids, weights: [tokens, k]. */
+ * not for binary64 have their shares).  ids, weights: [tokens, k].
+ *
+ * The bias moves the logit.  Routers that balance their experts by a selection
+ * bias on the score choose other experts, since the scores are not linear in
+ * the logits: for those pass the scores (binary32) as logits, which makes the
+ * key score + bias, take the ids from that call and the weights from the
+ * scores; ll_moe_route_grad takes these ids with the logits as it does any. */
 int ll_moe_route(const void *logits, size_t ld, size_t tokens, int experts, int k, ll_dtype dt, const float *bias,
                  ll_score score, int normalise, float scale, int32_t *ids, float *weights, void *stream);
 

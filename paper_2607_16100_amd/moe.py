@@ -96,7 +96,15 @@ def _no_grad(name: str) -> None:
 def route(logits, k: int, *, bias=None, score: str = "softmax", normalise: bool = False, scale: float = 1.0, ids=None,
           weights=None, stream=None):
     """(ids int32 [tokens, k], weights float32 [tokens, k]) of the k largest
-    logits + bias a row; see ll_moe_route."""
+    logits + bias a row; see ll_moe_route.  A selection bias that belongs to the
+    score, not the logit, chooses other experts and takes the scores instead:
+
+        scores = torch.sigmoid(logits.float())
+        ids, _ = moe.route(scores, k, bias=bias)
+        weights = scores.gather(1, ids.long())     # divided by their sum, scaled
+
+    with ``route_grad(logits, ids, dweights, score="sigmoid", ...)`` on the way
+    back."""
     dev = _device()
     ld = _mat(logits, "logits", dev)
     if logits.requires_grad:

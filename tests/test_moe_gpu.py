@@ -507,3 +507,28 @@ def test_a_refused_dispatch_leaves_the_plan_as_it_was():
         assert plan.tokens == 6 and plan.rows.shape == (6, 2) and plan.x.shape == (12, 16)
         assert torch.equal(plan.rows, kept)
     assert plan.dispatch(ids[:4], x[:4]).tokens == 4
+
+
+@pytest.mark.parametrize("tokens", [1, 300, 4200])
+@pytest.mark.parametrize("normalise", [False, True])
+def test_a_selection_bias_on_the_scores(tokens, normalise):
+    """The way route's documentation gives: choice by score + bias, weights and
+    gradient of the scores alone."""
+    e, k, scale = 64, 6, 2.5
+    logits = 2 * randn(gen(50), tokens, e)
+    bias = 0.2 * randn(gen(51), e)
+    scores = torch.sigmoid(logits)
+    ids, _ = moe.route(scores, k, bias=bias)
+    assert torch.equal(ids.long(), choose(scores, bias, k))
+    if tokens > 1:  # not what the same bias on the logits chooses
+        assert not torch.equal(ids, moe.route(logits, k, bias=bias, score="sigmoid")[0])
+    w = scores.gather(1, ids.long())
+    if normalise:
+        w = w / w.sum(1, keepdim=True)
+    want = route_weights64(logits.double(), ids.long(), "sigmoid", normalise, 1.0)
+    rel = (e + k + 48) * ref.EPS
+    ref.close(w, want, want * rel, F32)
+    g = randn(gen(52), tokens, k)
+    got = moe.route_grad(logits, ids, g, score="sigmoid", normalise=normalise, scale=scale)
+    want = route_grad64(logits.double(), ids.long(), g.double(), "sigmoid", normalise, scale)
+    ref.close(got, want, scale * g.abs().sum(1, keepdim=True).double() * rel * torch.ones_like(want), F32)
