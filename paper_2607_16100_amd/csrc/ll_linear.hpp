@@ -8,7 +8,7 @@
 // along m or n ("RM": a row is one k).
 //
 // A workgroup owns a BM x BN tile of C, in registers.  Both operands pass
-// through LDS in stages of 32 (bf16) or 16 (binary32) k, loaded straight from
+// through LDS in stages of 64 (bf16) or 32 (binary32) k, loaded straight from
 // memory into LDS.  The matrix instruction takes Q as its first operand, so a
 // lane ends up with four consecutive n of one m.
 #pragma once
@@ -1094,7 +1094,8 @@ __global__ __launch_bounds__(WM *WN * 64, ST *(BM + BN) > 640 && WM * WN == 4 ? 
 //
 // Adds the splits of each element in order and finishes it as the product
 // itself would have.  A lane has kEw columns of a row.  Bound by its launch
-// and two dependent loads (777 x 515, 3 splits: 7.8 us).
+// and the chain of loads that finds a row's group before the first part is read
+// (777 x 515 of 5 groups, 3 splits: 7.1-7.8 us).
 template <typename T, Pass PASS, bool GATED>
 __global__ __launch_bounds__(256) void k_join(Args a) {
   const uint32_t width = GATED ? a.n / 2 : a.n, cols = (width + kEw - 1) / kEw;
@@ -1307,7 +1308,8 @@ __global__ __launch_bounds__(kBiasChunks *kBiasLanes) void k_bias_grad(Args a) {
 }
 
 // ---------------------------------------------------------------- dz = dy * act'(z)
-// Bound by memory: one pass, 16 bytes a lane.
+// Bound by memory: one pass, 16 bytes a lane.  8192 x 4096 bfloat16 through
+// GELU 37-39 us (5.1-5.4 TB/s), through SwiGLU 66 us (5.1 TB/s).
 struct ActArgs {
   const void *dy, *z;
   void *dz;

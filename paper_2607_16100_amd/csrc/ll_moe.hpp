@@ -493,7 +493,7 @@ struct Raw {
 // One token's row to each of its local sorted rows; read once, written up to
 // k times, so a token's row comes from memory once however many experts it
 // has here.  Bound by memory: the whole dispatch of 8192 tokens of 14 KiB to
-// 12288 rows takes 58-70 us (3.9-4.7 TB/s).
+// 12288 rows takes 58-73 us (3.8-4.7 TB/s).
 template <typename T, bool VEC, int TPR>
 __device__ __forceinline__ void push_row(const RowArgs &a, uint32_t t, const int32_t *rows_of) {
   constexpr int C = chunk_elems<T, VEC>();
@@ -556,7 +556,9 @@ __global__ __launch_bounds__(kThreads) void k_dispatch_small(SortArgs s, RowArgs
 // out[t] = sum_j w[t,j] y[rows[t,j]] (+ residual).  The loads of up to
 // kBatch expert rows are issued before the first of them is used (converting
 // each as it is loaded made them wait for each other: 174 -> 98 us).  Bound by
-// memory: 8192 tokens of 14 KiB from 12288 rows in 95-103 us (4.0-4.3 TB/s).
+// memory: 8192 tokens of 14 KiB from 12288 rows in 91-106 us (3.9-4.6 TB/s).
+// Few tokens by the chain of four such batches a thread: 1, 16 and 64 tokens of
+// 8 rows of 14 KiB take 10.5, 11.0 and 11.6 us.
 constexpr int kBatch = 8;
 
 template <typename T, bool VEC, int TPR>
