@@ -1,0 +1,175 @@
+/*
+ * llblock -- what stands around and inside an expert layer for one MI355X
+ * (gfx950): C ABI, same library and status codes as llcoll.h, conventions of
+ * llmoe.h.
+ *
+ *   - rows and weights in 8 bits, and the grouped product of the two;
+ *   - the norms before and after a block with its gate and its residual;
+ *   - an AdamW step over many tensors, states in binary32 or in 8 bits.
+ *
+ * 8-bit values are e4m3: a sign, 4 bits of exponent (bias 7), 3 of mantissa,
+ * largest 448, 0x7F and 0xFF no numbers, no infinities.  A block of LL_BLOCK
+ * values has one scale, a power of two held as its exponent plus 127 (e8m0):
+ * 2^(s - 127), s in [1, 254].  It is the least one with which the block's
+ * largest magnitude is 448 or less, so that every value times its inverse is
+ * exact and the rounding to 8 bits (to nearest, ties to even) the only one.
+ * Infinities and NaN become no number and do not count for the scale.
+ *
+ * Scale arrays: rows start at multiples of 4 bytes (address and leading
+ * dimension), and a row's bytes up to the next multiple of 4 past its blocks
+ * can be read; they are not used.
+ */
+#ifndef LLBLOCK_H
+#define LLBLOCK_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "llcoll.h"
+#include "llmoe.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define LL_BLOCK 128
+#define LL_NORM_MAX_FEATURES 32768
+
+/* ---- 8-bit rows and weights ---- */
+
+/* q[r] = e4m3 of act(x[r]), a scale for each LL_BLOCK features from the row's
+ * first: scales[r, b] (ceil(features / LL_BLOCK) a row).  A gated activation
+ * takes rows x of 2*features.  `end` (device memory, may be NULL): only rows
+ * below *end are read and written, as behind the last group of a dispatch. */
+int ll_quantise(const void *x, size_t ldx, size_t rows, const int32_t *end, size_t features, ll_dtype dt, ll_act act,
+                uint8_t *q, size_t ldq, uint8_t *scales, size_t lds, void *stream);
+
+/* The same of weights [groups][out, in], a scale for each LL_BLOCK x LL_BLOCK
+ * of them: q [groups][out, in] (ldq, qstride), scales [groups][ceil(out /
+ * LL_BLOCK), ceil(in / LL_BLOCK)] (lds, sstride: a multiple of 4).  transpose:
+ * q is [groups][in, out] and scales are transposed likewise; the codes are the
+ * same, as the weight's gradient to its input takes them (ll_linear8). */
+int ll_quantise_weight(const void *w, size_t ldw, size_t wstride, int groups, size_t out, size_t in, ll_dtype dt,
+                       int transpose, uint8_t *q, size_t ldq, size_t qstride, uint8_t *scales, size_t lds,
+                       size_t sstride, void *stream);
+
+/* ---- grouped products of 8-bit rows and weights ---- */
+
+/* y[r] = act(x[r] w[g]^T + bias[g]) + residual[r], as ll_linear, for x [rows,
+ * in] and w [groups][out, in] of ll_quantise and ll_quantise_weight.  In the
+ * descriptor `dt` is the type of y, z, bias and residual, ldx, ldw and wstride
+ * count 8-bit values.  Scales are multiplied by the matrix instruction.  Sums
+ * are binary32, but for bfloat16 results the instruction cuts each of eight
+ * consecutive k's products (8j .. 8j + 7) off 2^-13 below the power of two of
+ * the largest of them, about 2^-15 of a result of normal values; binary32
+ * results are summed in binary32 throughout.
+ * xs: [rows, ceil(in / LL_BLOCK)] at ldxs; ws: [groups][ceil(out / LL_BLOCK),
+ * ceil(in / LL_BLOCK)] at ldws and wsstride.
+ *
+ * The gradient of x is the same call on dz in 8 bits and the transposed weight
+ * (then ll_act_grad through an activation below); the weight's gradient is
+ * ll_linear_grad_w on the rows as they were before. */
+int ll_linear8(const ll_linear_desc *d, const uint8_t *x, const uint8_t *xs, size_t ldxs, const uint8_t *w,
+               const uint8_t *ws, size_t ldws, size_t wsstride, const void *bias, const void *residual, void *y,
+               void *z, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace (bytes, 16-byte aligned) with which the product runs as fast as it
+ * can; 0 where it needs none.  It also runs without one. */
+int ll_linear8_bytes(const ll_linear_desc *d, size_t *bytes);
+
+/* ---- norms around a block ---- */
+
+/* One token's row:
+ *   u = post * y / sqrt(mean(y^2) + eps)      (post NULL: u = y)
+ *   r = x + scale * gate * u                  (gate NULL: 1; x NULL: 0)
+ *   h = weight * r / sqrt(mean(r^2) + eps)    (weight NULL: no h)
+ * y: a block's output, x: the residual stream before it, gate: one binary32
+ * value a token, h: the next block's input.  Everything is binary32 until a
+ * result is rounded to its type.  post and weight are of type wdt (dt or
+ * LL_F32).  Fill with ll_norm_desc_init (contiguous rows), then change. */
+typedef struct {
+  uint32_t size; /* sizeof(ll_norm_desc), set by ll_norm_desc_init */
+  ll_dtype dt;   /* y, x, r, h and their gradients */
+  ll_dtype wdt;  /* post, weight */
+  float eps, scale;
+  size_t rows, features;
+  size_t ldy, ldx, ldr, ldh; /* y, x, r, h and dh */
+  size_t ldq, lds;           /* q and its scales */
+  size_t ldd, ldo, lddy;     /* gradients: dr, dr_out, dy */
+} ll_norm_desc;
+
+int ll_norm_desc_init(ll_norm_desc *d, ll_dtype dt, ll_dtype wdt, size_t rows, size_t features, float eps,
+                      float scale);
+
+/* r (may be NULL: not wanted), h (NULL: not wanted) and q with its scales: h in
+ * 8 bits as ll_quantise makes them, from the binary32 h (NULL: not wanted).  r
+ * may be x or y itself, h may be y. */
+int ll_norm(const ll_norm_desc *d, const void *y, const void *x, const float *gate, const void *post,
+            const void *weight, void *r, void *h, uint8_t *q, uint8_t *scales, void *stream);
+
+/* Gradients of ll_norm, from those of h (dh) and of r (dr, NULL: 0), for the r
+ * it wrote:
+ *   dr_out = dr + dh through the norm to r   (it is x's gradient too)
+ *   dy     = scale * gate * dr_out through the norm to y
+ *   dgate[t] = scale * <dr_out, u>
+ *   dweight, dpost: binary32, summed over the rows in a fixed order.
+ * weight NULL (then dh, r and dweight NULL): dr_out = dr.  Without post, gate
+ * and scale dy is dr_out, and need not be asked for.  y: needed with post or
+ * dgate.  Outputs that are NULL are not wanted.  flags: LL_GRAD_ADD adds
+ * dweight and dpost to what they hold.  dr_out may be dr, dy may be y.
+ * workspace: ll_norm_bytes, 16-byte aligned, needed for dweight or dpost. */
+int ll_norm_grad(const ll_norm_desc *d, const void *dh, const void *r, const void *dr, const void *y,
+                 const float *gate, const void *post, const void *weight, void *dr_out, void *dy, float *dgate,
+                 float *dweight, float *dpost, uint32_t flags, void *workspace, size_t workspace_bytes,
+                 void *stream);
+
+int ll_norm_bytes(const ll_norm_desc *d, size_t *bytes);
+
+/* ---- weight update ---- */
+
+/* One tensor of an update.  dt: the parameter's type, gdt: the gradient's.  A
+ * bfloat16 parameter has a binary32 master, which is updated and rounded to
+ * it; for a binary32 one master is NULL.  m and v: binary32, or in 8 bits m
+ * e4m3 and v e5m2 (no sign is used: 5 bits of exponent, bias 15, 2 of
+ * mantissa, largest 57344), each with a scale a block of LL_BLOCK from the
+ * tensor's first value (m_scales, v_scales: ceil(n / LL_BLOCK) bytes).  `at`:
+ * number of the tensor's first value among all the optimiser's, for its random
+ * numbers. */
+typedef struct {
+  void *param;
+  const void *grad;
+  float *master;
+  void *m, *v;
+  uint8_t *m_scales, *v_scales;
+  size_t n;
+  uint64_t at;
+  ll_dtype dt, gdt;
+} ll_adamw_tensor;
+
+typedef struct {
+  uint32_t size; /* sizeof(ll_adamw_desc) */
+  int32_t bits;  /* 32 or 8: of a state value */
+  double lr, beta1, beta2, eps, decay;
+  uint32_t seed; /* of the random rounding of 8-bit states */
+} ll_adamw_desc;
+
+/* t = *step + 1 is written back to *step (device memory), then for every value
+ *   g = grad * grad_scale
+ *   m = beta1 m + (1 - beta1) g
+ *   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in binary32, the constants rounded once from binary64.  lr_ptr, grad_scale:
+ * one binary32 value each in device memory, or NULL (d->lr, 1).  8-bit states
+ * are rounded up or down at random, by a hash of seed, t and the value's
+ * number, with the probability that keeps their mean: a state that moves by a
+ * thousandth would else stay where it is.  workspace: LL_ADAMW_WORKSPACE bytes,
+ * 16-byte aligned.  The tensors lie apart. */
+#define LL_ADAMW_WORKSPACE 64
+int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t count, int32_t *step, const float *lr_ptr,
+             const float *grad_scale, void *workspace, size_t workspace_bytes, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* LLBLOCK_H */

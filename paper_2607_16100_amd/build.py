@@ -8,6 +8,8 @@ into ``paper_2607_16100_amd/libllcoll.so`` with hipcc:
 * ``csrc/llcoll.hip``: the host entry points, the fill and probe kernels;
 * ``csrc/ll_moe.hip`` and ``csrc/ll_linear.hip``: the expert-layer operators
   (routing, dispatch and combine; the grouped matrix products);
+* ``csrc/ll_block.hip`` and ``csrc/ll_linear8.hip``: 8-bit rows and weights,
+  norms and the weight update; the 8-bit grouped product;
 
 each to an object of its own, in parallel, then linked into one shared
 library.  Extra preprocessor definitions (diagnostic builds) can be passed
@@ -64,7 +66,7 @@ def build(verbose: bool = False, extra_defines=(), out: str | None = None, jobs:
     defs = [f"-D{d}" for d in extra_defines]
     with tempfile.TemporaryDirectory(prefix="llcoll_build_") as tmp:
         units = [([os.path.join(CSRC, f"{name}.hip")], os.path.join(tmp, f"{name}.o"))
-                 for name in ("ll_linear", "llcoll", "ll_moe")]
+                 for name in ("ll_linear", "ll_linear8", "llcoll", "ll_block", "ll_moe")]
         for p in RANKS:
             units.append(([f"-DLL_INST_P={p}", os.path.join(CSRC, "ll_inst.hip")], os.path.join(tmp, f"ll_inst_p{p}.o")))
         cmds = [[hipcc(), *HIPCC_FLAGS, *defs, "-c", *src, "-o", obj] for src, obj in units]

@@ -1,0 +1,675 @@
+// Rows and weights in 8 bits, the norms around a block, and the weight update
+// (include/llblock.h).  All of them are bound by memory where they are large
+// and by latency where they are small.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/llblock.h"
+#include "ll_e4m3.hpp"
+#include "ll_linear.hpp"
+#include "ll_num.hpp"
+
+namespace llc {
+namespace blk {
+
+constexpr int kW = 8;  // consecutive values of a lane
+
+// kW values of a row that has `left` from here; vec: the address is aligned for
+// 16 bytes, or for all of them.
+template <typename T, bool VEC>
+__device__ __forceinline__ lin::Vals get(const T *p, int left) {
+  return lin::get8<T>(p, left > 0 ? (uint32_t)left : 0u, VEC);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void put(T *p, const lin::Vals &v, int left) {
+  if (left > 0) lin::put8<T>(p, v, (uint32_t)left, VEC);
+}
+template <bool VEC>
+__device__ __forceinline__ void put_codes(uint8_t *p, const uint32_t *w, int left) {
+  if (VEC && left >= kW) {
+    *reinterpret_cast<uint2 *>(p) = uint2{w[0], w[1]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < kW; ++i)
+      if (i < left) p[i] = (uint8_t)(w[i / 4] >> (i % 4 * 8));
+  }
+}
+
+// kW values of a block of 16 lanes to codes; returns the block's scale.
+__device__ __forceinline__ uint32_t quantise8(const lin::Vals &v, uint32_t *w) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < kW; ++i) top = max(top, finite_bits(v.v[i]));
+  const uint32_t s = scale_of<8>(max16(top));
+  const float inv = scale_inverse(s);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    w[i] = to_e4m3(v.v[4 * i] * inv, v.v[4 * i + 1] * inv) | to_e4m3(v.v[4 * i + 2] * inv, v.v[4 * i + 3] * inv) << 16;
+  return s;
+}
+
+// ---------------------------------------------------------------- rows
+//
+// 16 lanes a block of 128 features, U blocks of a lane under way at a time.
+struct QuantArgs {
+  const void *x;
+  uint8_t *q, *scales;
+  const int32_t *end;
+  uint64_t ldx, ldq, lds;
+  uint32_t rows, features, blocks;  // blocks a row
+  int act;
+};
+
+template <typename T, bool VEC, int U>
+__global__ __launch_bounds__(256) void k_quantise(QuantArgs a) {
+  uint32_t rows = a.rows;
+  if (a.end != nullptr) rows = (uint32_t)min(max(*a.end, 0), (int)a.rows);
+  const uint64_t items = (uint64_t)rows * a.blocks;
+  const uint64_t first = (uint64_t)blockIdx.x * (16 * U) + threadIdx.x / 16;
+  if ((uint64_t)blockIdx.x * (16 * U) >= items) return;
+  const bool gate = lin::gated(a.act);
+  lin::Vals v[U], u[U];
+  uint32_t row[U], col[U];
+#pragma unroll
+  for (int n = 0; n < U; ++n) {
+    const uint64_t item = first + n * 16;
+    row[n] = item < items ? (uint32_t)(item / a.blocks) : 0u;
+    col[n] = item < items ? (uint32_t)(item % a.blocks) * kBlock + threadIdx.x % 16 * kW : 0xFFFFFFFFu;
+    const int left = col[n] < a.features ? (int)(a.features - col[n]) : 0;
+    const T *p = (const T *)a.x + (uint64_t)row[n] * a.ldx + (left > 0 ? col[n] : 0);
+    v[n] = get<T, VEC>(p, left);
+    if (gate) u[n] = get<T, VEC>(p + a.features, left);
+  }
+#pragma unroll
+  for (int n = 0; n < U; ++n) {
+    lin::act8(v[n], a.act);
+    if (gate) {
+#pragma unroll
+      for (int i = 0; i < kW; ++i) v[n].v[i] *= u[n].v[i];
+    }
+    uint32_t w[2];
+    const int left = col[n] < a.features ? (int)(a.features - col[n]) : 0;
+#pragma unroll
+    for (int i = 0; i < kW; ++i) v[n].v[i] = i < left ? v[n].v[i] : 0.f;
+    const uint32_t s = quantise8(v[n], w);
+    if (left > 0) {
+      put_codes<VEC>(a.q + (uint64_t)row[n] * a.ldq + col[n], w, left);
+      if (threadIdx.x % 16 == 0) a.scales[(uint64_t)row[n] * a.lds + col[n] / kBlock] = (uint8_t)s;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- weights
+//
+// A workgroup has one block of 128 x 128: a thread 8 rows of 8 columns, 16
+// threads a row.  Transposed, two codes of a column are rounded into one word
+// at a time, so the 8 of a column lie together without a permutation; they go
+// through LDS to leave in whole lines.
+struct WeightArgs {
+  const void *w;
+  uint8_t *q, *scales;
+  uint64_t ldw, wstride, ldq, qstride, lds, sstride;
+  uint32_t out, in;
+};
+
+template <typename T, bool VEC, bool TRANSPOSE>
+__global__ __launch_bounds__(256) void k_quantise_weight(WeightArgs a) {
+  constexpr int kPitch = 128 + 16;  // rows of the transposed block start 16 bytes on in the banks
+  __shared__ __attribute__((aligned(16))) uint8_t tile[TRANSPOSE ? 128 * kPitch : 16];
+  __shared__ uint32_t tops[4];
+  const uint32_t bi = blockIdx.x, bo = blockIdx.y, g = blockIdx.z;
+  const uint32_t tr = threadIdx.x / 16, tc = threadIdx.x % 16;
+  const uint32_t row0 = bo * kBlock + tr * 8, col0 = bi * kBlock + tc * 8;
+  const int left = col0 < a.in ? (int)(a.in - col0) : 0;
+  const T *p = (const T *)a.w + g * a.wstride + (uint64_t)row0 * a.ldw + col0;
+  lin::Vals v[8];
+  uint32_t top = 0;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) v[r] = get<T, VEC>(p + r * a.ldw, row0 + r < a.out ? left : 0);
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, finite_bits(v[r].v[i]));
+  top = max16(top);
+  top = max(top, max(lane_halves<16>(top)[0], lane_halves<16>(top)[1]));
+  top = max(top, max(lane_halves<32>(top)[0], lane_halves<32>(top)[1]));
+  if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
+  __syncthreads();
+  top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+  const uint32_t s = scale_of<8>(top);
+  const float inv = scale_inverse(s);
+  uint8_t *q = a.q + g * a.qstride;
+  if (threadIdx.x == 0) a.scales[g * a.sstride + (TRANSPOSE ? (uint64_t)bi * a.lds + bo : (uint64_t)bo * a.lds + bi)] = (uint8_t)s;
+  if constexpr (!TRANSPOSE) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      uint32_t w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        w[i] = to_e4m3(v[r].v[4 * i] * inv, v[r].v[4 * i + 1] * inv) |
+               to_e4m3(v[r].v[4 * i + 2] * inv, v[r].v[4 * i + 3] * inv) << 16;
+      if (row0 + r < a.out) put_codes<VEC>(q + (uint64_t)(row0 + r) * a.ldq + col0, w, left);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      uint32_t w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        w[i] = to_e4m3(v[4 * i].v[c] * inv, v[4 * i + 1].v[c] * inv) |
+               to_e4m3(v[4 * i + 2].v[c] * inv, v[4 * i + 3].v[c] * inv) << 16;
+      *reinterpret_cast<uint2 *>(tile + (tc * 8 + c) * kPitch + tr * 8) = uint2{w[0], w[1]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const uint32_t at = n * 256 + threadIdx.x, r = at / 8, c = at % 8 * 16;
+      const uint32_t orow = bi * kBlock + r, ocol = bo * kBlock + c;
+      if (orow >= a.in || ocol >= a.out) continue;
+      const u32x4 w = *reinterpret_cast<const u32x4 *>(tile + r * kPitch + c);
+      uint8_t *to = q + (uint64_t)orow * a.ldq + ocol;
+      if (VEC && ocol + 16 <= a.out) {
+        *reinterpret_cast<u32x4 *>(to) = w;
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i)
+          if (ocol + i < a.out) to[i] = (uint8_t)(w[i / 4] >> (i % 4 * 8));
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- norms
+struct NormArgs {
+  const void *y, *x, *post, *weight;
+  const float *gate;
+  void *r, *h;
+  uint8_t *q, *scales;
+  // gradients
+  const void *dh, *dr;
+  void *dr_out, *dy;
+  float *dgate, *parts;  // parts: [2][gridDim.x][features], of dweight and dpost
+  uint64_t ldy, ldx, ldr, ldh, ldq, lds, ldd, ldo, lddy;
+  uint32_t rows, features;
+  float eps, scale;
+  bool w32;  // post and weight are binary32
+};
+
+// Sums of N values over the TPR threads of a row; every thread gets the same
+// bits.  `red`: [N][TPR / 64] of this row and of this sum alone.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float *v, float *red) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = group_sum<64>(v[n]);
+  if constexpr (TPR > 64) {
+    constexpr int kWaves = TPR / 64;
+    if (threadIdx.x % 64 == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) red[n * kWaves + threadIdx.x / 64] = v[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float s = red[n * kWaves];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) s += red[n * kWaves + w];
+      v[n] = s;
+    }
+  }
+}
+
+// A norm's weights, of the rows' type or binary32.
+template <typename T, bool VEC>
+__device__ __forceinline__ lin::Vals get_weight(const void *w, bool w32, uint32_t at, int left) {
+  if (left <= 0) return get<float, VEC>((const float *)nullptr, 0);
+  return w32 ? get<float, VEC>((const float *)w + at, left) : get<T, VEC>((const T *)w + at, left);
+}
+
+template <typename T, bool VEC, int TPR, int C>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormArgs a) {
+  constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float red[2][TPR / 64];
+  const uint32_t t = threadIdx.x % TPR;
+  const uint32_t row = blockIdx.x * kRows + threadIdx.x / TPR;
+  if (kRows > 1 && row >= a.rows) return;  // (a wave has a row then, and no barrier comes)
+  lin::Vals v[C], x[C], post[C], weight[C];
+  const float n = (float)a.features;
+  auto left = [&](int c) { return (int)a.features - (int)((c * TPR + t) * kW); };
+  // everything the row needs is asked for at once
+#pragma unroll
+  for (int c = 0; c < C; ++c) v[c] = get<T, VEC>((const T *)a.y + row * a.ldy + (c * TPR + t) * kW, left(c));
+  if (a.x != nullptr) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) x[c] = get<T, VEC>((const T *)a.x + row * a.ldx + (c * TPR + t) * kW, left(c));
+  }
+  if (a.post != nullptr) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) post[c] = get_weight<T, VEC>(a.post, a.w32, (c * TPR + t) * kW, left(c));
+  }
+  if (a.weight != nullptr) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) weight[c] = get_weight<T, VEC>(a.weight, a.w32, (c * TPR + t) * kW, left(c));
+  }
+  const float by = a.gate != nullptr ? a.gate[row] * a.scale : a.scale;
+  auto squares = [&](float *s) {
+    *s = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < kW; ++i) *s += v[c].v[i] * v[c].v[i];
+  };
+  float s;
+  if (a.post != nullptr) {
+    squares(&s);
+    row_sums<TPR, 1>(&s, red[0]);
+    const float rstd = 1.f / sqrtf(s / n + a.eps);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < kW; ++i) v[c].v[i] = v[c].v[i] * rstd * post[c].v[i];
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < kW; ++i) v[c].v[i] *= by;
+  if (a.x != nullptr) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) lin::add8(v[c], x[c]);
+  }
+  if (a.r != nullptr) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) put<T, VEC>((T *)a.r + row * a.ldr + (c * TPR + t) * kW, v[c], left(c));
+  }
+  if (a.weight == nullptr) return;
+  squares(&s);
+  row_sums<TPR, 1>(&s, red[1]);
+  const float rstd = 1.f / sqrtf(s / n + a.eps);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+#pragma unroll
+    for (int i = 0; i < kW; ++i) v[c].v[i] = v[c].v[i] * rstd * weight[c].v[i];
+    if (a.h != nullptr) put<T, VEC>((T *)a.h + row * a.ldh + (c * TPR + t) * kW, v[c], left(c));
+    if (a.q != nullptr) {  // 16 lanes have a block, whole or to the row's end
+      uint32_t w[2];
+      const uint32_t at = (c * TPR + t) * kW;
+      const uint32_t sc = quantise8(v[c], w);
+      if (left(c) > 0) {
+        put_codes<VEC>(a.q + row * a.ldq + at, w, left(c));
+        if (t % 16 == 0) a.scales[row * a.lds + at / kBlock] = (uint8_t)sc;
+      }
+    }
+  }
+}
+
+// The gradients: a workgroup takes rows blockIdx.x, + gridDim.x, ... and keeps
+// its share of dweight and dpost in registers; k_norm_join adds the shares up.
+//
+// With n = r / d, d = sqrt(mean(r^2) + eps): dr_out = dr + (weight dh - n
+// mean(n weight dh)) / d, and the same once more from dr_out to y.  Two rounds
+// of sums a row: r^2, weight dh r and y^2; then dr_out post y, which gives both
+// dgate and what dy needs.
+template <typename T, bool VEC, int TPR, int C>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a) {
+  constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float red[2][2][3 * (TPR / 64)];
+  const uint32_t t = threadIdx.x % TPR;
+  const float n = (float)a.features, rn = 1.f / n;
+  const uint32_t lane_row = threadIdx.x / TPR;
+  auto left = [&](int c) { return (int)a.features - (int)((c * TPR + t) * kW); };
+  auto at = [&](int c) { return (c * TPR + t) * kW; };
+  const bool with_y = a.post != nullptr || a.dgate != nullptr;
+  lin::Vals dw[C], dp[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < kW; ++i) dw[c].v[i] = dp[c].v[i] = 0.f;
+  uint32_t turn = 0;
+  for (uint32_t row = blockIdx.x * kRows + lane_row; row < a.rows; row += gridDim.x * kRows, ++turn) {
+    float(*sums)[3 * (TPR / 64)] = red[turn & 1];
+    lin::Vals r[C], g[C], y[C], d[C];
+    if (a.weight != nullptr) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        r[c] = get<T, VEC>((const T *)a.r + row * a.ldr + at(c), left(c));
+        g[c] = get<T, VEC>((const T *)a.dh + row * a.ldh + at(c), left(c));
+      }
+    }
+    if (a.dr != nullptr) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) d[c] = get<T, VEC>((const T *)a.dr + row * a.ldd + at(c), left(c));
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < kW; ++i) d[c].v[i] = 0.f;
+    }
+    if (with_y) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) y[c] = get<T, VEC>((const T *)a.y + row * a.ldy + at(c), left(c));
+    }
+    float s[3] = {0.f, 0.f, 0.f};
+    if (a.weight != nullptr) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const lin::Vals w = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+          s[0] += r[c].v[i] * r[c].v[i];
+          s[1] += w.v[i] * g[c].v[i] * r[c].v[i];
+        }
+      }
+    }
+    if (a.post != nullptr) {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < kW; ++i) s[2] += y[c].v[i] * y[c].v[i];
+    }
+    row_sums<TPR, 3>(s, sums[0]);
+    if (a.weight != nullptr) {
+      const float rstd = 1.f / sqrtf(s[0] * rn + a.eps);
+      const float mean = s[1] * rstd * rn;  // of n weight dh
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const lin::Vals w = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+          const float u = r[c].v[i] * rstd;
+          dw[c].v[i] += g[c].v[i] * u;
+          d[c].v[i] += rstd * (w.v[i] * g[c].v[i] - u * mean);
+        }
+      }
+    }
+    if (a.dr_out != nullptr) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) put<T, VEC>((T *)a.dr_out + row * a.ldo + at(c), d[c], left(c));
+    }
+    if (!with_y && a.dy == nullptr) continue;
+    const float gate = a.gate != nullptr ? a.gate[row] : 1.f;
+    const float by = gate * a.scale;
+    if (with_y) {
+      float dot = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        if (a.post != nullptr) {
+          const lin::Vals p = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+#pragma unroll
+          for (int i = 0; i < kW; ++i) dot += d[c].v[i] * p.v[i] * y[c].v[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < kW; ++i) dot += d[c].v[i] * y[c].v[i];
+        }
+      }
+      row_sums<TPR, 1>(&dot, sums[1]);
+      const float rstd = a.post != nullptr ? 1.f / sqrtf(s[2] * rn + a.eps) : 1.f;
+      if (a.dgate != nullptr && t == 0) a.dgate[row] = a.scale * dot * rstd;
+      if (a.post != nullptr) {
+        const float mean = by * dot * rstd * rn;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const lin::Vals p = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+#pragma unroll
+          for (int i = 0; i < kW; ++i) {
+            const float e = by * d[c].v[i], u = y[c].v[i] * rstd;
+            dp[c].v[i] += e * u;
+            d[c].v[i] = rstd * (e * p.v[i] - u * mean);
+          }
+        }
+      }
+    }
+    if (a.dy != nullptr) {
+      if (a.post == nullptr) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < kW; ++i) d[c].v[i] *= by;
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) put<T, VEC>((T *)a.dy + row * a.lddy + at(c), d[c], left(c));
+    }
+  }
+  if (a.parts == nullptr) return;
+  const uint64_t part = (uint64_t)blockIdx.x * kRows + lane_row, parts = (uint64_t)gridDim.x * kRows;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    // (the parts' rows are 16-byte aligned where VEC)
+    put<float, VEC>(a.parts + part * a.features + at(c), dw[c], left(c));
+    if (a.post != nullptr) put<float, VEC>(a.parts + (parts + part) * a.features + at(c), dp[c], left(c));
+  }
+}
+
+// dweight and dpost from the workgroups' shares, in their order: 64 columns a
+// workgroup, kJoin threads a column, whose sums are added in order.
+constexpr int kJoin = 16;
+struct NormJoin {
+  const float *parts;
+  float *out[2];
+  uint32_t count, features;
+  bool add;
+};
+__global__ __launch_bounds__(64 * kJoin) void k_norm_join(NormJoin a) {
+  __shared__ float part[kJoin][64];
+  const uint32_t col = blockIdx.x * 64 + threadIdx.x % 64, lane = threadIdx.x / 64;
+  const float *from = a.parts + (uint64_t)blockIdx.y * a.count * a.features + col;
+  float s = 0.f;
+  if (col < a.features) {
+#pragma unroll 8
+    for (uint32_t i = lane; i < a.count; i += kJoin) s += from[(uint64_t)i * a.features];
+  }
+  part[lane][threadIdx.x % 64] = s;
+  __syncthreads();
+  float *out = blockIdx.y == 0 ? a.out[0] : a.out[1];
+  if (lane != 0 || col >= a.features || out == nullptr) return;
+#pragma unroll
+  for (int i = 1; i < kJoin; ++i) s += part[i][threadIdx.x % 64];
+  out[col] = a.add ? out[col] + s : s;
+}
+
+// ---------------------------------------------------------------- weight update
+//
+// The tensors' addresses travel with the launch, kTensors at a time, so that a
+// captured launch keeps them and nothing is copied first.  Coefficients that
+// depend on the step come from k_adamw_begin, which counts it: a replayed step
+// is the next one.
+struct AdamwCoef {
+  float step, rden, decay, grad_scale;  // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t), 1 - lr decay
+  uint32_t key;
+};
+struct AdamwBegin {
+  int32_t *step;
+  const float *lr_ptr, *grad_scale;
+  AdamwCoef *coef;
+  double lr, beta1, beta2, decay;
+  uint32_t seed;
+};
+
+// A bijection of 32-bit numbers whose every output bit depends on every input
+// bit: multiplications by odd numbers and xors with the upper half.
+__device__ __forceinline__ uint32_t mix32(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x7FEB352Du;
+  x = (x ^ (x >> 15)) * 0x846CA68Bu;
+  return x ^ (x >> 16);
+}
+
+__global__ void k_adamw_begin(AdamwBegin a) {
+  if (threadIdx.x != 0) return;
+  const int32_t t = *a.step + 1;
+  *a.step = t;
+  const double lr = a.lr_ptr != nullptr ? (double)*a.lr_ptr : a.lr;
+  AdamwCoef c;
+  c.step = (float)(lr / (1. - pow(a.beta1, (double)t)));
+  c.rden = (float)(1. / sqrt(1. - pow(a.beta2, (double)t)));
+  c.decay = (float)(1. - lr * a.decay);
+  c.grad_scale = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
+  c.key = mix32(a.seed + (uint32_t)t * 0x9E3779B9u);
+  *a.coef = c;
+}
+
+struct AdamwTensor {
+  void *param;
+  const void *grad;
+  float *master;
+  void *m, *v;
+  uint8_t *m_scales, *v_scales;
+  uint64_t n, at;
+  uint32_t chunk;  // the first of its chunks
+  uint32_t kind;   // kBf16 | kGradBf16 | kUnaligned
+};
+constexpr uint32_t kBf16 = 1, kGradBf16 = 2, kUnaligned = 4;
+constexpr int kTensors = 40;
+constexpr uint32_t kChunk = 4096;  // values a workgroup
+struct AdamwArgs {
+  const AdamwCoef *coef;
+  float beta1, rest1, beta2, rest2, eps;  // rest: 1 - beta
+  uint32_t count;
+  AdamwTensor t[kTensors];
+};
+static_assert(sizeof(AdamwArgs) <= 4000, "a launch's arguments");
+
+// Up or down to MANT bits of mantissa, of which a value has `r` / 2^(23 - MANT)
+// as its chance: the random bits are added below the last one kept.  Below the
+// least normal number 2^EMIN the steps are those of 2^EMIN, in whole numbers.
+// The value is at most the format's largest, so the code cannot pass it.
+template <int MANT, int EMIN, int BIAS>
+__device__ __forceinline__ uint32_t to_code(float y, uint32_t r) {
+  constexpr int kCut = 23 - MANT;
+  const uint32_t b = (uint32_t)__float_as_int(y) & 0x7FFFFFFFu;
+  if (b >= 0x7F800000u) return 0x7Fu;
+  const float mag = __int_as_float((int)b);
+  constexpr float kUp = (float)(1ull << (MANT - EMIN + kCut));
+  constexpr uint32_t kMin = (uint32_t)(EMIN + 127) << 23;
+  const uint32_t fine = ((b + r) >> kCut) - ((127u - BIAS) << MANT);
+  const uint32_t low = ((uint32_t)fminf(mag * kUp, 8388608.f) + r) >> kCut;
+  return (b < kMin ? low : fine) | ((uint32_t)__float_as_int(y) >> 31) << 7;
+}
+
+template <bool EIGHT>
+__global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
+  uint32_t lo = 0, hi = a.count;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (a.t[mid].chunk <= blockIdx.x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  const AdamwTensor &t = a.t[lo];
+  const AdamwCoef c = *a.coef;
+  const uint64_t n = t.n, base = (uint64_t)(blockIdx.x - t.chunk) * kChunk;
+  const bool vec = !(t.kind & kUnaligned), bf16 = t.kind & kBf16, gbf16 = t.kind & kGradBf16;
+  constexpr int U = kChunk / (256 * kW);
+  lin::Vals p[U], g[U], m[U], v[U];
+  uint2 m8[U], v8[U];
+  uint32_t ms[U], vs[U];
+  auto at = [&](int u) { return base + (uint64_t)(u * 256 + threadIdx.x) * kW; };
+  auto left = [&](int u) { return at(u) < n ? (int)min(n - at(u), (uint64_t)kW) : 0; };
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint64_t i = at(u);
+    const int l = left(u);
+    const uint64_t j = l > 0 ? i : 0;
+    p[u] = lin::get8((bf16 ? t.master : (const float *)t.param) + j, l, vec);
+    g[u] = gbf16 ? lin::get8((const __bf16 *)t.grad + j, l, vec) : lin::get8((const float *)t.grad + j, l, vec);
+    if constexpr (EIGHT) {
+      // the states' last block is whole in memory only as far as the tensor goes
+      m8[u] = v8[u] = uint2{0, 0};
+      ms[u] = vs[u] = 1;
+      if (l > 0) {
+        ms[u] = t.m_scales[i / kBlock];
+        vs[u] = t.v_scales[i / kBlock];
+        if (vec && l == kW) {
+          m8[u] = *reinterpret_cast<const uint2 *>((const uint8_t *)t.m + i);
+          v8[u] = *reinterpret_cast<const uint2 *>((const uint8_t *)t.v + i);
+        } else {
+          uint32_t mw[2] = {0, 0}, vw[2] = {0, 0};
+#pragma unroll
+          for (int e = 0; e < kW; ++e)
+            if (e < l) {
+              mw[e / 4] |= (uint32_t)((const uint8_t *)t.m)[i + e] << (e % 4 * 8);
+              vw[e / 4] |= (uint32_t)((const uint8_t *)t.v)[i + e] << (e % 4 * 8);
+            }
+          m8[u] = uint2{mw[0], mw[1]};
+          v8[u] = uint2{vw[0], vw[1]};
+        }
+      }
+    } else {
+      m[u] = lin::get8((const float *)t.m + j, l, vec);
+      v[u] = lin::get8((const float *)t.v + j, l, vec);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const uint64_t i = at(u);
+    const int l = left(u);
+    if constexpr (EIGHT) {
+      const float fm = scale_value(ms[u]), fv = scale_value(vs[u]);
+#pragma unroll
+      for (int e = 0; e < kW; ++e) {
+        const uint32_t wm = e < 4 ? m8[u].x : m8[u].y, wv = e < 4 ? v8[u].x : v8[u].y;
+        switch (e % 4) {
+          case 0: m[u].v[e] = __builtin_amdgcn_cvt_f32_fp8((int)wm, 0); v[u].v[e] = __builtin_amdgcn_cvt_f32_bf8((int)wv, 0); break;
+          case 1: m[u].v[e] = __builtin_amdgcn_cvt_f32_fp8((int)wm, 1); v[u].v[e] = __builtin_amdgcn_cvt_f32_bf8((int)wv, 1); break;
+          case 2: m[u].v[e] = __builtin_amdgcn_cvt_f32_fp8((int)wm, 2); v[u].v[e] = __builtin_amdgcn_cvt_f32_bf8((int)wv, 2); break;
+          default: m[u].v[e] = __builtin_amdgcn_cvt_f32_fp8((int)wm, 3); v[u].v[e] = __builtin_amdgcn_cvt_f32_bf8((int)wv, 3); break;
+        }
+        m[u].v[e] *= fm;
+        v[u].v[e] *= fv;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kW; ++e) {
+      const float gr = g[u].v[e] * c.grad_scale;
+      m[u].v[e] = m[u].v[e] * a.beta1 + gr * a.rest1;
+      v[u].v[e] = v[u].v[e] * a.beta2 + gr * gr * a.rest2;
+      p[u].v[e] = p[u].v[e] * c.decay - c.step * m[u].v[e] / (sqrtf(v[u].v[e]) * c.rden + a.eps);
+    }
+    if constexpr (EIGHT) {
+      uint32_t tm = 0, tv = 0;
+#pragma unroll
+      for (int e = 0; e < kW; ++e) {
+        tm = max(tm, e < l ? finite_bits(m[u].v[e]) : 0u);
+        tv = max(tv, e < l ? finite_bits(v[u].v[e]) : 0u);
+      }
+      const uint32_t sm = scale_of<8>(max16(tm)), sv = scale_of<15>(max16(tv));
+      if (l > 0) {
+        const float im = scale_inverse(sm), iv = scale_inverse(sv);
+        const uint64_t no = t.at + i;
+        uint32_t mw[2] = {0, 0}, vw[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < kW; ++e) {
+          const uint64_t k = no + e;
+          const uint32_t r = mix32((uint32_t)k ^ ((uint32_t)(k >> 32) * 0x9E3779B9u) ^ c.key);
+          mw[e / 4] |= to_code<3, -6, 7>(m[u].v[e] * im, r >> 16 << 4) << (e % 4 * 8);
+          vw[e / 4] |= to_code<2, -14, 15>(v[u].v[e] * iv, (r & 0xFFFFu) << 5) << (e % 4 * 8);
+        }
+        if (vec) {
+          put_codes<true>((uint8_t *)t.m + i, mw, l);
+          put_codes<true>((uint8_t *)t.v + i, vw, l);
+        } else {
+          put_codes<false>((uint8_t *)t.m + i, mw, l);
+          put_codes<false>((uint8_t *)t.v + i, vw, l);
+        }
+        if (threadIdx.x % 16 == 0) {
+          t.m_scales[i / kBlock] = (uint8_t)sm;
+          t.v_scales[i / kBlock] = (uint8_t)sv;
+        }
+      }
+    }
+    if (l <= 0) continue;
+    if constexpr (!EIGHT) {
+      lin::put8((float *)t.m + i, m[u], l, vec);
+      lin::put8((float *)t.v + i, v[u], l, vec);
+    }
+    if (bf16) {
+      lin::put8(t.master + i, p[u], l, vec);
+      lin::put8((__bf16 *)t.param + i, p[u], l, vec);
+    } else {
+      lin::put8((float *)t.param + i, p[u], l, vec);
+    }
+  }
+}
+
+}  // namespace blk
+}  // namespace llc

@@ -1,0 +1,520 @@
+// Grouped products of 8-bit rows and weights (include/llblock.h, ll_linear8).
+//
+// y[m, n] = sum over blocks b of 128 k of 2^(sx[m, b] + sw[n / 128, b]) times
+// the sum over the block of x(m, k) w(n, k).  The matrix instruction takes a
+// scale a row of each operand and 32 k, so the scales cost no instruction of
+// their own: a block's scale is given to all four of its 32 k.
+//
+// Tiles, their order, the loads into LDS and the epilogue are those of the
+// other products (ll_linear.hpp): a stage of 128 bytes of k is one block.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "ll_linear.hpp"
+
+namespace llc {
+namespace lin {
+
+typedef uint8_t e4m3;
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <>
+struct Step<e4m3> {
+  static constexpr int kBK = 128;
+};
+
+struct Args8 : Args {
+  const uint8_t *xs, *ws;
+  uint64_t ldxs, ldws, wsstride;
+};
+
+constexpr int kScaleStages = 4;  // stages of which a row's scales lie in one word
+
+// Which of a stage's 16-byte chunks a lane takes for half ks of its k does not
+// matter as long as both operands' lanes agree; the scale is the same for all.
+__device__ __forceinline__ uint32_t frag8_off(uint32_t dim0, int ks, int half) {
+  const uint32_t lane = threadIdx.x % 64, r = dim0 + lane % 32, chunk = ks * 4 + lane / 32 * 2 + half;
+  return r * 128 + ((chunk ^ (r & 7)) << 4);
+}
+
+union Frag8 {
+  u32x4 half[2];
+  i32x8 all;
+};
+
+// A lane's 32 codes of each operand, times their scales (low bytes), to the sums.
+//
+// For bfloat16 results by the 8-bit instruction.  It cuts each of eight
+// consecutive k's products off 2^-13 below the largest one's power of two and
+// adds the eights in binary32: about 2^-15 of a result of normal values, an
+// eightieth of what its rounding to bfloat16 loses.  For binary32 results that
+// would be most of the error, so the codes, which have four significant bits,
+// become bfloat16 with their scale (values below 2^-126 then are lost) and take
+// the bfloat16 instructions, whose products and sums are binary32 (777 x 1001 ->
+// 515: 2.6e-5 off with the one, 6e-8 with the other).
+__device__ __forceinline__ bf16x8 expand(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+template <typename O>
+__device__ __forceinline__ f32x16 mma8(const Frag8 &a, int sa, const Frag8 &b, int sb, f32x16 c) {
+  if constexpr (sizeof(O) == 2) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a.all, b.all, c, 0, 0, 0, sa, 0, sb);
+  } else {
+    const float fa = __int_as_float((sa & 0xFF) << 23), fb = __int_as_float((sb & 0xFF) << 23);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(expand(a.all[2 * t], a.all[2 * t + 1], fa),
+                                                  expand(b.all[2 * t], b.all[2 * t + 1], fb), c, 0, 0, 0);
+    return c;
+  }
+}
+template <typename O>
+__device__ __forceinline__ f32x4 mma8(const Frag8 &a, int sa, const Frag8 &b, int sb, f32x4 c) {
+  if constexpr (sizeof(O) == 2) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.all, b.all, c, 0, 0, 0, sa, 0, sb);
+  } else {
+    const float fa = __int_as_float((sa & 0xFF) << 23), fb = __int_as_float((sb & 0xFF) << 23);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(expand(a.all[2 * t], a.all[2 * t + 1], fa),
+                                                  expand(b.all[2 * t], b.all[2 * t + 1], fb), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// ---------------------------------------------------------------- the tile kernel
+//
+// Four waves of a quarter of the tile each, in fragments of 32 x 32 by the
+// matrix instruction of 64 k: it reads half as many registers a product as that
+// of 16 x 16, and a quarter needs fewer LDS reads than the halves of eight
+// waves.  A stage is two halves of its k; the fragments of one are read while
+// the other is multiplied.  In between, when all of a stage is in registers,
+// the only barrier of a stage frees its buffer for the loads of the stage ST
+// further on and says that the next stage has arrived.
+//
+// A row's scales come four stages to a word, through LDS like the operands; each
+// stage reads its words from there and moves them down to its byte.
+template <typename O, int BM, int BN, int ST, bool GATED, Rows ROWS>
+__global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args8 a) {
+  constexpr bool VEC = ROWS != kAnyRows;  // loads go straight into LDS
+  static_assert(VEC || ST == 2, "a stage in registers at a time");
+  constexpr int NW = 4, WTM = BM / 2, WTN = BN / 2, FM = WTM / 32, FN = WTN / 32;
+  constexpr int FH = FM > 1 ? FM / 2 : 1;  // fragments of a wave's rows in the tile's upper half
+  constexpr int BK = 128, kStage = (BM + BN) * 128, kScales = (BM + BN) * 4;
+  constexpr int kPitch = WTN + 4, kRowsE = FH * 32;  // an epilogue pass: rows of a wave
+  constexpr int kEpi = NW * kRowsE * kPitch * 4, kUse = ST * kStage + 2 * kScales + NW * 256;
+  constexpr int kLds = kUse > kEpi ? kUse : kEpi;
+  __shared__ __attribute__((aligned(1024))) char lds[kLds];
+  const int lane = threadIdx.x % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int wm = wave / 2, wn = wave % 2;
+
+  int g = 0;
+  uint32_t tn = 0, m0 = 0, m_end = a.m, k = a.k;
+  if (!find_rows(a, blockIdx.x, BM, &g, &m0, &m_end, &tn)) return;
+  const e4m3 *p = (const e4m3 *)a.p, *q = (const e4m3 *)a.q + (uint64_t)g * a.qstride;
+
+  // this workgroup's share of k: whole words of scales
+  constexpr uint32_t kWord = kScaleStages * BK;
+  const uint32_t share = a.splits == 1 ? k : ((k + kWord - 1) / kWord + a.splits - 1) / a.splits * kWord;
+  const uint32_t k_from = min(k, blockIdx.y * share);
+
+  Loader<e4m3, BM, NW, true, ROWS> lp;
+  Loader<e4m3, BN, NW, true, ROWS> lq;
+  lp.init(p, a.ldp, k, m_end, 0, m0, [&](uint32_t j, bool *ok) {
+    *ok = m0 + j < m_end;
+    return m0 + j;
+  });
+  lq.init(q, a.ldq, k, a.n, 0, GATED ? 0 : tn * BN,
+          [&](uint32_t j, bool *ok) { return q_row<WTN, GATED>(tn, BN, j, a.n, ok); });
+
+  // Scales of the tile's rows (first BM) and of its weight rows: segments of 64,
+  // dealt to the waves.
+  constexpr int kSegs = (BM + BN) / 64, kMine = (kSegs + NW - 1) / NW;
+  uint64_t sbase[kMine];
+  uint32_t soff[kMine];
+#pragma unroll
+  for (int c = 0; c < kMine; ++c) {
+    const uint32_t seg = wave + c * NW, e = seg * 64 + lane;
+    if (seg * 64 < BM) {
+      sbase[c] = (uint64_t)(a.xs + (uint64_t)m0 * a.ldxs);
+      soff[c] = m0 + e < m_end ? (uint32_t)(e * a.ldxs) : kOutside;
+    } else {
+      bool ok = false;
+      const uint32_t r = seg < kSegs ? q_row<WTN, GATED>(tn, BN, e - BM, a.n, &ok) : 0u;
+      sbase[c] = (uint64_t)(a.ws + (uint64_t)g * a.wsstride);
+      soff[c] = ok ? (uint32_t)(r / 128 * a.ldws) : kOutside;
+    }
+  }
+  if (a.splits > 1) {
+    lp.skip(k_from / BK);
+    lq.skip(k_from / BK);
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) sbase[c] += k_from / BK;
+    k = min(k - k_from, share);
+  }
+
+  f32x16 acc[FN][FM];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.f;
+
+  const uint32_t steps = (k + BK - 1) / BK;
+  constexpr int kLoads = lp.kChunks + lq.kChunks;  // of a thread, a stage
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+  const uint32_t at_p = lds0 + wave * lp.kChunks * 1024, at_q = lds0 + BM * 128 + wave * lq.kChunks * 1024;
+  char *const scale_lds = lds + ST * kStage;
+  auto issue = [&](int into, int n, auto whole, uint32_t have) __attribute__((always_inline)) {
+    if (n < lp.kChunks)
+      lp.template issue<decltype(whole)::value>(at_p + into * kStage, n, have);
+    else
+      lq.template issue<decltype(whole)::value>(at_q + into * kStage, n - lp.kChunks, have);
+  };
+  // The words of scales number `word` of the sum to their buffer (those past the
+  // sum are zeros), or, unless `wanted`, zeros to a place nobody reads: a branch
+  // here would let matrix instructions sink behind it.  As Loader's issue: in
+  // assembly, without a result register, wait states inside.
+  auto issue_scales = [&](uint32_t word, bool wanted) __attribute__((always_inline)) {
+    const bool in = wanted && word * kScaleStages * BK < k;
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) {
+      const uint32_t seg = wave + c * NW;
+      const uint64_t base = sbase[c] + (in ? word * 4 : 0);
+      const uint32_t o = in ? soff[c] : kOutside;
+      const uint32_t to = wanted && (kSegs % NW == 0 || seg < kSegs) ? (word & 1) * kScales + seg * 256 : 2 * kScales + wave * 256;
+      const u32x4 rs = {uniform_u32((uint32_t)base), uniform_u32((uint32_t)(base >> 32)), kOutside, (uint32_t)kRsrcWord3};
+      asm volatile(
+          "s_mov_b32 m0, %0\n\t"
+          "s_nop 3\n\t"
+          "buffer_load_dword %1, %2, 0 offen lds"
+          :
+          : "s"(uniform_u32(lds0 + ST * kStage + to)), "v"(o), "s"(rs)
+          : "memory");
+    }
+  };
+  // first entry of the wave's fragment i of the rows
+  auto dim_p = [&](int i) __attribute__((always_inline)) {
+    return FM > 1 ? (i < FH ? 0 : BM / 2) + wm * (WTM / 2) + (i % FH) * 32 : wm * 32;
+  };
+  uint32_t off_q[2][2], off_p[2][2];  // of the first fragment, by half of k and by 16 bytes; the others lie constants further
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      off_q[ks][h] = BM * 128 + frag8_off(wn * WTN, ks, h);
+      off_p[ks][h] = frag8_off(dim_p(0), ks, h);
+    }
+  auto read_q = [&](const char *from, int j, int ks, int h) __attribute__((always_inline)) {
+    return *reinterpret_cast<const u32x4 *>(from + off_q[ks][h] + j * 32 * 128);
+  };
+  auto read_p = [&](const char *from, int i, int ks, int h) __attribute__((always_inline)) {
+    return *reinterpret_cast<const u32x4 *>(from + off_p[ks][h] + (i < FH ? 0 : BM / 2 * 128) + (i % FH) * 32 * 128);
+  };
+  const bool lower = FM == 1 || m_end - m0 > BM / 2;  // the tile has rows in its lower half
+
+  if (steps > 0) {
+    issue_scales(0, true);
+#pragma unroll
+    for (int s = 0; s < ST; ++s) {
+      const int have = (int)k - s * BK;
+      if constexpr (VEC) {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) issue(s, n, std::false_type{}, have > 0 ? have : 0);
+      } else {
+        lp.fetch(have);
+        lq.fetch(have);
+        if (s == 0) {  // the second stage is committed during the first
+          lp.commit(lds);
+          lq.commit(lds + BM * 128);
+        }
+      }
+      lp.advance();
+      lq.advance();
+    }
+    wait_loads<VEC ? (ST - 1) * kLoads : 0>();
+    lp.clear_tail(lds, (int)k);
+    lq.clear_tail(lds + BM * 128, (int)k);
+    lds_barrier();
+
+    Frag8 fq[2][FN], fp[2][FM];  // by half of k
+    int sq[FN], sp[FM];          // scales, in the low byte
+    auto read_scales = [&](uint32_t s, int *sq, int *sp) __attribute__((always_inline)) {  // of stage s
+      const uint32_t *from = reinterpret_cast<const uint32_t *>(scale_lds + (s / kScaleStages & 1) * kScales);
+      const uint32_t down = s % kScaleStages * 8;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) sq[j] = (int)(from[BM + wn * WTN + j * 32 + lane % 32] >> down);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) sp[i] = (int)(from[dim_p(i) + lane % 32] >> down);
+    };
+    read_scales(0, sq, sp);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fq[0][j].half[h] = read_q(lds, j, 0, h);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fp[0][i].half[h] = read_p(lds, i, 0, h);
+    }
+
+    // One stage, number s, from LDS buffer b.  `whole`: the stage loaded meanwhile
+    // has BK k, else `have` of them (none: zeros are written).  next_has: k of the
+    // next one.
+    auto stage = [&](int b, uint32_t s, auto lower_c, auto whole, int have, int next_has) __attribute__((always_inline)) {
+      constexpr int kRowsF = decltype(lower_c)::value ? FM : FH;  // fragments of rows that have rows
+      constexpr int kMmas = FN * kRowsF, kReads = 2 * (FN + kRowsF);
+      const char *here = lds + b * kStage, *next = lds + (b + 1) % ST * kStage;
+      auto read = [&](const char *from, int n, int ks) __attribute__((always_inline)) {
+        const int f = n / 2, h = n % 2;
+        if (f < FN)
+          fq[ks][f < FN ? f : 0].half[h] = read_q(from, f, ks, h);
+        else
+          fp[ks][f - FN].half[h] = read_p(from, f - FN, ks, h);
+      };
+      auto multiply = [&](int t, int ks) __attribute__((always_inline)) {
+        const int j = t / kRowsF, i = t % kRowsF;
+        acc[j][i] = mma8<O>(fq[ks][j], sq[j], fp[ks][i], sp[i], acc[j][i]);
+      };
+#pragma unroll
+      for (int t = 0; t < kMmas; ++t) {
+#pragma unroll
+        for (int n = t * kReads / kMmas; n < (t + 1) * kReads / kMmas; ++n) read(here, n, 1);
+        multiply(t, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (!VEC) {  // the next stage's chunks, fetched a stage ago
+        lp.commit(const_cast<char *>(next));
+        lq.commit(const_cast<char *>(next) + BM * 128);
+      }
+      wait_loads<VEC ? (ST - 2) * kLoads : 0>();
+      if (ROWS == kDwordRows && next_has < BK) {
+        lp.clear_tail(const_cast<char *>(next), next_has);
+        lq.clear_tail(const_cast<char *>(next) + BM * 128, next_has);
+      }
+      lds_barrier();
+      issue_scales(s / kScaleStages + 1, s % kScaleStages == 1);
+      if constexpr (!VEC) {
+        lp.fetch(have);
+        lq.fetch(have);
+      }
+      int nq[FN], np[FM];
+      read_scales(s + 1, nq, np);
+#pragma unroll
+      for (int t = 0; t < kMmas; ++t) {
+        if constexpr (VEC) {
+#pragma unroll
+          for (int n = t * kLoads / kMmas; n < (t + 1) * kLoads / kMmas; ++n) issue(b, n, whole, have > 0 ? have : 0);
+        }
+#pragma unroll
+        for (int n = t * kReads / kMmas; n < (t + 1) * kReads / kMmas; ++n) read(next, n, 0);
+        multiply(t, 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < FN; ++j) sq[j] = nq[j];
+#pragma unroll
+      for (int i = 0; i < FM; ++i) sp[i] = np[i];
+      lp.advance();
+      lq.advance();
+    };
+    auto all = [&](auto lower_c) __attribute__((always_inline)) {
+      uint32_t s = 0;
+      if constexpr (VEC) {  // ST stages at a time: LDS addresses are constants
+        for (; (s + 2 * ST) * BK <= k; s += ST) {
+          stage(0, s, lower_c, std::true_type{}, BK, BK);
+          stage(1, s + 1, lower_c, std::true_type{}, BK, BK);
+          if constexpr (ST > 2) {
+            stage(2, s + 2, lower_c, std::true_type{}, BK, BK);
+            stage(3, s + 3, lower_c, std::true_type{}, BK, BK);
+          }
+        }
+      }
+      for (; s < steps; ++s)
+        stage(s % ST, s, lower_c, std::false_type{}, (int)k - (int)(s + ST) * BK, (int)k - (int)(s + 1) * BK);
+    };
+    if (FM == 1 || lower)
+      all(std::true_type{});
+    else
+      all(std::false_type{});
+  }
+  wait_loads<0>();
+  lds_barrier();  // every wave is past its last stage, and no load is under way
+
+  // As the other products' epilogue: kEw consecutive columns of a row a lane.
+  // A lane's sums are of one row, four consecutive columns at a time.
+  float *mine = reinterpret_cast<float *>(lds) + wave * kRowsE * kPitch;
+  auto finish = [&](auto half) __attribute__((always_inline)) {
+    constexpr int h = decltype(half)::value;
+#pragma unroll
+    for (int i = 0; i < FH; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const f32x16 &v = acc[j][h * FH + i];
+          *reinterpret_cast<f32x4 *>(mine + (i * 32 + lane % 32) * kPitch + j * 32 + c * 8 + lane / 32 * 4) =
+              f32x4{v[c * 4], v[c * 4 + 1], v[c * 4 + 2], v[c * 4 + 3]};
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    constexpr int kWidth = GATED ? WTN / 2 : WTN;  // columns of y a wave has
+    constexpr int kLanes = kWidth / kEw;           // lanes a row
+    const int c = lane % kLanes * kEw;
+    const uint32_t n0 = (GATED ? tn * (BN / 2) + wn * kWidth : tn * BN + wn * WTN) + c;
+#pragma unroll 1
+    for (int r = lane / kLanes; r < kRowsE; r += 64 / kLanes) {
+      const uint32_t m = m0 + (FM > 1 ? h * (BM / 2) + wm * kRowsE : wm * 32) + r;
+      if (m >= m_end) break;
+      Pack<float, kEw, true> v, u;
+      v.load(mine + r * kPitch + c);
+      if constexpr (GATED) u.load(mine + r * kPitch + kWidth + c);
+      if (a.parts != nullptr) {
+        if (n0 < a.part_half) {
+          float *to = a.parts + ((uint64_t)blockIdx.y * a.rows_c + m) * a.part_row + n0;
+          v.store(to);
+          if constexpr (GATED) u.store(to + a.part_half);
+        }
+      } else {
+        put_forward<O, GATED>(a, g, m, n0, v, u);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  };
+  finish(std::integral_constant<int, 0>{});
+  if constexpr (FM > 1) {
+    if (lower) finish(std::integral_constant<int, 1>{});
+  }
+}
+
+// ---------------------------------------------------------------- few rows a group
+//
+// Up to 16 * RB rows of a group, bound by reading the weight once, as k_stream:
+// a workgroup owns 2 x 16 weight rows (gated: 16 of each half), each of its
+// waves an equal run of the blocks of k, kAhead blocks' loads under way at a time.
+// A lane has one weight row's (and one row's) scales of those blocks in a
+// word, cut from the two words they lie in.
+template <typename O, int RB, int NW, bool GATED>
+__global__ __launch_bounds__(NW * 64, 4) void k_stream8(Args8 a) {
+  constexpr int kAhead = RB == 1 ? 4 : 2, kCols = GATED ? 16 : 32;  // columns of y
+  constexpr int kPitch = 2 * 16 + 4;
+  __shared__ float part[NW][RB * 16][kPitch];
+  const int lane = threadIdx.x % 64, i = lane % 16, q = lane / 16;
+  const uint32_t wave = uniform_u32(threadIdx.x / 64);
+  int g = 0;
+  uint32_t tn = 0, m0 = 0, m_end = 0;
+  if (!find_rows(a, blockIdx.x, RB * 16, &g, &m0, &m_end, &tn)) return;
+  const uint32_t width = GATED ? a.n / 2 : a.n;
+  auto rsrc = [](uint64_t b) {
+    return make_rsrc((const void *)(((uint64_t)uniform_u32((uint32_t)(b >> 32)) << 32) | uniform_u32((uint32_t)b)),
+                     kOutside);
+  };
+  const rsrc_t rw = rsrc((uint64_t)a.q + (uint64_t)g * a.qstride + (uint64_t)(tn * kCols) * a.ldq);
+  const rsrc_t rx = rsrc((uint64_t)a.p + (uint64_t)m0 * a.ldp);
+  const rsrc_t rws = rsrc((uint64_t)a.ws + (uint64_t)g * a.wsstride);
+  const rsrc_t rxs = rsrc((uint64_t)a.xs + (uint64_t)m0 * a.ldxs);
+  uint32_t ow[2], ox[RB], ows[2], oxs[RB];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t row = i + h * (GATED ? width : 16);
+    const bool ok = tn * kCols + (GATED ? i : row) < width;
+    ow[h] = ok ? (uint32_t)(row * a.ldq) + q * 16 : kOutside;
+    ows[h] = ok ? (uint32_t)((tn * kCols + row) / 128 * a.ldws) : kOutside;
+  }
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const bool ok = m0 + b * 16 + i < m_end;
+    ox[b] = ok ? (uint32_t)((b * 16 + i) * a.ldp) + q * 16 : kOutside;
+    oxs[b] = ok ? (uint32_t)((b * 16 + i) * a.ldxs) : kOutside;
+  }
+  f32x4 acc[2][RB];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int b = 0; b < RB; ++b) acc[h][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t steps = (a.k + 127) / 128, each = (steps + NW - 1) / NW;
+  const uint32_t s_end = min(steps, (wave + 1) * each);
+  auto load = [](rsrc_t rs, uint32_t off, uint32_t o, bool in) __attribute__((always_inline)) {
+    return __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(in && off != kOutside ? off + o : kOutside), 0, 0);
+  };
+  // four scales from block s0 on: words that hold blocks the sum has
+  auto load_scales = [&](rsrc_t rs, uint32_t off, uint32_t s0) __attribute__((always_inline)) {
+    const uint32_t at = s0 & ~3u;
+    const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b32(rs, (int)(off != kOutside ? off + at : kOutside), 0, 0);
+    const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b32(
+        rs, (int)(off != kOutside && at + 4 < steps ? off + at + 4 : kOutside), 0, 0);
+    return u32pair{lo, hi};
+  };
+  for (uint32_t s0 = wave * each; s0 < s_end; s0 += kAhead) {
+    Frag8 fw[kAhead][2], fx[kAhead][RB];
+    u32pair cw[2], cx[RB];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) cw[h] = load_scales(rws, ows[h], s0);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) cx[b] = load_scales(rxs, oxs[b], s0);
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const uint32_t o = (s0 + n) * 128 + c * 64;
+        const bool in = s0 + n < s_end && o + q * 16 < a.k;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fw[n][h].half[c] = load(rw, ow[h], o, in);
+#pragma unroll
+        for (int b = 0; b < RB; ++b) fx[n][b].half[c] = load(rx, ox[b], o, in);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);  // every load is issued before the first result is used
+    int sw[2], sx[RB];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) sw[h] = (int)__builtin_amdgcn_alignbyte(cw[h][1], cw[h][0], s0 & 3);
+#pragma unroll
+    for (int b = 0; b < RB; ++b) sx[b] = (int)__builtin_amdgcn_alignbyte(cx[b][1], cx[b][0], s0 & 3);
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      if (s0 + n >= s_end) break;  // another wave's block, or none: its scale may be no number
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+          acc[h][b] = mma8<O>(fw[n][h], sw[h] >> (8 * n), fx[n][b], sx[b] >> (8 * n), acc[h][b]);
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int b = 0; b < RB; ++b) *reinterpret_cast<f32x4 *>(&part[wave][b * 16 + i][h * 16 + q * 4]) = acc[h][b];
+  __syncthreads();
+  constexpr int kLanes = kCols / kEw;
+  for (int t = threadIdx.x; t < RB * 16 * kLanes; t += NW * 64) {
+    const int r = t / kLanes, c = t % kLanes * kEw;
+    const uint32_t m = m0 + r;
+    if (m >= m_end) continue;
+    Vals v, u;
+#pragma unroll
+    for (int e = 0; e < kEw; ++e) {
+      v.v[e] = part[0][r][c + e];
+      if constexpr (GATED) u.v[e] = part[0][r][16 + c + e];
+    }
+    for (int o = 1; o < NW; ++o)
+#pragma unroll
+      for (int e = 0; e < kEw; ++e) {
+        v.v[e] += part[o][r][c + e];
+        if constexpr (GATED) u.v[e] += part[o][r][16 + c + e];
+      }
+    put_forward<O, GATED>(a, g, m, tn * kCols + c, v, u);
+  }
+}
+
+}  // namespace lin
+}  // namespace llc

@@ -23,11 +23,15 @@ ReduceScatter:
 """
 from __future__ import annotations
 
+from typing import NamedTuple, Optional
+
 import torch
 
+from . import llblock as lb
 from . import llcoll as ll
 from . import llmoe as lm
 
+E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 _DT = {torch.float32: ll.LL_F32, torch.bfloat16: ll.LL_BF16}
 # the C functions themselves: llmoe's wrappers add a call and nothing else here
 _c = ll.library()
@@ -383,3 +387,286 @@ def act_grad(dy, z, act: str, *, out=None, stream=None):
     ll.check(_c.ll_act_grad(dy.data_ptr(), ldy, z.data_ptr(), ldz, n, h, _dt(dy), lm.ACTS[act], out.data_ptr(), ldo,
                             _stream(stream, dev)), "ll_act_grad")
     return out
+
+
+# ---------------------------------------------------------------- 8 bits
+def scales_of(*shape, device="cuda", stream=None) -> torch.Tensor:
+    """Memory for scales of ``shape`` (the last is the number of blocks a row):
+    a row starts at a multiple of 4 bytes, which is what the calls below need."""
+    wide = _new(stream, *shape[:-1], (shape[-1] + 3) // 4 * 4, dtype=torch.uint8, device=device)
+    return wide.view(E8M0)[..., :shape[-1]]
+
+
+def _codes(t, name: str, dev: int, rows: int, cols: int) -> int:
+    return _mat(t, name, dev, rows, cols, E4M3)
+
+
+def _scale_rows(t, name: str, dev: int, rows: int, blocks: int) -> int:
+    """Checks a matrix of scales; its leading dimension."""
+    if t.dtype is not E8M0 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != blocks or t.get_device() != dev:
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected ({rows}, {blocks}) {E8M0} on the current GPU")
+    ld, unit = t.stride()
+    wide = (blocks + 3) // 4 * 4
+    if (blocks > 1 and unit != 1) or (rows > 1 and (ld % 4 or ld < blocks)) or t.data_ptr() % 4:
+        raise ValueError(f"{name}: rows of scales start at multiples of 4 bytes (moe.scales_of makes such memory)")
+    if rows < 2:
+        ld = wide
+    _readable(t, name, (rows - 1) * ld + wide)
+    return ld
+
+
+def _readable(t, name: str, nbytes: int) -> None:
+    """Scales are read four at a time: the last row's four have to be there."""
+    if t.numel() and t.untyped_storage().nbytes() - t.storage_offset() < nbytes:
+        raise ValueError(f"{name}: the last row's memory ends inside four scales (moe.scales_of makes longer rows)")
+
+
+def quantise(x, *, act: str = "none", offsets=None, out=None, scales=None, stream=None):
+    """(out, scales): act(x) in 8 bits (float8_e4m3fn [rows, features]) with a
+    power of two (float8_e8m0fnu [rows, ceil(features / 128)]) for each 128
+    features of a row; see ll_quantise.  With ``offsets``, rows behind the last
+    group are left as they are."""
+    dev = _device()
+    ldx = _mat(x, "x", dev)
+    if x.requires_grad:
+        _no_grad("x")
+    n, width = x.shape
+    if act in lm.GATED and width % 2:
+        raise ValueError(f"x: {width} features, a gated activation needs an even number")
+    h = width // 2 if act in lm.GATED else width
+    if out is None:
+        out = _new(stream, n, h, dtype=E4M3, device=x.device)
+    if scales is None:
+        scales = scales_of(n, (h + 127) // 128, device=x.device, stream=stream)
+    end = None
+    if offsets is not None:
+        end = _flat(offsets, "offsets", dev, offsets.numel(), torch.int32) + (offsets.numel() - 1) * 4
+    ldq, lds = _codes(out, "out", dev, n, h), _scale_rows(scales, "scales", dev, n, (h + 127) // 128)
+    ll.check(_c.ll_quantise(x.data_ptr(), ldx, n, end, h, _dt(x), lm.ACTS[act], out.data_ptr(), ldq,
+                            scales.data_ptr(), lds, _stream(stream, dev)), "ll_quantise")
+    return out, scales
+
+
+def _weight_scales(t, name: str, dev: int, groups: int, rows: int, blocks: int):
+    """(leading dimension, group stride) of scales [rows, blocks] or [groups, rows, blocks]."""
+    if t.dim() == 2 and groups == 1:
+        return _scale_rows(t, name, dev, rows, blocks), 0
+    if t.dim() != 3 or t.shape[0] != groups:
+        raise ValueError(f"{name}: {tuple(t.shape)}, expected ({groups}, {rows}, {blocks})")
+    ld = _scale_rows(t[0], name, dev, rows, blocks)
+    stride = t.stride(0) if groups > 1 else 0
+    if stride % 4:
+        raise ValueError(f"{name}: groups of scales start at multiples of 4 bytes")
+    _readable(t, name, (groups - 1) * stride + (rows - 1) * ld + (blocks + 3) // 4 * 4)
+    return ld, stride
+
+
+def quantise_weight(w, *, transpose: bool = False, out=None, scales=None, stream=None):
+    """(out, scales): a weight [out, in] or [groups, out, in] in 8 bits with a
+    power of two for each 128 x 128 of it; ``transpose``: as [.., in, out], for
+    the gradient of the product's input.  See ll_quantise_weight."""
+    dev = _device()
+    g, o, i, ldw, gs = _weight(w, dev)
+    if w.requires_grad:
+        _no_grad("w")
+    rows, cols = (i, o) if transpose else (o, i)
+    lead = () if w.dim() == 2 else (g,)
+    if out is None:
+        out = _new(stream, *lead, rows, cols, dtype=E4M3, device=w.device)
+    if scales is None:
+        scales = scales_of(*lead, (rows + 127) // 128, (cols + 127) // 128, device=w.device, stream=stream)
+    if out.dtype is not E4M3 or out.dim() != w.dim():
+        raise ValueError(f"out: {tuple(out.shape)} {out.dtype}, expected {(*lead, rows, cols)} {E4M3}")
+    g2, r2, c2, ldq, qs = _weight(out, dev, "out")
+    if (g2, r2, c2) != (g, rows, cols):
+        raise ValueError(f"out: {tuple(out.shape)}, expected {(*lead, rows, cols)}")
+    lds, ss = _weight_scales(scales, "scales", dev, g, (rows + 127) // 128, (cols + 127) // 128)
+    ll.check(_c.ll_quantise_weight(w.data_ptr(), ldw, gs, g, o, i, _dt(w), int(transpose), out.data_ptr(), ldq, qs,
+                                   scales.data_ptr(), lds, ss, _stream(stream, dev)), "ll_quantise_weight")
+    return out, scales
+
+
+def linear8(x, x_scales, w, w_scales, *, bias=None, act: str = "none", residual=None, offsets=None, dtype=None,
+            out=None, z=None, stream=None):
+    """``linear`` of rows and weights in 8 bits (``quantise``,
+    ``quantise_weight``): act(x w^T + bias) + residual, by groups of rows where
+    ``offsets`` is given.  bias, residual, z and the result are of type
+    ``dtype`` (bfloat16 unless ``out`` or this says otherwise).  See ll_linear8.
+
+    The gradient of x is ``linear8`` of the rows' gradient and the transposed
+    weight, both in 8 bits, then ``act_grad`` through an activation below; the
+    weight's is ``linear_grad_w`` on the rows as they were before."""
+    dev = _device()
+    n = x.shape[0]
+    if w.dtype is not E4M3:
+        raise ValueError(f"w: {w.dtype}, expected {E4M3}")
+    g, o, i, ldw, gs = _weight(w, dev)
+    ldx = _codes(x, "x", dev, n, i)
+    kb = (i + 127) // 128
+    ldxs = _scale_rows(x_scales, "x_scales", dev, n, kb)
+    ldws, ss = _weight_scales(w_scales, "w_scales", dev, g, (o + 127) // 128, kb)
+    if (bias is not None and bias.requires_grad) or (residual is not None and residual.requires_grad):
+        _no_grad("bias or residual")
+    width = o // 2 if act in lm.GATED else o
+    if dtype is None:
+        dtype = torch.bfloat16 if out is None else out.dtype
+    if out is None:
+        out = _new(stream, n, width, dtype=dtype, device=x.device)
+    ldy = _mat(out, "out", dev, n, width, dtype)
+    ldr = ldz = max(o, 1)
+    rp = zp = None
+    if residual is not None:
+        ldr, rp = _mat(residual, "residual", dev, n, width, dtype), residual.data_ptr()
+    if z is not None:
+        ldz, zp = _mat(z, "z", dev, n, o, dtype), z.data_ptr()
+    d = lm.LLLinearDesc(lm.DESC_SIZE, _dt(out), lm.ACTS[act], g, n, i, o, _offsets(offsets, g, dev), ldx, ldw, gs, ldy,
+                        ldz, ldr)
+    key = (d.dt, d.act, g, n, i, o, offsets is None, ldx & 15, ldw & 15, gs & 15)
+    need = _needs8.get(key)
+    if need is None:
+        st, need = lb.ll_linear8_bytes(d)
+        ll.check(st, "ll_linear8_bytes")
+        if len(_needs8) >= 4096:
+            _needs8.clear()
+        _needs8[key] = need
+    ws = _new(stream, need, dtype=torch.uint8, device=x.device) if need else None
+    ll.check(_c.ll_linear8(d, x.data_ptr(), x_scales.data_ptr(), ldxs, w.data_ptr(), w_scales.data_ptr(), ldws, ss,
+                           None if bias is None else _flat(bias, "bias", dev, g * o, dtype), rp, out.data_ptr(), zp,
+                           None if ws is None else ws.data_ptr(), need, _stream(stream, dev)), "ll_linear8")
+    return out
+
+
+_needs8: dict = {}  # workspace bytes by shape (host arithmetic only)
+
+
+# ---------------------------------------------------------------- norms around a block
+class Normed(NamedTuple):
+    h: Optional[torch.Tensor]         # the next block's input
+    r: Optional[torch.Tensor]         # the residual stream
+    q: Optional[torch.Tensor]         # h in 8 bits
+    q_scales: Optional[torch.Tensor]
+
+
+class NormGrads(NamedTuple):
+    dr: torch.Tensor                  # of the residual stream before and behind the block's output was added
+    dy: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dweight: Optional[torch.Tensor]
+    dpost: Optional[torch.Tensor]
+
+
+def _norm_weights(post, weight, rows, dev: int):
+    """(their type's code, addresses) of a norm's weights."""
+    at, kind = [], None
+    for t, name in ((post, "post"), (weight, "weight")):
+        if t is None:
+            at.append(None)
+            continue
+        if t.dtype not in (rows.dtype, torch.float32) or (kind is not None and t.dtype is not kind):
+            raise ValueError(f"{name}: {t.dtype}, expected {rows.dtype} or float32, the same for post and weight")
+        kind = t.dtype
+        at.append(_flat(t, name, dev, rows.shape[1], t.dtype))
+    return _DT[kind or torch.float32], at
+
+
+def norm(y, weight=None, *, residual=None, gate=None, scale: float = 1.0, post=None, eps: float = 1e-6,
+         quantised: bool = False, h=None, r=None, q=None, q_scales=None, stream=None) -> Normed:
+    """What stands between two blocks, in one pass (see ll_norm):
+
+        u = post * y / sqrt(mean(y^2) + eps)        the block's own norm (without post: u = y)
+        r = residual + scale * gate * u             gate: float32, one a token
+        h = weight * r / sqrt(mean(r^2) + eps)      the next block's input (without weight: none)
+
+    ``norm(y, weight).h`` is a plain norm of y; r is computed where anything is
+    done to y, or where its memory is given.  ``quantised`` (or q given): h in 8
+    bits too, as ``quantise`` makes it.  r may be the residual's own memory."""
+    dev = _device()
+    ldy = _mat(y, "y", dev)
+    n, f = y.shape
+    for t, name in ((y, "y"), (residual, "residual"), (gate, "gate"), (post, "post"), (weight, "weight")):
+        if t is not None and t.requires_grad:
+            _no_grad(name)
+    wdt, (pp, wp) = _norm_weights(post, weight, y, dev)
+    if (quantised or q is not None or h is not None) and weight is None:
+        raise ValueError("weight is needed for h")
+    if r is None and (weight is None or residual is not None or gate is not None or post is not None or scale != 1):
+        r = _new(stream, n, f, dtype=y.dtype, device=y.device)
+    if h is None and weight is not None:
+        h = _new(stream, n, f, dtype=y.dtype, device=y.device)
+    if q is None and quantised:
+        q = _new(stream, n, f, dtype=E4M3, device=y.device)
+    if q is not None and q_scales is None:
+        q_scales = scales_of(n, (f + 127) // 128, device=y.device, stream=stream)
+    d = lb.LLNormDesc(lb.NORM_DESC_SIZE, _dt(y), wdt, eps, scale, n, f, ldy,
+                      f if residual is None else _mat(residual, "residual", dev, n, f, y.dtype),
+                      f if r is None else _mat(r, "r", dev, n, f, y.dtype),
+                      f if h is None else _mat(h, "h", dev, n, f, y.dtype),
+                      f if q is None else _codes(q, "q", dev, n, f),
+                      0 if q is None else _scale_rows(q_scales, "q_scales", dev, n, (f + 127) // 128), f, f, f)
+    ll.check(_c.ll_norm(d, y.data_ptr(), None if residual is None else residual.data_ptr(),
+                        None if gate is None else _flat(gate, "gate", dev, n, torch.float32), pp, wp,
+                        None if r is None else r.data_ptr(), None if h is None else h.data_ptr(),
+                        None if q is None else q.data_ptr(), None if q is None else q_scales.data_ptr(),
+                        _stream(stream, dev)), "ll_norm")
+    return Normed(h, r, q, q_scales if q is not None else None)
+
+
+def norm_grad(dh, r, weight=None, *, dr=None, y=None, gate=None, scale: float = 1.0, post=None, eps: float = 1e-6,
+              dr_out=None, dy=None, dgate=None, dweight=None, dpost=None, add: bool = False, stream=None) -> NormGrads:
+    """The gradients of ``norm`` from those of h (``dh``) and of r (``dr``), for
+    the r it returned (y itself where it returned none); see ll_norm_grad.  dr
+    of the result is the residual's gradient.  dy is computed where the block's
+    output was normed, gated or scaled, or where its memory is given (else it is
+    the result's dr); dgate and dpost where there is a gate and a post, dweight
+    (and dpost) in float32, ``add``: added to what their memory holds.  Without
+    ``weight``, dh and r are None."""
+    dev = _device()
+    rows = dr if weight is None else dh
+    if rows is None or (weight is None and dh is not None):
+        raise ValueError("dh goes with weight; without, dr is needed")
+    ld = _mat(rows, "dr" if weight is None else "dh", dev)
+    n, f = rows.shape
+    dt = rows.dtype
+    wdt, (pp, wp) = _norm_weights(post, weight, rows, dev)
+    if y is None and (post is not None or gate is not None):
+        raise ValueError("y is needed for the gradients of a gate and of the block's own norm")
+    if add and ((weight is not None and dweight is None) or (post is not None and dpost is None)):
+        raise ValueError("add needs the memory that is added to")
+
+    def fresh(*shape, dtype=dt):
+        return _new(stream, *shape, dtype=dtype, device=rows.device)
+
+    changed = post is not None or gate is not None or scale != 1
+    if dr_out is None:
+        dr_out = fresh(n, f)
+    if dy is None and changed:
+        dy = fresh(n, f)
+    if gate is not None and dgate is None:
+        dgate = fresh(n, dtype=torch.float32)
+    if weight is not None and dweight is None:
+        dweight = fresh(f, dtype=torch.float32)
+    if post is not None and dpost is None:
+        dpost = fresh(f, dtype=torch.float32)
+
+    def mat(t, name):
+        return f if t is None else _mat(t, name, dev, n, f, dt)
+
+    def flat(t, name, numel):
+        return None if t is None else _flat(t, name, dev, numel, torch.float32)
+
+    def at(t):
+        return None if t is None else t.data_ptr()
+
+    d = lb.LLNormDesc(lb.NORM_DESC_SIZE, _DT[dt] if dt in _DT else _dt(rows), wdt, eps, scale, n, f, mat(y, "y"), f,
+                      mat(r, "r"), f if weight is None else ld, f, 0, mat(dr, "dr"), mat(dr_out, "dr_out"),
+                      mat(dy, "dy"))
+    ws, need = None, 0
+    if dweight is not None or dpost is not None:
+        st, need = lb.ll_norm_bytes(d)
+        ll.check(st, "ll_norm_bytes")
+        ws = _new(stream, need, dtype=torch.uint8, device=rows.device)
+    ll.check(_c.ll_norm_grad(d, at(dh), at(r) if weight is not None else None, at(dr), at(y), flat(gate, "gate", n), pp,
+                             wp, at(dr_out), at(dy), flat(dgate, "dgate", n), flat(dweight, "dweight", f),
+                             flat(dpost, "dpost", f), lm.LL_GRAD_ADD if add else 0, at(ws), need,
+                             _stream(stream, dev)), "ll_norm_grad")
+    return NormGrads(dr_out, dy if dy is not None else dr_out, dgate, dweight, dpost)

@@ -1,0 +1,142 @@
+"""A weight update on torch tensors (``ll_adamw`` of ``include/llblock.h``).
+
+    opt = AdamW(params, lr=3e-4, weight_decay=0.1, states="8bit")
+    opt.step(grads)
+
+A step is one small launch and one for each 40 tensors, on the current stream
+(or ``stream``).  It counts in device memory, so that a step captured into a
+graph is the next one each time the graph is replayed.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence
+
+import torch
+
+from . import llblock as lb
+from . import llcoll as ll
+from .moe import _device, _flat, _stream
+
+_DT = {torch.float32: ll.LL_F32, torch.bfloat16: ll.LL_BF16}
+STATES = {"f32": 32, "8bit": 8}
+_TYPES = {32: (torch.float32, torch.float32), 8: (torch.float8_e4m3fn, torch.float8_e5m2)}
+
+
+class AdamW:
+    """Adam with decoupled weight decay over ``params`` (contiguous float32 or
+    bfloat16 tensors of one GPU, which are updated in place); see ll_adamw.
+
+    A bfloat16 parameter has a float32 master, made from it.  The states of all
+    parameters lie in one tensor each, a parameter's at a multiple of 128
+    (``offsets``): ``m`` and ``v`` in float32, or with states="8bit" m as
+    float8_e4m3fn and v as float8_e5m2 with a power of two (float8_e8m0fnu) for
+    each 128 values.  States in 8 bits are rounded at random, by ``seed``.
+    Values between a parameter's last and the next multiple of 128 stay 0.
+
+    ``state``: a ``state_dict()`` to go on from, whose tensors are used, not
+    copied.  The options may be changed between steps (``opt.lr = ...``)."""
+
+    def __init__(self, params: Sequence[torch.Tensor], *, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 0.0, states: str = "f32", seed: int = 0, state: Optional[dict] = None):
+        self.params = list(params)
+        self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
+        self.seed = seed
+        if states not in STATES:
+            raise ValueError(f"states: {states!r}, expected one of {sorted(STATES)}")
+        self.bits = STATES[states]
+        if not self.params:
+            raise ValueError("params: none")
+        dev = self.params[0].get_device()
+        self._dev = dev
+        seen, self.offsets, total = set(), [], 0
+        for i, p in enumerate(self.params):
+            if p.dtype not in _DT:
+                raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(p.dtype))
+            if dev < 0 or p.get_device() != dev or not p.is_contiguous():
+                raise ValueError(f"params[{i}]: a contiguous tensor is needed, all on one GPU")
+            if p.numel() and p.data_ptr() in seen:
+                raise ValueError(f"params[{i}]: given twice")
+            seen.add(p.data_ptr())
+            self.offsets.append(total)
+            total += (p.numel() + 127) // 128 * 128
+        device = self.params[0].device
+        mt, vt = _TYPES[self.bits]
+        eight = self.bits == 8
+        if state is None:
+            state = {"masters": [p.detach().float() if p.dtype is torch.bfloat16 else None for p in self.params],
+                     "m": torch.zeros(total, dtype=torch.uint8, device=device).view(mt) if eight
+                     else torch.zeros(total, dtype=mt, device=device),
+                     "v": torch.zeros(total, dtype=torch.uint8, device=device).view(vt) if eight
+                     else torch.zeros(total, dtype=vt, device=device),
+                     "m_scales": _ones(total // 128, device) if eight else None,
+                     "v_scales": _ones(total // 128, device) if eight else None,
+                     "count": torch.zeros(1, dtype=torch.int32, device=device)}
+        self._check(state, total, mt, vt)
+        self.masters, self.m, self.v = state["masters"], state["m"], state["v"]
+        self.m_scales, self.v_scales, self.count = state["m_scales"], state["v_scales"], state["count"]
+        self._work = torch.empty(lb.LL_ADAMW_WORKSPACE, dtype=torch.uint8, device=device)
+        self._table = (lb.LLAdamwTensor * len(self.params))()
+        es = 1 if eight else 4
+        for t, p, w, at in zip(self._table, self.params, self.masters, self.offsets):
+            t.param, t.n, t.at, t.dt = p.data_ptr(), p.numel(), at, _DT[p.dtype]
+            t.master = None if w is None else w.data_ptr()
+            t.m, t.v = self.m.data_ptr() + at * es, self.v.data_ptr() + at * es
+            if eight:
+                t.m_scales, t.v_scales = self.m_scales.data_ptr() + at // 128, self.v_scales.data_ptr() + at // 128
+
+    def _check(self, state: dict, total: int, mt, vt) -> None:
+        dev = self._dev
+        if len(state["masters"]) != len(self.params):
+            raise ValueError(f"masters: {len(state['masters'])}, expected {len(self.params)}")
+        for i, (p, w) in enumerate(zip(self.params, state["masters"])):
+            if (w is None) != (p.dtype is torch.float32):
+                raise ValueError(f"masters[{i}]: one goes with a bfloat16 parameter")
+            if w is not None:
+                _flat(w, f"masters[{i}]", dev, p.numel(), torch.float32)
+        _flat(state["m"], "m", dev, total, mt)
+        _flat(state["v"], "v", dev, total, vt)
+        _flat(state["count"], "count", dev, 1, torch.int32)
+        for name in ("m_scales", "v_scales"):
+            if self.bits == 8:
+                _flat(state[name], name, dev, total // 128, torch.float8_e8m0fnu)
+            elif state[name] is not None:
+                raise ValueError(f"{name}: states in float32 have none")
+
+    def state_dict(self) -> dict:
+        """The state's own tensors (``AdamW(..., state=...)`` goes on from them)."""
+        return {"masters": self.masters, "m": self.m, "v": self.v, "m_scales": self.m_scales,
+                "v_scales": self.v_scales, "count": self.count}
+
+    def step(self, grads: Sequence[torch.Tensor], *, lr=None, grad_scale=None, stream=None) -> None:
+        """One update.  ``grads``: one contiguous float32 or bfloat16 tensor a
+        parameter.  ``lr``: this step's, a number or a float32 tensor of one
+        value; ``grad_scale``: a float32 tensor of one value that gradients are
+        multiplied by.  Tensors are read when the step runs, so a captured step
+        takes what they hold then."""
+        dev = _device()
+        if dev != self._dev:
+            raise ValueError("the parameters are not on the current GPU")
+        table = self._table
+        if len(grads) != len(table):
+            raise ValueError(f"grads: {len(grads)}, expected {len(table)}")
+        for i, (t, g) in enumerate(zip(table, grads)):
+            dt = _DT.get(g.dtype)
+            if dt is None:
+                raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(g.dtype))
+            if g.numel() != t.n or g.get_device() != dev or not g.is_contiguous():
+                raise ValueError(f"grads[{i}]: a contiguous tensor of {t.n} values on the parameters' GPU is needed")
+            t.grad, t.gdt = g.data_ptr(), dt
+        rate, rate_at = self.lr if lr is None else lr, None
+        if isinstance(rate, torch.Tensor):
+            rate, rate_at = 0.0, _flat(rate, "lr", dev, 1, torch.float32)
+        d = lb.LLAdamwDesc(lb.ADAMW_DESC_SIZE, self.bits, rate, self.betas[0], self.betas[1], self.eps,
+                           self.weight_decay, self.seed & 0xFFFFFFFF)
+        ll.check(lb.ll_adamw(d, table, len(table), self.count.data_ptr(), rate_at,
+                             None if grad_scale is None else _flat(grad_scale, "grad_scale", dev, 1, torch.float32),
+                             self._work.data_ptr(), lb.LL_ADAMW_WORKSPACE, _stream(stream, dev)), "ll_adamw")
+
+
+def _ones(n: int, device) -> torch.Tensor:
+    """Scales of 1."""
+    return torch.full((n,), 127, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
