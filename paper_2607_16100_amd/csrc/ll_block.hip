@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "../../include/llblock.h"
 #include "ll_block.hpp"
@@ -74,11 +75,11 @@ struct NormShape {
   uint32_t tpr, chunks, rows;
 };
 
-NormShape norm_shape(size_t rows, size_t features) {
+NormShape norm_shape(size_t rows, size_t features, bool grad) {
   if (features <= 512) return {64, 1, 4};
   if (features <= 2048) return {256, 1, 1};
   // few rows: more threads a row, whose loads are all under way at once
-  if (features <= 8192 && rows <= 512) return {1024, 1, 1};
+  if (features <= 8192 && (grad || rows <= 512)) return {1024, 1, 1};
   if (features <= 4096) return {256, 2, 1};
   if (features <= 8192) return {256, 4, 1};
   return {1024, 4, 1};
@@ -87,9 +88,10 @@ NormShape norm_shape(size_t rows, size_t features) {
 template <typename T, bool GRAD>
 norm_fn pick_norm(const NormShape &s, bool vec) {
   if (s.tpr == 64) return norm_of<T, GRAD, 64, 1>(vec);
-  if (s.tpr == 256)
-    return s.chunks == 1 ? norm_of<T, GRAD, 256, 1>(vec)
-                         : s.chunks == 2 ? norm_of<T, GRAD, 256, 2>(vec) : norm_of<T, GRAD, 256, 4>(vec);
+  if (s.tpr == 256) {
+    if (s.chunks == 1) return norm_of<T, GRAD, 256, 1>(vec);
+    if constexpr (!GRAD) return s.chunks == 2 ? norm_of<T, GRAD, 256, 2>(vec) : norm_of<T, GRAD, 256, 4>(vec);
+  }
   return s.chunks == 1 ? norm_of<T, GRAD, 1024, 1>(vec) : norm_of<T, GRAD, 1024, 4>(vec);
 }
 
@@ -252,7 +254,7 @@ int ll_norm(const ll_norm_desc *d, const void *y, const void *x, const float *ga
   a.w32 = d->wdt == LL_F32;
   const bool vec = rows16(y, d->ldy, es) && rows16(x, d->ldx, es) && rows16(r, d->ldr, es) && rows16(h, d->ldh, es) &&
                    rows8(q, d->ldq) && aligned(post, 16) && aligned(weight, 16);
-  const NormShape s = norm_shape(n, f);
+  const NormShape s = norm_shape(n, f, false);
   const norm_fn fn = d->dt == LL_F32 ? pick_norm<float, false>(s, vec) : pick_norm<__bf16, false>(s, vec);
   const uint32_t threads = s.tpr < 256 ? 256 : s.tpr;
   const uint64_t grid = (n + s.rows - 1) / s.rows;
@@ -265,7 +267,7 @@ int ll_norm_bytes(const ll_norm_desc *d, size_t *bytes) {
   if (bytes == nullptr) return LL_ERR_INVALID;
   const int st = check_norm(d);
   if (st != LL_OK) return st;
-  const NormShape s = norm_shape(d->rows, d->features);
+  const NormShape s = norm_shape(d->rows, d->features, true);
   *bytes = (size_t)2 * grad_grid(s, d->rows) * s.rows * d->features * 4;
   return LL_OK;
 }
@@ -329,7 +331,7 @@ int ll_norm_grad(const ll_norm_desc *d, const void *dh, const void *r, const voi
   a.eps = d->eps;
   a.scale = d->scale;
   a.w32 = d->wdt == LL_F32;
-  const NormShape s = norm_shape(n, f);
+  const NormShape s = norm_shape(n, f, true);
   const uint32_t grid = grad_grid(s, n);
   if (n != 0 && (sums || dr_out != nullptr || dy != nullptr || dgate != nullptr)) {
     // (the shares' rows are `features` long)
@@ -372,7 +374,7 @@ int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t coun
     if (!aligned(t.param, esize(t.dt)) || !aligned(t.grad, esize(t.gdt)) || !aligned(t.master, 4)) return LL_ERR_INVALID;
     if (!eight && (!aligned(t.m, 4) || !aligned(t.v, 4))) return LL_ERR_INVALID;
   }
-  AdamwBegin b{step, lr_ptr, grad_scale, (AdamwCoef *)workspace, d->lr, d->beta1, d->beta2, d->decay, d->seed};
+  AdamwBegin b{step, lr_ptr, grad_scale, (AdamwCoef *)workspace, d->lr, log2(d->beta1), log2(d->beta2), d->decay, d->seed};
   hipLaunchKernelGGL(k_adamw_begin, dim3(1), dim3(64), 0, (hipStream_t)stream, b);
   int st = launch_status();
   AdamwArgs a{};

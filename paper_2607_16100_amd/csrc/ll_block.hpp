@@ -37,17 +37,47 @@ __device__ __forceinline__ void put_codes(uint8_t *p, const uint32_t *w, int lef
   }
 }
 
-// kW values of a block of 16 lanes to codes; returns the block's scale.
-__device__ __forceinline__ uint32_t quantise8(const lin::Vals &v, uint32_t *w) {
+// The largest magnitude's bits; at least those of Infinity where a value is not finite.
+__device__ __forceinline__ uint32_t top_bits(const lin::Vals &v) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < kW; ++i) top = max(top, finite_bits(v.v[i]));
+  for (int i = 0; i < kW; ++i) top = max(top, (uint32_t)__float_as_int(v.v[i]) & 0x7FFFFFFFu);
+  return top;
+}
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// kW values of a block of 16 lanes to codes; returns the block's scale.  Every
+// value is looked at one by one only in a wave that has one that is not finite.
+__device__ __forceinline__ uint32_t quantise8(const lin::Vals &v, uint32_t *w) {
+  uint32_t top = top_bits(v);
+  if (__any(top >= kInfBits)) {
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < kW; ++i) top = max(top, finite_bits(v.v[i]));
+    const uint32_t s = scale_of<8>(max16(top));
+    const float inv = scale_inverse(s);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      w[i] = to_e4m3(v.v[4 * i] * inv, v.v[4 * i + 1] * inv) | to_e4m3(v.v[4 * i + 2] * inv, v.v[4 * i + 3] * inv) << 16;
+    return s;
+  }
   const uint32_t s = scale_of<8>(max16(top));
   const float inv = scale_inverse(s);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    w[i] = to_e4m3(v.v[4 * i] * inv, v.v[4 * i + 1] * inv) | to_e4m3(v.v[4 * i + 2] * inv, v.v[4 * i + 3] * inv) << 16;
+  for (int i = 0; i < 2; ++i) w[i] = pack_e4m3(v.v[4 * i] * inv, v.v[4 * i + 1] * inv, v.v[4 * i + 2] * inv, v.v[4 * i + 3] * inv);
   return s;
+}
+
+// Activations in front of the rounding to 8 bits: the exponential and the
+// reciprocal to two units in the last place instead of the library's division,
+// which was most of the kernel's time (16384 x 2 x 2048 through SwiGLU: 57 us).
+__device__ __forceinline__ void act_rows(lin::Vals &v, int act) {
+  if (act == LL_ACT_SILU || act == LL_ACT_SWIGLU) {
+#pragma unroll
+    for (int i = 0; i < kW; ++i) v.v[i] *= __builtin_amdgcn_rcpf(1.f + exp_f32(-v.v[i]));
+  } else {
+    lin::act8(v, act);
+  }
 }
 
 // ---------------------------------------------------------------- rows
@@ -84,7 +114,7 @@ __global__ __launch_bounds__(256) void k_quantise(QuantArgs a) {
   }
 #pragma unroll
   for (int n = 0; n < U; ++n) {
-    lin::act8(v[n], a.act);
+    act_rows(v[n], a.act);
     if (gate) {
 #pragma unroll
       for (int i = 0; i < kW; ++i) v[n].v[i] *= u[n].v[i];
@@ -210,12 +240,17 @@ __device__ __forceinline__ void row_sums(float *v, float *red) {
       for (int n = 0; n < N; ++n) red[n * kWaves + threadIdx.x / 64] = v[n];
     }
     __syncthreads();
+    // (lane i of 4 or 16 takes wave i's part; those 4 or 16 lanes add them up)
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      float s = red[n * kWaves];
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) s += red[n * kWaves + w];
-      v[n] = s;
+      float s = red[n * kWaves + threadIdx.x % kWaves];
+      static_assert(kWaves == 4 || kWaves == 16, "a quad or a row of lanes");
+      if constexpr (kWaves == 16) {
+        v[n] = group_sum<16>(s);
+      } else {
+        s += dpp_f32<0xB1>(s);
+        v[n] = s + dpp_f32<0x4E>(s);
+      }
     }
   }
 }
@@ -227,38 +262,36 @@ __device__ __forceinline__ lin::Vals get_weight(const void *w, bool w32, uint32_
   return w32 ? get<float, VEC>((const float *)w + at, left) : get<T, VEC>((const T *)w + at, left);
 }
 
+// A thread's only chunk: everything the row needs is asked for at once, weights
+// too.  Several: the weights are read when they are used, from L2, and the
+// registers go to more rows a CU (8192 x 7168 bfloat16, residual and norm: 118
+// us with all of it in registers).
 template <typename T, bool VEC, int TPR, int C>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormArgs a) {
+  constexpr bool kEarly = C == 1;
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
   __shared__ float red[2][TPR / 64];
   const uint32_t t = threadIdx.x % TPR;
   const uint32_t row = blockIdx.x * kRows + threadIdx.x / TPR;
   if (kRows > 1 && row >= a.rows) return;  // (a wave has a row then, and no barrier comes)
-  lin::Vals v[C], x[C], post[C], weight[C];
+  lin::Vals v[C], x[C], post[kEarly ? C : 1], weight[kEarly ? C : 1];
   const float n = (float)a.features;
   auto left = [&](int c) { return (int)a.features - (int)((c * TPR + t) * kW); };
-  // everything the row needs is asked for at once
 #pragma unroll
   for (int c = 0; c < C; ++c) v[c] = get<T, VEC>((const T *)a.y + row * a.ldy + (c * TPR + t) * kW, left(c));
   if (a.x != nullptr) {
 #pragma unroll
     for (int c = 0; c < C; ++c) x[c] = get<T, VEC>((const T *)a.x + row * a.ldx + (c * TPR + t) * kW, left(c));
   }
-  if (a.post != nullptr) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) post[c] = get_weight<T, VEC>(a.post, a.w32, (c * TPR + t) * kW, left(c));
-  }
-  if (a.weight != nullptr) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) weight[c] = get_weight<T, VEC>(a.weight, a.w32, (c * TPR + t) * kW, left(c));
-  }
+  if (kEarly && a.post != nullptr) post[0] = get_weight<T, VEC>(a.post, a.w32, t * kW, left(0));
+  if (kEarly && a.weight != nullptr) weight[0] = get_weight<T, VEC>(a.weight, a.w32, t * kW, left(0));
   const float by = a.gate != nullptr ? a.gate[row] * a.scale : a.scale;
   auto squares = [&](float *s) {
     *s = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int i = 0; i < kW; ++i) *s += v[c].v[i] * v[c].v[i];
+      for (int i = 0; i < kW; ++i) *s = __builtin_fmaf(v[c].v[i], v[c].v[i], *s);
   };
   float s;
   if (a.post != nullptr) {
@@ -266,9 +299,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormArgs a) {
     row_sums<TPR, 1>(&s, red[0]);
     const float rstd = 1.f / sqrtf(s / n + a.eps);
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      if constexpr (!kEarly) post[0] = get_weight<T, VEC>(a.post, a.w32, (c * TPR + t) * kW, left(c));
 #pragma unroll
-      for (int i = 0; i < kW; ++i) v[c].v[i] = v[c].v[i] * rstd * post[c].v[i];
+      for (int i = 0; i < kW; ++i) v[c].v[i] = v[c].v[i] * rstd * post[0].v[i];
+    }
   }
 #pragma unroll
   for (int c = 0; c < C; ++c)
@@ -288,8 +323,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormArgs a) {
   const float rstd = 1.f / sqrtf(s / n + a.eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
+    if constexpr (!kEarly) weight[0] = get_weight<T, VEC>(a.weight, a.w32, (c * TPR + t) * kW, left(c));
 #pragma unroll
-    for (int i = 0; i < kW; ++i) v[c].v[i] = v[c].v[i] * rstd * weight[c].v[i];
+    for (int i = 0; i < kW; ++i) v[c].v[i] = v[c].v[i] * rstd * weight[0].v[i];
     if (a.h != nullptr) put<T, VEC>((T *)a.h + row * a.ldh + (c * TPR + t) * kW, v[c], left(c));
     if (a.q != nullptr) {  // 16 lanes have a block, whole or to the row's end
       uint32_t w[2];
@@ -303,61 +339,109 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormArgs a) {
   }
 }
 
+// kW values of a row as they lie in memory, loaded while another row is worked on.
+template <typename T, bool VEC>
+struct Chunk {
+  union {
+    T e[kW];
+    u32x4 raw[kW * sizeof(T) / 16];
+  };
+  __device__ __forceinline__ void load(const T *p, int left) {
+    if (VEC && left >= kW) {
+#pragma unroll
+      for (int i = 0; i < (int)(kW * sizeof(T) / 16); ++i) raw[i] = reinterpret_cast<const u32x4 *>(p)[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kW; ++i) e[i] = i < left ? p[i] : (T)0.f;
+    }
+  }
+  __device__ __forceinline__ lin::Vals vals() const {
+    lin::Vals v;
+#pragma unroll
+    for (int i = 0; i < kW; ++i) v.v[i] = Num<T>::get(e[i]);
+    return v;
+  }
+};
+
 // The gradients: a workgroup takes rows blockIdx.x, + gridDim.x, ... and keeps
 // its share of dweight and dpost in registers; k_norm_join adds the shares up.
 //
-// With n = r / d, d = sqrt(mean(r^2) + eps): dr_out = dr + (weight dh - n
-// mean(n weight dh)) / d, and the same once more from dr_out to y.  Two rounds
+// With u = r / d, d = sqrt(mean(r^2) + eps): dr_out = dr + (weight dh - u
+// mean(u weight dh)) / d, and the same once more from dr_out to y.  Two rounds
 // of sums a row: r^2, weight dh r and y^2; then dr_out post y, which gives both
 // dgate and what dy needs.
+//
+// The next row is loaded while one is worked on, and a thread has one chunk of
+// it (with four chunks, all read when their row comes: 8192 x 7168 bfloat16 with
+// post and gate 460 us).  Rows of more than 8192 features have four.
 template <typename T, bool VEC, int TPR, int C>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a) {
   constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
+  constexpr bool kHold = C == 1;  // the weights stay in registers
   __shared__ float red[2][2][3 * (TPR / 64)];
   const uint32_t t = threadIdx.x % TPR;
-  const float n = (float)a.features, rn = 1.f / n;
-  const uint32_t lane_row = threadIdx.x / TPR;
+  const float rn = 1.f / (float)a.features;
+  const uint32_t lane_row = threadIdx.x / TPR, step = gridDim.x * kRows;
   auto left = [&](int c) { return (int)a.features - (int)((c * TPR + t) * kW); };
-  auto at = [&](int c) { return (c * TPR + t) * kW; };
+  auto at = [&](int c) { return left(c) > 0 ? (c * TPR + t) * kW : 0u; };
   const bool with_y = a.post != nullptr || a.dgate != nullptr;
-  lin::Vals dw[C], dp[C];
+  lin::Vals dw[C], dp[C], weight[1], post[1];
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int i = 0; i < kW; ++i) dw[c].v[i] = dp[c].v[i] = 0.f;
-  uint32_t turn = 0;
-  for (uint32_t row = blockIdx.x * kRows + lane_row; row < a.rows; row += gridDim.x * kRows, ++turn) {
-    float(*sums)[3 * (TPR / 64)] = red[turn & 1];
-    lin::Vals r[C], g[C], y[C], d[C];
+  if constexpr (kHold) {
+    if (a.weight != nullptr) weight[0] = get_weight<T, VEC>(a.weight, a.w32, at(0), left(0));
+    if (a.post != nullptr) post[0] = get_weight<T, VEC>(a.post, a.w32, at(0), left(0));
+  }
+  Chunk<T, VEC> nr[C], ng[C], ny[C], nd[C];
+  auto load = [&](uint32_t row) {
     if (a.weight != nullptr) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        r[c] = get<T, VEC>((const T *)a.r + row * a.ldr + at(c), left(c));
-        g[c] = get<T, VEC>((const T *)a.dh + row * a.ldh + at(c), left(c));
+        nr[c].load((const T *)a.r + row * a.ldr + at(c), left(c));
+        ng[c].load((const T *)a.dh + row * a.ldh + at(c), left(c));
       }
     }
     if (a.dr != nullptr) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) d[c] = get<T, VEC>((const T *)a.dr + row * a.ldd + at(c), left(c));
-    } else {
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < kW; ++i) d[c].v[i] = 0.f;
+      for (int c = 0; c < C; ++c) nd[c].load((const T *)a.dr + row * a.ldd + at(c), left(c));
     }
     if (with_y) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) y[c] = get<T, VEC>((const T *)a.y + row * a.ldy + at(c), left(c));
+      for (int c = 0; c < C; ++c) ny[c].load((const T *)a.y + row * a.ldy + at(c), left(c));
     }
+  };
+  uint32_t row = blockIdx.x * kRows + lane_row;
+  if (row < a.rows) load(row);
+  uint32_t turn = 0;
+  for (; row < a.rows; row += step, ++turn) {
+    float(*sums)[3 * (TPR / 64)] = red[turn & 1];
+    lin::Vals r[C], g[C], y[C], d[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (a.weight != nullptr) {
+        r[c] = nr[c].vals();
+        g[c] = ng[c].vals();
+      }
+      if (with_y) y[c] = ny[c].vals();
+      if (a.dr != nullptr) {
+        d[c] = nd[c].vals();
+      } else {
+#pragma unroll
+        for (int i = 0; i < kW; ++i) d[c].v[i] = 0.f;
+      }
+    }
+    if (row + step < a.rows) load(row + step);
     float s[3] = {0.f, 0.f, 0.f};
     if (a.weight != nullptr) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const lin::Vals w = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+        if constexpr (!kHold) weight[0] = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
-          s[0] += r[c].v[i] * r[c].v[i];
-          s[1] += w.v[i] * g[c].v[i] * r[c].v[i];
+          s[0] = __builtin_fmaf(r[c].v[i], r[c].v[i], s[0]);
+          s[1] = __builtin_fmaf(weight[0].v[i] * g[c].v[i], r[c].v[i], s[1]);
         }
       }
     }
@@ -365,20 +449,20 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a)
 #pragma unroll
       for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < kW; ++i) s[2] += y[c].v[i] * y[c].v[i];
+        for (int i = 0; i < kW; ++i) s[2] = __builtin_fmaf(y[c].v[i], y[c].v[i], s[2]);
     }
     row_sums<TPR, 3>(s, sums[0]);
     if (a.weight != nullptr) {
       const float rstd = 1.f / sqrtf(s[0] * rn + a.eps);
-      const float mean = s[1] * rstd * rn;  // of n weight dh
+      const float mean = s[1] * rstd * rn;  // of u weight dh
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const lin::Vals w = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+        if constexpr (!kHold) weight[0] = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
           const float u = r[c].v[i] * rstd;
-          dw[c].v[i] += g[c].v[i] * u;
-          d[c].v[i] += rstd * (w.v[i] * g[c].v[i] - u * mean);
+          dw[c].v[i] = __builtin_fmaf(g[c].v[i], u, dw[c].v[i]);
+          d[c].v[i] = __builtin_fmaf(rstd, weight[0].v[i] * g[c].v[i] - u * mean, d[c].v[i]);
         }
       }
     }
@@ -387,19 +471,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a)
       for (int c = 0; c < C; ++c) put<T, VEC>((T *)a.dr_out + row * a.ldo + at(c), d[c], left(c));
     }
     if (!with_y && a.dy == nullptr) continue;
-    const float gate = a.gate != nullptr ? a.gate[row] : 1.f;
-    const float by = gate * a.scale;
+    const float by = (a.gate != nullptr ? a.gate[row] : 1.f) * a.scale;
     if (with_y) {
       float dot = 0.f;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         if (a.post != nullptr) {
-          const lin::Vals p = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+          if constexpr (!kHold) post[0] = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
 #pragma unroll
-          for (int i = 0; i < kW; ++i) dot += d[c].v[i] * p.v[i] * y[c].v[i];
+          for (int i = 0; i < kW; ++i) dot = __builtin_fmaf(d[c].v[i] * post[0].v[i], y[c].v[i], dot);
         } else {
 #pragma unroll
-          for (int i = 0; i < kW; ++i) dot += d[c].v[i] * y[c].v[i];
+          for (int i = 0; i < kW; ++i) dot = __builtin_fmaf(d[c].v[i], y[c].v[i], dot);
         }
       }
       row_sums<TPR, 1>(&dot, sums[1]);
@@ -409,12 +492,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a)
         const float mean = by * dot * rstd * rn;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          const lin::Vals p = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+          if constexpr (!kHold) post[0] = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
 #pragma unroll
           for (int i = 0; i < kW; ++i) {
             const float e = by * d[c].v[i], u = y[c].v[i] * rstd;
-            dp[c].v[i] += e * u;
-            d[c].v[i] = rstd * (e * p.v[i] - u * mean);
+            dp[c].v[i] = __builtin_fmaf(e, u, dp[c].v[i]);
+            d[c].v[i] = rstd * (e * post[0].v[i] - u * mean);
           }
         }
       }
@@ -481,7 +564,7 @@ struct AdamwBegin {
   int32_t *step;
   const float *lr_ptr, *grad_scale;
   AdamwCoef *coef;
-  double lr, beta1, beta2, decay;
+  double lr, log_beta1, log_beta2, decay;  // logarithms to base 2
   uint32_t seed;
 };
 
@@ -499,8 +582,8 @@ __global__ void k_adamw_begin(AdamwBegin a) {
   *a.step = t;
   const double lr = a.lr_ptr != nullptr ? (double)*a.lr_ptr : a.lr;
   AdamwCoef c;
-  c.step = (float)(lr / (1. - pow(a.beta1, (double)t)));
-  c.rden = (float)(1. / sqrt(1. - pow(a.beta2, (double)t)));
+  c.step = (float)(lr / (1. - exp2(a.log_beta1 * t)));
+  c.rden = (float)(1. / sqrt(1. - exp2(a.log_beta2 * t)));
   c.decay = (float)(1. - lr * a.decay);
   c.grad_scale = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
   c.key = mix32(a.seed + (uint32_t)t * 0x9E3779B9u);

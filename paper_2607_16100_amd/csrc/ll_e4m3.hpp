@@ -48,4 +48,9 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xFFFFu;
 }
 
+// Four values, scaled to at most 448 or no numbers, in a word.
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}
+
 }  // namespace llc
