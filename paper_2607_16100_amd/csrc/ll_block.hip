@@ -41,12 +41,12 @@ int check_scales(const uint8_t *p, size_t ld, size_t blocks) {
 
 template <typename T>
 int launch_quantise(const QuantArgs &a, bool vec, uint64_t items, void *stream) {
-  // Many rows: four blocks of a lane's loads under way.  Few: as many waves as there are blocks.
+  // Many rows: two blocks of a lane's loads under way.  Few: as many waves as there are blocks.
   const bool many = items >= 65536;
-  const uint64_t per = many ? 64 : 16;
+  const uint64_t per = many ? 32 : 16;
   const uint64_t grid = (items + per - 1) / per;
   if (grid * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
-  const auto fn = many ? (vec ? k_quantise<T, true, 4> : k_quantise<T, false, 4>)
+  const auto fn = many ? (vec ? k_quantise<T, true, 2> : k_quantise<T, false, 2>)
                        : (vec ? k_quantise<T, true, 1> : k_quantise<T, false, 1>);
   hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
   return launch_status();

@@ -96,17 +96,17 @@ template <typename T, bool VEC, int U>
 __global__ __launch_bounds__(256) void k_quantise(QuantArgs a) {
   uint32_t rows = a.rows;
   if (a.end != nullptr) rows = (uint32_t)min(max(*a.end, 0), (int)a.rows);
-  const uint64_t items = (uint64_t)rows * a.blocks;
-  const uint64_t first = (uint64_t)blockIdx.x * (16 * U) + threadIdx.x / 16;
-  if ((uint64_t)blockIdx.x * (16 * U) >= items) return;
+  const uint32_t items = rows * a.blocks;  // (fewer than 2^30, by the launch's limit)
+  const uint32_t first = blockIdx.x * (16 * U) + threadIdx.x / 16;
+  if (blockIdx.x * (16 * U) >= items) return;
   const bool gate = lin::gated(a.act);
   lin::Vals v[U], u[U];
   uint32_t row[U], col[U];
 #pragma unroll
   for (int n = 0; n < U; ++n) {
-    const uint64_t item = first + n * 16;
-    row[n] = item < items ? (uint32_t)(item / a.blocks) : 0u;
-    col[n] = item < items ? (uint32_t)(item % a.blocks) * kBlock + threadIdx.x % 16 * kW : 0xFFFFFFFFu;
+    const uint32_t item = first + n * 16;
+    row[n] = item < items ? item / a.blocks : 0u;
+    col[n] = item < items ? item % a.blocks * kBlock + threadIdx.x % 16 * kW : 0xFFFFFFFFu;
     const int left = col[n] < a.features ? (int)(a.features - col[n]) : 0;
     const T *p = (const T *)a.x + (uint64_t)row[n] * a.ldx + (left > 0 ? col[n] : 0);
     v[n] = get<T, VEC>(p, left);

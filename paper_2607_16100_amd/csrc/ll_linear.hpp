@@ -360,7 +360,8 @@ enum Rows {
 //   kAnyRows: fetch() brings them to registers, 16 bytes at any alignment where
 //   they lie inside the matrix and single elements at its end, and commit()
 //   writes them to LDS.
-template <typename T, int R, int NW, bool KM, Rows ROWS>
+// KM: SHIFT 1 puts chunk c of entry r at c ^ (r / 2 & 7) instead of c ^ (r & 7).
+template <typename T, int R, int NW, bool KM, Rows ROWS, int SHIFT = 0>
 struct Loader {
   static constexpr int kEpc = 16 / (int)sizeof(T);
   static constexpr int kBK = Step<T>::kBK;
@@ -393,10 +394,11 @@ struct Loader {
     for (int c = 0; c < kChunks; ++c) {
       const uint32_t pos = (uint32_t)(threadIdx.x / 64 * kChunks + c) * 64 + threadIdx.x % 64;
       if constexpr (KM) {
-        const uint32_t r = pos / 8, chunk = (pos % 8) ^ (r & 7);
+        static_assert(SHIFT == 0 || kChunks % 2 == 0, "chunk c's place depends on c % 2");
+        const uint32_t r = pos / 8, chunk = (pos % 8) ^ (r >> SHIFT & 7);
         bool ok;
         const uint32_t mr = row_of(r, &ok);
-        kk0 = chunk * kEpc;  // the same for every c: rows are 8 apart
+        if (SHIFT == 0 || c == 0) kk0 = chunk * kEpc;  // SHIFT 0: the same for every c, rows are 8 apart
         off[c] = ok ? (uint32_t)((uint64_t)(mr - first) * ld * kEs) + chunk * 16 : kOutside;
       } else {
         const uint32_t krow = pos / kRowChunks, chunk = (pos % kRowChunks) ^ rm_swz<T, R>(krow);
@@ -407,7 +409,10 @@ struct Loader {
   }
 
   // chunk c's first k (KM) or its k row (RM) within a stage
-  __device__ __forceinline__ uint32_t kk(int c) const { return KM ? kk0 : kk0 + c * (64 / kRowChunks); }
+  __device__ __forceinline__ uint32_t kk(int c) const {
+    if constexpr (KM && SHIFT == 1) return kk0 ^ (c % 2 * 4 * kEpc);
+    return KM ? kk0 : kk0 + c * (64 / kRowChunks);
+  }
 
   __device__ __forceinline__ void advance() {
     base += step;
@@ -448,11 +453,11 @@ struct Loader {
   // `have` k hold past them.  After the thread's loads have arrived.
   __device__ __forceinline__ void clear_tail(char *tile, int have) const {
     if constexpr (KM && ROWS == kDwordRows) {
-      const int from = have - (int)kk0;
-      if (from <= 0 || from >= kEpc) return;
       const uint32_t chunk0 = threadIdx.x / 64 * kChunks;
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
+        const int from = have - (int)kk(c);
+        if (from <= 0 || from >= kEpc) continue;
         T *e = reinterpret_cast<T *>(tile + (chunk0 + c) * 1024 + threadIdx.x % 64 * 16);
         for (int i = from; i < kEpc; ++i) e[i] = (T)0.f;
       }

@@ -65,7 +65,8 @@ Plan plan_of8(const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
 
 template <typename O, int B, int ST, Rows ROWS>
 tile8_fn pick8(bool gate) {
-  return gate ? k_tile8<O, B, B, ST, true, ROWS> : k_tile8<O, B, B, ST, false, ROWS>;
+  if constexpr (B == 256 && ROWS == kChunkRows) return gate ? k_wide8<O, true> : k_wide8<O, false>;
+  else return gate ? k_tile8<O, B, B, ST, true, ROWS> : k_tile8<O, B, B, ST, false, ROWS>;
 }
 
 template <typename O, int B, int ST, Rows ROWS>

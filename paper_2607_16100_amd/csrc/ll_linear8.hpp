@@ -37,9 +37,11 @@ constexpr int kScaleStages = 4;  // stages of which a row's scales lie in one wo
 
 // Which of a stage's 16-byte chunks a lane takes for half ks of its k does not
 // matter as long as both operands' lanes agree; the scale is the same for all.
+// An entry's chunks lie at chunk ^ (entry / 2 & 7): of 16 lanes that a read
+// serves at a time, two entries 8 apart are in different banks then.
 __device__ __forceinline__ uint32_t frag8_off(uint32_t dim0, int ks, int half) {
   const uint32_t lane = threadIdx.x % 64, r = dim0 + lane % 32, chunk = ks * 4 + lane / 32 * 2 + half;
-  return r * 128 + ((chunk ^ (r & 7)) << 4);
+  return r * 128 + ((chunk ^ (r / 2 & 7)) << 4);
 }
 
 union Frag8 {
@@ -91,6 +93,64 @@ __device__ __forceinline__ f32x4 mma8(const Frag8 &a, int sa, const Frag8 &b, in
   }
 }
 
+// Bytes of LDS the epilogue takes.
+constexpr int epilogue8(int bm, int bn) { return 4 * (bm > 64 ? bm / 4 : 32) * (bn / 2 + 4) * 4; }
+
+// As the other products' epilogue: kEw consecutive columns of a row a lane, a
+// wave's rows of one half of the tile at a time.  A lane's sums are of one row,
+// four consecutive columns at a time.
+template <typename O, int BM, int BN, bool GATED, int FM, int FN>
+__device__ __forceinline__ void finish_tile8(const Args8 &a, int g, uint32_t tn, uint32_t m0, uint32_t m_end, bool lower,
+                                             const f32x16 (&acc)[FN][FM], char *lds) {
+  constexpr int WTN = BN / 2, FH = FM > 1 ? FM / 2 : 1, kPitch = WTN + 4, kRowsE = FH * 32;
+  const int lane = threadIdx.x % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int wm = wave / 2, wn = wave % 2;
+  float *mine = reinterpret_cast<float *>(lds) + wave * kRowsE * kPitch;
+  auto finish = [&](auto half) __attribute__((always_inline)) {
+    constexpr int h = decltype(half)::value;
+#pragma unroll
+    for (int i = 0; i < FH; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const f32x16 &v = acc[j][h * FH + i];
+          *reinterpret_cast<f32x4 *>(mine + (i * 32 + lane % 32) * kPitch + j * 32 + c * 8 + lane / 32 * 4) =
+              f32x4{v[c * 4], v[c * 4 + 1], v[c * 4 + 2], v[c * 4 + 3]};
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    constexpr int kWidth = GATED ? WTN / 2 : WTN;  // columns of y a wave has
+    constexpr int kLanes = kWidth / kEw;           // lanes a row
+    const int c = lane % kLanes * kEw;
+    const uint32_t n0 = (GATED ? tn * (BN / 2) + wn * kWidth : tn * BN + wn * WTN) + c;
+#pragma unroll 1
+    for (int r = lane / kLanes; r < kRowsE; r += 64 / kLanes) {
+      const uint32_t m = m0 + (FM > 1 ? h * (BM / 2) + wm * kRowsE : wm * 32) + r;
+      if (m >= m_end) break;
+      Pack<float, kEw, true> v, u;
+      v.load(mine + r * kPitch + c);
+      if constexpr (GATED) u.load(mine + r * kPitch + kWidth + c);
+      if (a.parts != nullptr) {
+        if (n0 < a.part_half) {
+          float *to = a.parts + ((uint64_t)blockIdx.y * a.rows_c + m) * a.part_row + n0;
+          v.store(to);
+          if constexpr (GATED) u.store(to + a.part_half);
+        }
+      } else {
+        put_forward<O, GATED>(a, g, m, n0, v, u);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  };
+  finish(std::integral_constant<int, 0>{});
+  if constexpr (FM > 1) {
+    if (lower) finish(std::integral_constant<int, 1>{});
+  }
+}
+
 // ---------------------------------------------------------------- the tile kernel
 //
 // Four waves of a quarter of the tile each, in fragments of 32 x 32 by the
@@ -110,8 +170,7 @@ __global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args
   constexpr int NW = 4, WTM = BM / 2, WTN = BN / 2, FM = WTM / 32, FN = WTN / 32;
   constexpr int FH = FM > 1 ? FM / 2 : 1;  // fragments of a wave's rows in the tile's upper half
   constexpr int BK = 128, kStage = (BM + BN) * 128, kScales = (BM + BN) * 4;
-  constexpr int kPitch = WTN + 4, kRowsE = FH * 32;  // an epilogue pass: rows of a wave
-  constexpr int kEpi = NW * kRowsE * kPitch * 4, kUse = ST * kStage + 2 * kScales + NW * 256;
+  constexpr int kEpi = epilogue8(BM, BN), kUse = ST * kStage + 2 * kScales + NW * 256;
   constexpr int kLds = kUse > kEpi ? kUse : kEpi;
   __shared__ __attribute__((aligned(1024))) char lds[kLds];
   const int lane = threadIdx.x % 64;
@@ -128,8 +187,8 @@ __global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args
   const uint32_t share = a.splits == 1 ? k : ((k + kWord - 1) / kWord + a.splits - 1) / a.splits * kWord;
   const uint32_t k_from = min(k, blockIdx.y * share);
 
-  Loader<e4m3, BM, NW, true, ROWS> lp;
-  Loader<e4m3, BN, NW, true, ROWS> lq;
+  Loader<e4m3, BM, NW, true, ROWS, 1> lp;
+  Loader<e4m3, BN, NW, true, ROWS, 1> lq;
   lp.init(p, a.ldp, k, m_end, 0, m0, [&](uint32_t j, bool *ok) {
     *ok = m0 + j < m_end;
     return m0 + j;
@@ -350,51 +409,274 @@ __global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args
   wait_loads<0>();
   lds_barrier();  // every wave is past its last stage, and no load is under way
 
-  // As the other products' epilogue: kEw consecutive columns of a row a lane.
-  // A lane's sums are of one row, four consecutive columns at a time.
-  float *mine = reinterpret_cast<float *>(lds) + wave * kRowsE * kPitch;
-  auto finish = [&](auto half) __attribute__((always_inline)) {
-    constexpr int h = decltype(half)::value;
-#pragma unroll
-    for (int i = 0; i < FH; ++i)
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const f32x16 &v = acc[j][h * FH + i];
-          *reinterpret_cast<f32x4 *>(mine + (i * 32 + lane % 32) * kPitch + j * 32 + c * 8 + lane / 32 * 4) =
-              f32x4{v[c * 4], v[c * 4 + 1], v[c * 4 + 2], v[c * 4 + 3]};
-        }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-    constexpr int kWidth = GATED ? WTN / 2 : WTN;  // columns of y a wave has
-    constexpr int kLanes = kWidth / kEw;           // lanes a row
-    const int c = lane % kLanes * kEw;
-    const uint32_t n0 = (GATED ? tn * (BN / 2) + wn * kWidth : tn * BN + wn * WTN) + c;
-#pragma unroll 1
-    for (int r = lane / kLanes; r < kRowsE; r += 64 / kLanes) {
-      const uint32_t m = m0 + (FM > 1 ? h * (BM / 2) + wm * kRowsE : wm * 32) + r;
-      if (m >= m_end) break;
-      Pack<float, kEw, true> v, u;
-      v.load(mine + r * kPitch + c);
-      if constexpr (GATED) u.load(mine + r * kPitch + kWidth + c);
-      if (a.parts != nullptr) {
-        if (n0 < a.part_half) {
-          float *to = a.parts + ((uint64_t)blockIdx.y * a.rows_c + m) * a.part_row + n0;
-          v.store(to);
-          if constexpr (GATED) u.store(to + a.part_half);
-        }
-      } else {
-        put_forward<O, GATED>(a, g, m, n0, v, u);
-      }
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-  };
-  finish(std::integral_constant<int, 0>{});
-  if constexpr (FM > 1) {
-    if (lower) finish(std::integral_constant<int, 1>{});
+  finish_tile8<O, BM, BN, GATED>(a, g, tn, m0, m_end, lower, acc, lds);
+}
+
+// ---------------------------------------------------------------- the wide tile kernel
+//
+// Tiles of 256 x 256, the only ones with enough matrix instructions a stage to
+// hide what a stage loads (64 KB, half the time that the vector cache needs for
+// it).  In k_tile8's schedule those loads all go out in half of the stage, which
+// makes the waves wait for the cache (dense 8192^3: 450 us, the matrix cores busy
+// 61 % of the cycles).  Here a stage has four clusters of eight matrix
+// instructions, one pair of quarters each, and everything is spread over them
+// evenly:
+//
+//   cluster      U x Qf     U x Qs   |   L x Qs     L x Qf
+//   reads        Qs         L        |   U of s+1   Qf of s+1
+//   loads s+2    U          Qf       |   Qs         L
+//
+// U and L are the tile's upper and lower 128 rows, Q0 and Q1 the first and second
+// half of each wave's columns; Qf is Q0 in even stages and Q1 in odd ones, so
+// that the registers of one are free when the next stage's are read.  There is a
+// barrier before the first cluster and one in the middle.  What a cluster loads
+// was read by every wave before the barrier in front of it, and is waited for a
+// stage and a half later.
+//
+// Rows are whole 16-byte chunks; others run k_tile8.
+struct QuarterLoader {
+  uint64_t base;  // of the stage to load next
+  uint32_t off[8], kk0;
+
+  // Which eight entries chunk c of this wave is: 0 .. 3 of the first quarter, 4 ..
+  // 7 of the second.  `apart`: a quarter is the halves' halves (the weight).
+  static __device__ __forceinline__ uint32_t block(uint32_t wave, int c, bool apart) {
+    const uint32_t i = wave * 4 + c % 4;
+    return apart ? i / 8 * 16 + i % 8 + c / 4 * 8 : i + c / 4 * 16;
   }
+  template <typename F>
+  __device__ __forceinline__ void init(const e4m3 *mat, uint64_t ld, uint32_t first, uint32_t wave, bool apart, F row_of) {
+    const uint32_t lane = threadIdx.x % 64;
+    base = (uint64_t)(mat + (uint64_t)first * ld);
+    kk0 = ((lane % 8) ^ (lane / 16)) * 16;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      bool ok;
+      const uint32_t r = row_of(block(wave, c, apart) * 8 + lane / 8, &ok);
+      off[c] = ok ? (uint32_t)((uint64_t)(r - first) * ld) + kk(c) : kOutside;
+    }
+  }
+  // chunk c's first k within a stage
+  __device__ __forceinline__ uint32_t kk(int c) const { return kk0 ^ (c % 2 * 64); }
+  __device__ __forceinline__ void advance() { base += 128; }
+  // As Loader's issue, to LDS byte `at`.
+  template <bool WHOLE>
+  __device__ __forceinline__ void issue(uint32_t at, int c, uint32_t have) {
+    const u32x4 rs = {uniform_u32((uint32_t)base), uniform_u32((uint32_t)(base >> 32)), kOutside, (uint32_t)kRsrcWord3};
+    const uint32_t o = WHOLE || kk(c) < have ? off[c] : kOutside;
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 3\n\t"
+        "buffer_load_dwordx4 %1, %2, 0 offen lds"
+        :
+        : "s"(uniform_u32(at)), "v"(o), "s"(rs)
+        : "memory");
+  }
+};
+
+template <typename O, bool GATED>
+__global__ __launch_bounds__(256, 1) void k_wide8(Args8 a) {
+  constexpr int BM = 256, BN = 256, WTN = 128, BK = 128, kStage = 65536, kScales = 2048;
+  constexpr int kUse = 2 * kStage + 2 * kScales + 1024, kEpi = epilogue8(BM, BN);
+  __shared__ __attribute__((aligned(1024))) char lds[kUse > kEpi ? kUse : kEpi];
+  const int lane = threadIdx.x % 64;
+  const uint32_t wave = uniform_u32(threadIdx.x / 64);
+  const uint32_t wm = wave / 2, wn = wave % 2;
+
+  int g = 0;
+  uint32_t tn = 0, m0 = 0, m_end = a.m;
+  const uint32_t k = a.k;
+  if (!find_rows(a, blockIdx.x, BM, &g, &m0, &m_end, &tn)) return;
+  QuarterLoader lp, lq;
+  lp.init((const e4m3 *)a.p, a.ldp, m0, wave, false, [&](uint32_t j, bool *ok) {
+    *ok = m0 + j < m_end;
+    return m0 + j;
+  });
+  lq.init((const e4m3 *)a.q + (uint64_t)g * a.qstride, a.ldq, GATED ? 0 : tn * BN, wave, true,
+          [&](uint32_t j, bool *ok) { return q_row<WTN, GATED>(tn, BN, j, a.n, ok); });
+  // scales of the tile's rows, then of its weight rows: two segments of 64 each wave
+  uint64_t sbase[2];
+  uint32_t soff[2];
+  {
+    const uint32_t e = wave * 64 + lane;
+    bool ok;
+    const uint32_t r = q_row<WTN, GATED>(tn, BN, e, a.n, &ok);
+    sbase[0] = (uint64_t)(a.xs + (uint64_t)m0 * a.ldxs);
+    soff[0] = m0 + e < m_end ? (uint32_t)(e * a.ldxs) : kOutside;
+    sbase[1] = (uint64_t)(a.ws + (uint64_t)g * a.wsstride);
+    soff[1] = ok ? (uint32_t)(r / 128 * a.ldws) : kOutside;
+  }
+
+  f32x16 acc[4][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[j][i][e] = 0.f;
+
+  const uint32_t steps = (k + BK - 1) / BK;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+  char *const scale_lds = lds + 2 * kStage;
+  auto issue_p = [&](int b, int c, auto whole, uint32_t have) __attribute__((always_inline)) {
+    lp.template issue<decltype(whole)::value>(lds0 + b * kStage + lp.block(wave, c, false) * 1024, c, have);
+  };
+  auto issue_q = [&](int b, int c, auto whole, uint32_t have) __attribute__((always_inline)) {
+    lq.template issue<decltype(whole)::value>(lds0 + b * kStage + BM * 128 + lq.block(wave, c, true) * 1024, c, have);
+  };
+  // as k_tile8's
+  auto issue_scales = [&](uint32_t word, bool wanted) __attribute__((always_inline)) {
+    const bool in = wanted && word * kScaleStages * BK < k;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const uint64_t base = sbase[c] + (in ? word * 4 : 0);
+      const uint32_t o = in ? soff[c] : kOutside;
+      const uint32_t to = wanted ? (word & 1) * kScales + (c * 4 + wave) * 256 : 2 * kScales + wave * 256;
+      const u32x4 rs = {uniform_u32((uint32_t)base), uniform_u32((uint32_t)(base >> 32)), kOutside, (uint32_t)kRsrcWord3};
+      asm volatile(
+          "s_mov_b32 m0, %0\n\t"
+          "s_nop 3\n\t"
+          "buffer_load_dword %1, %2, 0 offen lds"
+          :
+          : "s"(uniform_u32(lds0 + 2 * kStage + to)), "v"(o), "s"(rs)
+          : "memory");
+    }
+  };
+  uint32_t off_q[2][2], off_p[2][2];  // by half of k and by 16 bytes
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t chunk = ks * 4 + lane / 32 * 2 + h, at = lane % 32 * 128 + ((chunk ^ (lane % 32 / 2 & 7)) << 4);
+      off_p[ks][h] = wm * 64 * 128 + at;
+      off_q[ks][h] = BM * 128 + wn * 128 * 128 + at;
+    }
+  const bool lower = m_end - m0 > BM / 2;  // the tile has rows in its lower half
+
+  if (steps > 0) {
+    issue_scales(0, true);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int left_k = (int)k - s * BK;
+      const uint32_t have = left_k > 0 ? left_k : 0;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) issue_p(s, half * 4 + c, std::false_type{}, have);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) issue_q(s, (half ^ s) * 4 + c, std::false_type{}, have);
+      }
+      lp.advance();
+      lq.advance();
+    }
+    wait_loads<16>();
+    lds_barrier();
+
+    Frag8 fq[2][2][2], fu[2][2], fl[2][2];  // halves of the columns; then fragment, half of k
+    int sq[4], sp[4];                       // scales, in the low byte
+    auto read_scales = [&](uint32_t s, int *sq, int *sp) __attribute__((always_inline)) {  // of stage s
+      const uint32_t *from = reinterpret_cast<const uint32_t *>(scale_lds + (s / kScaleStages & 1) * kScales);
+      const uint32_t down = s % kScaleStages * 8;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sq[j] = (int)(from[BM + wn * WTN + j * 32 + lane % 32] >> down);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sp[i] = (int)(from[i / 2 * 128 + wm * 64 + i % 2 * 32 + lane % 32] >> down);
+    };
+    // read n (of 8) of a quarter's fragments
+    auto read_q = [&](const char *from, int half, int n) __attribute__((always_inline)) {
+      const int ks = n / 4, f = n / 2 % 2, h = n % 2;
+      fq[half][f][ks].half[h] = *reinterpret_cast<const u32x4 *>(from + off_q[ks][h] + (half * 2 + f) * 32 * 128);
+    };
+    auto read_p = [&](const char *from, int low, int n) __attribute__((always_inline)) {
+      const int ks = n / 4, f = n / 2 % 2, h = n % 2;
+      (low ? fl : fu)[f][ks].half[h] = *reinterpret_cast<const u32x4 *>(from + off_p[ks][h] + low * 128 * 128 + f * 32 * 128);
+    };
+    read_scales(0, sq, sp);
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      read_p(lds, 0, n);
+      read_q(lds, 0, n);
+    }
+    // matrix instruction t (of 8) of a cluster
+    auto multiply = [&](int half, int low, int t) __attribute__((always_inline)) {
+      const int ks = t / 4, j = t / 2 % 2, i = t % 2;
+      acc[half * 2 + j][low * 2 + i] =
+          mma8<O>(fq[half][j][ks], sq[half * 2 + j], (low ? fl : fu)[i][ks], sp[low * 2 + i], acc[half * 2 + j][low * 2 + i]);
+    };
+    // Stage s in buffer B (s % 2).  `whole`: the stage loaded meanwhile has BK k,
+    // else `have_k` of them.  next_has: k of the next one.
+    auto stage = [&](auto b_c, uint32_t s, auto lower_c, auto whole, int next_has, int have_k) __attribute__((always_inline)) {
+      constexpr int B = decltype(b_c)::value, F = B, S = 1 - B;
+      constexpr bool kLower = decltype(lower_c)::value;
+      const char *here = lds + B * kStage, *next = lds + (1 - B) * kStage;
+      const uint32_t have = have_k > 0 ? have_k : 0;
+      wait_loads<16>();
+      lds_barrier();
+      issue_scales(s / kScaleStages + 1, s % kScaleStages == 1);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        if (t % 2 == 0) issue_p(B, t / 2, whole, have);
+        read_q(here, S, t);
+        multiply(F, 0, t);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        if (t % 2 == 0) issue_q(B, F * 4 + t / 2, whole, have);
+        if (kLower) read_p(here, 1, t);
+        multiply(S, 0, t);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      wait_loads<16>();
+      lds_barrier();
+      int nq[4], np[4];
+      read_scales(s + 1, nq, np);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        if (t % 2 == 0) issue_q(B, S * 4 + t / 2, whole, have);
+        read_p(next, 0, t);
+        if (kLower) multiply(S, 1, t);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        if (t % 2 == 0) issue_p(B, 4 + t / 2, whole, have);
+        read_q(next, S, t);
+        if (kLower) multiply(F, 1, t);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // a stage past the sum is zeros times what may be no number
+      const bool none = !decltype(whole)::value && next_has <= 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sq[j] = none ? 0 : nq[j];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sp[i] = none ? 0 : np[i];
+      lp.advance();
+      lq.advance();
+    };
+    auto all = [&](auto lower_c) __attribute__((always_inline)) {
+      constexpr auto c0 = std::integral_constant<int, 0>{};
+      constexpr auto c1 = std::integral_constant<int, 1>{};
+      uint32_t s = 0;
+      for (; (s + 4) * BK <= k; s += 2) {
+        stage(c0, s, lower_c, std::true_type{}, BK, BK);
+        stage(c1, s + 1, lower_c, std::true_type{}, BK, BK);
+      }
+      // an even number of stages, the last of zeros where there is none
+      for (; s < steps; s += 2) {
+        const int has = (int)(k - s * BK);
+        stage(c0, s, lower_c, std::false_type{}, has - BK, has - 2 * BK);
+        stage(c1, s + 1, lower_c, std::false_type{}, has - 2 * BK, has - 3 * BK);
+      }
+    };
+    if (lower)
+      all(std::true_type{});
+    else
+      all(std::false_type{});
+  }
+  wait_loads<0>();
+  lds_barrier();  // every wave is past its last stage, and no load is under way
+  finish_tile8<O, BM, BN, GATED>(a, g, tn, m0, m_end, lower, acc, lds);
 }
 
 // ---------------------------------------------------------------- few rows a group

@@ -124,6 +124,8 @@ LARGE = {
     "full": (None, 4096, 256, 4096),
     "quarters": (None, 4100, 320, 4352),
     "groups": ([700, 0, 130, 2049, 1200, 257], 0, 192, 4104),
+    "deep": (None, 4096, 1424, 4096),  # twelve stages, the last short
+    "odd": (None, 4000, 1408, 4096),   # eleven
     "wide128": (None, 2048, 1664, 2048),
     "many128": (None, 2500, 384, 2048),
 }
