@@ -397,13 +397,20 @@ def scales_of(*shape, device="cuda", stream=None) -> torch.Tensor:
     return wide.view(E8M0)[..., :shape[-1]]
 
 
+def _like(t, name: str, dev: int, rows: int, cols: int, dtype) -> int:
+    """_mat, sooner done where the rows are contiguous."""
+    if t.shape == (rows, cols) and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev:
+        return cols or 1
+    return _mat(t, name, dev, rows, cols, dtype)
+
+
 def _codes(t, name: str, dev: int, rows: int, cols: int) -> int:
-    return _mat(t, name, dev, rows, cols, E4M3)
+    return _like(t, name, dev, rows, cols, E4M3)
 
 
 def _scale_rows(t, name: str, dev: int, rows: int, blocks: int) -> int:
     """Checks a matrix of scales; its leading dimension."""
-    if t.dtype is not E8M0 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != blocks or t.get_device() != dev:
+    if t.dtype is not E8M0 or t.shape != (rows, blocks) or t.get_device() != dev:
         raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected ({rows}, {blocks}) {E8M0} on the current GPU")
     ld, unit = t.stride()
     wide = (blocks + 3) // 4 * 4
@@ -411,7 +418,8 @@ def _scale_rows(t, name: str, dev: int, rows: int, blocks: int) -> int:
         raise ValueError(f"{name}: rows of scales start at multiples of 4 bytes (moe.scales_of makes such memory)")
     if rows < 2:
         ld = wide
-    _readable(t, name, (rows - 1) * ld + wide)
+    if wide != blocks:
+        _readable(t, name, (rows - 1) * ld + wide)
     return ld
 
 
@@ -512,13 +520,13 @@ def linear8(x, x_scales, w, w_scales, *, bias=None, act: str = "none", residual=
         dtype = torch.bfloat16 if out is None else out.dtype
     if out is None:
         out = _new(stream, n, width, dtype=dtype, device=x.device)
-    ldy = _mat(out, "out", dev, n, width, dtype)
+    ldy = _like(out, "out", dev, n, width, dtype)
     ldr = ldz = max(o, 1)
     rp = zp = None
     if residual is not None:
-        ldr, rp = _mat(residual, "residual", dev, n, width, dtype), residual.data_ptr()
+        ldr, rp = _like(residual, "residual", dev, n, width, dtype), residual.data_ptr()
     if z is not None:
-        ldz, zp = _mat(z, "z", dev, n, o, dtype), z.data_ptr()
+        ldz, zp = _like(z, "z", dev, n, o, dtype), z.data_ptr()
     d = lm.LLLinearDesc(lm.DESC_SIZE, _dt(out), lm.ACTS[act], g, n, i, o, _offsets(offsets, g, dev), ldx, ldw, gs, ldy,
                         ldz, ldr)
     key = (d.dt, d.act, g, n, i, o, offsets is None, ldx & 15, ldw & 15, gs & 15)
@@ -557,16 +565,12 @@ class NormGrads(NamedTuple):
 
 def _norm_weights(post, weight, rows, dev: int):
     """(their type's code, addresses) of a norm's weights."""
-    at, kind = [], None
-    for t, name in ((post, "post"), (weight, "weight")):
-        if t is None:
-            at.append(None)
-            continue
-        if t.dtype not in (rows.dtype, torch.float32) or (kind is not None and t.dtype is not kind):
-            raise ValueError(f"{name}: {t.dtype}, expected {rows.dtype} or float32, the same for post and weight")
-        kind = t.dtype
-        at.append(_flat(t, name, dev, rows.shape[1], t.dtype))
-    return _DT[kind or torch.float32], at
+    kind = weight.dtype if weight is not None else post.dtype if post is not None else torch.float32
+    if kind is not rows.dtype and kind is not torch.float32:
+        raise ValueError(f"weight or post: {kind}, expected {rows.dtype} or float32")
+    f = rows.shape[1]
+    pp = None if post is None else _flat(post, "post", dev, f, kind)
+    return _DT.get(kind, ll.LL_F32), (pp, None if weight is None else _flat(weight, "weight", dev, f, kind))
 
 
 def norm(y, weight=None, *, residual=None, gate=None, scale: float = 1.0, post=None, eps: float = 1e-6,
@@ -583,32 +587,51 @@ def norm(y, weight=None, *, residual=None, gate=None, scale: float = 1.0, post=N
     dev = _device()
     ldy = _mat(y, "y", dev)
     n, f = y.shape
-    for t, name in ((y, "y"), (residual, "residual"), (gate, "gate"), (post, "post"), (weight, "weight")):
-        if t is not None and t.requires_grad:
-            _no_grad(name)
+    dt, device = y.dtype, y.device
+    if torch.is_grad_enabled():
+        for t, name in ((y, "y"), (residual, "residual"), (gate, "gate"), (post, "post"), (weight, "weight")):
+            if t is not None and t.requires_grad:
+                _no_grad(name)
     wdt, (pp, wp) = _norm_weights(post, weight, y, dev)
-    if (quantised or q is not None or h is not None) and weight is None:
+    if weight is None and (quantised or q is not None or h is not None):
         raise ValueError("weight is needed for h")
     if r is None and (weight is None or residual is not None or gate is not None or post is not None or scale != 1):
-        r = _new(stream, n, f, dtype=y.dtype, device=y.device)
+        r = _new(stream, n, f, dtype=dt, device=device)
     if h is None and weight is not None:
-        h = _new(stream, n, f, dtype=y.dtype, device=y.device)
+        h = _new(stream, n, f, dtype=dt, device=device)
     if q is None and quantised:
-        q = _new(stream, n, f, dtype=E4M3, device=y.device)
-    if q is not None and q_scales is None:
-        q_scales = scales_of(n, (f + 127) // 128, device=y.device, stream=stream)
-    d = lb.LLNormDesc(lb.NORM_DESC_SIZE, _dt(y), wdt, eps, scale, n, f, ldy,
-                      f if residual is None else _mat(residual, "residual", dev, n, f, y.dtype),
-                      f if r is None else _mat(r, "r", dev, n, f, y.dtype),
-                      f if h is None else _mat(h, "h", dev, n, f, y.dtype),
-                      f if q is None else _codes(q, "q", dev, n, f),
-                      0 if q is None else _scale_rows(q_scales, "q_scales", dev, n, (f + 127) // 128), f, f, f)
-    ll.check(_c.ll_norm(d, y.data_ptr(), None if residual is None else residual.data_ptr(),
-                        None if gate is None else _flat(gate, "gate", dev, n, torch.float32), pp, wp,
-                        None if r is None else r.data_ptr(), None if h is None else h.data_ptr(),
-                        None if q is None else q.data_ptr(), None if q is None else q_scales.data_ptr(),
-                        _stream(stream, dev)), "ll_norm")
-    return Normed(h, r, q, q_scales if q is not None else None)
+        q = _new(stream, n, f, dtype=E4M3, device=device)
+    xp = gp = rp = hp = qp = sp = None
+    ldx = ldr = ldh = ldq = f
+    lds = 0
+    if residual is not None:
+        ldx, xp = _like(residual, "residual", dev, n, f, dt), residual.data_ptr()
+    if gate is not None:
+        gp = _flat(gate, "gate", dev, n, torch.float32)
+    if r is not None:
+        ldr, rp = _like(r, "r", dev, n, f, dt), r.data_ptr()
+    if h is not None:
+        ldh, hp = _like(h, "h", dev, n, f, dt), h.data_ptr()
+    if q is not None:
+        if q_scales is None:
+            q_scales = scales_of(n, (f + 127) // 128, device=device, stream=stream)
+        ldq, lds = _codes(q, "q", dev, n, f), _scale_rows(q_scales, "q_scales", dev, n, (f + 127) // 128)
+        qp, sp = q.data_ptr(), q_scales.data_ptr()
+    d = _norm_desc(_dt(y), wdt, eps, scale, n, f, ldy, ldx, ldr, ldh, ldq, lds, f, f, f)
+    ll.check(_c.ll_norm(d, y.data_ptr(), xp, gp, pp, wp, rp, hp, qp, sp, _stream(stream, dev)), "ll_norm")
+    return Normed(h, r, q, None if q is None else q_scales)
+
+
+_norm_descs: dict = {}  # by their own fields: a descriptor is only read
+
+
+def _norm_desc(*fields):
+    d = _norm_descs.get(fields)
+    if d is None:
+        if len(_norm_descs) >= 4096:
+            _norm_descs.clear()
+        d = _norm_descs[fields] = lb.LLNormDesc(lb.NORM_DESC_SIZE, *fields)
+    return d
 
 
 def norm_grad(dh, r, weight=None, *, dr=None, y=None, gate=None, scale: float = 1.0, post=None, eps: float = 1e-6,
@@ -649,7 +672,7 @@ def norm_grad(dh, r, weight=None, *, dr=None, y=None, gate=None, scale: float = 
         dpost = fresh(f, dtype=torch.float32)
 
     def mat(t, name):
-        return f if t is None else _mat(t, name, dev, n, f, dt)
+        return f if t is None else _like(t, name, dev, n, f, dt)
 
     def flat(t, name, numel):
         return None if t is None else _flat(t, name, dev, numel, torch.float32)
@@ -657,9 +680,8 @@ def norm_grad(dh, r, weight=None, *, dr=None, y=None, gate=None, scale: float = 
     def at(t):
         return None if t is None else t.data_ptr()
 
-    d = lb.LLNormDesc(lb.NORM_DESC_SIZE, _DT[dt] if dt in _DT else _dt(rows), wdt, eps, scale, n, f, mat(y, "y"), f,
-                      mat(r, "r"), f if weight is None else ld, f, 0, mat(dr, "dr"), mat(dr_out, "dr_out"),
-                      mat(dy, "dy"))
+    d = _norm_desc(_dt(rows), wdt, eps, scale, n, f, mat(y, "y"), f, mat(r, "r"), f if weight is None else ld, f, 0,
+                   mat(dr, "dr"), mat(dr_out, "dr_out"), mat(dy, "dy"))
     ws, need = None, 0
     if dweight is not None or dpost is not None:
         st, need = lb.ll_norm_bytes(d)

@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 from typing import Optional, Sequence
 
+import numpy as np
 import torch
 
 from . import llblock as lb
@@ -21,6 +22,11 @@ from .moe import _device, _flat, _stream
 _DT = {torch.float32: ll.LL_F32, torch.bfloat16: ll.LL_BF16}
 STATES = {"f32": 32, "8bit": 8}
 _TYPES = {32: (torch.float32, torch.float32), 8: (torch.float8_e4m3fn, torch.float8_e5m2)}
+
+# what changes from step to step of a row of ll_adamw's table
+_ROW = np.dtype({"names": ["grad", "gdt"], "formats": [np.uint64, np.int32],
+                 "offsets": [lb.LLAdamwTensor.grad.offset, lb.LLAdamwTensor.gdt.offset],
+                 "itemsize": ctypes.sizeof(lb.LLAdamwTensor)})
 
 
 class AdamW:
@@ -77,6 +83,8 @@ class AdamW:
         self.m_scales, self.v_scales, self.count = state["m_scales"], state["v_scales"], state["count"]
         self._work = torch.empty(lb.LL_ADAMW_WORKSPACE, dtype=torch.uint8, device=device)
         self._table = (lb.LLAdamwTensor * len(self.params))()
+        self._fields = np.frombuffer(self._table, dtype=_ROW)  # the same memory
+        self._sizes = [p.numel() for p in self.params]
         es = 1 if eight else 4
         for t, p, w, at in zip(self._table, self.params, self.masters, self.offsets):
             t.param, t.n, t.at, t.dt = p.data_ptr(), p.numel(), at, _DT[p.dtype]
@@ -117,16 +125,17 @@ class AdamW:
         dev = _device()
         if dev != self._dev:
             raise ValueError("the parameters are not on the current GPU")
-        table = self._table
-        if len(grads) != len(table):
-            raise ValueError(f"grads: {len(grads)}, expected {len(table)}")
-        for i, (t, g) in enumerate(zip(table, grads)):
-            dt = _DT.get(g.dtype)
-            if dt is None:
-                raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(g.dtype))
-            if g.numel() != t.n or g.get_device() != dev or not g.is_contiguous():
-                raise ValueError(f"grads[{i}]: a contiguous tensor of {t.n} values on the parameters' GPU is needed")
-            t.grad, t.gdt = g.data_ptr(), dt
+        if len(grads) != len(self._sizes):
+            raise ValueError(f"grads: {len(grads)}, expected {len(self._sizes)}")
+        for i, (n, g) in enumerate(zip(self._sizes, grads)):
+            if g.numel() != n or g.get_device() != dev or not g.is_contiguous():
+                raise ValueError(f"grads[{i}]: a contiguous tensor of {n} values on the parameters' GPU is needed")
+        table, fields = self._table, self._fields
+        try:
+            fields["gdt"] = [_DT[g.dtype] for g in grads]
+        except KeyError as e:
+            raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(e)) from None
+        fields["grad"] = [g.data_ptr() for g in grads]
         rate, rate_at = self.lr if lr is None else lr, None
         if isinstance(rate, torch.Tensor):
             rate, rate_at = 0.0, _flat(rate, "lr", dev, 1, torch.float32)
