@@ -172,10 +172,11 @@ int ll_quantise_weight(const void *w, size_t ldw, size_t wstride, int groups, si
   const size_t wb = all(wstride, (out - 1) * ldw + in) * es, qb = all(qstride, (qr - 1) * ldq + qc);
   const size_t sb = all(sstride, (sr - 1) * lds + sc);
   if (overlap(w, wb, q, qb) || overlap(w, wb, scales, sb) || overlap(q, qb, scales, sb)) return LL_ERR_INVALID;
-  const WeightArgs a{w, q, scales, ldw, wstride, ldq, qstride, lds, sstride, (uint32_t)out, (uint32_t)in};
-  const size_t to = transpose ? 16 : 8;
-  const bool vec = rows16(w, ldw, es) && aligned(q, to) && ldq % to == 0 &&
-                   (groups == 1 || (wstride * es % 16 == 0 && qstride % to == 0));
+  uint32_t wide = 16;
+  while (wide > 1 && (!aligned(q, wide) || ldq % wide != 0 || (groups > 1 && qstride % wide != 0))) wide /= 2;
+  if (wide == 2) wide = 1;
+  const WeightArgs a{w, q, scales, ldw, wstride, ldq, qstride, lds, sstride, (uint32_t)out, (uint32_t)in, wide};
+  const bool vec = rows16(w, ldw, es) && (groups == 1 || wstride * es % 16 == 0);
   const dim3 grid((unsigned)blocks_of(in), (unsigned)blocks_of(out), (unsigned)groups);
   if (dt == LL_F32)
     launch_weight<float>(a, vec, transpose != 0, grid, stream);

@@ -142,6 +142,7 @@ struct WeightArgs {
   uint8_t *q, *scales;
   uint64_t ldw, wstride, ldq, qstride, lds, sstride;
   uint32_t out, in;
+  uint32_t wide;  // bytes that every row of q is aligned to: 16, 8, 4 or 1
 };
 
 template <typename T, bool VEC, bool TRANSPOSE>
@@ -180,7 +181,12 @@ __global__ __launch_bounds__(256) void k_quantise_weight(WeightArgs a) {
       for (int i = 0; i < 2; ++i)
         w[i] = to_e4m3(v[r].v[4 * i] * inv, v[r].v[4 * i + 1] * inv) |
                to_e4m3(v[r].v[4 * i + 2] * inv, v[r].v[4 * i + 3] * inv) << 16;
-      if (row0 + r < a.out) put_codes<VEC>(q + (uint64_t)(row0 + r) * a.ldq + col0, w, left);
+      if (row0 + r >= a.out) continue;
+      uint8_t *to = q + (uint64_t)(row0 + r) * a.ldq + col0;
+      if (a.wide >= 8)
+        put_codes<true>(to, w, left);
+      else
+        put_codes<false>(to, w, left);
     }
   } else {
 #pragma unroll
@@ -200,8 +206,11 @@ __global__ __launch_bounds__(256) void k_quantise_weight(WeightArgs a) {
       if (orow >= a.in || ocol >= a.out) continue;
       const u32x4 w = *reinterpret_cast<const u32x4 *>(tile + r * kPitch + c);
       uint8_t *to = q + (uint64_t)orow * a.ldq + ocol;
-      if (VEC && ocol + 16 <= a.out) {
+      if (a.wide >= 16 && ocol + 16 <= a.out) {
         *reinterpret_cast<u32x4 *>(to) = w;
+      } else if (a.wide >= 4 && ocol + 16 <= a.out) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t *>(to)[i] = w[i];
       } else {
 #pragma unroll
         for (uint32_t i = 0; i < 16; ++i)

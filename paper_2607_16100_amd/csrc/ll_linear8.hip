@@ -31,19 +31,35 @@ int check_scales(const uint8_t *p, size_t ld, size_t blocks, bool any) {
 using tile8_fn = void (*)(Args8);
 using join_fn = void (*)(Args);
 
+// How a product runs.  A stage has the bytes of the bfloat16 products' stages and
+// matrix instructions that take as long, so their rules hold (ll_linear.hip),
+// with a stage of 128 k.  Measured with cold caches, us with tiles of 256 / 128
+// with 2 and 4 stages / 64 with 2 and 4; in front what the rule's choice takes:
+//   128 x 4096 -> 4096    11.5   34 / 25, 18.7 / 19.0, 11.1   128 of 64
+//   512 x 8192 -> 2048    18.5   80 / 44, 30 / 34, 18.4       256 of 64
+//   301 x 1024 -> 8192    11.8   23 / 11.5, 11.0 / 10.7, 12.0
+//  1024 x 4096 -> 4096    21.8   48 / 27.5, 21.9 / 31, 31     256 of 128
+//  2048 x 7168 -> 2048    32.7   74 / 45, 34 / 49, 50         256 of 128
+//  4096 x 4096 -> 2048    36.1   51 / 35.6, 42 / 55, 57       512 of 128
+//  8 x 100 x 4096 -> 4096  44.6  49 / 45, 42 / 46, 46
+//    48 x 7168 -> 1024    14.2   - / -, 21.8 / 29, 15.6; 2 splits 14.8    16 of 64
+//  1000 x 7008 -> 200     15.1   - / -, 36 / 29, 19.1; 4 splits 15.6      64 of 64
+// binary32 4096 x 4096 -> 4096  122   - / 124, 145 / 161, 176
+// Rows that pass through registers always take tiles of 64: a stage of 128 does
+// not fit a thread's registers (1995 x 159 -> 6254: 59 us, with 128 74; 4000 x
+// 1001 -> 2001 58 either way).
 Plan plan_of8(const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
   Plan p{64, 2, 1};
   const uint64_t steps = (a.k + 127) / 128;
   const uint64_t t128 = expect_tiles(kForward, a, 128), t64 = expect_tiles(kForward, a, 64);
   if (rows != kAnyRows && dt == LL_BF16 && expect_tiles(kForward, a, 256) >= kFill) {
     p.tile = 256;
-  } else if (t128 >= kFill) {
+  } else if (rows != kAnyRows && t128 >= kFill) {
     p.tile = 128;
     if (t128 <= kFill * 9 / 8 && steps >= 12) p.stages = 4;
   } else {
-    if (t64 <= 2 * kFill) p.stages = 4;
-    if (t64 < 200) {
-      // splits of whole words of scales
+    if (rows != kAnyRows && t64 <= 2 * kFill) p.stages = 4;
+    if (t64 < 200) {  // too few tiles: splits of whole words of scales
       const uint64_t words = (steps + kScaleStages - 1) / kScaleStages;
       const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
       const uint64_t most = std::min<uint64_t>(std::min<uint64_t>(16, words), std::min(room, kMaxParts) / std::max<uint64_t>(one, 1));
@@ -59,7 +75,6 @@ Plan plan_of8(const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
       }
     }
   }
-  if (rows == kAnyRows) p.stages = 2;
   return p;
 }
 
@@ -100,7 +115,7 @@ int launch_tiles8(Args8 &a, bool gate, void *stream) {
 template <typename O, Rows ROWS>
 int launch_plan8(Args8 &a, const Plan &p, bool gate, void *stream) {
   if constexpr (ROWS == kAnyRows) {
-    return p.tile == 128 ? launch_tiles8<O, 128, 2, ROWS>(a, gate, stream) : launch_tiles8<O, 64, 2, ROWS>(a, gate, stream);
+    return launch_tiles8<O, 64, 2, ROWS>(a, gate, stream);
   } else {
     if constexpr (sizeof(O) == 2) {
       if (p.tile == 256) return launch_tiles8<O, 256, 2, ROWS>(a, gate, stream);

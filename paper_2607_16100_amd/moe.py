@@ -397,6 +397,14 @@ def scales_of(*shape, device="cuda", stream=None) -> torch.Tensor:
     return wide.view(E8M0)[..., :shape[-1]]
 
 
+def _codes_for(stream, *shape, device) -> torch.Tensor:
+    """Memory for codes, whose rows start at multiples of 16 bytes: products load
+    those straight into shared memory."""
+    wide = (shape[-1] + 15) // 16 * 16
+    t = _new(stream, *shape[:-1], wide, dtype=E4M3, device=device)
+    return t if wide == shape[-1] else t[..., :shape[-1]]
+
+
 def _like(t, name: str, dev: int, rows: int, cols: int, dtype) -> int:
     """_mat, sooner done where the rows are contiguous."""
     if t.shape == (rows, cols) and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev:
@@ -432,7 +440,8 @@ def _readable(t, name: str, nbytes: int) -> None:
 def quantise(x, *, act: str = "none", offsets=None, out=None, scales=None, stream=None):
     """(out, scales): act(x) in 8 bits (float8_e4m3fn [rows, features]) with a
     power of two (float8_e8m0fnu [rows, ceil(features / 128)]) for each 128
-    features of a row; see ll_quantise.  With ``offsets``, rows behind the last
+    features of a row; see ll_quantise.  Memory it makes has rows at multiples of
+    16 codes and of 4 scales.  With ``offsets``, rows behind the last
     group are left as they are."""
     dev = _device()
     ldx = _mat(x, "x", dev)
@@ -443,7 +452,7 @@ def quantise(x, *, act: str = "none", offsets=None, out=None, scales=None, strea
         raise ValueError(f"x: {width} features, a gated activation needs an even number")
     h = width // 2 if act in lm.GATED else width
     if out is None:
-        out = _new(stream, n, h, dtype=E4M3, device=x.device)
+        out = _codes_for(stream, n, h, device=x.device)
     if scales is None:
         scales = scales_of(n, (h + 127) // 128, device=x.device, stream=stream)
     end = None
@@ -480,7 +489,7 @@ def quantise_weight(w, *, transpose: bool = False, out=None, scales=None, stream
     rows, cols = (i, o) if transpose else (o, i)
     lead = () if w.dim() == 2 else (g,)
     if out is None:
-        out = _new(stream, *lead, rows, cols, dtype=E4M3, device=w.device)
+        out = _codes_for(stream, *lead, rows, cols, device=w.device)
     if scales is None:
         scales = scales_of(*lead, (rows + 127) // 128, (cols + 127) // 128, device=w.device, stream=stream)
     if out.dtype is not E4M3 or out.dim() != w.dim():
@@ -600,7 +609,7 @@ def norm(y, weight=None, *, residual=None, gate=None, scale: float = 1.0, post=N
     if h is None and weight is not None:
         h = _new(stream, n, f, dtype=dt, device=device)
     if q is None and quantised:
-        q = _new(stream, n, f, dtype=E4M3, device=device)
+        q = _codes_for(stream, n, f, device=device)
     xp = gp = rp = hp = qp = sp = None
     ldx = ldr = ldh = ldq = f
     lds = 0
