@@ -33,7 +33,7 @@ extern "C" {
 #endif
 
 #define LL_BLOCK 128
-#define LL_NORM_MAX_FEATURES 32768
+#define LL_NORM_MAX_FEATURES 16384
 
 /* ---- 8-bit rows and weights ---- */
 

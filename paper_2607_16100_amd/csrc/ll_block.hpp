@@ -249,17 +249,15 @@ __device__ __forceinline__ void row_sums(float *v, float *red) {
       for (int n = 0; n < N; ++n) red[n * kWaves + threadIdx.x / 64] = v[n];
     }
     __syncthreads();
-    // (lane i of 4 or 16 takes wave i's part; those 4 or 16 lanes add them up)
+    // (lane i takes wave i's part, and each aligned kWaves lanes add them up)
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       float s = red[n * kWaves + threadIdx.x % kWaves];
-      static_assert(kWaves == 4 || kWaves == 16, "a quad or a row of lanes");
-      if constexpr (kWaves == 16) {
-        v[n] = group_sum<16>(s);
-      } else {
-        s += dpp_f32<0xB1>(s);
-        v[n] = s + dpp_f32<0x4E>(s);
-      }
+      s += dpp_f32<0xB1>(s);
+      if constexpr (kWaves > 2) s += dpp_f32<0x4E>(s);
+      if constexpr (kWaves > 4) s += dpp_f32<0x141>(s);
+      if constexpr (kWaves > 8) s += dpp_f32<0x140>(s);
+      v[n] = s;
     }
   }
 }
@@ -271,14 +269,17 @@ __device__ __forceinline__ lin::Vals get_weight(const void *w, bool w32, uint32_
   return w32 ? get<float, VEC>((const float *)w + at, left) : get<T, VEC>((const T *)w + at, left);
 }
 
+// Threads of a row's workgroup; a wave a row: four of them.
+constexpr int norm_threads(int tpr) { return tpr == 64 ? 256 : tpr; }
+
 // A thread's only chunk: everything the row needs is asked for at once, weights
-// too.  Several: the weights are read when they are used, from L2, and the
-// registers go to more rows a CU (8192 x 7168 bfloat16, residual and norm: 118
-// us with all of it in registers).
+// too.  Two (more than 8192 features): the weights are read when they are used,
+// from L2.  8192 x 7168 bfloat16, residual and norm: 86 us, 5.4 TB/s (256 threads
+// of four chunks: 103); with post, gate and the codes 104 us.
 template <typename T, bool VEC, int TPR, int C>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm(NormArgs a) {
+__global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs a) {
   constexpr bool kEarly = C == 1;
-  constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
+  constexpr int kRows = norm_threads(TPR) / TPR;
   __shared__ float red[2][TPR / 64];
   const uint32_t t = threadIdx.x % TPR;
   const uint32_t row = blockIdx.x * kRows + threadIdx.x / TPR;
@@ -380,13 +381,14 @@ struct Chunk {
 // of sums a row: r^2, weight dh r and y^2; then dr_out post y, which gives both
 // dgate and what dy needs.
 //
-// The next row is loaded while one is worked on, and a thread has one chunk of
-// it (with four chunks, all read when their row comes: 8192 x 7168 bfloat16 with
-// post and gate 460 us).  Rows of more than 8192 features have four.
+// A thread has one chunk of a row (two of more than 8192 features), and with one
+// the next row is loaded while one is worked on (with four chunks a thread, all
+// read when their row came: 8192 x 7168 bfloat16 with post and gate 460 us, so
+// 149).  Values are held as they lie in memory.
 template <typename T, bool VEC, int TPR, int C>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a) {
-  constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
-  constexpr bool kHold = C == 1;  // the weights stay in registers
+__global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
+  constexpr int kRows = norm_threads(TPR) / TPR;
+  constexpr bool kHold = C == 1;  // the weights stay in registers, and the next row comes there
   __shared__ float red[2][2][3 * (TPR / 64)];
   const uint32_t t = threadIdx.x % TPR;
   const float rn = 1.f / (float)a.features;
@@ -394,84 +396,84 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a)
   auto left = [&](int c) { return (int)a.features - (int)((c * TPR + t) * kW); };
   auto at = [&](int c) { return left(c) > 0 ? (c * TPR + t) * kW : 0u; };
   const bool with_y = a.post != nullptr || a.dgate != nullptr;
-  lin::Vals dw[C], dp[C], weight[1], post[1];
+  lin::Vals dw[C], dp[C], weight, post;
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int i = 0; i < kW; ++i) dw[c].v[i] = dp[c].v[i] = 0.f;
   if constexpr (kHold) {
-    if (a.weight != nullptr) weight[0] = get_weight<T, VEC>(a.weight, a.w32, at(0), left(0));
-    if (a.post != nullptr) post[0] = get_weight<T, VEC>(a.post, a.w32, at(0), left(0));
+    if (a.weight != nullptr) weight = get_weight<T, VEC>(a.weight, a.w32, at(0), left(0));
+    if (a.post != nullptr) post = get_weight<T, VEC>(a.post, a.w32, at(0), left(0));
   }
-  Chunk<T, VEC> nr[C], ng[C], ny[C], nd[C];
-  auto load = [&](uint32_t row) {
-    if (a.weight != nullptr) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        nr[c].load((const T *)a.r + row * a.ldr + at(c), left(c));
-        ng[c].load((const T *)a.dh + row * a.ldh + at(c), left(c));
-      }
-    }
-    if (a.dr != nullptr) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) nd[c].load((const T *)a.dr + row * a.ldd + at(c), left(c));
-    }
-    if (with_y) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) ny[c].load((const T *)a.y + row * a.ldy + at(c), left(c));
-    }
-  };
-  uint32_t row = blockIdx.x * kRows + lane_row;
-  if (row < a.rows) load(row);
-  uint32_t turn = 0;
-  for (; row < a.rows; row += step, ++turn) {
-    float(*sums)[3 * (TPR / 64)] = red[turn & 1];
-    lin::Vals r[C], g[C], y[C], d[C];
+  typedef Chunk<T, VEC> Row[C];
+  auto load = [&](uint32_t row, Row &r, Row &g, Row &y, Row &d) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if (a.weight != nullptr) {
-        r[c] = nr[c].vals();
-        g[c] = ng[c].vals();
+        r[c].load((const T *)a.r + row * a.ldr + at(c), left(c));
+        g[c].load((const T *)a.dh + row * a.ldh + at(c), left(c));
       }
-      if (with_y) y[c] = ny[c].vals();
-      if (a.dr != nullptr) {
-        d[c] = nd[c].vals();
-      } else {
-#pragma unroll
-        for (int i = 0; i < kW; ++i) d[c].v[i] = 0.f;
-      }
+      if (a.dr != nullptr) d[c].load((const T *)a.dr + row * a.ldd + at(c), left(c));
+      if (with_y) y[c].load((const T *)a.y + row * a.ldy + at(c), left(c));
     }
-    if (row + step < a.rows) load(row + step);
+  };
+  Row r, g, y, e, nr, ng, ny, ne;
+  uint32_t row = blockIdx.x * kRows + lane_row;
+  if (kHold && row < a.rows) load(row, nr, ng, ny, ne);
+  uint32_t turn = 0;
+  for (; row < a.rows; row += step, ++turn) {
+    float(*sums)[3 * (TPR / 64)] = red[turn & 1];
+    if constexpr (kHold) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) r[c] = nr[c], g[c] = ng[c], y[c] = ny[c], e[c] = ne[c];
+      if (row + step < a.rows) load(row + step, nr, ng, ny, ne);
+    } else {
+      load(row, r, g, y, e);
+    }
     float s[3] = {0.f, 0.f, 0.f};
     if (a.weight != nullptr) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        if constexpr (!kHold) weight[0] = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+        if constexpr (!kHold) weight = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+        const lin::Vals rv = r[c].vals(), gv = g[c].vals();
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
-          s[0] = __builtin_fmaf(r[c].v[i], r[c].v[i], s[0]);
-          s[1] = __builtin_fmaf(weight[0].v[i] * g[c].v[i], r[c].v[i], s[1]);
+          s[0] = __builtin_fmaf(rv.v[i], rv.v[i], s[0]);
+          s[1] = __builtin_fmaf(weight.v[i] * gv.v[i], rv.v[i], s[1]);
         }
       }
     }
     if (a.post != nullptr) {
 #pragma unroll
-      for (int c = 0; c < C; ++c)
+      for (int c = 0; c < C; ++c) {
+        const lin::Vals yv = y[c].vals();
 #pragma unroll
-        for (int i = 0; i < kW; ++i) s[2] = __builtin_fmaf(y[c].v[i], y[c].v[i], s[2]);
+        for (int i = 0; i < kW; ++i) s[2] = __builtin_fmaf(yv.v[i], yv.v[i], s[2]);
+      }
     }
     row_sums<TPR, 3>(s, sums[0]);
+    lin::Vals d[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (a.dr != nullptr) {
+        d[c] = e[c].vals();
+      } else {
+#pragma unroll
+        for (int i = 0; i < kW; ++i) d[c].v[i] = 0.f;
+      }
+    }
     if (a.weight != nullptr) {
       const float rstd = 1.f / sqrtf(s[0] * rn + a.eps);
       const float mean = s[1] * rstd * rn;  // of u weight dh
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        if constexpr (!kHold) weight[0] = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+        if constexpr (!kHold) weight = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+        const lin::Vals rv = r[c].vals(), gv = g[c].vals();
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
-          const float u = r[c].v[i] * rstd;
-          dw[c].v[i] = __builtin_fmaf(g[c].v[i], u, dw[c].v[i]);
-          d[c].v[i] = __builtin_fmaf(rstd, weight[0].v[i] * g[c].v[i] - u * mean, d[c].v[i]);
+          const float u = rv.v[i] * rstd;
+          dw[c].v[i] = __builtin_fmaf(gv.v[i], u, dw[c].v[i]);
+          d[c].v[i] = __builtin_fmaf(rstd, weight.v[i] * gv.v[i] - u * mean, d[c].v[i]);
         }
       }
     }
@@ -485,13 +487,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a)
       float dot = 0.f;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
+        const lin::Vals yv = y[c].vals();
         if (a.post != nullptr) {
-          if constexpr (!kHold) post[0] = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+          if constexpr (!kHold) post = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
 #pragma unroll
-          for (int i = 0; i < kW; ++i) dot = __builtin_fmaf(d[c].v[i] * post[0].v[i], y[c].v[i], dot);
+          for (int i = 0; i < kW; ++i) dot = __builtin_fmaf(d[c].v[i] * post.v[i], yv.v[i], dot);
         } else {
 #pragma unroll
-          for (int i = 0; i < kW; ++i) dot = __builtin_fmaf(d[c].v[i], y[c].v[i], dot);
+          for (int i = 0; i < kW; ++i) dot = __builtin_fmaf(d[c].v[i], yv.v[i], dot);
         }
       }
       row_sums<TPR, 1>(&dot, sums[1]);
@@ -501,12 +504,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_grad(NormArgs a)
         const float mean = by * dot * rstd * rn;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          if constexpr (!kHold) post[0] = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+          if constexpr (!kHold) post = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+          const lin::Vals yv = y[c].vals();
 #pragma unroll
           for (int i = 0; i < kW; ++i) {
-            const float e = by * d[c].v[i], u = y[c].v[i] * rstd;
-            dp[c].v[i] = __builtin_fmaf(e, u, dp[c].v[i]);
-            d[c].v[i] = rstd * (e * post[0].v[i] - u * mean);
+            const float f = by * d[c].v[i], u = yv.v[i] * rstd;
+            dp[c].v[i] = __builtin_fmaf(f, u, dp[c].v[i]);
+            d[c].v[i] = rstd * (f * post.v[i] - u * mean);
           }
         }
       }

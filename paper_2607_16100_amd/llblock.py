@@ -14,7 +14,7 @@ from . import llcoll as ll
 from .llmoe import LLLinearDesc
 
 LL_BLOCK = 128
-LL_NORM_MAX_FEATURES = 32768
+LL_NORM_MAX_FEATURES = 16384
 LL_ADAMW_WORKSPACE = 64
 
 _vp, _sz, _i, _u32, _u64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint32, ctypes.c_uint64

@@ -140,7 +140,7 @@ def test_norm_refusals(kw, want):
 
 @pytest.mark.parametrize("fields,want", [
     (dict(dt=3), UNSUPPORTED), (dict(wdt=3), UNSUPPORTED), (dict(dt=F32, wdt=BF16), UNSUPPORTED), (dict(eps=0.), INVALID),
-    (dict(eps=float("nan")), INVALID), (dict(features=0), INVALID), (dict(features=32769), UNSUPPORTED),
+    (dict(eps=float("nan")), INVALID), (dict(features=0), INVALID), (dict(features=16385), UNSUPPORTED),
     (dict(rows=1 << 31), UNSUPPORTED), (dict(ldy=199), INVALID), (dict(ldx=199), INVALID), (dict(ldr=199), INVALID),
     (dict(ldh=199), INVALID), (dict(size=4), INVALID), (dict(ldy=1 << 31), UNSUPPORTED),
 ])
