@@ -15,6 +15,13 @@
  * exact and the rounding to 8 bits (to nearest, ties to even) the only one.
  * Infinities and NaN become no number and do not count for the scale.
  *
+ * Errors are those of llmoe.h.  LL_ERR_UNSUPPORTED besides: more than
+ * LL_NORM_MAX_FEATURES features of a norm, 2^22 rows or more of one of over 4096
+ * features (2^23 of over 2048, and so on), 2^29 blocks or more of rows to
+ * quantise, scale rows of a product more than 2^18 apart, a gated ll_linear8
+ * with a weight of more than 0xF0000000 bytes a group, more than 2^40 values of a
+ * tensor to update.
+ *
  * Scale arrays: rows start at multiples of 4 bytes (address and leading
  * dimension), and a row's bytes up to the next multiple of 4 past its blocks
  * can be read; they are not used.
@@ -163,7 +170,8 @@ typedef struct {
  * are rounded up or down at random, by a hash of seed, t and the value's
  * number, with the probability that keeps their mean: a state that moves by a
  * thousandth would else stay where it is.  workspace: LL_ADAMW_WORKSPACE bytes,
- * 16-byte aligned.  The tensors lie apart. */
+ * 16-byte aligned.  The tensors lie apart; eps is above 0.  Steps that share
+ * states or the workspace follow one another. */
 #define LL_ADAMW_WORKSPACE 64
 int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t count, int32_t *step, const float *lr_ptr,
              const float *grad_scale, void *workspace, size_t workspace_bytes, void *stream);

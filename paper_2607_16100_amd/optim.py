@@ -24,9 +24,8 @@ STATES = {"f32": 32, "8bit": 8}
 _TYPES = {32: (torch.float32, torch.float32), 8: (torch.float8_e4m3fn, torch.float8_e5m2)}
 
 # what changes from step to step of a row of ll_adamw's table
-_ROW = np.dtype({"names": ["grad", "gdt"], "formats": [np.uint64, np.int32],
-                 "offsets": [lb.LLAdamwTensor.grad.offset, lb.LLAdamwTensor.gdt.offset],
-                 "itemsize": ctypes.sizeof(lb.LLAdamwTensor)})
+_ROW = np.dtype({"names": ["param", "grad", "gdt"], "formats": [np.uint64, np.uint64, np.int32],
+                 "offsets": [getattr(lb.LLAdamwTensor, f).offset for f in ("param", "grad", "gdt")], "itemsize": ctypes.sizeof(lb.LLAdamwTensor)})
 
 
 class AdamW:
@@ -41,7 +40,9 @@ class AdamW:
     Values between a parameter's last and the next multiple of 128 stay 0.
 
     ``state``: a ``state_dict()`` to go on from, whose tensors are used, not
-    copied.  The options may be changed between steps (``opt.lr = ...``)."""
+    copied.  The options may be changed between steps (``opt.lr = ...``).  Steps of
+    one optimiser follow one another: two at once, on two streams, are not
+    meant."""
 
     def __init__(self, params: Sequence[torch.Tensor], *, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.0, states: str = "f32", seed: int = 0, state: Optional[dict] = None):
@@ -84,10 +85,10 @@ class AdamW:
         self._work = torch.empty(lb.LL_ADAMW_WORKSPACE, dtype=torch.uint8, device=device)
         self._table = (lb.LLAdamwTensor * len(self.params))()
         self._fields = np.frombuffer(self._table, dtype=_ROW)  # the same memory
-        self._sizes = [p.numel() for p in self.params]
+        self._sizes, self._types = [p.numel() for p in self.params], [p.dtype for p in self.params]
         es = 1 if eight else 4
         for t, p, w, at in zip(self._table, self.params, self.masters, self.offsets):
-            t.param, t.n, t.at, t.dt = p.data_ptr(), p.numel(), at, _DT[p.dtype]
+            t.n, t.at, t.dt = p.numel(), at, _DT[p.dtype]
             t.master = None if w is None else w.data_ptr()
             t.m, t.v = self.m.data_ptr() + at * es, self.v.data_ptr() + at * es
             if eight:
@@ -127,10 +128,16 @@ class AdamW:
             raise ValueError("the parameters are not on the current GPU")
         if len(grads) != len(self._sizes):
             raise ValueError(f"grads: {len(grads)}, expected {len(self._sizes)}")
-        for i, (n, g) in enumerate(zip(self._sizes, grads)):
+        # (a parameter's memory may be another than at the last step)
+        for i, (n, p, g) in enumerate(zip(self._sizes, self.params, grads)):
             if g.numel() != n or g.get_device() != dev or not g.is_contiguous():
                 raise ValueError(f"grads[{i}]: a contiguous tensor of {n} values on the parameters' GPU is needed")
+            if p.numel() != n or p.get_device() != dev or not p.is_contiguous():
+                raise ValueError(f"params[{i}]: no longer a contiguous tensor of {n} values on its GPU")
+        if [p.dtype for p in self.params] != self._types:
+            raise ValueError("params: their types have changed")
         table, fields = self._table, self._fields
+        fields["param"] = [p.data_ptr() for p in self.params]
         try:
             fields["gdt"] = [_DT[g.dtype] for g in grads]
         except KeyError as e:

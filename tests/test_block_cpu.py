@@ -105,6 +105,15 @@ def test_linear8_descriptor_refusals(fields, want):
         assert lb.ll_linear8_bytes(desc)[0] == want
 
 
+@pytest.mark.parametrize("features,rows", [(8192, 1 << 22), (4096, 1 << 23), (2048, 1 << 24), (1024, 1 << 25), (16384, 1 << 22)])
+def test_norm_rows_past_a_launch(features, rows):
+    assert norm(nd(rows=rows, features=features, ldy=features), x=0, r=0, h=1 << 50) == UNSUPPORTED
+
+
+def test_quantise_blocks_past_a_launch():
+    assert quantise(rows=1 << 29, features=128, ldx=128, ldq=128, q=1 << 50, scales=1 << 51) == UNSUPPORTED
+
+
 def test_linear8_of_no_rows():
     assert linear8(d(rows=0), x=0, xs=0, w=0, ws=0, y=0) == OK
     assert lb.ll_linear8_bytes(d(rows=0)) == (OK, 0)
@@ -187,7 +196,7 @@ def adamw(count=1, step=A, work=B, work_bytes=64, lr=1e-3, beta1=0.9, beta2=0.99
 
 @pytest.mark.parametrize("kw,want", [
     (dict(size=8), INVALID), (dict(bits=16), INVALID), (dict(beta1=1.0), INVALID), (dict(beta2=-0.5), INVALID),
-    (dict(beta1=float("nan")), INVALID), (dict(eps=-1.0), INVALID), (dict(decay=-1.0), INVALID),
+    (dict(beta1=float("nan")), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=0.0), INVALID), (dict(decay=-1.0), INVALID),
     (dict(lr=float("nan")), INVALID), (dict(lr=-1.0), INVALID), (dict(step=0), INVALID), (dict(step=A + 2), INVALID),
     (dict(work=0), INVALID), (dict(work=B + 8), INVALID), (dict(work_bytes=63), SCRATCH), (dict(lr_ptr=G + 1), INVALID),
     (dict(scale=G + 2), INVALID), (dict(null=True), INVALID), (dict(param=0), INVALID), (dict(grad=0), INVALID),

@@ -231,6 +231,25 @@ def test_going_on_from_a_state():
         assert torch.equal(a.m.view(torch.uint8), b.m.view(torch.uint8)) and int(b.count) == 2
 
 
+def test_parameters_that_move():
+    """A parameter whose memory is another one now is updated there; one of another shape or type is refused."""
+    g = gen(14)
+    p = randn(g, 300)
+    opt = AdamW([p], **OPTS)
+    old, grad = p.data, randn(g, 300)
+    p.data = old.clone()
+    opt.step([grad])
+    assert not torch.equal(p, old)
+    twin = old.clone()
+    AdamW([twin], **OPTS).step([grad])
+    assert torch.equal(p, twin)
+    for other in (torch.zeros(301, device=DEV), torch.zeros(300, dtype=BF16, device=DEV), torch.zeros(600, device=DEV)[::2]):
+        p.data = other
+        with pytest.raises(ValueError):
+            opt.step([grad])
+    assert int(opt.count) == 1
+
+
 def test_unaligned_tensors_and_a_side_stream():
     g = gen(13)
     for states in ("f32", "8bit"):
@@ -280,7 +299,7 @@ def test_refusals():
         opt.step([p.half()])
     with pytest.raises(ValueError):
         opt.step([p.clone()], lr=torch.zeros(2, device=DEV))
-    for kw in (dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=-1.0), dict(lr=math.nan),
+    for kw in (dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=-1.0), dict(eps=0.0), dict(lr=math.nan),
                dict(weight_decay=-1.0)):
         with pytest.raises(ll.LLError):
             AdamW([p], **kw).step([p.clone()])
