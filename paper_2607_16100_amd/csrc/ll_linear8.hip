@@ -92,15 +92,16 @@ int launch_tiles8(Args8 &a, bool gate, void *stream) {
   a.tiles_m = (a.m + B - 1) / B;
   const uint64_t grid = count_tiles(kForward, a, B) / ((a.n + B - 1) / B) * a.tiles_n;
   if (grid * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
-  // a short last round of 256-wide tiles runs in quarters, as in the other products
+  // a short last round of 256-wide tiles runs in parts
   const uint64_t rest = grid % kRound;
   const bool tail = B == 256 && grid > kRound && (a.offsets != nullptr || (rest != 0 && rest <= kMaxTail));
   if (tail) a.tail = 1;
   hipLaunchKernelGGL((pick8<O, B, ST, ROWS>(gate)), dim3((unsigned)grid, a.splits), dim3(256), 0, (hipStream_t)stream, a);
   if constexpr (B == 256) {
     if (tail) {
-      a.tail = 2;
-      hipLaunchKernelGGL((pick8<O, 128, 4, ROWS>(gate)), dim3(4 * kMaxTail), dim3(256), 0, (hipStream_t)stream, a);
+      const tile8_fn parts = gate ? k_tail8<O, true, ROWS> : k_tail8<O, false, ROWS>;
+      static_assert(8 * kEighths <= 4 * kMaxTail, "a workgroup a part");
+      hipLaunchKernelGGL(parts, dim3(4 * kMaxTail), dim3(256), 0, (hipStream_t)stream, a);
     }
   }
   if (a.parts != nullptr) {

@@ -163,23 +163,23 @@ __device__ __forceinline__ void finish_tile8(const Args8 &a, int g, uint32_t tn,
 //
 // A row's scales come four stages to a word, through LDS like the operands; each
 // stage reads its words from there and moves them down to its byte.
+// LDS of a tile: its stages and scales, or its epilogue.
+constexpr int tile8_lds(int bm, int bn, int st) {
+  const int use = st * (bm + bn) * 128 + 2 * (bm + bn) * 4 + 1024, epi = epilogue8(bm, bn);
+  return use > epi ? use : epi;
+}
+
 template <typename O, int BM, int BN, int ST, bool GATED, Rows ROWS>
-__global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args8 a) {
+__device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32_t m0, uint32_t m_end, char *lds) {
   constexpr bool VEC = ROWS != kAnyRows;  // loads go straight into LDS
   static_assert(VEC || ST == 2, "a stage in registers at a time");
   constexpr int NW = 4, WTM = BM / 2, WTN = BN / 2, FM = WTM / 32, FN = WTN / 32;
   constexpr int FH = FM > 1 ? FM / 2 : 1;  // fragments of a wave's rows in the tile's upper half
   constexpr int BK = 128, kStage = (BM + BN) * 128, kScales = (BM + BN) * 4;
-  constexpr int kEpi = epilogue8(BM, BN), kUse = ST * kStage + 2 * kScales + NW * 256;
-  constexpr int kLds = kUse > kEpi ? kUse : kEpi;
-  __shared__ __attribute__((aligned(1024))) char lds[kLds];
   const int lane = threadIdx.x % 64;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int wm = wave / 2, wn = wave % 2;
-
-  int g = 0;
-  uint32_t tn = 0, m0 = 0, m_end = a.m, k = a.k;
-  if (!find_rows(a, blockIdx.x, BM, &g, &m0, &m_end, &tn)) return;
+  uint32_t k = a.k;
   const e4m3 *p = (const e4m3 *)a.p, *q = (const e4m3 *)a.q + (uint64_t)g * a.qstride;
 
   // this workgroup's share of k: whole words of scales
@@ -410,6 +410,73 @@ __global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args
   lds_barrier();  // every wave is past its last stage, and no load is under way
 
   finish_tile8<O, BM, BN, GATED>(a, g, tn, m0, m_end, lower, acc, lds);
+}
+
+template <typename O, int BM, int BN, int ST, bool GATED, Rows ROWS>
+__global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args8 a) {
+  __shared__ __attribute__((aligned(1024))) char lds[tile8_lds(BM, BN, ST)];
+  int g = 0;
+  uint32_t tn = 0, m0 = 0, m_end = a.m;
+  if (!find_rows(a, blockIdx.x, BM, &g, &m0, &m_end, &tn)) return;
+  tile8<O, BM, BN, ST, GATED, ROWS>(a, g, tn, m0, m_end, lds);
+}
+
+// The short last round of 256-wide tiles that their launch leaves out (tail_tiles):
+// each tile in quarters of 128 x 128, or in eighths of 128 x 64 where there are so
+// few of them that quarters would leave half of the CUs without one.
+constexpr uint32_t kEighths = 32;
+
+// Part `id`: as find_rows, and *cols, the columns of parts a tile has.
+__device__ __forceinline__ bool find_part(const Args &a, uint32_t id, int *group, uint32_t *row0, uint32_t *row1,
+                                          uint32_t *tn, uint32_t *cols) {
+  constexpr uint32_t bm = 256;
+  uint32_t lo, hi, tiles, incl = 0, rows = 0, tm;
+  if (a.offsets == nullptr) {
+    rows = (a.rows + bm - 1) / bm;
+  } else {
+    for (int g0 = 0; g0 < a.groups; g0 += 64) {
+      incl = scan_tiles(a, g0, bm, &lo, &hi, &tiles);
+      rows += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+    }
+  }
+  const uint32_t total = rows * a.tiles_n, rest = tail_tiles(total);
+  *cols = rest <= kEighths ? 4 : 2;
+  if (id >= 2 * *cols * rest) return false;
+  const uint32_t part = id / rest;
+  number_of(total - rest + id % rest, rows, a.tiles_n, &tm, tn);
+  *tn = *tn * *cols + part % *cols;
+  auto place = [&](int g, uint32_t first, uint32_t end) {
+    *group = g;
+    *row0 = first + part / *cols * (bm / 2);
+    *row1 = end;
+    return *row0 < *row1;
+  };
+  if (a.offsets == nullptr) return place(0, tm * bm, a.rows);
+  uint32_t before = 0;
+  for (int g0 = 0; g0 < a.groups; g0 += 64) {
+    if (a.groups > 64) incl = scan_tiles(a, g0, bm, &lo, &hi, &tiles);
+    const uint64_t past = __ballot(before + incl > tm);
+    if (past != 0) {
+      const int who = __ffsll((unsigned long long)past) - 1;
+      const uint32_t skip = before + __builtin_amdgcn_readlane((int)(incl - tiles), who);
+      return place(g0 + who, __builtin_amdgcn_readlane((int)lo, who) + (tm - skip) * bm,
+                   __builtin_amdgcn_readlane((int)hi, who));
+    }
+    before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+  }
+  return false;
+}
+
+template <typename O, bool GATED, Rows ROWS>
+__global__ __launch_bounds__(256, 1) void k_tail8(Args8 a) {
+  __shared__ __attribute__((aligned(1024))) char lds[tile8_lds(128, 128, 4)];
+  int g = 0;
+  uint32_t tn = 0, m0 = 0, m_end = 0, cols = 0;
+  if (!find_part(a, blockIdx.x, &g, &m0, &m_end, &tn, &cols)) return;
+  if (cols == 4)
+    tile8<O, 128, 64, 4, GATED, ROWS>(a, g, tn, m0, m_end, lds);
+  else
+    tile8<O, 128, 128, 4, GATED, ROWS>(a, g, tn, m0, m_end, lds);
 }
 
 // ---------------------------------------------------------------- the wide tile kernel

@@ -118,12 +118,15 @@ def test_product(name, dtype, act, bias, residual, save, layout):
     check(name, dtype, act, bias, residual, save, layout)
 
 
-# 256-wide tiles: whole ones, a short last round in quarters, groups whose last
-# tile has no lower half; 128-wide ones at one and at two a CU
+# 256-wide tiles: whole ones, a short last round in quarters and in eighths, groups
+# whose last tile has no lower half; 128-wide ones at one and at two a CU
 LARGE = {
     "full": (None, 4096, 256, 4096),
     "quarters": (None, 4100, 320, 4352),
     "groups": ([700, 0, 130, 2049, 1200, 257], 0, 192, 4104),
+    "eighths": (None, 4100, 336, 4096),
+    "eighths_groups": ([700, 0, 130, 2049, 1000], 0, 640, 4096),
+    "eighths_many": ([40] * 30 + [0] * 40 + [37] * 30 + [1500], 0, 128, 1024),  # more than 64 groups
     "deep": (None, 4096, 1424, 4096),  # twelve stages, the last short
     "odd": (None, 4000, 1408, 4096),   # eleven
     "wide128": (None, 2048, 1664, 2048),
