@@ -79,13 +79,14 @@ class AdamW:
                      "m_scales": _ones(total // 128, device) if eight else None,
                      "v_scales": _ones(total // 128, device) if eight else None,
                      "count": torch.zeros(1, dtype=torch.int32, device=device)}
-        self._check(state, total, mt, vt)
+        self._check_state(state, total, mt, vt)
         self.masters, self.m, self.v = state["masters"], state["m"], state["v"]
         self.m_scales, self.v_scales, self.count = state["m_scales"], state["v_scales"], state["count"]
         self._work = torch.empty(lb.LL_ADAMW_WORKSPACE, dtype=torch.uint8, device=device)
         self._table = (lb.LLAdamwTensor * len(self.params))()
         self._fields = np.frombuffer(self._table, dtype=_ROW)  # the same memory
-        self._sizes, self._types = [p.numel() for p in self.params], [p.dtype for p in self.params]
+        self._sizes = [p.numel() for p in self.params]
+        self._at: list = []  # the parameters' addresses in the table
         es = 1 if eight else 4
         for t, p, w, at in zip(self._table, self.params, self.masters, self.offsets):
             t.n, t.at, t.dt = p.numel(), at, _DT[p.dtype]
@@ -94,7 +95,18 @@ class AdamW:
             if eight:
                 t.m_scales, t.v_scales = self.m_scales.data_ptr() + at // 128, self.v_scales.data_ptr() + at // 128
 
-    def _check(self, state: dict, total: int, mt, vt) -> None:
+    def _check(self, tensors, name: str, dev: int) -> list:
+        """The tensors' type codes; one contiguous tensor of a parameter's size each."""
+        if [t.numel() for t in tensors] != self._sizes or [t.get_device() for t in tensors] != [dev] * len(self._sizes) \
+                or not all([t.is_contiguous() for t in tensors]):
+            raise ValueError(f"{name}: one contiguous tensor on the parameters' GPU a parameter, of its number of values, "
+                             "is needed")
+        try:
+            return [_DT[t.dtype] for t in tensors]
+        except KeyError as e:
+            raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(e)) from None
+
+    def _check_state(self, state: dict, total: int, mt, vt) -> None:
         dev = self._dev
         if len(state["masters"]) != len(self.params):
             raise ValueError(f"masters: {len(state['masters'])}, expected {len(self.params)}")
@@ -126,23 +138,14 @@ class AdamW:
         dev = _device()
         if dev != self._dev:
             raise ValueError("the parameters are not on the current GPU")
-        if len(grads) != len(self._sizes):
-            raise ValueError(f"grads: {len(grads)}, expected {len(self._sizes)}")
-        # (a parameter's memory may be another than at the last step)
-        for i, (n, p, g) in enumerate(zip(self._sizes, self.params, grads)):
-            if g.numel() != n or g.get_device() != dev or not g.is_contiguous():
-                raise ValueError(f"grads[{i}]: a contiguous tensor of {n} values on the parameters' GPU is needed")
-            if p.numel() != n or p.get_device() != dev or not p.is_contiguous():
-                raise ValueError(f"params[{i}]: no longer a contiguous tensor of {n} values on its GPU")
-        if [p.dtype for p in self.params] != self._types:
-            raise ValueError("params: their types have changed")
         table, fields = self._table, self._fields
-        fields["param"] = [p.data_ptr() for p in self.params]
-        try:
-            fields["gdt"] = [_DT[g.dtype] for g in grads]
-        except KeyError as e:
-            raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(e)) from None
+        fields["gdt"] = self._check(grads, "grads", dev)
         fields["grad"] = [g.data_ptr() for g in grads]
+        at = [p.data_ptr() for p in self.params]
+        if at != self._at:  # a parameter's memory is another than at the last step
+            if self._check(self.params, "params", dev) != [t.dt for t in table]:
+                raise ValueError("params: their types have changed")
+            fields["param"] = self._at = at
         rate, rate_at = self.lr if lr is None else lr, None
         if isinstance(rate, torch.Tensor):
             rate, rate_at = 0.0, _flat(rate, "lr", dev, 1, torch.float32)
