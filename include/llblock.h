@@ -69,7 +69,8 @@ int ll_quantise_weight(const void *w, size_t ldw, size_t wstride, int groups, si
  * are binary32, but for bfloat16 results the instruction cuts each of eight
  * consecutive k's products (8j .. 8j + 7) off 2^-13 below the power of two of
  * the largest of them, about 2^-15 of a result of normal values; binary32
- * results are summed in binary32 throughout.
+ * results are summed in binary32 throughout, from values that are bfloat16
+ * numbers with their scales (below 2^-126 they are 0, past its range infinite).
  * xs: [rows, ceil(in / LL_BLOCK)] at ldxs; ws: [groups][ceil(out / LL_BLOCK),
  * ceil(in / LL_BLOCK)] at ldws and wsstride.
  *
@@ -92,7 +93,8 @@ int ll_linear8_bytes(const ll_linear_desc *d, size_t *bytes);
  *   h = weight * r / sqrt(mean(r^2) + eps)    (weight NULL: no h)
  * y: a block's output, x: the residual stream before it, gate: one binary32
  * value a token, h: the next block's input.  Everything is binary32 until a
- * result is rounded to its type.  post and weight are of type wdt (dt or
+ * result is rounded to its type, sums of squares too: a row whose overflows
+ * (values of about 1e18 and more) becomes zeros.  post and weight are of type wdt (dt or
  * LL_F32).  Fill with ll_norm_desc_init (contiguous rows), then change. */
 typedef struct {
   uint32_t size; /* sizeof(ll_norm_desc), set by ll_norm_desc_init */

@@ -27,11 +27,6 @@ bool overlap(const void *a, size_t an, const void *b, size_t bn) {
 size_t span(size_t rows, size_t ld, size_t len, size_t es) {
   return rows == 0 || len == 0 ? 0 : ((rows - 1) * ld + len) * es;
 }
-// Every row starts at a 16-byte address (NULL: no rows).
-bool rows16(const void *p, size_t ld, size_t es) { return p == nullptr || (aligned(p, 16) && ld * es % 16 == 0); }
-// Every row of codes starts at an 8-byte address.
-bool rows8(const void *p, size_t ld) { return p == nullptr || (aligned(p, 8) && ld % 8 == 0); }
-
 size_t blocks_of(size_t n) { return (n + LL_BLOCK - 1) / LL_BLOCK; }
 
 int check_scales(const uint8_t *p, size_t ld, size_t blocks) {
@@ -40,34 +35,30 @@ int check_scales(const uint8_t *p, size_t ld, size_t blocks) {
 }
 
 template <typename T>
-int launch_quantise(const QuantArgs &a, bool vec, uint64_t items, void *stream) {
+int launch_quantise(const QuantArgs &a, uint64_t items, void *stream) {
   // Many rows: two blocks of a lane's loads under way.  Few: as many waves as there are blocks.
   const bool many = items >= 65536;
   const uint64_t per = many ? 32 : 16;
   const uint64_t grid = (items + per - 1) / per;
   if (grid * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
-  const auto fn = many ? (vec ? k_quantise<T, true, 2> : k_quantise<T, false, 2>)
-                       : (vec ? k_quantise<T, true, 1> : k_quantise<T, false, 1>);
-  hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
+  hipLaunchKernelGGL((many ? k_quantise<T, 2> : k_quantise<T, 1>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream, a);
   return launch_status();
 }
 
 template <typename T>
-void launch_weight(const WeightArgs &a, bool vec, bool transpose, dim3 grid, void *stream) {
-  const auto fn = transpose ? (vec ? k_quantise_weight<T, true, true> : k_quantise_weight<T, false, true>)
-                            : (vec ? k_quantise_weight<T, true, false> : k_quantise_weight<T, false, false>);
-  hipLaunchKernelGGL(fn, grid, dim3(256), 0, (hipStream_t)stream, a);
+void launch_weight(const WeightArgs &a, bool transpose, dim3 grid, void *stream) {
+  hipLaunchKernelGGL((transpose ? k_quantise_weight<T, true> : k_quantise_weight<T, false>), grid, dim3(256), 0, (hipStream_t)stream, a);
 }
 
 // ---------------------------------------------------------------- norms
 using norm_fn = void (*)(NormArgs);
 
 template <typename T, bool GRAD, int TPR, int C>
-norm_fn norm_of(bool vec) {
+norm_fn norm_of() {
   if constexpr (GRAD)
-    return vec ? k_norm_grad<T, true, TPR, C> : k_norm_grad<T, false, TPR, C>;
+    return k_norm_grad<T, TPR, C>;
   else
-    return vec ? k_norm<T, true, TPR, C> : k_norm<T, false, TPR, C>;
+    return k_norm<T, TPR, C>;
 }
 
 // Threads a row, its chunks a thread, and rows a workgroup takes at a time.
@@ -84,14 +75,14 @@ NormShape norm_shape(size_t features) {
 }
 
 template <typename T, bool GRAD>
-norm_fn pick_norm(const NormShape &s, bool vec) {
+norm_fn pick_norm(const NormShape &s) {
   switch (s.tpr * s.chunks) {
-    case 64: return norm_of<T, GRAD, 64, 1>(vec);
-    case 128: return norm_of<T, GRAD, 128, 1>(vec);
-    case 256: return norm_of<T, GRAD, 256, 1>(vec);
-    case 512: return norm_of<T, GRAD, 512, 1>(vec);
-    case 1024: return norm_of<T, GRAD, 1024, 1>(vec);
-    default: return norm_of<T, GRAD, 1024, 2>(vec);
+    case 64: return norm_of<T, GRAD, 64, 1>();
+    case 128: return norm_of<T, GRAD, 128, 1>();
+    case 256: return norm_of<T, GRAD, 256, 1>();
+    case 512: return norm_of<T, GRAD, 512, 1>();
+    case 1024: return norm_of<T, GRAD, 1024, 1>();
+    default: return norm_of<T, GRAD, 1024, 2>();
   }
 }
 
@@ -149,9 +140,8 @@ int ll_quantise(const void *x, size_t ldx, size_t rows, const int32_t *end, size
       overlap(end, 4, scales, sb))
     return LL_ERR_INVALID;
   QuantArgs a{x, q, scales, end, ldx, ldq, lds, (uint32_t)rows, (uint32_t)features, (uint32_t)blocks_of(features), (int)act};
-  const bool vec = rows16(x, ldx, es) && rows8(q, ldq) && (!lin::gated((int)act) || features * es % 16 == 0);
   const uint64_t items = (uint64_t)rows * a.blocks;
-  return dt == LL_F32 ? launch_quantise<float>(a, vec, items, stream) : launch_quantise<__bf16>(a, vec, items, stream);
+  return dt == LL_F32 ? launch_quantise<float>(a, items, stream) : launch_quantise<__bf16>(a, items, stream);
 }
 
 int ll_quantise_weight(const void *w, size_t ldw, size_t wstride, int groups, size_t out, size_t in, ll_dtype dt,
@@ -174,16 +164,12 @@ int ll_quantise_weight(const void *w, size_t ldw, size_t wstride, int groups, si
   const size_t wb = all(wstride, (out - 1) * ldw + in) * es, qb = all(qstride, (qr - 1) * ldq + qc);
   const size_t sb = all(sstride, (sr - 1) * lds + sc);
   if (overlap(w, wb, q, qb) || overlap(w, wb, scales, sb) || overlap(q, qb, scales, sb)) return LL_ERR_INVALID;
-  uint32_t wide = 16;
-  while (wide > 1 && (!aligned(q, wide) || ldq % wide != 0 || (groups > 1 && qstride % wide != 0))) wide /= 2;
-  if (wide == 2) wide = 1;
-  const WeightArgs a{w, q, scales, ldw, wstride, ldq, qstride, lds, sstride, (uint32_t)out, (uint32_t)in, wide};
-  const bool vec = rows16(w, ldw, es) && (groups == 1 || wstride * es % 16 == 0);
+  const WeightArgs a{w, q, scales, ldw, wstride, ldq, qstride, lds, sstride, (uint32_t)out, (uint32_t)in};
   const dim3 grid((unsigned)blocks_of(in), (unsigned)blocks_of(out), (unsigned)groups);
   if (dt == LL_F32)
-    launch_weight<float>(a, vec, transpose != 0, grid, stream);
+    launch_weight<float>(a, transpose != 0, grid, stream);
   else
-    launch_weight<__bf16>(a, vec, transpose != 0, grid, stream);
+    launch_weight<__bf16>(a, transpose != 0, grid, stream);
   return launch_status();
 }
 
@@ -255,10 +241,8 @@ int ll_norm(const ll_norm_desc *d, const void *y, const void *x, const float *ga
   a.eps = d->eps;
   a.scale = d->scale;
   a.w32 = d->wdt == LL_F32;
-  const bool vec = rows16(y, d->ldy, es) && rows16(x, d->ldx, es) && rows16(r, d->ldr, es) && rows16(h, d->ldh, es) &&
-                   rows8(q, d->ldq) && aligned(post, 16) && aligned(weight, 16);
   const NormShape s = norm_shape(f);
-  const norm_fn fn = d->dt == LL_F32 ? pick_norm<float, false>(s, vec) : pick_norm<__bf16, false>(s, vec);
+  const norm_fn fn = d->dt == LL_F32 ? pick_norm<float, false>(s) : pick_norm<__bf16, false>(s);
   const uint32_t threads = norm_threads(s.tpr);
   const uint64_t grid = (n + s.rows - 1) / s.rows;
   if (grid * threads >= 1ull << 32) return LL_ERR_UNSUPPORTED;
@@ -271,7 +255,7 @@ int ll_norm_bytes(const ll_norm_desc *d, size_t *bytes) {
   const int st = check_norm(d);
   if (st != LL_OK) return st;
   const NormShape s = norm_shape(d->features);
-  *bytes = (size_t)2 * grad_grid(s, d->rows) * s.rows * d->features * 4;
+  *bytes = (size_t)2 * grad_grid(s, d->rows) * d->features * 4;
   return LL_OK;
 }
 
@@ -338,16 +322,13 @@ int ll_norm_grad(const ll_norm_desc *d, const void *dh, const void *r, const voi
   const uint32_t grid = grad_grid(s, n);
   if (n != 0 && (sums || dr_out != nullptr || dy != nullptr || dgate != nullptr)) {
     // (the shares' rows are `features` long)
-    const bool vec = rows16(y, d->ldy, es) && rows16(r, d->ldr, es) && rows16(dh, d->ldh, es) && rows16(dr, d->ldd, es) &&
-                     rows16(dr_out, d->ldo, es) && rows16(dy, d->lddy, es) && aligned(post, 16) && aligned(weight, 16) &&
-                     f % 4 == 0;
-    const norm_fn fn = d->dt == LL_F32 ? pick_norm<float, true>(s, vec) : pick_norm<__bf16, true>(s, vec);
+      const norm_fn fn = d->dt == LL_F32 ? pick_norm<float, true>(s) : pick_norm<__bf16, true>(s);
     hipLaunchKernelGGL(fn, dim3(grid), dim3(norm_threads(s.tpr)), 0, (hipStream_t)stream, a);
     const int lst = launch_status();
     if (lst != LL_OK) return lst;
   }
   if (!sums) return LL_OK;
-  const NormJoin j{(const float *)workspace, {dweight, dpost}, n == 0 ? 0 : grid * s.rows, (uint32_t)f, (flags & LL_GRAD_ADD) != 0};
+  const NormJoin j{(const float *)workspace, {dweight, dpost}, n == 0 ? 0 : grid, (uint32_t)f, (flags & LL_GRAD_ADD) != 0};
   hipLaunchKernelGGL(k_norm_join, dim3((unsigned)((f + 63) / 64), dpost != nullptr ? 2 : 1), dim3(64 * kJoin), 0,
                      (hipStream_t)stream, j);
   return launch_status();
@@ -404,11 +385,8 @@ int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t coun
       if (st != LL_OK) break;
       AdamwTensor &k = a.t[a.count++];
       k = AdamwTensor{t.param, t.grad, t.master, t.m, t.v, t.m_scales, t.v_scales, n, t.at, chunks, 0};
-      const size_t sa = eight ? 8 : 16;
       if (t.dt == LL_BF16) k.kind |= kBf16;
       if (t.gdt == LL_BF16) k.kind |= kGradBf16;
-      if (!aligned(t.param, 16) || !aligned(t.grad, 16) || !aligned(t.master, 16) || !aligned(t.m, sa) || !aligned(t.v, sa))
-        k.kind |= kUnaligned;
       chunks += mine;
       t.n -= n;
       t.at += n;

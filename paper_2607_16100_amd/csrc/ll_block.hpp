@@ -16,20 +16,60 @@ namespace blk {
 
 constexpr int kW = 8;  // consecutive values of a lane
 
-// kW values of a row that has `left` from here; vec: the address is aligned for
-// 16 bytes, or for all of them.
-template <typename T, bool VEC>
+// kW values of a row as they lie in memory.  All of them are loaded and stored 16
+// bytes at a time whatever the address is aligned to, which the vector memory unit
+// takes (8 of 6896 x 809 bfloat16 weights by single elements: 111 us).
+template <typename T>
+struct Chunk {
+  static constexpr int kPer = 16 / (int)sizeof(T), kParts = kW / kPer;
+  typedef T vec __attribute__((ext_vector_type(kPer)));
+  vec r[kParts];
+  // the first `left` (any number) of the kW; the others are 0
+  __device__ __forceinline__ void load(const T *p, int left) {
+    if (left >= kW) {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) __builtin_memcpy(&r[i], p + i * kPer, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kW; ++i) r[i / kPer][i % kPer] = i < left ? p[i] : (T)0.f;
+    }
+  }
+  __device__ __forceinline__ void store(T *p, int left) const {
+    if (left >= kW) {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) __builtin_memcpy(p + i * kPer, &r[i], 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kW; ++i)
+        if (i < left) p[i] = r[i / kPer][i % kPer];
+    }
+  }
+  __device__ __forceinline__ lin::Vals vals() const {
+    lin::Vals v;
+#pragma unroll
+    for (int i = 0; i < kW; ++i) v.v[i] = Num<T>::get(r[i / kPer][i % kPer]);
+    return v;
+  }
+  __device__ __forceinline__ void set(const lin::Vals &v) {
+#pragma unroll
+    for (int i = 0; i < kW; ++i) r[i / kPer][i % kPer] = Num<T>::put(v.v[i]);
+  }
+};
+template <typename T>
 __device__ __forceinline__ lin::Vals get(const T *p, int left) {
-  return lin::get8<T>(p, left > 0 ? (uint32_t)left : 0u, VEC);
+  Chunk<T> c;
+  c.load(p, left);
+  return c.vals();
 }
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ void put(T *p, const lin::Vals &v, int left) {
-  if (left > 0) lin::put8<T>(p, v, (uint32_t)left, VEC);
+  Chunk<T> c;
+  c.set(v);
+  c.store(p, left);
 }
-template <bool VEC>
 __device__ __forceinline__ void put_codes(uint8_t *p, const uint32_t *w, int left) {
-  if (VEC && left >= kW) {
-    *reinterpret_cast<uint2 *>(p) = uint2{w[0], w[1]};
+  if (left >= kW) {
+    __builtin_memcpy(p, w, 8);
   } else {
 #pragma unroll
     for (int i = 0; i < kW; ++i)
@@ -98,7 +138,7 @@ struct QuantArgs {
   int act;
 };
 
-template <typename T, bool VEC, int U>
+template <typename T, int U>
 __global__ __launch_bounds__(256) void k_quantise(QuantArgs a) {
   uint32_t rows = a.rows;
   if (a.end != nullptr) rows = (uint32_t)min(max(*a.end, 0), (int)a.rows);
@@ -115,8 +155,8 @@ __global__ __launch_bounds__(256) void k_quantise(QuantArgs a) {
     col[n] = item < items ? item % a.blocks * kBlock + threadIdx.x % 16 * kW : 0xFFFFFFFFu;
     const int left = col[n] < a.features ? (int)(a.features - col[n]) : 0;
     const T *p = (const T *)a.x + (uint64_t)row[n] * a.ldx + (left > 0 ? col[n] : 0);
-    v[n] = get<T, VEC>(p, left);
-    if (gate) u[n] = get<T, VEC>(p + a.features, left);
+    v[n] = get<T>(p, left);
+    if (gate) u[n] = get<T>(p + a.features, left);
   }
 #pragma unroll
   for (int n = 0; n < U; ++n) {
@@ -131,7 +171,7 @@ __global__ __launch_bounds__(256) void k_quantise(QuantArgs a) {
     for (int i = 0; i < kW; ++i) v[n].v[i] = i < left ? v[n].v[i] : 0.f;
     const uint32_t s = quantise8(v[n], w);
     if (left > 0) {
-      put_codes<VEC>(a.q + (uint64_t)row[n] * a.ldq + col[n], w, left);
+      put_codes(a.q + (uint64_t)row[n] * a.ldq + col[n], w, left);
       if (threadIdx.x % 16 == 0) a.scales[(uint64_t)row[n] * a.lds + col[n] / kBlock] = (uint8_t)s;
     }
   }
@@ -149,10 +189,9 @@ struct WeightArgs {
   uint8_t *q, *scales;
   uint64_t ldw, wstride, ldq, qstride, lds, sstride;
   uint32_t out, in;
-  uint32_t wide;  // bytes that every row of q is aligned to: 16, 8, 4 or 1
 };
 
-template <typename T, bool VEC, bool TRANSPOSE>
+template <typename T, bool TRANSPOSE>
 __global__ __launch_bounds__(256) void k_quantise_weight(WeightArgs a) {
   constexpr int kPitch = 128 + 16;  // rows of the transposed block start 16 bytes on in the banks
   __shared__ __attribute__((aligned(16))) uint8_t tile[TRANSPOSE ? 128 * kPitch : 16];
@@ -165,7 +204,7 @@ __global__ __launch_bounds__(256) void k_quantise_weight(WeightArgs a) {
   lin::Vals v[8];
   uint32_t top = 0;
 #pragma unroll
-  for (int r = 0; r < 8; ++r) v[r] = get<T, VEC>(p + r * a.ldw, row0 + r < a.out ? left : 0);
+  for (int r = 0; r < 8; ++r) v[r] = get<T>(p + r * a.ldw, row0 + r < a.out ? left : 0);
 #pragma unroll
   for (int r = 0; r < 8; ++r)
 #pragma unroll
@@ -189,11 +228,7 @@ __global__ __launch_bounds__(256) void k_quantise_weight(WeightArgs a) {
         w[i] = to_e4m3(v[r].v[4 * i] * inv, v[r].v[4 * i + 1] * inv) |
                to_e4m3(v[r].v[4 * i + 2] * inv, v[r].v[4 * i + 3] * inv) << 16;
       if (row0 + r >= a.out) continue;
-      uint8_t *to = q + (uint64_t)(row0 + r) * a.ldq + col0;
-      if (a.wide >= 8)
-        put_codes<true>(to, w, left);
-      else
-        put_codes<false>(to, w, left);
+      put_codes(q + (uint64_t)(row0 + r) * a.ldq + col0, w, left);
     }
   } else {
 #pragma unroll
@@ -213,11 +248,8 @@ __global__ __launch_bounds__(256) void k_quantise_weight(WeightArgs a) {
       if (orow >= a.in || ocol >= a.out) continue;
       const u32x4 w = *reinterpret_cast<const u32x4 *>(tile + r * kPitch + c);
       uint8_t *to = q + (uint64_t)orow * a.ldq + ocol;
-      if (a.wide >= 16 && ocol + 16 <= a.out) {
-        *reinterpret_cast<u32x4 *>(to) = w;
-      } else if (a.wide >= 4 && ocol + 16 <= a.out) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t *>(to)[i] = w[i];
+      if (ocol + 16 <= a.out) {
+        __builtin_memcpy(to, &w, 16);
       } else {
 #pragma unroll
         for (uint32_t i = 0; i < 16; ++i)
@@ -270,10 +302,10 @@ __device__ __forceinline__ void row_sums(float *v, float *red) {
 }
 
 // A norm's weights, of the rows' type or binary32.
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ lin::Vals get_weight(const void *w, bool w32, uint32_t at, int left) {
-  if (left <= 0) return get<float, VEC>((const float *)nullptr, 0);
-  return w32 ? get<float, VEC>((const float *)w + at, left) : get<T, VEC>((const T *)w + at, left);
+  if (left <= 0) return get<float>((const float *)nullptr, 0);
+  return w32 ? get<float>((const float *)w + at, left) : get<T>((const T *)w + at, left);
 }
 
 // Threads of a row's workgroup; a wave a row: four of them.
@@ -283,7 +315,7 @@ constexpr int norm_threads(int tpr) { return tpr == 64 ? 256 : tpr; }
 // too.  Two (more than 8192 features): the weights are read when they are used,
 // from L2.  8192 x 7168 bfloat16, residual and norm: 86 us, 5.4 TB/s (256 threads
 // of four chunks: 103); with post, gate and the codes 104 us.
-template <typename T, bool VEC, int TPR, int C>
+template <typename T, int TPR, int C>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs a) {
   constexpr bool kEarly = C == 1;
   constexpr int kRows = norm_threads(TPR) / TPR;
@@ -295,13 +327,13 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs a) {
   const float n = (float)a.features;
   auto left = [&](int c) { return (int)a.features - (int)((c * TPR + t) * kW); };
 #pragma unroll
-  for (int c = 0; c < C; ++c) v[c] = get<T, VEC>((const T *)a.y + row * a.ldy + (c * TPR + t) * kW, left(c));
+  for (int c = 0; c < C; ++c) v[c] = get<T>((const T *)a.y + row * a.ldy + (c * TPR + t) * kW, left(c));
   if (a.x != nullptr) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) x[c] = get<T, VEC>((const T *)a.x + row * a.ldx + (c * TPR + t) * kW, left(c));
+    for (int c = 0; c < C; ++c) x[c] = get<T>((const T *)a.x + row * a.ldx + (c * TPR + t) * kW, left(c));
   }
-  if (kEarly && a.post != nullptr) post[0] = get_weight<T, VEC>(a.post, a.w32, t * kW, left(0));
-  if (kEarly && a.weight != nullptr) weight[0] = get_weight<T, VEC>(a.weight, a.w32, t * kW, left(0));
+  if (kEarly && a.post != nullptr) post[0] = get_weight<T>(a.post, a.w32, t * kW, left(0));
+  if (kEarly && a.weight != nullptr) weight[0] = get_weight<T>(a.weight, a.w32, t * kW, left(0));
   const float by = a.gate != nullptr ? a.gate[row] * a.scale : a.scale;
   auto squares = [&](float *s) {
     *s = 0.f;
@@ -317,7 +349,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs a) {
     const float rstd = 1.f / sqrtf(s / n + a.eps);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if constexpr (!kEarly) post[0] = get_weight<T, VEC>(a.post, a.w32, (c * TPR + t) * kW, left(c));
+      if constexpr (!kEarly) post[0] = get_weight<T>(a.post, a.w32, (c * TPR + t) * kW, left(c));
 #pragma unroll
       for (int i = 0; i < kW; ++i) v[c].v[i] = v[c].v[i] * rstd * post[0].v[i];
     }
@@ -332,7 +364,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs a) {
   }
   if (a.r != nullptr) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) put<T, VEC>((T *)a.r + row * a.ldr + (c * TPR + t) * kW, v[c], left(c));
+    for (int c = 0; c < C; ++c) put<T>((T *)a.r + row * a.ldr + (c * TPR + t) * kW, v[c], left(c));
   }
   if (a.weight == nullptr) return;
   squares(&s);
@@ -340,45 +372,21 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm(NormArgs a) {
   const float rstd = 1.f / sqrtf(s / n + a.eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    if constexpr (!kEarly) weight[0] = get_weight<T, VEC>(a.weight, a.w32, (c * TPR + t) * kW, left(c));
+    if constexpr (!kEarly) weight[0] = get_weight<T>(a.weight, a.w32, (c * TPR + t) * kW, left(c));
 #pragma unroll
     for (int i = 0; i < kW; ++i) v[c].v[i] = v[c].v[i] * rstd * weight[0].v[i];
-    if (a.h != nullptr) put<T, VEC>((T *)a.h + row * a.ldh + (c * TPR + t) * kW, v[c], left(c));
+    if (a.h != nullptr) put<T>((T *)a.h + row * a.ldh + (c * TPR + t) * kW, v[c], left(c));
     if (a.q != nullptr) {  // 16 lanes have a block, whole or to the row's end
       uint32_t w[2];
       const uint32_t at = (c * TPR + t) * kW;
       const uint32_t sc = quantise8(v[c], w);
       if (left(c) > 0) {
-        put_codes<VEC>(a.q + row * a.ldq + at, w, left(c));
+        put_codes(a.q + row * a.ldq + at, w, left(c));
         if (t % 16 == 0) a.scales[row * a.lds + at / kBlock] = (uint8_t)sc;
       }
     }
   }
 }
-
-// kW values of a row as they lie in memory, loaded while another row is worked on.
-template <typename T, bool VEC>
-struct Chunk {
-  union {
-    T e[kW];
-    u32x4 raw[kW * sizeof(T) / 16];
-  };
-  __device__ __forceinline__ void load(const T *p, int left) {
-    if (VEC && left >= kW) {
-#pragma unroll
-      for (int i = 0; i < (int)(kW * sizeof(T) / 16); ++i) raw[i] = reinterpret_cast<const u32x4 *>(p)[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < kW; ++i) e[i] = i < left ? p[i] : (T)0.f;
-    }
-  }
-  __device__ __forceinline__ lin::Vals vals() const {
-    lin::Vals v;
-#pragma unroll
-    for (int i = 0; i < kW; ++i) v.v[i] = Num<T>::get(e[i]);
-    return v;
-  }
-};
 
 // The gradients: a workgroup takes rows blockIdx.x, + gridDim.x, ... and keeps
 // its share of dweight and dpost in registers; k_norm_join adds the shares up.
@@ -392,7 +400,7 @@ struct Chunk {
 // the next row is loaded while one is worked on (with four chunks a thread, all
 // read when their row came: 8192 x 7168 bfloat16 with post and gate 460 us, so
 // 149).  Values are held as they lie in memory.
-template <typename T, bool VEC, int TPR, int C>
+template <typename T, int TPR, int C>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
   constexpr int kRows = norm_threads(TPR) / TPR;
   constexpr bool kHold = C == 1;  // the weights stay in registers, and the next row comes there
@@ -409,10 +417,10 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < kW; ++i) dw[c].v[i] = dp[c].v[i] = 0.f;
   if constexpr (kHold) {
-    if (a.weight != nullptr) weight = get_weight<T, VEC>(a.weight, a.w32, at(0), left(0));
-    if (a.post != nullptr) post = get_weight<T, VEC>(a.post, a.w32, at(0), left(0));
+    if (a.weight != nullptr) weight = get_weight<T>(a.weight, a.w32, at(0), left(0));
+    if (a.post != nullptr) post = get_weight<T>(a.post, a.w32, at(0), left(0));
   }
-  typedef Chunk<T, VEC> Row[C];
+  typedef Chunk<T> Row[C];
   auto load = [&](uint32_t row, Row &r, Row &g, Row &y, Row &d) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -441,7 +449,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
     if (a.weight != nullptr) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        if constexpr (!kHold) weight = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+        if constexpr (!kHold) weight = get_weight<T>(a.weight, a.w32, at(c), left(c));
         const lin::Vals rv = r[c].vals(), gv = g[c].vals();
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
@@ -474,7 +482,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
       const float mean = s[1] * rstd * rn;  // of u weight dh
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        if constexpr (!kHold) weight = get_weight<T, VEC>(a.weight, a.w32, at(c), left(c));
+        if constexpr (!kHold) weight = get_weight<T>(a.weight, a.w32, at(c), left(c));
         const lin::Vals rv = r[c].vals(), gv = g[c].vals();
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
@@ -486,7 +494,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
     }
     if (a.dr_out != nullptr) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) put<T, VEC>((T *)a.dr_out + row * a.ldo + at(c), d[c], left(c));
+      for (int c = 0; c < C; ++c) put<T>((T *)a.dr_out + row * a.ldo + at(c), d[c], left(c));
     }
     if (!with_y && a.dy == nullptr) continue;
     const float by = (a.gate != nullptr ? a.gate[row] : 1.f) * a.scale;
@@ -496,7 +504,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
       for (int c = 0; c < C; ++c) {
         const lin::Vals yv = y[c].vals();
         if (a.post != nullptr) {
-          if constexpr (!kHold) post = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+          if constexpr (!kHold) post = get_weight<T>(a.post, a.w32, at(c), left(c));
 #pragma unroll
           for (int i = 0; i < kW; ++i) dot = __builtin_fmaf(d[c].v[i] * post.v[i], yv.v[i], dot);
         } else {
@@ -511,7 +519,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
         const float mean = by * dot * rstd * rn;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          if constexpr (!kHold) post = get_weight<T, VEC>(a.post, a.w32, at(c), left(c));
+          if constexpr (!kHold) post = get_weight<T>(a.post, a.w32, at(c), left(c));
           const lin::Vals yv = y[c].vals();
 #pragma unroll
           for (int i = 0; i < kW; ++i) {
@@ -530,16 +538,29 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_norm_grad(NormArgs a) {
           for (int i = 0; i < kW; ++i) d[c].v[i] *= by;
       }
 #pragma unroll
-      for (int c = 0; c < C; ++c) put<T, VEC>((T *)a.dy + row * a.lddy + at(c), d[c], left(c));
+      for (int c = 0; c < C; ++c) put<T>((T *)a.dy + row * a.lddy + at(c), d[c], left(c));
     }
   }
   if (a.parts == nullptr) return;
-  const uint64_t part = (uint64_t)blockIdx.x * kRows + lane_row, parts = (uint64_t)gridDim.x * kRows;
+  if constexpr (kRows > 1) {  // the waves' shares in their order
+    __shared__ lin::Vals others[2][kRows - 1][TPR];
+    if (lane_row != 0) {
+      others[0][lane_row - 1][t] = dw[0];
+      others[1][lane_row - 1][t] = dp[0];
+    }
+    __syncthreads();
+    if (lane_row != 0) return;
+#pragma unroll
+    for (int i = 0; i < kRows - 1; ++i) {
+      lin::add8(dw[0], others[0][i][t]);
+      lin::add8(dp[0], others[1][i][t]);
+    }
+  }
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    // (the parts' rows are 16-byte aligned where VEC)
-    put<float, VEC>(a.parts + part * a.features + at(c), dw[c], left(c));
-    if (a.post != nullptr) put<float, VEC>(a.parts + (parts + part) * a.features + at(c), dp[c], left(c));
+    put<float>(a.parts + (uint64_t)blockIdx.x * a.features + at(c), dw[c], left(c));
+    if (a.post != nullptr)
+      put<float>(a.parts + ((uint64_t)gridDim.x + blockIdx.x) * a.features + at(c), dp[c], left(c));
   }
 }
 
@@ -623,9 +644,9 @@ struct AdamwTensor {
   uint8_t *m_scales, *v_scales;
   uint64_t n, at;
   uint32_t chunk;  // the first of its chunks
-  uint32_t kind;   // kBf16 | kGradBf16 | kUnaligned
+  uint32_t kind;   // kBf16 | kGradBf16
 };
-constexpr uint32_t kBf16 = 1, kGradBf16 = 2, kUnaligned = 4;
+constexpr uint32_t kBf16 = 1, kGradBf16 = 2;
 constexpr int kTensors = 40;
 constexpr uint32_t kChunk = 4096;  // values a workgroup
 struct AdamwArgs {
@@ -666,7 +687,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   const AdamwTensor &t = a.t[lo];
   const AdamwCoef c = *a.coef;
   const uint64_t n = t.n, base = (uint64_t)(blockIdx.x - t.chunk) * kChunk;
-  const bool vec = !(t.kind & kUnaligned), bf16 = t.kind & kBf16, gbf16 = t.kind & kGradBf16;
+  const bool bf16 = t.kind & kBf16, gbf16 = t.kind & kGradBf16;
   constexpr int U = kChunk / (256 * kW);
   lin::Vals p[U], g[U], m[U], v[U];
   uint2 m8[U], v8[U];
@@ -678,8 +699,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
     const uint64_t i = at(u);
     const int l = left(u);
     const uint64_t j = l > 0 ? i : 0;
-    p[u] = lin::get8((bf16 ? t.master : (const float *)t.param) + j, l, vec);
-    g[u] = gbf16 ? lin::get8((const __bf16 *)t.grad + j, l, vec) : lin::get8((const float *)t.grad + j, l, vec);
+    p[u] = get<float>((bf16 ? t.master : (const float *)t.param) + j, l);
+    g[u] = gbf16 ? get<__bf16>((const __bf16 *)t.grad + j, l) : get<float>((const float *)t.grad + j, l);
     if constexpr (EIGHT) {
       // the states' last block is whole in memory only as far as the tensor goes
       m8[u] = v8[u] = uint2{0, 0};
@@ -687,9 +708,9 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
       if (l > 0) {
         ms[u] = t.m_scales[i / kBlock];
         vs[u] = t.v_scales[i / kBlock];
-        if (vec && l == kW) {
-          m8[u] = *reinterpret_cast<const uint2 *>((const uint8_t *)t.m + i);
-          v8[u] = *reinterpret_cast<const uint2 *>((const uint8_t *)t.v + i);
+        if (l == kW) {
+          __builtin_memcpy(&m8[u], (const uint8_t *)t.m + i, 8);
+          __builtin_memcpy(&v8[u], (const uint8_t *)t.v + i, 8);
         } else {
           uint32_t mw[2] = {0, 0}, vw[2] = {0, 0};
 #pragma unroll
@@ -703,8 +724,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
         }
       }
     } else {
-      m[u] = lin::get8((const float *)t.m + j, l, vec);
-      v[u] = lin::get8((const float *)t.v + j, l, vec);
+      m[u] = get<float>((const float *)t.m + j, l);
+      v[u] = get<float>((const float *)t.v + j, l);
     }
   }
 #pragma unroll
@@ -752,13 +773,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
           mw[e / 4] |= to_code<3, -6, 7>(m[u].v[e] * im, r >> 16 << 4) << (e % 4 * 8);
           vw[e / 4] |= to_code<2, -14, 15>(v[u].v[e] * iv, (r & 0xFFFFu) << 5) << (e % 4 * 8);
         }
-        if (vec) {
-          put_codes<true>((uint8_t *)t.m + i, mw, l);
-          put_codes<true>((uint8_t *)t.v + i, vw, l);
-        } else {
-          put_codes<false>((uint8_t *)t.m + i, mw, l);
-          put_codes<false>((uint8_t *)t.v + i, vw, l);
-        }
+        put_codes((uint8_t *)t.m + i, mw, l);
+        put_codes((uint8_t *)t.v + i, vw, l);
         if (threadIdx.x % 16 == 0) {
           t.m_scales[i / kBlock] = (uint8_t)sm;
           t.v_scales[i / kBlock] = (uint8_t)sv;
@@ -767,14 +783,14 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
     }
     if (l <= 0) continue;
     if constexpr (!EIGHT) {
-      lin::put8((float *)t.m + i, m[u], l, vec);
-      lin::put8((float *)t.v + i, v[u], l, vec);
+      put<float>((float *)t.m + i, m[u], l);
+      put<float>((float *)t.v + i, v[u], l);
     }
     if (bf16) {
-      lin::put8(t.master + i, p[u], l, vec);
-      lin::put8((__bf16 *)t.param + i, p[u], l, vec);
+      put<float>(t.master + i, p[u], l);
+      put<__bf16>((__bf16 *)t.param + i, p[u], l);
     } else {
-      lin::put8((float *)t.param + i, p[u], l, vec);
+      put<float>((float *)t.param + i, p[u], l);
     }
   }
 }

@@ -457,6 +457,8 @@ def quantise(x, *, act: str = "none", offsets=None, out=None, scales=None, strea
         scales = scales_of(n, (h + 127) // 128, device=x.device, stream=stream)
     end = None
     if offsets is not None:
+        if offsets.numel() == 0:
+            raise ValueError("offsets: none")
         end = _flat(offsets, "offsets", dev, offsets.numel(), torch.int32) + (offsets.numel() - 1) * 4
     ldq, lds = _codes(out, "out", dev, n, h), _scale_rows(scales, "scales", dev, n, (h + 127) // 128)
     ll.check(_c.ll_quantise(x.data_ptr(), ldx, n, end, h, _dt(x), lm.ACTS[act], out.data_ptr(), ldq,
@@ -632,6 +634,7 @@ def norm(y, weight=None, *, residual=None, gate=None, scale: float = 1.0, post=N
 
 
 _norm_descs: dict = {}  # by their own fields: a descriptor is only read
+_norm_needs: dict = {}  # workspace bytes by rows and features
 
 
 def _norm_desc(*fields):
@@ -693,8 +696,13 @@ def norm_grad(dh, r, weight=None, *, dr=None, y=None, gate=None, scale: float = 
                    mat(dr, "dr"), mat(dr_out, "dr_out"), mat(dy, "dy"))
     ws, need = None, 0
     if dweight is not None or dpost is not None:
-        st, need = lb.ll_norm_bytes(d)
-        ll.check(st, "ll_norm_bytes")
+        need = _norm_needs.get((n, f))
+        if need is None:
+            st, need = lb.ll_norm_bytes(d)
+            ll.check(st, "ll_norm_bytes")
+            if len(_norm_needs) >= 4096:
+                _norm_needs.clear()
+            _norm_needs[n, f] = need
         ws = _new(stream, need, dtype=torch.uint8, device=rows.device)
     ll.check(_c.ll_norm_grad(d, at(dh), at(r) if weight is not None else None, at(dr), at(y), flat(gate, "gate", n), pp,
                              wp, at(dr_out), at(dy), flat(dgate, "dgate", n), flat(dweight, "dweight", f),

@@ -148,6 +148,8 @@ def test_refusals():
     with pytest.raises(ValueError):
         moe.quantise(torch.zeros(4, 200))
     with pytest.raises(ValueError):
+        moe.quantise(x, offsets=torch.zeros(0, dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError):
         moe.quantise(x.clone().requires_grad_())
     with pytest.raises(ValueError):
         moe.quantise_weight(x.view(2, 2, 200), out=torch.zeros(2, 2, 199, dtype=torch.uint8, device=DEV).view(moe.E4M3))
