@@ -91,17 +91,21 @@ int launch_tiles8(Args8 &a, bool gate, void *stream) {
   a.tiles_n = (width + per_n - 1) / per_n;
   a.tiles_m = (a.m + B - 1) / B;
   const uint64_t grid = count_tiles(kForward, a, B) / ((a.n + B - 1) / B) * a.tiles_n;
-  if (grid * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
+  if ((grid + 4 * kMaxTail) * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
   // a short last round of 256-wide tiles runs in parts
   const uint64_t rest = grid % kRound;
   const bool tail = B == 256 && grid > kRound && (a.offsets != nullptr || (rest != 0 && rest <= kMaxTail));
+  constexpr uint32_t kParts = 4 * kMaxTail;
+  static_assert(8 * kEighths <= kParts, "a workgroup a part");
+  constexpr bool kOne = B == 256 && ROWS == kChunkRows;  // tiles and parts in one launch
   if (tail) a.tail = 1;
-  hipLaunchKernelGGL((pick8<O, B, ST, ROWS>(gate)), dim3((unsigned)grid, a.splits), dim3(256), 0, (hipStream_t)stream, a);
-  if constexpr (B == 256) {
+  a.first_part = (uint32_t)grid;
+  const uint32_t all = (uint32_t)grid + (kOne && tail ? kParts : 0);
+  hipLaunchKernelGGL((pick8<O, B, ST, ROWS>(gate)), dim3(all, a.splits), dim3(256), 0, (hipStream_t)stream, a);
+  if constexpr (B == 256 && !kOne) {
     if (tail) {
       const tile8_fn parts = gate ? k_tail8<O, true, ROWS> : k_tail8<O, false, ROWS>;
-      static_assert(8 * kEighths <= 4 * kMaxTail, "a workgroup a part");
-      hipLaunchKernelGGL(parts, dim3(4 * kMaxTail), dim3(256), 0, (hipStream_t)stream, a);
+      hipLaunchKernelGGL(parts, dim3(kParts), dim3(256), 0, (hipStream_t)stream, a);
     }
   }
   if (a.parts != nullptr) {

@@ -31,6 +31,7 @@ struct Step<e4m3> {
 struct Args8 : Args {
   const uint8_t *xs, *ws;
   uint64_t ldxs, ldws, wsstride;
+  uint32_t first_part;  // k_wide8: workgroups from here on run the short last round's parts
 };
 
 constexpr int kScaleStages = 4;  // stages of which a row's scales lie in one word
@@ -470,15 +471,20 @@ __device__ __forceinline__ bool find_part(const Args &a, uint32_t id, int *group
 }
 
 template <typename O, bool GATED, Rows ROWS>
-__global__ __launch_bounds__(256, 1) void k_tail8(Args8 a) {
-  __shared__ __attribute__((aligned(1024))) char lds[tile8_lds(128, 128, 4)];
+__device__ __forceinline__ void part8(const Args8 &a, uint32_t id, char *lds) {
   int g = 0;
   uint32_t tn = 0, m0 = 0, m_end = 0, cols = 0;
-  if (!find_part(a, blockIdx.x, &g, &m0, &m_end, &tn, &cols)) return;
+  if (!find_part(a, id, &g, &m0, &m_end, &tn, &cols)) return;
   if (cols == 4)
     tile8<O, 128, 64, 4, GATED, ROWS>(a, g, tn, m0, m_end, lds);
   else
     tile8<O, 128, 128, 4, GATED, ROWS>(a, g, tn, m0, m_end, lds);
+}
+
+template <typename O, bool GATED, Rows ROWS>
+__global__ __launch_bounds__(256, 1) void k_tail8(Args8 a) {
+  __shared__ __attribute__((aligned(1024))) char lds[tile8_lds(128, 128, 4)];
+  part8<O, GATED, ROWS>(a, blockIdx.x, lds);
 }
 
 // ---------------------------------------------------------------- the wide tile kernel
@@ -504,7 +510,9 @@ __global__ __launch_bounds__(256, 1) void k_tail8(Args8 a) {
 // busy 70 % of the cycles at 1.7 GHz; 16384 rows over 32 groups, 7168 -> 2 x 2048:
 // 490-515 us.
 //
-// Rows are whole 16-byte chunks; others run k_tile8.
+// The short last round's parts are the last workgroups of the same launch and
+// start where whole tiles, some of which have no lower half, leave a CU first.
+// Rows are whole 16-byte chunks; others run k_tile8, and k_tail8 after it.
 struct QuarterLoader {
   uint64_t base;  // of the stage to load next
   uint32_t off[8], kk0;
@@ -548,8 +556,12 @@ struct QuarterLoader {
 template <typename O, bool GATED>
 __global__ __launch_bounds__(256, 1) void k_wide8(Args8 a) {
   constexpr int BM = 256, BN = 256, WTN = 128, BK = 128, kStage = 65536, kScales = 2048;
-  constexpr int kUse = 2 * kStage + 2 * kScales + 1024, kEpi = epilogue8(BM, BN);
-  __shared__ __attribute__((aligned(1024))) char lds[kUse > kEpi ? kUse : kEpi];
+  static_assert(tile8_lds(BM, BN, 2) >= tile8_lds(128, 128, 4), "the parts' LDS");
+  __shared__ __attribute__((aligned(1024))) char lds[tile8_lds(BM, BN, 2)];
+  if (blockIdx.x >= a.first_part) {
+    part8<O, GATED, kChunkRows>(a, blockIdx.x - a.first_part, lds);
+    return;
+  }
   const int lane = threadIdx.x % 64;
   const uint32_t wave = uniform_u32(threadIdx.x / 64);
   const uint32_t wm = wave / 2, wn = wave % 2;
