@@ -91,12 +91,12 @@ int launch_tiles8(Args8 &a, bool gate, void *stream) {
   a.tiles_n = (width + per_n - 1) / per_n;
   a.tiles_m = (a.m + B - 1) / B;
   const uint64_t grid = count_tiles(kForward, a, B) / ((a.n + B - 1) / B) * a.tiles_n;
-  if ((grid + 4 * kMaxTail) * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
+  constexpr uint32_t kParts = 2 * kMaxTail;
+  if ((grid + kParts) * 256 >= 1ull << 32) return LL_ERR_UNSUPPORTED;
   // a short last round of 256-wide tiles runs in parts
   const uint64_t rest = grid % kRound;
   const bool tail = B == 256 && grid > kRound && (a.offsets != nullptr || (rest != 0 && rest <= kMaxTail));
-  constexpr uint32_t kParts = 4 * kMaxTail;
-  static_assert(8 * kEighths <= kParts, "a workgroup a part");
+  static_assert(8 * kEighths <= kParts && 4 * kQuarters <= kParts, "a workgroup a part");
   constexpr bool kOne = B == 256 && ROWS == kChunkRows;  // tiles and parts in one launch
   if (tail) a.tail = 1;
   a.first_part = (uint32_t)grid;

@@ -424,10 +424,11 @@ __global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args
 }
 
 // The short last round of 256-wide tiles that their launch leaves out (tail_tiles):
-// each tile in quarters of 128 x 128, or in eighths of 128 x 64 where there are so
-// few of them that quarters would leave half of the CUs without one (32 tiles of
-// 7168 k: 31 us, in quarters 39).
-constexpr uint32_t kEighths = 32;
+// each tile in eighths of 128 x 64, quarters of 128 x 128 or halves of 128 x 256,
+// the smallest that are no more than the CUs (32 tiles of 7168 k: eighths 31 us,
+// quarters 39; 96 after a whole round: quarters 172, halves 163; 128: 183, 173,
+// and as whole tiles 184).
+constexpr uint32_t kEighths = 32, kQuarters = 64;
 
 // Part `id`: as find_rows, and *cols, the columns of parts a tile has.
 __device__ __forceinline__ bool find_part(const Args &a, uint32_t id, int *group, uint32_t *row0, uint32_t *row1,
@@ -443,7 +444,7 @@ __device__ __forceinline__ bool find_part(const Args &a, uint32_t id, int *group
     }
   }
   const uint32_t total = rows * a.tiles_n, rest = tail_tiles(total);
-  *cols = rest <= kEighths ? 4 : 2;
+  *cols = rest <= kEighths ? 4 : rest <= kQuarters ? 2 : 1;
   if (id >= 2 * *cols * rest) return false;
   const uint32_t part = id / rest;
   number_of(total - rest + id % rest, rows, a.tiles_n, &tm, tn);
@@ -477,8 +478,10 @@ __device__ __forceinline__ void part8(const Args8 &a, uint32_t id, char *lds) {
   if (!find_part(a, id, &g, &m0, &m_end, &tn, &cols)) return;
   if (cols == 4)
     tile8<O, 128, 64, 4, GATED, ROWS>(a, g, tn, m0, m_end, lds);
-  else
+  else if (cols == 2)
     tile8<O, 128, 128, 4, GATED, ROWS>(a, g, tn, m0, m_end, lds);
+  else
+    tile8<O, 128, 256, 2, GATED, ROWS>(a, g, tn, m0, m_end, lds);
 }
 
 template <typename O, bool GATED, Rows ROWS>

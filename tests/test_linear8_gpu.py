@@ -118,12 +118,14 @@ def test_product(name, dtype, act, bias, residual, save, layout):
     check(name, dtype, act, bias, residual, save, layout)
 
 
-# 256-wide tiles: whole ones, a short last round in quarters and in eighths, groups
-# whose last tile has no lower half; 128-wide ones at one and at two a CU
+# 256-wide tiles: whole ones, a short last round in halves ("groups" too), quarters
+# and eighths, groups whose last tile has no lower half; 128-wide ones at one and at
+# two a CU
 LARGE = {
     "full": (None, 4096, 256, 4096),
     "quarters": (None, 4100, 320, 4352),
     "groups": ([700, 0, 130, 2049, 1200, 257], 0, 192, 4104),
+    "halves": (None, 4100, 1360, 4880),
     "eighths": (None, 4100, 336, 4096),
     "eighths_groups": ([700, 0, 130, 2049, 1000], 0, 640, 4096),
     "eighths_many": ([40] * 30 + [0] * 40 + [37] * 30 + [1500], 0, 128, 1024),  # more than 64 groups
