@@ -321,8 +321,7 @@ int ll_norm_grad(const ll_norm_desc *d, const void *dh, const void *r, const voi
   const NormShape s = norm_shape(f);
   const uint32_t grid = grad_grid(s, n);
   if (n != 0 && (sums || dr_out != nullptr || dy != nullptr || dgate != nullptr)) {
-    // (the shares' rows are `features` long)
-      const norm_fn fn = d->dt == LL_F32 ? pick_norm<float, true>(s) : pick_norm<__bf16, true>(s);
+    const norm_fn fn = d->dt == LL_F32 ? pick_norm<float, true>(s) : pick_norm<__bf16, true>(s);
     hipLaunchKernelGGL(fn, dim3(grid), dim3(norm_threads(s.tpr)), 0, (hipStream_t)stream, a);
     const int lst = launch_status();
     if (lst != LL_OK) return lst;

@@ -14,6 +14,7 @@ from typing import Optional, Sequence
 
 import numpy as np
 import torch
+from torch.autograd.graph import increment_version
 
 from . import llblock as lb
 from . import llcoll as ll
@@ -42,7 +43,8 @@ class AdamW:
     ``state``: a ``state_dict()`` to go on from, whose tensors are used, not
     copied.  The options may be changed between steps (``opt.lr = ...``).  Steps of
     one optimiser follow one another: two at once, on two streams, are not
-    meant."""
+    meant.  Its memory is of the stream it was made on: keep it until steps on
+    other streams have run."""
 
     def __init__(self, params: Sequence[torch.Tensor], *, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.0, states: str = "f32", seed: int = 0, state: Optional[dict] = None):
@@ -56,17 +58,15 @@ class AdamW:
             raise ValueError("params: none")
         dev = self.params[0].get_device()
         self._dev = dev
-        seen, self.offsets, total = set(), [], 0
+        self.offsets, total = [], 0
         for i, p in enumerate(self.params):
             if p.dtype not in _DT:
                 raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(p.dtype))
             if dev < 0 or p.get_device() != dev or not p.is_contiguous():
                 raise ValueError(f"params[{i}]: a contiguous tensor is needed, all on one GPU")
-            if p.numel() and p.data_ptr() in seen:
-                raise ValueError(f"params[{i}]: given twice")
-            seen.add(p.data_ptr())
             self.offsets.append(total)
             total += (p.numel() + 127) // 128 * 128
+        self._apart()
         device = self.params[0].device
         mt, vt = _TYPES[self.bits]
         eight = self.bits == 8
@@ -87,6 +87,7 @@ class AdamW:
         self._fields = np.frombuffer(self._table, dtype=_ROW)  # the same memory
         self._sizes = [p.numel() for p in self.params]
         self._at: list = []  # the parameters' addresses in the table
+        self._versioned = [p for p in self.params if not p.is_inference()]
         es = 1 if eight else 4
         for t, p, w, at in zip(self._table, self.params, self.masters, self.offsets):
             t.n, t.at, t.dt = p.numel(), at, _DT[p.dtype]
@@ -105,6 +106,13 @@ class AdamW:
             return [_DT[t.dtype] for t in tensors]
         except KeyError as e:
             raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(e)) from None
+
+    def _apart(self) -> None:
+        """Two parameters in the same memory would be updated at the same time."""
+        spans = sorted((p.data_ptr(), p.numel() * p.element_size(), i) for i, p in enumerate(self.params) if p.numel())
+        for (at, size, _), (behind, _, i) in zip(spans, spans[1:]):
+            if behind < at + size:
+                raise ValueError(f"params[{i}]: given twice, or shares memory with another")
 
     def _check_state(self, state: dict, total: int, mt, vt) -> None:
         dev = self._dev
@@ -145,6 +153,7 @@ class AdamW:
         if at != self._at:  # a parameter's memory is another than at the last step
             if self._check(self.params, "params", dev) != [t.dt for t in table]:
                 raise ValueError("params: their types have changed")
+            self._apart()
             fields["param"] = self._at = at
         rate, rate_at = self.lr if lr is None else lr, None
         if isinstance(rate, torch.Tensor):
@@ -154,6 +163,7 @@ class AdamW:
         ll.check(lb.ll_adamw(d, table, len(table), self.count.data_ptr(), rate_at,
                              None if grad_scale is None else _flat(grad_scale, "grad_scale", dev, 1, torch.float32),
                              self._work.data_ptr(), lb.LL_ADAMW_WORKSPACE, _stream(stream, dev)), "ll_adamw")
+        increment_version(self._versioned)  # a backward pass that still needs the old values says so
 
 
 def _ones(n: int, device) -> torch.Tensor:

@@ -309,3 +309,24 @@ def test_refusals():
     with pytest.raises(ValueError):
         AdamW([p], states="8bit", state=state)
     assert int(opt.count) == 0
+
+
+def test_parameters_in_the_same_memory_are_refused():
+    flat = torch.zeros(300, device=DEV)
+    for params in ([flat[:200], flat[100:]], [flat[100:], flat[:101]], [flat, flat]):
+        with pytest.raises(ValueError):
+            AdamW(params)
+    a, b = flat[:100], flat[100:200]
+    opt = AdamW([a, b, flat[200:200]])
+    opt.step([torch.ones(100, device=DEV)] * 2 + [torch.ones(0, device=DEV)])
+    b.data = flat[50:150]  # moves into the other
+    with pytest.raises(ValueError):
+        opt.step([torch.ones(100, device=DEV)] * 2 + [torch.ones(0, device=DEV)])
+
+
+def test_a_backward_pass_behind_a_step_says_so():
+    w = torch.ones(8, device=DEV, requires_grad=True)
+    loss = (w * w).sum()
+    AdamW([w]).step([torch.ones(8, device=DEV)])
+    with pytest.raises(RuntimeError):
+        loss.backward()
