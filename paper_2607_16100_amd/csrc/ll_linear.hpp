@@ -498,11 +498,14 @@ struct Loader {
     }
   }
   __device__ __forceinline__ void commit(char *tile) {
+    if constexpr (ROWS == kAnyRows) commit(tile, raw);
+  }
+  __device__ __forceinline__ void commit(char *tile, const u32x4 (&from)[kChunks]) {
     if constexpr (ROWS == kAnyRows) {
       const uint32_t chunk0 = threadIdx.x / 64 * kChunks;
 #pragma unroll
       for (int c = 0; c < kChunks; ++c)
-        *reinterpret_cast<u32x4 *>(tile + (chunk0 + c) * 1024 + threadIdx.x % 64 * 16) = raw[c];
+        *reinterpret_cast<u32x4 *>(tile + (chunk0 + c) * 1024 + threadIdx.x % 64 * 16) = from[c];
     }
   }
 };

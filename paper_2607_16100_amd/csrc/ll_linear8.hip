@@ -45,9 +45,9 @@ using join_fn = void (*)(Args);
 //    48 x 7168 -> 1024    14.2   - / -, 21.8 / 29, 15.6; 2 splits 14.8    16 of 64
 //  1000 x 7008 -> 200     15.1   - / -, 36 / 29, 19.1; 4 splits 15.6      64 of 64
 // binary32 4096 x 4096 -> 4096  122   - / 124, 145 / 161, 176
-// Rows that pass through registers always take tiles of 64: a stage of 128 does
-// not fit a thread's registers (1995 x 159 -> 6254: 59 us, with 128 74; 4000 x
-// 1001 -> 2001 58 either way).
+// Rows that pass through registers always take tiles of 64: three stages of 128
+// do not fit a thread's registers (1995 x 159 -> 6254: 54 us, with one stage of 128
+// ahead 74; 4000 x 1001 -> 2001 52, so 58).  One of their stages takes 0.5-0.6 us.
 Plan plan_of8(const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
   Plan p{64, 2, 1};
   const uint64_t steps = (a.k + 127) / 128;
@@ -63,7 +63,7 @@ Plan plan_of8(const Args &a, ll_dtype dt, Rows rows, uint64_t room) {
       const uint64_t words = (steps + kScaleStages - 1) / kScaleStages;
       const uint64_t one = (uint64_t)a.rows_c * a.part_row * 4;
       const uint64_t most = std::min<uint64_t>(std::min<uint64_t>(16, words), std::min(room, kMaxParts) / std::max<uint64_t>(one, 1));
-      const double whole = .33 * (rows == kAnyRows ? 2.4 : 1.) * (double)steps;
+      const double whole = .33 * (rows == kAnyRows ? 1.6 : 1.) * (double)steps;
       double best = whole;
       for (uint64_t s = 2; s <= most; ++s) {
         const double rounds = (double)((t64 * s + kFill - 1) / kFill);

@@ -171,6 +171,58 @@ constexpr int tile8_lds(int bm, int bn, int st) {
   return use > epi ? use : epi;
 }
 
+// Rows at any address go through registers, two stages ahead of the one that is
+// written to LDS, with the same loads in every stage, so that the wait for a
+// stage's loads leaves the next one's under way (777 x 1001 -> 515 to binary32, GELU:
+// one stage ahead 16.6 us, so 13.3; 8000 x 4001 -> 4001: 573 us, so 472).  16 bytes of
+// a row that is not there come from the tile's first, those that would pass the
+// matrix's end from in front of it; end8() puts those of the last stage in place.
+template <typename L>
+__device__ __forceinline__ void fetch8(const L &l, u32x4 (&to)[L::kChunks]) {
+#pragma unroll
+  for (int c = 0; c < L::kChunks; ++c) {
+    const uint64_t o = l.off[c] != kOutside ? l.off[c] : 0;
+    __builtin_memcpy(&to[c], (const __attribute__((address_space(1))) char *)(l.base + (o + 16 > l.left ? l.left - 16 : o)), 16);
+  }
+}
+// The last stage, which has `have` k: bytes to their places, zeros behind the row.
+template <typename L>
+__device__ __forceinline__ void end8(const L &l, u32x4 (&v)[L::kChunks], int have) {
+#pragma unroll
+  for (int c = 0; c < L::kChunks; ++c) {
+    const uint64_t past = (l.off[c] != kOutside ? l.off[c] : 0) + 16ull;
+    const uint32_t by = past > l.left ? (uint32_t)(past - l.left) : 0u;  // (above 15 nothing of it is kept)
+    const int n = (int)l.kk(c) < have ? have - (int)l.kk(c) : 0;
+    uint64_t lo = (uint64_t)v[c][1] << 32 | v[c][0], hi = (uint64_t)v[c][3] << 32 | v[c][2];
+    lo = by & 8 ? hi : lo;
+    hi = by & 8 ? 0 : hi;
+    const uint32_t bits = by % 8 * 8;
+    lo = lo >> bits | hi << 1 << (63 - bits);
+    hi >>= bits;
+    const uint32_t keep_lo = (uint32_t)min(n, 8) * 8, keep_hi = (uint32_t)min(max(n - 8, 0), 8) * 8;
+    lo &= keep_lo == 64 ? ~0ull : (1ull << keep_lo) - 1;
+    hi &= keep_hi == 64 ? ~0ull : (1ull << keep_hi) - 1;
+    v[c] = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+  }
+}
+// An only stage of a matrix of fewer than 16 bytes.
+template <typename L>
+__device__ __forceinline__ void bytes8(const L &l, u32x4 (&to)[L::kChunks], int have) {
+#pragma unroll
+  for (int c = 0; c < L::kChunks; ++c) {
+    const int n = l.off[c] != kOutside ? min(have - (int)l.kk(c), 16) : 0;
+    const auto p = (const __attribute__((address_space(1))) uint8_t *)(l.base + l.off[c]);
+    uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      const uint64_t b = (uint64_t)p[i] << i % 8 * 8;
+      lo |= i < 8 ? b : 0;
+      hi |= i < 8 ? 0 : b;
+    }
+    to[c] = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+  }
+}
+
 template <typename O, int BM, int BN, int ST, bool GATED, Rows ROWS>
 __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32_t m0, uint32_t m_end, char *lds) {
   constexpr bool VEC = ROWS != kAnyRows;  // loads go straight into LDS
@@ -201,11 +253,12 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
   // Scales of the tile's rows (first BM) and of its weight rows: segments of 64,
   // dealt to the waves.
   constexpr int kSegs = (BM + BN) / 64, kMine = (kSegs + NW - 1) / NW;
+  static_assert(VEC || NW % kSegs == 0, "a wave's only segment, which others have too");
   uint64_t sbase[kMine];
   uint32_t soff[kMine];
 #pragma unroll
   for (int c = 0; c < kMine; ++c) {
-    const uint32_t seg = wave + c * NW, e = seg * 64 + lane;
+    const uint32_t seg = VEC ? wave + c * NW : wave % kSegs, e = seg * 64 + lane;
     if (seg * 64 < BM) {
       sbase[c] = (uint64_t)(a.xs + (uint64_t)m0 * a.ldxs);
       soff[c] = m0 + e < m_end ? (uint32_t)(e * a.ldxs) : kOutside;
@@ -216,6 +269,7 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
       soff[c] = ok ? (uint32_t)(r / 128 * a.ldws) : kOutside;
     }
   }
+  const bool tiny = !VEC && (m0 * a.ldp + lp.left < 16 || (GATED ? 0 : (uint64_t)tn * BN * a.ldq) + lq.left < 16);
   if (a.splits > 1) {
     lp.skip(k_from / BK);
     lq.skip(k_from / BK);
@@ -265,6 +319,30 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
           : "memory");
     }
   };
+  // Rows through registers: a stage's chunks and scales.
+  struct Ahead {
+    u32x4 p[decltype(lp)::kChunks], q[decltype(lq)::kChunks];
+    uint32_t scales;
+  };
+  auto fetch = [&](Ahead &to, uint32_t s) __attribute__((always_inline)) {  // stage s, the next one, or the last again
+    fetch8(lp, to.p);
+    fetch8(lq, to.q);
+    to.scales = *(const __attribute__((address_space(1))) uint32_t *)(sbase[0] + min(s, steps - 1) / kScaleStages * 4 +
+                                                                     (soff[0] != kOutside ? soff[0] : 0));
+    if (s + 1 < steps) {
+      lp.advance();
+      lq.advance();
+    }
+  };
+  auto commit = [&](Ahead &from, uint32_t s, char *to) __attribute__((always_inline)) {
+    if (s + 1 == steps) {
+      end8(lp, from.p, (int)(k - s * BK));
+      end8(lq, from.q, (int)(k - s * BK));
+    }
+    lp.commit(to, from.p);
+    lq.commit(to + BM * 128, from.q);
+    *reinterpret_cast<uint32_t *>(scale_lds + (s / kScaleStages & 1) * kScales + (wave % kSegs * 64 + lane) * 4) = from.scales;
+  };
   // first entry of the wave's fragment i of the rows
   auto dim_p = [&](int i) __attribute__((always_inline)) {
     return FM > 1 ? (i < FH ? 0 : BM / 2) + wm * (WTM / 2) + (i % FH) * 32 : wm * 32;
@@ -286,27 +364,36 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
   const bool lower = FM == 1 || m_end - m0 > BM / 2;  // the tile has rows in its lower half
 
   if (steps > 0) {
-    issue_scales(0, true);
+    Ahead ahead[2];  // !VEC: the two stages behind the next, by the lowest bit of the one that commits them
+    if constexpr (VEC) {
+      issue_scales(0, true);
 #pragma unroll
-    for (int s = 0; s < ST; ++s) {
-      const int have = (int)k - s * BK;
-      if constexpr (VEC) {
+      for (int s = 0; s < ST; ++s) {
+        const int have = (int)k - s * BK;
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) issue(s, n, std::false_type{}, have > 0 ? have : 0);
-      } else {
-        lp.fetch(have);
-        lq.fetch(have);
-        if (s == 0) {  // the second stage is committed during the first
-          lp.commit(lds);
-          lq.commit(lds + BM * 128);
-        }
+        lp.advance();
+        lq.advance();
       }
-      lp.advance();
-      lq.advance();
+      wait_loads<(ST - 1) * kLoads>();
+      lp.clear_tail(lds, (int)k);
+      lq.clear_tail(lds + BM * 128, (int)k);
+    } else {
+      Ahead first;
+      if (tiny) {
+        bytes8(lp, first.p, (int)k);
+        bytes8(lq, first.q, (int)k);
+        first.scales = *(const __attribute__((address_space(1))) uint32_t *)(sbase[0] + (soff[0] != kOutside ? soff[0] : 0));
+        asm volatile("" : "+v"(first.scales));  // (waited for here, not where the other branch's loads would be too)
+        lp.left = lq.left = kOutside;           // nothing to move
+        ahead[0] = ahead[1] = first;
+      } else {
+        fetch(first, 0);
+        fetch(ahead[0], 1);
+        fetch(ahead[1], 2);
+      }
+      commit(first, 0, lds);
     }
-    wait_loads<VEC ? (ST - 1) * kLoads : 0>();
-    lp.clear_tail(lds, (int)k);
-    lq.clear_tail(lds + BM * 128, (int)k);
     lds_barrier();
 
     Frag8 fq[2][FN], fp[2][FM];  // by half of k
@@ -330,7 +417,7 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
 
     // One stage, number s, from LDS buffer b.  `whole`: the stage loaded meanwhile
     // has BK k, else `have` of them (none: zeros are written).  next_has: k of the
-    // next one.
+    // next one.  !VEC: stage s + 3 is fetched meanwhile if `whole`.
     auto stage = [&](int b, uint32_t s, auto lower_c, auto whole, int have, int next_has) __attribute__((always_inline)) {
       constexpr int kRowsF = decltype(lower_c)::value ? FM : FH;  // fragments of rows that have rows
       constexpr int kMmas = FN * kRowsF, kReads = 2 * (FN + kRowsF);
@@ -353,21 +440,19 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
         multiply(t, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (!VEC) {  // the next stage's chunks, fetched a stage ago
-        lp.commit(const_cast<char *>(next));
-        lq.commit(const_cast<char *>(next) + BM * 128);
-      }
-      wait_loads<VEC ? (ST - 2) * kLoads : 0>();
+      if constexpr (VEC)
+        wait_loads<(ST - 2) * kLoads>();
+      else  // the next stage's chunks, fetched two stages ago
+        commit(ahead[b], s + 1, const_cast<char *>(next));
       if (ROWS == kDwordRows && next_has < BK) {
         lp.clear_tail(const_cast<char *>(next), next_has);
         lq.clear_tail(const_cast<char *>(next) + BM * 128, next_has);
       }
       lds_barrier();
-      issue_scales(s / kScaleStages + 1, s % kScaleStages == 1);
-      if constexpr (!VEC) {
-        lp.fetch(have);
-        lq.fetch(have);
-      }
+      if constexpr (VEC)
+        issue_scales(s / kScaleStages + 1, s % kScaleStages == 1);
+      else if constexpr (decltype(whole)::value)
+        fetch(ahead[b], s + 3);
       int nq[FN], np[FM];
       read_scales(s + 1, nq, np);
 #pragma unroll
@@ -385,8 +470,10 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
       for (int j = 0; j < FN; ++j) sq[j] = nq[j];
 #pragma unroll
       for (int i = 0; i < FM; ++i) sp[i] = np[i];
-      lp.advance();
-      lq.advance();
+      if constexpr (VEC) {
+        lp.advance();
+        lq.advance();
+      }
     };
     auto all = [&](auto lower_c) __attribute__((always_inline)) {
       uint32_t s = 0;
@@ -400,8 +487,24 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
           }
         }
       }
-      for (; s < steps; ++s)
-        stage(s % ST, s, lower_c, std::false_type{}, (int)k - (int)(s + ST) * BK, (int)k - (int)(s + 1) * BK);
+      if constexpr (VEC) {
+        for (; s < steps; ++s)
+          stage(s % ST, s, lower_c, std::false_type{}, (int)k - (int)(s + ST) * BK, (int)k - (int)(s + 1) * BK);
+      } else {
+        for (; s + 4 < steps; s += 2) {
+          stage(0, s, lower_c, std::true_type{}, 0, 0);
+          stage(1, s + 1, lower_c, std::true_type{}, 0, 0);
+        }
+        if (s + 3 < steps) {
+          stage(0, s, lower_c, std::true_type{}, 0, 0);
+          stage(1, s + 1, lower_c, std::false_type{}, 0, 0);
+          s += 2;
+        }
+        for (; s < steps; s += 2) {
+          stage(0, s, lower_c, std::false_type{}, 0, 0);
+          if (s + 1 < steps) stage(1, s + 1, lower_c, std::false_type{}, 0, 0);
+        }
+      }
     };
     if (FM == 1 || lower)
       all(std::true_type{});
@@ -415,7 +518,7 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
 }
 
 template <typename O, int BM, int BN, int ST, bool GATED, Rows ROWS>
-__global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : 2) void k_tile8(Args8 a) {
+__global__ __launch_bounds__(256, ST *(BM + BN) > 640 ? 1 : ROWS == kAnyRows && sizeof(O) == 4 ? 3 : 2) void k_tile8(Args8 a) {
   __shared__ __attribute__((aligned(1024))) char lds[tile8_lds(BM, BN, ST)];
   int g = 0;
   uint32_t tn = 0, m0 = 0, m_end = a.m;

@@ -144,6 +144,16 @@ def test_large_products(name, dtype, act, save, layout):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", [0, 1, 3])
+@pytest.mark.parametrize("rows,k,out", [(1, 1, 1), (3, 5, 2), (40, 1, 3), (40, 7, 2), (17, 15, 1), (70, 17, 1), (5, 3, 40),
+                                        (66, 129, 65), (66, 143, 3), (66, 257, 3), (66, 385, 3), (66, 511, 3), (66, 641, 3)])
+def test_few_bytes(rows, k, out, layout, dtype):
+    """Matrices shorter than what is read at a time, sums that end anywhere in it, and every number of stages up to six."""
+    check((None, rows, k, out), dtype, "none", False, False, False, layout, seed=k)
+    check(([rows - 1, 0, 1], 0, k, out), dtype, "none", False, False, False, layout, seed=k)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,k", [(3, 256), (40, 300), (300, 384)])
 def test_codes_that_are_no_number_stay_in_their_row_and_column(dtype, rows, k):
     g = gen(k)
