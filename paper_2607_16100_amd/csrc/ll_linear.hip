@@ -343,8 +343,6 @@ int ll_linear(const ll_linear_desc *d, const void *x, const void *w, const void 
   a.c = y;
   a.ldc = d->ldy;
   a.act = (int)d->act;
-  a.vec_b = rows16(bias, d->out, es);
-  a.vec_c = rows16(y, d->ldy, es) && rows16(z, d->ldz, es) && rows16(residual, d->ldr, es);
   Rows rows = std::min(rows_of(x, d->ldx, d->in, es), weight_rows(d, w, es));
 
   const int blocks = stream_blocks(a, rows);
@@ -428,8 +426,6 @@ int ll_linear_grad_w(const ll_linear_desc *d, const void *dz, const void *x, voi
   a.ldc = d->ldw;
   a.dbias = dbias;
   a.flags = flags;
-  // the gradient's own element size decides its alignment
-  a.vec_c = rows16(dw, d->ldw, gs) && d->wstride * gs % 16 == 0;
   const Rows rows = std::min(rows_of(dz, d->ldy, d->out, es), rows_of(x, d->ldx, d->in, es));
   a.k = a.rows;
   return launch_product<kGradW>(a, d->dt, false, rows, workspace, workspace_bytes, stream);

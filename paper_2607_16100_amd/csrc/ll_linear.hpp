@@ -40,8 +40,7 @@ struct Args {
   void *c, *zout, *dbias;
   int act;
   uint32_t flags;  // LL_GRAD_*
-  bool vec_c;      // every epilogue row starts at a 16-byte address
-  bool vec_b;      // so does every group's bias
+  bool vec_c;      // dx: every epilogue row starts at a 16-byte address
   float *parts;      // sums of the splits of k, [splits][rows of C][part_row], or NULL
   uint32_t splits, rows_c;
   bool sum_bias;  // grad_w: the tile kernel computes dbias too
@@ -518,28 +517,42 @@ struct Loader {
 constexpr int kEw = 8;
 typedef Pack<float, kEw, true> Vals;
 
-// kEw values at p, of which the row has n; vec: p is aligned for 16 bytes (or
-// for all kEw elements, if they are fewer).
+// kEw values at p, of which the row has n: 16 bytes at a time at any alignment,
+// single ones at the row's end (8-bit 777 x 1001 -> 515, two results of binary32 rows
+// of 515: 13.4 us with single ones everywhere, so 11.2).
 template <typename T>
-__device__ __forceinline__ void put8(T *p, const Vals &v, uint32_t n, bool vec) {
-  Pack<T, kEw, true> o;
+__device__ __forceinline__ void put8(T *p, const Vals &v, uint32_t n) {
+  constexpr int kEach = 16 / (int)sizeof(T);
+  if (n >= kEw) {
 #pragma unroll
-  for (int i = 0; i < kEw; ++i) o.v[i] = v.v[i];
-  if (vec && n >= kEw)
-    o.store(p);
-  else
-    o.store_some(p, (int)n);
+    for (int i = 0; i < kEw; i += kEach) {
+      T r __attribute__((ext_vector_type(kEach)));
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) r[j] = Num<T>::put(v.v[i + j]);
+      __builtin_memcpy(p + i, &r, 16);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEw; ++i)
+      if (i < (int)n) p[i] = Num<T>::put(v.v[i]);
+  }
 }
 template <typename T>
-__device__ __forceinline__ Vals get8(const T *p, uint32_t n, bool vec) {
-  Pack<T, kEw, true> o;
-  if (vec && n >= kEw)
-    o.load(p);
-  else
-    o.load_some(p, (int)n, 0.f);
+__device__ __forceinline__ Vals get8(const T *p, uint32_t n) {
+  constexpr int kEach = 16 / (int)sizeof(T);
   Vals v;
+  if (n >= kEw) {
 #pragma unroll
-  for (int i = 0; i < kEw; ++i) v.v[i] = o.v[i];
+    for (int i = 0; i < kEw; i += kEach) {
+      T r __attribute__((ext_vector_type(kEach)));
+      __builtin_memcpy(&r, p + i, 16);
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) v.v[i + j] = Num<T>::get(r[j]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEw; ++i) v.v[i] = i < (int)n ? Num<T>::get(p[i]) : 0.f;
+  }
   return v;
 }
 // kEw elements as they lie in memory, converted where they are used.
@@ -608,21 +621,21 @@ __device__ __forceinline__ void put_forward(const Args &a, int g, uint64_t r, ui
   const uint32_t left = width - n0;
   if (a.bias != nullptr) {
     const T *b = (const T *)a.bias + (uint64_t)g * a.n + n0;
-    add8(v, get8(b, left, a.vec_b));
-    if constexpr (GATED) add8(u, get8(b + width, left, a.vec_b && width % kEw == 0));
+    add8(v, get8(b, left));
+    if constexpr (GATED) add8(u, get8(b + width, left));
   }
   if (a.zout != nullptr) {
     T *z = (T *)a.zout + r * a.ldz + n0;
-    put8(z, v, left, a.vec_c);
-    if constexpr (GATED) put8(z + width, u, left, a.vec_c && width % kEw == 0);
+    put8(z, v, left);
+    if constexpr (GATED) put8(z + width, u, left);
   }
   act8(v, a.act);
   if constexpr (GATED) {
 #pragma unroll
     for (int i = 0; i < kEw; ++i) v.v[i] *= u.v[i];
   }
-  if (a.res != nullptr) add8(v, get8((const T *)a.res + r * a.ldr + n0, left, a.vec_c));
-  put8((T *)a.c + r * a.ldc + n0, v, left, a.vec_c);
+  if (a.res != nullptr) add8(v, get8((const T *)a.res + r * a.ldr + n0, left));
+  put8((T *)a.c + r * a.ldc + n0, v, left);
 }
 
 // The sums v through the activation of the layer below, whose pre-activations
@@ -650,15 +663,14 @@ __device__ __forceinline__ void put_grad_x(const Args &a, uint64_t r, uint32_t n
   const uint32_t left = a.n - n0;
   T *out = (T *)a.c + r * a.ldc + n0;
   if (a.act != LL_ACT_NONE) {
-    const bool vec = a.vec_c && a.n % kEw == 0;
     const T *zp = (const T *)a.z + r * a.ldz + n0;
     Vals u, w;
-    const Vals z = get8(zp, left, a.vec_c);
-    if (gated(a.act)) u = get8(zp + a.n, left, vec);
+    const Vals z = get8(zp, left);
+    if (gated(a.act)) u = get8(zp + a.n, left);
     through_act(a, v, z, u, w);
-    if (gated(a.act)) put8(out + a.n, w, left, vec);
+    if (gated(a.act)) put8(out + a.n, w, left);
   }
-  put8(out, v, left, a.vec_c);
+  put8(out, v, left);
 }
 
 template <typename G>
@@ -666,8 +678,8 @@ __device__ __forceinline__ void put_grad_w(const Args &a, int g, uint32_t m, uin
   if (n0 >= a.n) return;
   const uint32_t left = a.n - n0;
   G *out = (G *)a.c + (uint64_t)g * a.cstride + (uint64_t)m * a.ldc + n0;
-  if (a.flags & LL_GRAD_ADD) add8(v, get8(out, left, a.vec_c));
-  put8(out, v, left, a.vec_c);
+  if (a.flags & LL_GRAD_ADD) add8(v, get8(out, left));
+  put8(out, v, left);
 }
 
 template <typename T>
@@ -1054,8 +1066,8 @@ __global__ __launch_bounds__(WM *WN * 64, ST *(BM + BN) > 640 && WM * WN == 4 ? 
             for (int e = 0; e < kEw; ++e) v.v[e] = sums.v[e];
             through_act(a, v, z[i].vals(), u[i].vals(), w);
             T *out = (T *)a.c + (uint64_t)m * a.ldc + n0;
-            if (gated(a.act)) put8(out + a.n, w, kEw, true);
-            put8(out, v, kEw, true);
+            if (gated(a.act)) put8(out + a.n, w, kEw);
+            put8(out, v, kEw);
           }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

@@ -250,8 +250,6 @@ int ll_linear8(const ll_linear_desc *d, const uint8_t *x, const uint8_t *xs, siz
   a.c = y;
   a.ldc = d->ldy;
   a.act = (int)d->act;
-  a.vec_b = rows16(bias, d->out, es);
-  a.vec_c = rows16(y, d->ldy, es) && rows16(z, d->ldz, es) && rows16(residual, d->ldr, es);
   a.xs = xs;
   a.ws = ws;
   a.ldxs = ldxs;

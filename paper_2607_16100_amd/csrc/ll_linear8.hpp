@@ -174,7 +174,7 @@ constexpr int tile8_lds(int bm, int bn, int st) {
 // Rows at any address go through registers, two stages ahead of the one that is
 // written to LDS, with the same loads in every stage, so that the wait for a
 // stage's loads leaves the next one's under way (777 x 1001 -> 515 to binary32, GELU:
-// one stage ahead 16.6 us, so 13.3; 8000 x 4001 -> 4001: 573 us, so 472).  16 bytes of
+// one stage ahead 16.6 us, two 13.3; 8000 x 4001 -> 4001: 573 us, 472).  16 bytes of
 // a row that is not there come from the tile's first, those that would pass the
 // matrix's end from in front of it; end8() puts those of the last stage in place.
 template <typename L>
