@@ -172,8 +172,8 @@ typedef struct {
  * are rounded up or down at random, by a hash of seed, t and the value's
  * number, with the probability that keeps their mean: a state that moves by a
  * thousandth would else stay where it is.  workspace: LL_ADAMW_WORKSPACE bytes,
- * 16-byte aligned.  The tensors lie apart; eps is above 0.  Steps that share
- * states or the workspace follow one another. */
+ * 16-byte aligned.  The tensors lie apart; eps is above 0 in binary32.  Steps
+ * that share states or the workspace follow one another. */
 #define LL_ADAMW_WORKSPACE 64
 int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t count, int32_t *step, const float *lr_ptr,
              const float *grad_scale, void *workspace, size_t workspace_bytes, void *stream);

@@ -337,7 +337,7 @@ int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t coun
              const float *grad_scale, void *workspace, size_t workspace_bytes, void *stream) {
   if (d == nullptr || d->size != sizeof(ll_adamw_desc) || (d->bits != 32 && d->bits != 8)) return LL_ERR_INVALID;
   // (written so that NaN is refused)
-  if (!(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !(d->eps > 0.) || !(d->decay >= 0.) ||
+  if (!(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !((float)d->eps > 0.f) || !(d->decay >= 0.) ||
       !(d->lr >= 0.))
     return LL_ERR_INVALID;
   if ((count != 0 && tensors == nullptr) || step == nullptr || !aligned(step, 4) || !aligned(lr_ptr, 4) ||

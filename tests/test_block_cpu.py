@@ -196,7 +196,8 @@ def adamw(count=1, step=A, work=B, work_bytes=64, lr=1e-3, beta1=0.9, beta2=0.99
 
 @pytest.mark.parametrize("kw,want", [
     (dict(size=8), INVALID), (dict(bits=16), INVALID), (dict(beta1=1.0), INVALID), (dict(beta2=-0.5), INVALID),
-    (dict(beta1=float("nan")), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=0.0), INVALID), (dict(decay=-1.0), INVALID),
+    (dict(beta1=float("nan")), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=0.0), INVALID), (dict(eps=1e-50), INVALID),
+    (dict(decay=-1.0), INVALID),
     (dict(lr=float("nan")), INVALID), (dict(lr=-1.0), INVALID), (dict(step=0), INVALID), (dict(step=A + 2), INVALID),
     (dict(work=0), INVALID), (dict(work=B + 8), INVALID), (dict(work_bytes=63), SCRATCH), (dict(lr_ptr=G + 1), INVALID),
     (dict(scale=G + 2), INVALID), (dict(null=True), INVALID), (dict(param=0), INVALID), (dict(grad=0), INVALID),
