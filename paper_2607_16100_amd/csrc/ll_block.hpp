@@ -113,7 +113,7 @@ __device__ __forceinline__ uint32_t quantise8(const lin::Vals &v, uint32_t *w) {
 // |x| 2^-24 and a few units in the last place, where a code's half step is 2^-4.
 // With the library's exponential and division they were most of the kernel's time
 // (16384 x 2 x 2048 through SwiGLU 57 us, with an exponential corrected for the
-// product's rounding 39.3, so 36.7).
+// product's rounding 39.3, so 36.7; with 16 bytes at any alignment 33.9).
 __device__ __forceinline__ void act_rows(lin::Vals &v, int act) {
   if (act == LL_ACT_SILU || act == LL_ACT_SWIGLU) {
 #pragma unroll
@@ -127,8 +127,8 @@ __device__ __forceinline__ void act_rows(lin::Vals &v, int act) {
 // ---------------------------------------------------------------- rows
 //
 // 16 lanes a block of 128 features, U blocks of a lane under way at a time.  Bound
-// by memory: 16384 x 2 x 2048 bfloat16 through SwiGLU 36.7 us, 4.6 TB/s of what is
-// read and written (four blocks at a time 38); 16 x 7168 2.6 us, a load's latency.
+// by memory: 16384 x 2 x 2048 bfloat16 through SwiGLU 33.9 us, 5.0 TB/s of what is
+// read and written; 16 x 7168 2.6 us, a load's latency.
 struct QuantArgs {
   const void *x;
   uint8_t *q, *scales;

@@ -870,10 +870,11 @@ __global__ __launch_bounds__(256, 1) void k_wide8(Args8 a) {
 
 // ---------------------------------------------------------------- few rows a group
 //
-// Up to 16 * RB rows of a group, bound by reading the weight once, as k_stream:
-// (16 rows over 32 groups of 7168 -> 2 x 2048: 60-64 us, 5.9-6.2 TB/s of the
-// weights that have rows): a workgroup owns 2 x 16 weight rows (gated: 16 of each half), each of its
-// waves an equal run of the blocks of k, kAhead blocks' loads under way at a time.
+// Up to 16 * RB rows of a group, bound by reading the weight once, as k_stream (16
+// rows over 32 groups of 7168 -> 2 x 2048: 60-64 us, 5.9-6.2 TB/s of the weights
+// that have rows): a workgroup owns 2 x 16 weight rows (gated: 16 of each half),
+// each of its waves an equal run of the blocks of k, kAhead blocks' loads under way
+// at a time.
 // A lane has one weight row's (and one row's) scales of those blocks in a
 // word, cut from the two words they lie in.
 template <typename O, int RB, int NW, bool GATED>
