@@ -442,7 +442,10 @@ __device__ __forceinline__ void tile8(const Args8 &a, int g, uint32_t tn, uint32
       }
       if constexpr (VEC)
         wait_loads<(ST - 2) * kLoads>();
-      else  // the next stage's chunks, fetched two stages ago
+      // The next stage's chunks, fetched two stages ago.  Behind the last stage the slot
+      // holds an older one, whose word of scales may be the other of two words and would
+      // go over the one that late waves still read for this stage.
+      else if (decltype(whole)::value || s + 1 < steps)
         commit(ahead[b], s + 1, const_cast<char *>(next));
       if (ROWS == kDwordRows && next_has < BK) {
         lp.clear_tail(const_cast<char *>(next), next_has);
