@@ -84,19 +84,20 @@ class ExpertLayer:
         if products == "e4m3":
             self.quantise_weights()
 
-    def quantise_weights(self) -> None:
+    def quantise_weights(self, stream=None) -> None:
         """Codes and scales of ``up`` and ``down`` as they are now, and of their
-        transposes for the way back."""
+        transposes for the way back; on ``stream``, behind what changed them."""
         if self.products != "e4m3":
             return
         if self._up8 is None:
-            self._up8, self._down8 = ([(moe.quantise_weight(w), moe.quantise_weight(w, transpose=True)) for w in ws]
+            self._up8, self._down8 = ([(moe.quantise_weight(w, stream=stream),
+                                        moe.quantise_weight(w, transpose=True, stream=stream)) for w in ws]
                                       for ws in (self.up, self.down))
             return
         for held, ws in ((self._up8, self.up), (self._down8, self.down)):
             for ((q, s), (qt, st)), w in zip(held, ws):
-                moe.quantise_weight(w, out=q, scales=s)
-                moe.quantise_weight(w, transpose=True, out=qt, scales=st)
+                moe.quantise_weight(w, out=q, scales=s, stream=stream)
+                moe.quantise_weight(w, transpose=True, out=qt, scales=st, stream=stream)
 
     # -- the regions as matrices
     def _slice(self, region: SymRegion, r: int, rows: int, cols: int) -> torch.Tensor:
@@ -214,10 +215,11 @@ class ExpertBlock:
         first = moe.norm_grad(dh.view(rows.shape), rows, self.pre, dr=last.dr, eps=self.eps)
         return first.dr.view(dout.shape), [first.dweight, last.dpost, drouter, *dup, *ddown]
 
-    def step(self, grads, **options) -> None:
-        """One update of ``params`` (options: those of ``AdamW.step``)."""
-        self.optimiser.step(grads, **options)
-        self.layer.quantise_weights()
+    def step(self, grads, *, stream=None, **options) -> None:
+        """One update of ``params``, and the codes of the layer's weights behind it on
+        the same stream (options: those of ``AdamW.step``)."""
+        self.optimiser.step(grads, stream=stream, **options)
+        self.layer.quantise_weights(stream)
 
 
 def main() -> None:
