@@ -187,16 +187,21 @@ class ExpertBlock:
 
         out = x + scale * post * unit(layer(pre * unit(x)))
 
-    unit(v) = v / sqrt(mean(v^2) + eps).  ``layer`` takes the options of
-    ExpertLayer; ``pre`` and ``post`` [hidden] are binary32 and start at 1.
-    ``options`` are those of ``optim.AdamW``."""
+    unit(v) = v / sqrt(mean(v^2) + eps).  ``layer`` is an ExpertLayer; ``pre`` and
+    ``post`` [hidden] are binary32 and start at 1.  ``options`` are those of
+    ``optim.AdamW``.  The block updates the tensors that it and the layer have when
+    it is made: assign others before; ``step`` refuses others."""
 
     def __init__(self, layer: ExpertLayer, scale: float = 1.0, eps: float = 1e-6, **options):
         self.layer, self.scale, self.eps = layer, scale, eps
         device = layer.router.device
         self.pre, self.post = (torch.ones(layer.hidden, device=device) for _ in range(2))
-        self.params = [self.pre, self.post, layer.router, *layer.up, *layer.down]
+        self.params = self._present()
         self.optimiser = AdamW(self.params, **options)
+
+    def _present(self) -> list:
+        """The tensors that forward and backward use now."""
+        return [self.pre, self.post, self.layer.router, *self.layer.up, *self.layer.down]
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         """[P, tokens, hidden] -> the same shape.  A token is on one rank, so the
@@ -218,6 +223,10 @@ class ExpertBlock:
     def step(self, grads, *, stream=None, **options) -> None:
         """One update of ``params``, and the codes of the layer's weights behind it on
         the same stream (options: those of ``AdamW.step``)."""
+        present = self._present()
+        if len(present) != len(self.params) or any(a is not b for a, b in zip(present, self.params)):
+            raise ValueError("the layer's or the block's weights are other tensors than those the block was made with: "
+                             "make it anew")
         self.optimiser.step(grads, stream=stream, **options)
         self.layer.quantise_weights(stream)
 

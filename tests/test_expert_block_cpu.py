@@ -40,3 +40,31 @@ def test_codes_are_made_on_the_updates_stream(monkeypatch, stream):
         block.step([], stream=stream, lr=1e-3)
         assert calls[0] == ("step", {"stream": stream, "lr": 1e-3})
         assert calls[1:] == [("codes", {"stream": stream})] * 8
+
+
+@pytest.mark.parametrize("where", ["router", "up", "down", "pre", "post", "more"])
+def test_other_tensors_than_the_blocks_own_are_refused(monkeypatch, where):
+    block, calls = make()
+    recorded(monkeypatch, calls)
+    layer = block.layer
+    if where == "router":
+        layer.router = layer.router.clone()
+    elif where == "up":
+        layer.up[1] = layer.up[1].clone()
+    elif where == "down":
+        layer.down = [w.clone() for w in layer.down]
+    elif where == "more":
+        layer.up.append(layer.up[0])
+    else:
+        setattr(block, where, getattr(block, where).clone())
+    with pytest.raises(ValueError):
+        block.step([])
+    assert not calls
+
+
+def test_the_blocks_own_tensors_in_another_list(monkeypatch):
+    block, calls = make("same")
+    recorded(monkeypatch, calls)
+    block.layer.up = list(block.layer.up)
+    block.step([])
+    assert calls == [("step", {"stream": None})]

@@ -52,3 +52,18 @@ def test_a_step_on_a_busy_side_stream():
             assert torch.equal(x, y)
         codes_are_the_weights(a.layer)
         codes_are_the_weights(b.layer)
+
+
+def test_other_weights_than_the_blocks_own():
+    """Assigned before the block is made they are updated; behind that a step is refused."""
+    layer = ExpertLayer(2, 16, 128, 64, 4, 2, seed=1)
+    layer.up = [w.clone() for w in layer.up]
+    block = ExpertBlock(layer, lr=1e-2)
+    before = [w.clone() for w in layer.up]
+    block.step(grads_of(block, 1))
+    assert not any(torch.equal(a, b) for a, b in zip(before, layer.up))
+    layer.down[1] = layer.down[1].clone()
+    kept = [p.clone() for p in block.params]
+    with pytest.raises(ValueError):
+        block.step(grads_of(block, 2))
+    assert all(torch.equal(a, b) for a, b in zip(kept, block.params)) and int(block.optimiser.count) == 1
