@@ -10,6 +10,7 @@ graph is the next one each time the graph is replayed.
 from __future__ import annotations
 
 import ctypes
+from operator import attrgetter
 from typing import Optional, Sequence
 
 import numpy as np
@@ -23,6 +24,10 @@ from .moe import _device, _flat, _stream
 _DT = {torch.float32: ll.LL_F32, torch.bfloat16: ll.LL_BF16}
 STATES = {"f32": 32, "8bit": 8}
 _TYPES = {32: (torch.float32, torch.float32), 8: (torch.float8_e4m3fn, torch.float8_e5m2)}
+
+# of a list of tensors, by map: less host work than a comprehension
+_dtype, _numel, _ptr = attrgetter("dtype"), torch.Tensor.numel, torch.Tensor.data_ptr
+_contiguous, _get_device = torch.Tensor.is_contiguous, torch.Tensor.get_device
 
 # what changes from step to step of a row of ll_adamw's table
 _ROW = np.dtype({"names": ["param", "grad", "gdt"], "formats": [np.uint64, np.uint64, np.int32],
@@ -85,8 +90,9 @@ class AdamW:
         self._work = torch.empty(lb.LL_ADAMW_WORKSPACE, dtype=torch.uint8, device=device)
         self._table = (lb.LLAdamwTensor * len(self.params))()
         self._fields = np.frombuffer(self._table, dtype=_ROW)  # the same memory
-        self._sizes = [p.numel() for p in self.params]
+        self._sizes, self._dtypes = [p.numel() for p in self.params], [p.dtype for p in self.params]
         self._at: list = []  # the parameters' addresses in the table
+        self._grad_dtypes: list = []  # the gradients' types there
         self._versioned = [p for p in self.params if not p.is_inference()]
         es = 1 if eight else 4
         for t, p, w, at in zip(self._table, self.params, self.masters, self.offsets):
@@ -96,16 +102,19 @@ class AdamW:
             if eight:
                 t.m_scales, t.v_scales = self.m_scales.data_ptr() + at // 128, self.v_scales.data_ptr() + at // 128
 
-    def _check(self, tensors, name: str, dev: int) -> list:
-        """The tensors' type codes; one contiguous tensor of a parameter's size each."""
-        if [t.numel() for t in tensors] != self._sizes or [t.get_device() for t in tensors] != [dev] * len(self._sizes) \
-                or not all([t.is_contiguous() for t in tensors]):
-            raise ValueError(f"{name}: one contiguous tensor on the parameters' GPU a parameter, of its number of values, "
+    def _check(self, grads, dev: int) -> None:
+        """One contiguous tensor of a parameter's size and a known type each; their types go into the table."""
+        if list(map(_numel, grads)) != self._sizes or list(map(_get_device, grads)) != [dev] * len(self._sizes) \
+                or not all(map(_contiguous, grads)):
+            raise ValueError("grads: one contiguous tensor on the parameters' GPU a parameter, of its number of values, "
                              "is needed")
-        try:
-            return [_DT[t.dtype] for t in tensors]
-        except KeyError as e:
-            raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(e)) from None
+        types = list(map(_dtype, grads))
+        if types != self._grad_dtypes:
+            try:
+                self._fields["gdt"] = [_DT[t] for t in types]
+            except KeyError as e:
+                raise ll.LLError(ll.LL_ERR_UNSUPPORTED, str(e)) from None
+            self._grad_dtypes = types
 
     def _apart(self) -> None:
         """Two parameters in the same memory would be updated at the same time."""
@@ -147,12 +156,16 @@ class AdamW:
         if dev != self._dev:
             raise ValueError("the parameters are not on the current GPU")
         table, fields = self._table, self._fields
-        fields["gdt"] = self._check(grads, "grads", dev)
-        fields["grad"] = [g.data_ptr() for g in grads]
-        at = [p.data_ptr() for p in self.params]
+        self._check(grads, dev)
+        fields["grad"] = list(map(_ptr, grads))
+        # (other memory may lie at the same address, or the same memory be strided otherwise)
+        if list(map(_numel, self.params)) != self._sizes or list(map(_dtype, self.params)) != self._dtypes \
+                or not all(map(_contiguous, self.params)):
+            raise ValueError("params: their sizes, types or strides have changed")
+        at = list(map(_ptr, self.params))
         if at != self._at:  # a parameter's memory is another than at the last step
-            if self._check(self.params, "params", dev) != [t.dt for t in table]:
-                raise ValueError("params: their types have changed")
+            if list(map(_get_device, self.params)) != [dev] * len(at):
+                raise ValueError("params: not all on the GPU they were on")
             self._apart()
             fields["param"] = self._at = at
         rate, rate_at = self.lr if lr is None else lr, None
