@@ -9,6 +9,7 @@ graph is the next one each time the graph is replayed.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from operator import attrgetter
 from typing import Optional, Sequence
@@ -38,7 +39,11 @@ class AdamW:
     """Adam with decoupled weight decay over ``params`` (contiguous float32 or
     bfloat16 tensors of one GPU, which are updated in place); see ll_adamw.
 
-    A bfloat16 parameter has a float32 master, made from it.  The states of all
+    A bfloat16 parameter has a float32 master, made from it, which holds its value:
+    the parameter is written from it at each step.  Call ``read_params`` where a
+    parameter has got other values otherwise, in its memory or with another one (a
+    step does so by itself for parameters that it finds at another address than the
+    step before, but freed memory may come back at the same one).  The states of all
     parameters lie in one tensor each, a parameter's at a multiple of 128
     (``offsets``): ``m`` and ``v`` in float32, or with states="8bit" m as
     float8_e4m3fn and v as float8_e5m2 with a power of two (float8_e8m0fnu) for
@@ -91,7 +96,7 @@ class AdamW:
         self._table = (lb.LLAdamwTensor * len(self.params))()
         self._fields = np.frombuffer(self._table, dtype=_ROW)  # the same memory
         self._sizes, self._dtypes = [p.numel() for p in self.params], [p.dtype for p in self.params]
-        self._at: list = []  # the parameters' addresses in the table
+        self._fields["param"] = self._at = list(map(_ptr, self.params))
         self._grad_dtypes: list = []  # the gradients' types there
         self._versioned = [p for p in self.params if not p.is_inference()]
         es = 1 if eight else 4
@@ -146,6 +151,16 @@ class AdamW:
         return {"masters": self.masters, "m": self.m, "v": self.v, "m_scales": self.m_scales,
                 "v_scales": self.v_scales, "count": self.count}
 
+    def read_params(self, which: Optional[Sequence[int]] = None, stream=None) -> None:
+        """Takes up what bfloat16 parameters (all, or those numbered ``which``) hold
+        now: a value that is not its master rounded becomes its master.  The others
+        keep the bits that the parameter does not have."""
+        with torch.no_grad(), contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            for i in range(len(self.params)) if which is None else which:
+                if self.masters[i] is not None:
+                    p, w = self.params[i].detach().reshape(-1), self.masters[i].view(-1)
+                    w.copy_(torch.where(w.to(p.dtype) == p, w, p.float()))
+
     def step(self, grads: Sequence[torch.Tensor], *, lr=None, grad_scale=None, stream=None) -> None:
         """One update.  ``grads``: one contiguous float32 or bfloat16 tensor a
         parameter.  ``lr``: this step's, a number or a float32 tensor of one
@@ -167,6 +182,7 @@ class AdamW:
             if list(map(_get_device, self.params)) != [dev] * len(at):
                 raise ValueError("params: not all on the GPU they were on")
             self._apart()
+            self.read_params([i for i, (a, b) in enumerate(zip(at, self._at)) if a != b], stream)
             fields["param"] = self._at = at
         rate, rate_at = self.lr if lr is None else lr, None
         if isinstance(rate, torch.Tensor):
