@@ -157,7 +157,7 @@ typedef struct {
 
 typedef struct {
   uint32_t size; /* sizeof(ll_adamw_desc) */
-  int32_t bits;  /* 32 or 8: of a state value */
+  int32_t bits;  /* 32 or 8: of a state value; 8 | LL_ADAMW_FLOOR */
   double lr, beta1, beta2, eps, decay;
   uint32_t seed; /* of the random rounding of 8-bit states */
 } ll_adamw_desc;
@@ -171,10 +171,19 @@ typedef struct {
  * one binary32 value each in device memory, or NULL (d->lr, 1).  8-bit states
  * are rounded up or down at random, by a hash of seed, t and the value's
  * number, with the probability that keeps their mean: a state that moves by a
- * thousandth would else stay where it is.  workspace: LL_ADAMW_WORKSPACE bytes,
+ * thousandth would else stay where it is.
+ *
+ * v has 2^32 from its least code to its block's largest value, 2^16 of a gradient,
+ * and m 2^18.  A value whose gradients are 2^-14 and less of its block's largest has
+ * v at 0 most of the time and m now and then at its least code; its next step is m
+ * / (nearly eps), more than 1000 lr where gradients are far above eps.  With
+ * LL_ADAMW_FLOOR a v above 0 is kept at its least code at least: the same steps stay
+ * below about 2 lr, and nothing else changes.  Leave it out only for states that
+ * have to come out as they did without it.  workspace: LL_ADAMW_WORKSPACE bytes,
  * 16-byte aligned.  The tensors lie apart; eps is above 0 in binary32.  Steps
  * that share states or the workspace follow one another. */
 #define LL_ADAMW_WORKSPACE 64
+#define LL_ADAMW_FLOOR 0x100 /* in `bits`: v above 0 is never stored as 0 */
 int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t count, int32_t *step, const float *lr_ptr,
              const float *grad_scale, void *workspace, size_t workspace_bytes, void *stream);
 

@@ -335,7 +335,9 @@ int ll_norm_grad(const ll_norm_desc *d, const void *dh, const void *r, const voi
 
 int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t count, int32_t *step, const float *lr_ptr,
              const float *grad_scale, void *workspace, size_t workspace_bytes, void *stream) {
-  if (d == nullptr || d->size != sizeof(ll_adamw_desc) || (d->bits != 32 && d->bits != 8)) return LL_ERR_INVALID;
+  if (d == nullptr || d->size != sizeof(ll_adamw_desc)) return LL_ERR_INVALID;
+  const bool floor = d->bits == (8 | LL_ADAMW_FLOOR), eight = floor || d->bits == 8;
+  if (!eight && d->bits != 32) return LL_ERR_INVALID;
   // (written so that NaN is refused)
   if (!(d->beta1 >= 0. && d->beta1 < 1.) || !(d->beta2 >= 0. && d->beta2 < 1.) || !((float)d->eps > 0.f) || !(d->decay >= 0.) ||
       !(d->lr >= 0.))
@@ -345,7 +347,6 @@ int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t coun
     return LL_ERR_INVALID;
   static_assert(sizeof(AdamwCoef) <= LL_ADAMW_WORKSPACE, "the coefficients");
   if (workspace_bytes < LL_ADAMW_WORKSPACE) return LL_ERR_SCRATCH;
-  const bool eight = d->bits == 8;
   for (size_t i = 0; i < count; ++i) {
     const ll_adamw_tensor &t = tensors[i];
     if (!known(t.dt) || !known(t.gdt)) return LL_ERR_UNSUPPORTED;
@@ -369,7 +370,7 @@ int ll_adamw(const ll_adamw_desc *d, const ll_adamw_tensor *tensors, size_t coun
   a.eps = (float)d->eps;
   uint32_t chunks = 0;
   auto launch = [&]() {
-    hipLaunchKernelGGL(eight ? k_adamw<true> : k_adamw<false>, dim3(chunks), dim3(256), 0, (hipStream_t)stream, a);
+    hipLaunchKernelGGL((floor ? k_adamw<true, true> : eight ? k_adamw<true, false> : k_adamw<false, false>), dim3(chunks), dim3(256), 0, (hipStream_t)stream, a);
     a.count = chunks = 0;
     return launch_status();
   };

@@ -674,7 +674,10 @@ __device__ __forceinline__ uint32_t to_code(float y, uint32_t r) {
   return (b < kMin ? low : fine) | ((uint32_t)__float_as_int(y) >> 31) << 7;
 }
 
-template <bool EIGHT>
+// FLOOR: a v above 0 has its least code at least.  Rounded to 0, as its mean asks for,
+// it leaves m alone in front of next to nothing (blocks of one gradient of 1 and the
+// others of 2^-16, 400 steps: single steps of 1367 lr, so 1.22).
+template <bool EIGHT, bool FLOOR>
 __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
   uint32_t lo = 0, hi = a.count;
   while (hi - lo > 1) {
@@ -771,7 +774,9 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a) {
           const uint64_t k = no + e;
           const uint32_t r = mix32((uint32_t)k ^ ((uint32_t)(k >> 32) * 0x9E3779B9u) ^ c.key);
           mw[e / 4] |= to_code<3, -6, 7>(m[u].v[e] * im, r >> 16 << 4) << (e % 4 * 8);
-          vw[e / 4] |= to_code<2, -14, 15>(v[u].v[e] * iv, (r & 0xFFFFu) << 5) << (e % 4 * 8);
+          uint32_t vc = to_code<2, -14, 15>(v[u].v[e] * iv, (r & 0xFFFFu) << 5);
+          if (FLOOR && v[u].v[e] > 0.f) vc = max(vc, 1u);  // (the product may underflow)
+          vw[e / 4] |= vc << (e % 4 * 8);
         }
         put_codes((uint8_t *)t.m + i, mw, l);
         put_codes((uint8_t *)t.v + i, vw, l);

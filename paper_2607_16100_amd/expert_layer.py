@@ -189,7 +189,7 @@ class ExpertBlock:
 
     unit(v) = v / sqrt(mean(v^2) + eps).  ``layer`` is an ExpertLayer; ``pre`` and
     ``post`` [hidden] are binary32 and start at 1.  ``options`` are those of
-    ``optim.AdamW``.  The block updates the tensors that it and the layer have when
+    ``optim.AdamW`` (``floor`` is on unless they say otherwise).  The block updates the tensors that it and the layer have when
     it is made: assign others before; ``step`` refuses others.  After other values
     were copied into them call ``optimiser.read_params()`` (bfloat16), and the layer's
     ``quantise_weights()``."""
@@ -199,7 +199,7 @@ class ExpertBlock:
         device = layer.router.device
         self.pre, self.post = (torch.ones(layer.hidden, device=device) for _ in range(2))
         self.params = self._present()
-        self.optimiser = AdamW(self.params, **options)
+        self.optimiser = AdamW(self.params, **{"floor": True, **options})
 
     def _present(self) -> list:
         """The tensors that forward and backward use now."""

@@ -16,6 +16,7 @@ from .llmoe import LLLinearDesc
 LL_BLOCK = 128
 LL_NORM_MAX_FEATURES = 16384
 LL_ADAMW_WORKSPACE = 64
+LL_ADAMW_FLOOR = 0x100
 
 _vp, _sz, _i, _u32, _u64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint32, ctypes.c_uint64
 _f, _d = ctypes.c_float, ctypes.c_double

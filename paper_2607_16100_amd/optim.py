@@ -1,6 +1,6 @@
 """A weight update on torch tensors (``ll_adamw`` of ``include/llblock.h``).
 
-    opt = AdamW(params, lr=3e-4, weight_decay=0.1, states="8bit")
+    opt = AdamW(params, lr=3e-4, weight_decay=0.1, states="8bit", floor=True)
     opt.step(grads)
 
 A step is one small launch and one for each 40 tensors, on the current stream
@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import warnings
 from operator import attrgetter
 from typing import Optional, Sequence
 
@@ -47,7 +48,10 @@ class AdamW:
     parameters lie in one tensor each, a parameter's at a multiple of 128
     (``offsets``): ``m`` and ``v`` in float32, or with states="8bit" m as
     float8_e4m3fn and v as float8_e5m2 with a power of two (float8_e8m0fnu) for
-    each 128 values.  States in 8 bits are rounded at random, by ``seed``.
+    each 128 values.  States in 8 bits are rounded at random, by ``seed``; with
+    ``floor`` a v above 0 is never rounded to 0 (LL_ADAMW_FLOOR).  Without it a value
+    whose gradients are 2^-14 and less of the largest of its 128 can move by a thousand
+    times lr in a step; floor=False is for runs that have to go on as they were.
     Values between a parameter's last and the next multiple of 128 stay 0.
 
     ``state``: a ``state_dict()`` to go on from, whose tensors are used, not
@@ -57,13 +61,18 @@ class AdamW:
     other streams have run."""
 
     def __init__(self, params: Sequence[torch.Tensor], *, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
-                 weight_decay: float = 0.0, states: str = "f32", seed: int = 0, state: Optional[dict] = None):
+                 weight_decay: float = 0.0, states: str = "f32", seed: int = 0, state: Optional[dict] = None,
+                 floor: Optional[bool] = None):
         self.params = list(params)
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
         self.seed = seed
         if states not in STATES:
             raise ValueError(f"states: {states!r}, expected one of {sorted(STATES)}")
         self.bits = STATES[states]
+        self.floor = bool(floor)
+        if self.bits == 8 and floor is None:
+            warnings.warn("8-bit states without floor=True: values whose gradients are far below the largest of their 128 can "
+                          "move by many times lr (floor=False says that this is meant)", stacklevel=2)
         if not self.params:
             raise ValueError("params: none")
         dev = self.params[0].get_device()
@@ -187,7 +196,8 @@ class AdamW:
         rate, rate_at = self.lr if lr is None else lr, None
         if isinstance(rate, torch.Tensor):
             rate, rate_at = 0.0, _flat(rate, "lr", dev, 1, torch.float32)
-        d = lb.LLAdamwDesc(lb.ADAMW_DESC_SIZE, self.bits, rate, self.betas[0], self.betas[1], self.eps,
+        bits = self.bits | (lb.LL_ADAMW_FLOOR if self.floor and self.bits == 8 else 0)
+        d = lb.LLAdamwDesc(lb.ADAMW_DESC_SIZE, bits, rate, self.betas[0], self.betas[1], self.eps,
                            self.weight_decay, self.seed & 0xFFFFFFFF)
         ll.check(lb.ll_adamw(d, table, len(table), self.count.data_ptr(), rate_at,
                              None if grad_scale is None else _flat(grad_scale, "grad_scale", dev, 1, torch.float32),
