@@ -178,8 +178,9 @@ typedef struct {
  * v at 0 most of the time and m now and then at its least code; its next step is m
  * / (nearly eps), more than 1000 lr where gradients are far above eps.  With
  * LL_ADAMW_FLOOR a v above 0 is kept at its least code at least: the same steps stay
- * below about 2 lr, and nothing else changes.  Leave it out only for states that
- * have to come out as they did without it.  workspace: LL_ADAMW_WORKSPACE bytes,
+ * below about 2 lr, and nothing else changes (in states that were made without it
+ * put 1 where v is 0 and m is not).  Leave it out only for states that have to come
+ * out as they did without it.  workspace: LL_ADAMW_WORKSPACE bytes,
  * 16-byte aligned.  The tensors lie apart; eps is above 0 in binary32.  Steps
  * that share states or the workspace follow one another. */
 #define LL_ADAMW_WORKSPACE 64

@@ -69,7 +69,6 @@ class AdamW:
         if states not in STATES:
             raise ValueError(f"states: {states!r}, expected one of {sorted(STATES)}")
         self.bits = STATES[states]
-        self.floor = bool(floor)
         if self.bits == 8 and floor is None:
             warnings.warn("8-bit states without floor=True: values whose gradients are far below the largest of their 128 can "
                           "move by many times lr (floor=False says that this is meant)", stacklevel=2)
@@ -101,6 +100,7 @@ class AdamW:
         self._check_state(state, total, mt, vt)
         self.masters, self.m, self.v = state["masters"], state["m"], state["v"]
         self.m_scales, self.v_scales, self.count = state["m_scales"], state["v_scales"], state["count"]
+        self.floor = bool(floor)
         self._work = torch.empty(lb.LL_ADAMW_WORKSPACE, dtype=torch.uint8, device=device)
         self._table = (lb.LLAdamwTensor * len(self.params))()
         self._fields = np.frombuffer(self._table, dtype=_ROW)  # the same memory
@@ -154,6 +154,18 @@ class AdamW:
                 _flat(state[name], name, dev, total // 128, torch.float8_e8m0fnu)
             elif state[name] is not None:
                 raise ValueError(f"{name}: states in float32 have none")
+
+    @property
+    def floor(self) -> bool:
+        return self._floor
+
+    @floor.setter
+    def floor(self, on: bool) -> None:
+        """On states that were made without it, a v of 0 beside an m goes up to its least code."""
+        self._floor = bool(on)
+        if on and self.bits == 8:
+            m, v = self.m.view(torch.uint8), self.v.view(torch.uint8)
+            v.masked_fill_((v == 0) & ((m & 0x7F) != 0), 1)
 
     def state_dict(self) -> dict:
         """The state's own tensors (``AdamW(..., state=...)`` goes on from them)."""

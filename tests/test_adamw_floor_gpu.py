@@ -76,6 +76,30 @@ def test_a_step_is_bounded(rel, betas, noisy):
     assert largest_step(grads, betas, 8 * 128, states="f32") <= most * (1 + 2.0 ** -18)
 
 
+@pytest.mark.parametrize("later", [False, True])
+@pytest.mark.parametrize("betas", BETAS)
+def test_going_on_from_states_that_were_made_without(betas, later):
+    """Where v is 0 beside an m already, it is the least code from then on."""
+    n = 64 * 128
+    p = torch.zeros(n, device=DEV)
+    opt = AdamW([p], lr=1.0, betas=betas, seed=3, states="8bit", floor=False)
+    grads = [torch.from_numpy(g).to(DEV) for g in gradients(64, 2.0 ** -16, 60, 1)]
+    for g in grads[:40]:
+        opt.step([g])
+    lost = (opt.v.view(torch.uint8) == 0) & ((opt.m.view(torch.uint8) & 0x7F) != 0)
+    assert bool(lost.any())
+    held = opt.v.view(torch.uint8).clone()
+    if later:
+        opt.floor = True
+    else:
+        opt = AdamW([p], lr=1.0, betas=betas, seed=3, states="8bit", floor=True, state=opt.state_dict())
+    assert torch.equal(opt.v.view(torch.uint8), torch.where(lost, torch.ones_like(held), held))
+    for g in grads[40:]:
+        p.zero_()
+        opt.step([g])
+        assert float(p.view(-1, 128)[:, 1:].abs().max()) <= LIMIT
+
+
 def test_where_it_is_asked_for():
     p = torch.zeros(300, device=DEV)
     with pytest.warns(UserWarning):
