@@ -67,16 +67,6 @@ struct Pack {
       for (int i = 0; i < N; ++i) p[i] = Num<T>::put(v[i]);
     }
   }
-  // The first n of the N elements (n may be 0 or less); the others read as `fill`.
-  __device__ __forceinline__ void load_some(const T *p, int n, float fill) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = i < n ? Num<T>::get(p[i]) : fill;
-  }
-  __device__ __forceinline__ void store_some(T *p, int n) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < n) p[i] = Num<T>::put(v[i]);
-  }
 };
 
 // e^x to about two units in the last place: 2^t with t = x log2(e) rounded,
