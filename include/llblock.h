@@ -46,7 +46,8 @@ extern "C" {
 
 /* q[r] = e4m3 of act(x[r]), a scale for each LL_BLOCK features from the row's
  * first: scales[r, b] (ceil(features / LL_BLOCK) a row).  A gated activation
- * takes rows x of 2*features.  `end` (device memory, may be NULL): only rows
+ * takes rows x of 2*features.  The SiLU of values below about -87.3, less than
+ * 2^-119 in magnitude, may be 0.  `end` (device memory, may be NULL): only rows
  * below *end are read and written, as behind the last group of a dispatch. */
 int ll_quantise(const void *x, size_t ldx, size_t rows, const int32_t *end, size_t features, ll_dtype dt, ll_act act,
                 uint8_t *q, size_t ldq, uint8_t *scales, size_t lds, void *stream);

@@ -111,6 +111,9 @@ __device__ __forceinline__ uint32_t quantise8(const lin::Vals &v, uint32_t *w) {
 // Activations in front of the rounding to 8 bits.  SiLU is x / (1 + 2^(-x log2
 // e)) by the exponential and the reciprocal of the vector unit: relatively off by
 // |x| 2^-24 and a few units in the last place, where a code's half step is 2^-4.
+// Below about -87.3 the reciprocal is that of a number above 2^126 and may be 0: so
+// then is the result, less than 2^-119 in magnitude (a code only in a block that has
+// no value above 2^-110).
 // With the library's exponential and division they were most of the kernel's time
 // (16384 x 2 x 2048 through SwiGLU 57 us, with an exponential corrected for the
 // product's rounding 39.3, so 36.7; with 16 bytes at any alignment 33.9).
@@ -614,8 +617,10 @@ struct AdamwBegin {
   uint32_t seed;
 };
 
-// A bijection of 32-bit numbers whose every output bit depends on every input
-// bit: multiplications by odd numbers and xors with the upper half.
+// A bijection of 32-bit numbers whose every output bit depends on every input bit:
+// multiplications by odd numbers and xors with the upper half.  Its constants are those
+// of the 32-bit hash that Chris Wellons published as "lowbias32" (Prospecting for Hash
+// Functions, 2018), found there by a search for the least bias.
 __device__ __forceinline__ uint32_t mix32(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x7FEB352Du;
   x = (x ^ (x >> 15)) * 0x846CA68Bu;

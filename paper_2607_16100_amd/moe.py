@@ -512,6 +512,11 @@ def linear8(x, x_scales, w, w_scales, *, bias=None, act: str = "none", residual=
     ``offsets`` is given.  bias, residual, z and the result are of type
     ``dtype`` (bfloat16 unless ``out`` or this says otherwise).  See ll_linear8.
 
+    For bfloat16 results products are cut off 2^-13 below the largest of eight
+    consecutive ones, about 2^-15 of a result of normal values (they are rounded at
+    2^-9): more where a sum's terms cancel than its rounding loses.  With
+    dtype=torch.float32 products and sums are binary32.
+
     The gradient of x is ``linear8`` of the rows' gradient and the transposed
     weight, both in 8 bits, then ``act_grad`` through an activation below; the
     weight's is ``linear_grad_w`` on the rows as they were before."""
