@@ -174,7 +174,7 @@ constexpr int tile8_lds(int bm, int bn, int st) {
 // Rows at any address go through registers, two stages ahead of the one that is
 // written to LDS, with the same loads in every stage, so that the wait for a
 // stage's loads leaves the next one's under way (777 x 1001 -> 515 to binary32, GELU:
-// one stage ahead 16.6 us, two 13.3; 8000 x 4001 -> 4001: 573 us, 472).  16 bytes of
+// one stage ahead 16.6 us, two 13.3; 8000 x 4001 -> 4001: 573 us, 472-481).  16 bytes of
 // a row that is not there come from the tile's first, those that would pass the
 // matrix's end from in front of it; end8() puts those of the last stage in place.
 template <typename L>
@@ -617,7 +617,7 @@ __global__ __launch_bounds__(256, 1) void k_tail8(Args8 a) {
 // was read by every wave before the barrier in front of it, and is waited for a
 // stage or more later.  8192^3: 417-428 us, 2570-2640 TFLOP/s, the matrix cores
 // busy 70 % of the cycles at 1.7 GHz; 16384 rows over 32 groups, 7168 -> 2 x 2048:
-// 490-515 us.
+// 481-515 us.
 //
 // The short last round's parts are the last workgroups of the same launch and
 // start where whole tiles, some of which have no lower half, leave a CU first.
@@ -874,7 +874,7 @@ __global__ __launch_bounds__(256, 1) void k_wide8(Args8 a) {
 // ---------------------------------------------------------------- few rows a group
 //
 // Up to 16 * RB rows of a group, bound by reading the weight once, as k_stream (16
-// rows over 32 groups of 7168 -> 2 x 2048: 60-64 us, 5.9-6.2 TB/s of the weights
+// rows over 32 groups of 7168 -> 2 x 2048: 60-68 us, 5.9-6.2 TB/s of the weights
 // that have rows): a workgroup owns 2 x 16 weight rows (gated: 16 of each half),
 // each of its waves an equal run of the blocks of k, kAhead blocks' loads under way
 // at a time.
