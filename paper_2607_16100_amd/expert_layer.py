@@ -189,10 +189,10 @@ class ExpertBlock:
 
     unit(v) = v / sqrt(mean(v^2) + eps).  ``layer`` is an ExpertLayer; ``pre`` and
     ``post`` [hidden] are binary32 and start at 1.  ``options`` are those of
-    ``optim.AdamW`` (``floor`` is on unless they say otherwise).  The block updates the tensors that it and the layer have when
-    it is made: assign others before; ``step`` refuses others.  After other values
-    were copied into them call ``optimiser.read_params()`` (bfloat16), and the layer's
-    ``quantise_weights()``."""
+    ``optim.AdamW`` (``floor`` is on unless they say otherwise).  The block updates the
+    tensors that it and the layer have when it is made: assign others before; ``step``
+    refuses others.  After other values were copied into them call
+    ``optimiser.read_params()`` and the layer's ``quantise_weights()``."""
 
     def __init__(self, layer: ExpertLayer, scale: float = 1.0, eps: float = 1e-6, **options):
         self.layer, self.scale, self.eps = layer, scale, eps

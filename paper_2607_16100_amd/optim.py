@@ -41,10 +41,9 @@ class AdamW:
     bfloat16 tensors of one GPU, which are updated in place); see ll_adamw.
 
     A bfloat16 parameter has a float32 master, made from it, which holds its value:
-    the parameter is written from it at each step.  Call ``read_params`` where a
-    parameter has got other values otherwise, in its memory or with another one (a
-    step does so by itself for parameters that it finds at another address than the
-    step before, but freed memory may come back at the same one).  The states of all
+    a step writes the parameter from it, whatever is there and wherever its memory is
+    by then.  Call ``read_params`` where a parameter has got other values than a step's,
+    in its memory or with another one.  The states of all
     parameters lie in one tensor each, a parameter's at a multiple of 128
     (``offsets``): ``m`` and ``v`` in float32, or with states="8bit" m as
     float8_e4m3fn and v as float8_e5m2 with a power of two (float8_e8m0fnu) for
@@ -172,14 +171,14 @@ class AdamW:
         return {"masters": self.masters, "m": self.m, "v": self.v, "m_scales": self.m_scales,
                 "v_scales": self.v_scales, "count": self.count}
 
-    def read_params(self, which: Optional[Sequence[int]] = None, stream=None) -> None:
-        """Takes up what bfloat16 parameters (all, or those numbered ``which``) hold
-        now: a value that is not its master rounded becomes its master.  The others
-        keep the bits that the parameter does not have."""
+    def read_params(self, stream=None) -> None:
+        """Takes up what the bfloat16 parameters hold now: a value that is not its master
+        rounded becomes its master.  The others keep the bits that a parameter does not
+        have."""
         with torch.no_grad(), contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            for i in range(len(self.params)) if which is None else which:
-                if self.masters[i] is not None:
-                    p, w = self.params[i].detach().reshape(-1), self.masters[i].view(-1)
+            for p, w in zip(self.params, self.masters):
+                if w is not None:
+                    p, w = p.detach().reshape(-1), w.view(-1)
                     w.copy_(torch.where(w.to(p.dtype) == p, w, p.float()))
 
     def step(self, grads: Sequence[torch.Tensor], *, lr=None, grad_scale=None, stream=None) -> None:
@@ -203,7 +202,6 @@ class AdamW:
             if list(map(_get_device, self.params)) != [dev] * len(at):
                 raise ValueError("params: not all on the GPU they were on")
             self._apart()
-            self.read_params([i for i, (a, b) in enumerate(zip(at, self._at)) if a != b], stream)
             fields["param"] = self._at = at
         rate, rate_at = self.lr if lr is None else lr, None
         if isinstance(rate, torch.Tensor):

@@ -67,3 +67,19 @@ def test_other_weights_than_the_blocks_own():
     with pytest.raises(ValueError):
         block.step(grads_of(block, 2))
     assert all(torch.equal(a, b) for a, b in zip(kept, block.params)) and int(block.optimiser.count) == 1
+
+
+def test_values_copied_into_the_blocks_weights():
+    """A step goes on from them once they are read."""
+    a = make()
+    a.step(grads_of(a, 1))
+    g = gen(8)
+    for w in a.params:
+        w.copy_(randn(g, *w.shape) * 0.1)
+    a.optimiser.read_params()
+    a.layer.quantise_weights()
+    codes_are_the_weights(a.layer)
+    before = [w.clone() for w in a.params]
+    a.step(grads_of(a, 2), lr=0.0)
+    assert all(torch.equal(x, y) for x, y in zip(before, a.params))
+    codes_are_the_weights(a.layer)

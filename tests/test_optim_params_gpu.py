@@ -48,7 +48,7 @@ def twin_of(opt, p, master, states):
 @pytest.mark.parametrize("states", ["f32", "8bit"])
 @pytest.mark.parametrize("how", ["moved", "moved with other values", "refilled", "refilled through data", "moved at first"])
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_the_values_a_parameter_has_are_the_ones_it_goes_on_from(dtype, how, states):
+def test_values_that_are_read_are_the_ones_a_parameter_goes_on_from(dtype, how, states):
     g = gen(3)
     n = 700
     p = randn(g, n, dtype=dtype)
@@ -66,7 +66,7 @@ def test_the_values_a_parameter_has_are_the_ones_it_goes_on_from(dtype, how, sta
         p.data = other.clone()
     else:
         (p.data if how == "refilled through data" else p).copy_(other)
-        opt.read_params()
+    opt.read_params()
     q, twin = twin_of(opt, p, want, states)
     grad = randn(g, n)
     opt.step([grad])
@@ -76,7 +76,23 @@ def test_the_values_a_parameter_has_are_the_ones_it_goes_on_from(dtype, how, sta
         assert torch.equal(opt.masters[0], twin.masters[0]) and torch.equal(p, opt.masters[0].to(BF16))
 
 
-def test_parameters_are_read_on_the_steps_stream_and_in_a_graph():
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_a_bfloat16_parameter_is_written_from_its_master(states):
+    """Whatever its memory holds, and wherever it is, if nobody says that it should be read."""
+    g = gen(6)
+    p, grad = randn(g, 700, dtype=BF16), randn(g, 700)
+    opt = AdamW([p], states=states, **OPTS)
+    opt.step([grad])
+    q, twin = twin_of(opt, p, opt.masters[0], states)
+    p.data = torch.full_like(p, float("nan"))
+    for _ in range(2):
+        opt.step([grad])
+        twin.step([grad])
+        assert torch.equal(p, q) and torch.equal(opt.masters[0], twin.masters[0])
+        p.zero_()
+
+
+def test_parameters_are_read_on_a_side_stream_and_in_a_graph():
     g = gen(4)
     p, fixed = randn(g, 500, dtype=BF16), randn(g, 300, dtype=BF16)
     opt = AdamW([p, fixed], **OPTS)
@@ -88,16 +104,11 @@ def test_parameters_are_read_on_the_steps_stream_and_in_a_graph():
     state["masters"][0] = other.float()
     q = [other.clone(), fixed.clone()]
     twin = AdamW(q, state=state, **OPTS)
-    kept = [p.data]  # so that no later memory is at its address
-    p.data = torch.zeros_like(other)
-    kept.append(p.data)
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(side):
-        p.copy_(other)
+    p.data = other.clone()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):  # takes the parameter's values up too
+    with torch.cuda.graph(graph):
+        opt.read_params()
         opt.step(grads)
     for _ in range(4):
         graph.replay()
@@ -108,12 +119,14 @@ def test_parameters_are_read_on_the_steps_stream_and_in_a_graph():
     # and on a stream of its own, behind what fills the parameter there
     later = torch.empty_like(other)
     big = torch.ones(2048, 2048, device=DEV)
+    side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         for _ in range(20):
             big = (big @ big).clamp(0, 1)
         later.copy_(other)
     p.data = later
+    opt.read_params(side)
     opt.step(grads, stream=side)
     side.synchronize()
     q[0].copy_(other)
